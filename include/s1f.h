@@ -255,6 +255,71 @@ int s1f_kv_grad_emit(const s1f_desc *desc, const float *dk_prefix_acc, const flo
                      int64_t seg_len, void *dk_seg, void *dv_seg, int64_t seg_stride_b, int64_t seg_stride_h,
                      int64_t seg_stride_s, void *hip_stream);
 
+/* What a pipeline stage computes per segment beside attention, for the rows of hidden states [batch, rows, hidden] of a segment: the
+ * first stage makes them out of tokens, every stage normalises them, the last stage turns them into a loss.  Like the attention
+ * calls they run forward for the segments of a sequence in order and backward in reverse order, and the gradients of what all
+ * segments share (table, gamma and beta, weight) are added into fp32 accumulators, which the caller zeroes before the backward of the
+ * last segment; with a table that is also the loss's weight, both may add into one.
+ *   - Rows have strides of their own on either side of a call, in elements, hidden contiguous: a segment is a range of rows of a longer
+ *     sequence, no copy.  Sides and rows may not overlap, and an output may be no input, unless a call says so.
+ *   - Per-row values (mean, rstd, loss, lse, dloss) are dense fp32 arrays [batch, rows].  Tokens and targets are int64 [batch, rows], rows
+ *     contiguous, batch entries `*_stride_b` apart.
+ *   - Pointers are aligned to their element; where rows also start on 16 bytes and hold a whole number of them, calls are faster.
+ *   - The same arguments give the same bits: no atomics.
+ * Errors as for the attention calls: S1F_EINVAL (null or misaligned pointer, bad size or stride, workspace too small), S1F_EUNSUPPORTED (dtype, or
+ * sizes beyond a limit: hidden <= 16384, batch * rows <= 2^24), S1F_ERANGE (rows < 1), S1F_EDEVICE. */
+typedef struct {
+  int32_t batch;
+  int32_t hidden;
+  int32_t dtype;     /* s1f_dtype of rows, table, gamma, beta and weight */
+  int32_t reserved;  /* must be 0 */
+  int64_t rows;      /* per batch entry: the tokens of the segment */
+  int64_t x_stride_b, x_stride_s; /* rows that a call reads (x) and their gradient (dx) */
+  int64_t y_stride_b, y_stride_s; /* rows that a call makes (out, y) and their gradient (dout, dy) */
+} s1f_rows;
+
+/* Embedding: out[r] = scale * table[ids[r]], computed in fp32 and rounded once.  A token outside [0, vocab) gives a row of zeros, and no
+ * gradient.  table [vocab, hidden], rows table_stride elements apart; vocab <= 2^26.  x_stride_* are not used.
+ * The backward adds scale * (sum of dout[r] over the rows with ids[r] = t) to row t of the fp32 accumulators dtable_acc (rows
+ * acc_stride elements apart); rows of tokens that do not occur are not touched.  workspace: device memory, 16-byte aligned, of at
+ * least s1f_embed_bwd_workspace_bytes(desc, vocab) bytes (0: invalid arguments); contents undefined afterwards. */
+int s1f_embed_fwd(const s1f_rows *desc, const int64_t *ids, int64_t ids_stride_b, const void *table, int64_t table_stride, int64_t vocab,
+                  float scale, void *out, void *hip_stream);
+int s1f_embed_bwd(const s1f_rows *desc, const int64_t *ids, int64_t ids_stride_b, const void *dout, int64_t vocab, float scale,
+                  float *dtable_acc, int64_t acc_stride, void *workspace, size_t workspace_bytes, void *hip_stream);
+size_t s1f_embed_bwd_workspace_bytes(const s1f_rows *desc, int64_t vocab);
+
+/* Layer norm of every row: mean, rstd = 1 / sqrt(variance + eps) (the variance around the mean, over hidden elements),
+ * y = (x - mean) * rstd * gamma + beta, in fp32, rounded once.  gamma, beta [hidden] in the element type; eps >= 0.
+ * The backward takes mean and rstd as the forward has left them, overwrites dx and adds the sums over all rows of dy * (x - mean) * rstd and
+ * of dy to the fp32 accumulators dgamma_acc, dbeta_acc [hidden].  workspace: device memory, 16-byte aligned, of at least
+ * s1f_layer_norm_bwd_workspace_bytes(desc) bytes (0: invalid arguments); contents undefined afterwards. */
+int s1f_layer_norm_fwd(const s1f_rows *desc, const void *x, const void *gamma, const void *beta, float eps, void *y, float *mean, float *rstd,
+                       void *hip_stream);
+int s1f_layer_norm_bwd(const s1f_rows *desc, const void *dy, const void *x, const void *gamma, const float *mean, const float *rstd, void *dx,
+                       float *dgamma_acc, float *dbeta_acc, void *workspace, size_t workspace_bytes, void *hip_stream);
+size_t s1f_layer_norm_bwd_workspace_bytes(const s1f_rows *desc);
+
+/* Cross entropy of every row over a vocabulary: scores z = x W^T with weight W [vocab, hidden] (rows weight_stride elements apart),
+ * lse = log sum exp z, loss = lse - z[target].  The scores are never written to memory as a whole.  A row whose target lies outside
+ * [0, vocab) takes no part: loss and lse 0, dx a row of zeros, no share in dweight, whatever x, lse and dloss hold there.
+ * The backward takes lse as the forward has left it and dloss, the gradient of each row's loss:
+ *   dz = (exp(z - lse) - [target]) * dloss,  dx = dz W (overwritten),  dweight: dz^T x
+ *   dweight_dtype S1F_F32   added to fp32 accumulators
+ *   dweight_dtype S1F_BF16  (bf16 rows only) overwritten, rounded once: the gradient of this call alone
+ * bf16: dz is rounded to bf16 before its products, like the score gradients of the attention; sums are fp32.  fp32: products to fp32 precision (operands as
+ * three exact bf16 parts each); a score that an infinity or NaN, or an operand from 2^127 on, takes part in is NaN.
+ * y_stride_* are not used.  weight is 16-byte aligned; vocab <= 2^24, weight_stride < 2^22, batch * rows <= 2^20.  workspace: device
+ * memory, 16-byte aligned, of at least s1f_token_loss_*_workspace_bytes(desc, vocab, weight_stride) bytes (0: invalid arguments); contents
+ * undefined afterwards. */
+int s1f_token_loss_fwd(const s1f_rows *desc, const void *x, const void *weight, int64_t weight_stride, int64_t vocab, const int64_t *targets,
+                       int64_t targets_stride_b, float *loss, float *lse, void *workspace, size_t workspace_bytes, void *hip_stream);
+int s1f_token_loss_bwd(const s1f_rows *desc, const float *dloss, const void *x, const void *weight, int64_t weight_stride, int64_t vocab,
+                       const int64_t *targets, int64_t targets_stride_b, const float *lse, void *dx, void *dweight, int64_t dweight_stride,
+                       int32_t dweight_dtype, void *workspace, size_t workspace_bytes, void *hip_stream);
+size_t s1f_token_loss_fwd_workspace_bytes(const s1f_rows *desc, int64_t vocab, int64_t weight_stride);
+size_t s1f_token_loss_bwd_workspace_bytes(const s1f_rows *desc, int64_t vocab, int64_t weight_stride);
+
 /* Order of passes of one pipeline device under the sequence-level 1F1B schedule (Section 3.2).  HOST
  * functions, no device work.
  *

@@ -27,6 +27,13 @@ class Desc(ctypes.Structure):
                 ("kv_capacity", ctypes.c_int64)]
 
 
+class Rows(ctypes.Structure):
+    """Mirror of s1f_rows."""
+    _fields_ = [("batch", ctypes.c_int32), ("hidden", ctypes.c_int32), ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("rows", ctypes.c_int64), ("x_stride_b", ctypes.c_int64), ("x_stride_s", ctypes.c_int64),
+                ("y_stride_b", ctypes.c_int64), ("y_stride_s", ctypes.c_int64)]
+
+
 class Pass(ctypes.Structure):
     _fields_ = [("micro_batch", ctypes.c_int32), ("segment", ctypes.c_int32), ("backward", ctypes.c_int32)]
 
@@ -92,6 +99,22 @@ def load_library():
     lib.s1f_kv_append.restype = ctypes.c_int
     lib.s1f_kv_grad_emit.argtypes = [dp, vp, vp, i64, i64, vp, vp, i64, i64, i64, vp]
     lib.s1f_kv_grad_emit.restype = ctypes.c_int
+    rp, f32 = ctypes.POINTER(Rows), ctypes.c_float
+    lib.s1f_embed_fwd.argtypes = [rp, vp, i64, vp, i64, i64, f32, vp, vp]
+    lib.s1f_embed_bwd.argtypes = [rp, vp, i64, vp, i64, f32, vp, i64, vp, sz, vp]
+    lib.s1f_embed_bwd_workspace_bytes.argtypes = [rp, i64]
+    lib.s1f_layer_norm_fwd.argtypes = [rp, vp, vp, vp, f32, vp, vp, vp, vp]
+    lib.s1f_layer_norm_bwd.argtypes = [rp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.s1f_layer_norm_bwd_workspace_bytes.argtypes = [rp]
+    lib.s1f_token_loss_fwd.argtypes = [rp, vp, vp, i64, i64, vp, i64, vp, vp, vp, sz, vp]
+    lib.s1f_token_loss_bwd.argtypes = [rp, vp, vp, vp, i64, i64, vp, i64, vp, vp, vp, i64, i32, vp, sz, vp]
+    lib.s1f_token_loss_fwd_workspace_bytes.argtypes = lib.s1f_token_loss_bwd_workspace_bytes.argtypes = [rp, i64, i64]
+    for f in (lib.s1f_embed_fwd, lib.s1f_embed_bwd, lib.s1f_layer_norm_fwd, lib.s1f_layer_norm_bwd, lib.s1f_token_loss_fwd,
+              lib.s1f_token_loss_bwd):
+        f.restype = ctypes.c_int
+    for f in (lib.s1f_embed_bwd_workspace_bytes, lib.s1f_layer_norm_bwd_workspace_bytes, lib.s1f_token_loss_fwd_workspace_bytes,
+              lib.s1f_token_loss_bwd_workspace_bytes):
+        f.restype = sz
     lib.s1f_seq1f1b_warmup.argtypes = [i32, i32, i32, i32, ctypes.POINTER(i64)]
     lib.s1f_seq1f1b_warmup.restype = ctypes.c_int
     lib.s1f_seq1f1b_order.argtypes = [i32, i32, i32, i32, ctypes.POINTER(Pass), i64, ctypes.POINTER(i64)]
@@ -562,3 +585,205 @@ def kv_grad_emit(dk_prefix_acc, dv_prefix_acc, seg_off: int, dk_seg, dv_seg):
                               dk_seg.shape[2], dk_seg.data_ptr(), dv_seg.data_ptr(), s[0], s[1], s[2], _stream_ptr())
     if rc != 0:
         raise S1FError(rc, "s1f_kv_grad_emit")
+
+
+# ---- rows of hidden states: embedding, layer norm, token loss ---------------------------------------------------------------------
+
+def _strides(t):
+    """(batch, row) strides of a [batch, rows, hidden] tensor.  torch gives a dimension of one element any stride: such a one is
+    not used, and 0 here."""
+    s = t.stride()
+    return (s[0] if t.shape[0] > 1 else 0, s[1] if t.shape[1] > 1 else 0)
+
+
+def _rows_desc(x=None, y=None) -> Rows:
+    """Descriptor from [batch, rows, hidden] tensors on either side of a call."""
+    a = y if x is None else x
+    for t in (x, y):
+        if t is None:
+            continue
+        if t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] > 1):
+            raise ValueError("expected [batch, rows, hidden] tensors with contiguous hidden")
+        if t.shape != a.shape:
+            raise ValueError("tensors of a call must have the same [batch, rows, hidden]")
+        if t.dtype != a.dtype:
+            raise TypeError("tensors of a call must share the element type")
+    b, n, h = a.shape
+    return Rows(b, h, _dtype_code(a), 0, n, *(_strides(x) if x is not None else (0, 0)), *(_strides(y) if y is not None else (0, 0)))
+
+
+def _same_rows(ref, other):
+    """Two tensors of one side of a call."""
+    if other.shape != ref.shape or _strides(other) != _strides(ref) or (other.stride(2) != 1 and other.shape[2] > 1):
+        raise ValueError("tensors of one side of a call must have identical shape and strides")
+    if other.dtype != ref.dtype:
+        raise TypeError("tensors of a call must share the element type")
+
+
+def _check_device(*tensors):
+    """All on the current device: the call runs on its stream."""
+    import torch
+    device = tensors[0].device
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError("all tensors of a call must be on the same device")
+    if device.type != "cuda":
+        raise ValueError(f"expected tensors in device memory, got {device}")
+    if device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors are on {device}, the current device is {torch.cuda.current_device()}")
+
+
+def _tokens(t, like):
+    """Pointer and batch stride of [batch, rows] int64 tokens."""
+    import torch
+    if t.dtype != torch.int64:
+        raise TypeError("tokens are int64")
+    if t.shape != like.shape[:2] or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("tokens must be [batch, rows] with contiguous rows")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else 0
+
+
+def _row_values(like, *values):
+    import torch
+    for v in values:
+        if v.dtype != torch.float32:
+            raise TypeError("per-row values are fp32")
+        if not v.is_contiguous() or v.shape != like.shape[:2]:
+            raise ValueError("per-row values must be contiguous [batch, rows] tensors")
+
+
+def _matrix(t, hidden, dtype, what):
+    """Row stride of a [vocab, hidden] tensor."""
+    if t.dtype != dtype:
+        raise TypeError(f"{what}: expected {dtype}")
+    if t.dim() != 2 or t.shape[1] != hidden or (t.stride(1) != 1 and hidden > 1):
+        raise ValueError(f"{what} must be [vocab, hidden] with contiguous hidden")
+    return t.stride(0) if t.shape[0] > 1 else hidden
+
+
+def _vectors(hidden, dtype, *vectors):
+    for v in vectors:
+        if v.dtype != dtype:
+            raise TypeError(f"expected a vector of {dtype}")
+        if v.shape != (hidden,) or not v.is_contiguous():
+            raise ValueError("expected contiguous [hidden] vectors")
+
+
+def _space(workspace):
+    """Pointer and bytes of a workspace, or of none."""
+    if workspace is None:
+        return None, 0
+    if not workspace.is_contiguous():
+        raise ValueError("a workspace must be contiguous")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _checked(rc, name):
+    if rc != 0:
+        raise S1FError(rc, name)
+
+
+def embed_fwd(ids, table, scale: float, out):
+    """s1f_embed_fwd on torch device tensors: out[b, r] = scale * table[ids[b, r]], zeros where the token is outside the table.
+
+    ids [B, rows] int64; table [vocab, hidden]; out [B, rows, hidden] of the table's type.  Enqueued on torch's current stream.
+    """
+    _check_device(out, ids, table)
+    desc = _rows_desc(y=out)
+    at, ids_sb = _tokens(ids, out)
+    stride = _matrix(table, out.shape[2], out.dtype, "table")
+    _checked(load_library().s1f_embed_fwd(ctypes.byref(desc), at, ids_sb, table.data_ptr(), stride, table.shape[0], float(scale),
+                                          out.data_ptr(), _stream_ptr()), "s1f_embed_fwd")
+
+
+def embed_bwd_workspace_bytes(ids, dout, dtable_acc) -> int:
+    return int(load_library().s1f_embed_bwd_workspace_bytes(ctypes.byref(_rows_desc(y=dout)), dtable_acc.shape[0]))
+
+
+def embed_bwd(ids, dout, scale: float, dtable_acc, workspace):
+    """s1f_embed_bwd on torch device tensors: adds scale times the rows of dout to the fp32 rows of dtable_acc [vocab, hidden] that
+    their tokens name; workspace is any device tensor of at least embed_bwd_workspace_bytes(...) bytes."""
+    import torch
+    _check_device(dout, ids, dtable_acc, workspace)
+    desc = _rows_desc(y=dout)
+    at, ids_sb = _tokens(ids, dout)
+    stride = _matrix(dtable_acc, dout.shape[2], torch.float32, "dtable_acc")
+    _checked(load_library().s1f_embed_bwd(ctypes.byref(desc), at, ids_sb, dout.data_ptr(), dtable_acc.shape[0], float(scale),
+                                          dtable_acc.data_ptr(), stride, *_space(workspace), _stream_ptr()), "s1f_embed_bwd")
+
+
+def layer_norm_fwd(x, gamma, beta, eps: float, y, mean, rstd):
+    """s1f_layer_norm_fwd on torch device tensors: x, y [B, rows, hidden]; gamma, beta [hidden] of their type; mean, rstd
+    [B, rows] fp32, overwritten.  Enqueued on torch's current stream."""
+    _check_device(x, gamma, beta, y, mean, rstd)
+    desc = _rows_desc(x, y)
+    _vectors(x.shape[2], x.dtype, gamma, beta)
+    _row_values(x, mean, rstd)
+    _checked(load_library().s1f_layer_norm_fwd(ctypes.byref(desc), x.data_ptr(), gamma.data_ptr(), beta.data_ptr(), float(eps), y.data_ptr(),
+                                               mean.data_ptr(), rstd.data_ptr(), _stream_ptr()), "s1f_layer_norm_fwd")
+
+
+def layer_norm_bwd_workspace_bytes(dy, x) -> int:
+    return int(load_library().s1f_layer_norm_bwd_workspace_bytes(ctypes.byref(_rows_desc(x, dy))))
+
+
+def layer_norm_bwd(dy, x, gamma, mean, rstd, dx, dgamma_acc, dbeta_acc, workspace):
+    """s1f_layer_norm_bwd on torch device tensors: dx, with the shape and strides of x, is overwritten; dgamma_acc and dbeta_acc
+    [hidden] fp32 are added to; workspace is any device tensor of at least layer_norm_bwd_workspace_bytes(...) bytes."""
+    import torch
+    _check_device(dy, x, gamma, mean, rstd, dx, dgamma_acc, dbeta_acc, workspace)
+    desc = _rows_desc(x, dy)
+    _same_rows(x, dx)
+    _vectors(x.shape[2], x.dtype, gamma)
+    _vectors(x.shape[2], torch.float32, dgamma_acc, dbeta_acc)
+    _row_values(x, mean, rstd)
+    _checked(load_library().s1f_layer_norm_bwd(ctypes.byref(desc), dy.data_ptr(), x.data_ptr(), gamma.data_ptr(), mean.data_ptr(),
+                                               rstd.data_ptr(), dx.data_ptr(), dgamma_acc.data_ptr(), dbeta_acc.data_ptr(),
+                                               *_space(workspace), _stream_ptr()), "s1f_layer_norm_bwd")
+
+
+def token_loss_fwd_workspace_bytes(x, weight) -> int:
+    stride = _matrix(weight, x.shape[2], x.dtype, "weight")
+    return int(load_library().s1f_token_loss_fwd_workspace_bytes(ctypes.byref(_rows_desc(x)), weight.shape[0], stride))
+
+
+def token_loss_fwd(x, weight, targets, loss, lse, workspace):
+    """s1f_token_loss_fwd on torch device tensors: cross entropy of every row of x [B, rows, hidden] over the scores x weight^T,
+    weight [vocab, hidden].
+
+    targets [B, rows] int64 (outside [0, vocab): the row takes no part); loss, lse [B, rows] fp32, overwritten; workspace is any device
+    tensor of at least token_loss_fwd_workspace_bytes(...) bytes.  Enqueued on torch's current stream.
+    """
+    _check_device(x, weight, targets, loss, lse, workspace)
+    desc = _rows_desc(x)
+    stride = _matrix(weight, x.shape[2], x.dtype, "weight")
+    at, targets_sb = _tokens(targets, x)
+    _row_values(x, loss, lse)
+    _checked(load_library().s1f_token_loss_fwd(ctypes.byref(desc), x.data_ptr(), weight.data_ptr(), stride, weight.shape[0], at, targets_sb,
+                                               loss.data_ptr(), lse.data_ptr(), *_space(workspace), _stream_ptr()), "s1f_token_loss_fwd")
+
+
+def token_loss_bwd_workspace_bytes(x, weight) -> int:
+    stride = _matrix(weight, x.shape[2], x.dtype, "weight")
+    return int(load_library().s1f_token_loss_bwd_workspace_bytes(ctypes.byref(_rows_desc(x)), weight.shape[0], stride))
+
+
+def token_loss_bwd(dloss, x, weight, targets, lse, dx, dweight, workspace):
+    """s1f_token_loss_bwd on torch device tensors.
+
+    dloss, lse [B, rows] fp32; dx, with the shape and strides of x, is overwritten; dweight [vocab, hidden] is added to if it is fp32 and
+    overwritten if it is bf16 (bf16 rows only); workspace is any device tensor of at least token_loss_bwd_workspace_bytes(...) bytes.
+    """
+    _check_device(dloss, x, weight, targets, lse, dx, dweight, workspace)
+    desc = _rows_desc(x)
+    _same_rows(x, dx)
+    stride = _matrix(weight, x.shape[2], x.dtype, "weight")
+    code = _dtype_code(dweight)
+    into = _matrix(dweight, x.shape[2], dweight.dtype, "dweight")
+    if dweight.shape != weight.shape:
+        raise ValueError("dweight must have the shape of weight")
+    at, targets_sb = _tokens(targets, x)
+    _row_values(x, dloss, lse)
+    _checked(load_library().s1f_token_loss_bwd(ctypes.byref(desc), dloss.data_ptr(), x.data_ptr(), weight.data_ptr(), stride,
+                                               weight.shape[0], at, targets_sb, lse.data_ptr(), dx.data_ptr(), dweight.data_ptr(), into,
+                                               code, *_space(workspace), _stream_ptr()), "s1f_token_loss_bwd")

@@ -1,0 +1,187 @@
+"""What the calls of embedding, layer norm and token loss refuse: the C entry points before anything is launched, and their Python forms before the
+library is called.  No device."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2406_03488_amd as s1f
+from paper_2406_03488_amd import binding
+from paper_2406_03488_amd.binding import Rows
+
+P, ODD, OFF = 4096, 4097, 4104     # addresses: aligned, not even, on 8 bytes (none is looked at)
+BIG = 1 << 50
+
+
+def rows(**kw):
+    base = dict(batch=2, hidden=64, dtype=1, reserved=0, rows=5, x_stride_b=320, x_stride_s=64, y_stride_b=320, y_stride_s=64)
+    base.update(kw)
+    return Rows(**base)
+
+
+def embed_fwd(d, ids=P, table=P, stride=64, vocab=10, out=P):
+    return s1f.load_library().s1f_embed_fwd(ctypes.byref(d) if d else None, ids, 5, table, stride, vocab, 1.0, out, None)
+
+
+def embed_bwd(d, ids=P, dout=P, vocab=10, acc=P, stride=64, ws=P, n=BIG):
+    return s1f.load_library().s1f_embed_bwd(ctypes.byref(d) if d else None, ids, 5, dout, vocab, 1.0, acc, stride, ws, n, None)
+
+
+def norm_fwd(d, x=P, gamma=P, beta=P, eps=1e-5, y=P, mean=P, rstd=P):
+    return s1f.load_library().s1f_layer_norm_fwd(ctypes.byref(d) if d else None, x, gamma, beta, eps, y, mean, rstd, None)
+
+
+def norm_bwd(d, dy=P, x=P, gamma=P, mean=P, rstd=P, dx=P, dg=P, db=P, ws=P, n=BIG):
+    return s1f.load_library().s1f_layer_norm_bwd(ctypes.byref(d) if d else None, dy, x, gamma, mean, rstd, dx, dg, db, ws, n, None)
+
+
+def loss_fwd(d, x=P, weight=P, stride=64, vocab=10, targets=P, loss=P, lse=P, ws=P, n=BIG):
+    return s1f.load_library().s1f_token_loss_fwd(ctypes.byref(d) if d else None, x, weight, stride, vocab, targets, 5, loss, lse, ws, n, None)
+
+
+def loss_bwd(d, dloss=P, x=P, weight=P, stride=64, vocab=10, targets=P, lse=P, dx=P, dw=P, into=64, code=0, ws=P, n=BIG):
+    return s1f.load_library().s1f_token_loss_bwd(ctypes.byref(d) if d else None, dloss, x, weight, stride, vocab, targets, 5, lse, dx, dw, into, code,
+                                                 ws, n, None)
+
+
+CALLS = {embed_fwd: "y", embed_bwd: "y", norm_fwd: "xy", norm_bwd: "xy", loss_fwd: "x", loss_bwd: "x"}
+
+
+@pytest.mark.parametrize("call", CALLS)
+def test_descriptors_refused(call):
+    assert call(None) == 1
+    for bad in (dict(batch=0), dict(batch=-1), dict(hidden=0), dict(reserved=1)):
+        assert call(rows(**bad)) == 1, bad
+    for bad in (dict(dtype=2), dict(dtype=-1), dict(hidden=16385), dict(rows=(1 << 24) + 1), dict(batch=1 << 20, rows=1 << 20),
+                dict(batch=1 << 30, rows=1 << 34)):
+        h = bad.get("hidden", 64)
+        d = rows(**{"x_stride_s": h, "y_stride_s": h, "x_stride_b": 1 << 40, "y_stride_b": 1 << 40, **bad})
+        kw = {} if call in (norm_fwd, norm_bwd) else {"stride": h}
+        assert call(d, **kw) == 2, bad
+    for bad in (0, -1, -(1 << 40)):
+        assert call(rows(rows=bad)) == 3
+    for side in CALLS[call]:
+        for bad in ({f"{side}_stride_s": 63}, {f"{side}_stride_s": -64}, {f"{side}_stride_b": 63}):
+            assert call(rows(**bad)) == 1, bad
+
+
+@pytest.mark.parametrize("call", CALLS)
+def test_pointers_and_sizes_refused(call):
+    """Whatever is checked last would be launched here, where there is no device: every call has to end before."""
+    names = {embed_fwd: ("ids", "table", "out"), embed_bwd: ("ids", "dout", "acc", "ws"), norm_fwd: ("x", "gamma", "beta", "y", "mean", "rstd"),
+             norm_bwd: ("dy", "x", "gamma", "mean", "rstd", "dx", "dg", "db", "ws"), loss_fwd: ("x", "weight", "targets", "loss", "lse", "ws"),
+             loss_bwd: ("dloss", "x", "weight", "targets", "lse", "dx", "dw", "ws")}[call]
+    for name in names:
+        assert call(rows(), **{name: None}) == 1, name
+        assert call(rows(), **{name: ODD}) == 1, name
+    if "ws" in names:
+        assert call(rows(), ws=OFF) == 1 and call(rows(), n=255) == 1 and call(rows(), n=0) == 1
+    if call in (embed_fwd, loss_fwd, loss_bwd):
+        assert call(rows(), stride=63) == 1
+    if call not in (norm_fwd, norm_bwd):
+        assert call(rows(), vocab=0) == 1 and call(rows(), vocab=-5) == 1
+        assert call(rows(), vocab=(1 << 26) + 1) == 2
+    if call is norm_fwd:
+        assert call(rows(), eps=-1e-9) == 1 and call(rows(), eps=float("nan")) == 1
+    if call in (loss_fwd, loss_bwd):
+        assert call(rows(), weight=OFF) == 1
+        assert call(rows(), vocab=(1 << 24) + 1) == 2 and call(rows(), stride=1 << 22) == 2
+        assert call(rows(batch=1, rows=(1 << 20) + 1)) == 2
+    if call is loss_bwd:
+        assert call(rows(), into=63) == 1 and call(rows(), code=2) == 2 and call(rows(dtype=0), code=1) == 2
+
+
+def test_workspace_sizes():
+    lib = s1f.load_library()
+    ask = lambda f, d, *a: f(ctypes.byref(d) if d else None, *a)
+    queries = [(lib.s1f_embed_bwd_workspace_bytes, (10,)), (lib.s1f_layer_norm_bwd_workspace_bytes, ()),
+               (lib.s1f_token_loss_fwd_workspace_bytes, (10, 64)), (lib.s1f_token_loss_bwd_workspace_bytes, (10, 64))]
+    for f, a in queries:
+        assert ask(f, rows(), *a) > 0
+        assert ask(f, None, *a) == 0 and ask(f, rows(rows=0), *a) == 0 and ask(f, rows(hidden=0), *a) == 0 and ask(f, rows(dtype=5), *a) == 0
+    # scores never exist as a whole: a piece of them is at most 1 GiB, however many there are
+    d = rows(batch=1, rows=1 << 17, hidden=1024, x_stride_s=1024, x_stride_b=0)
+    fwd, bwd = ask(lib.s1f_token_loss_fwd_workspace_bytes, d, 200000, 1024), ask(lib.s1f_token_loss_bwd_workspace_bytes, d, 200000, 1024)
+    assert fwd < 4 << 30 and bwd < 12 << 30
+
+
+class Library:
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        return lambda *args: self.calls.append(name) or 0
+
+
+@pytest.fixture
+def library(monkeypatch):
+    lib = Library()
+    monkeypatch.setattr(binding, "load_library", lambda: lib)
+    monkeypatch.setattr(binding, "_stream_ptr", lambda: 0)
+    monkeypatch.setattr(binding, "_check_device", lambda *t: None)
+    return lib
+
+
+def bf16(*shape):
+    return torch.zeros(shape, dtype=torch.bfloat16)
+
+
+def f32(*shape):
+    return torch.zeros(shape)
+
+
+def ids(*shape):
+    return torch.zeros(shape, dtype=torch.int64)
+
+
+def good():
+    """Arguments of every call, by name; all of them fit."""
+    x, ws = bf16(2, 5, 16), torch.zeros(64, dtype=torch.uint8)
+    return {"embed_fwd": [ids(2, 5), bf16(9, 16), 1.0, x], "embed_bwd": [ids(2, 5), x, 1.0, f32(9, 16), ws],
+            "layer_norm_fwd": [x, bf16(16), bf16(16), 1e-5, bf16(2, 5, 16), f32(2, 5), f32(2, 5)],
+            "layer_norm_bwd": [bf16(2, 5, 16), x, bf16(16), f32(2, 5), f32(2, 5), bf16(2, 5, 16), f32(16), f32(16), ws],
+            "token_loss_fwd": [x, bf16(9, 16), ids(2, 5), f32(2, 5), f32(2, 5), ws],
+            "token_loss_bwd": [f32(2, 5), x, bf16(9, 16), ids(2, 5), f32(2, 5), bf16(2, 5, 16), f32(9, 16), ws]}
+
+
+def test_good_calls_reach_the_library(library):
+    for name, args in good().items():
+        getattr(s1f, name)(*args)
+        assert library.calls.pop() == "s1f_" + name and not library.calls
+
+
+BAD = [("embed_fwd", 0, ids(2, 4)), ("embed_fwd", 0, ids(5)), ("embed_fwd", 0, ids(2, 10)[:, ::2]), ("embed_fwd", 0, ids(2, 5).int()),
+       ("embed_fwd", 1, bf16(9, 8)), ("embed_fwd", 1, f32(9, 16)), ("embed_fwd", 1, bf16(16, 9).t()), ("embed_fwd", 3, bf16(2, 5, 32)[..., ::2]),
+       ("embed_fwd", 3, bf16(5, 16)), ("embed_fwd", 3, bf16(2, 5, 16).half()), ("embed_bwd", 3, bf16(9, 16)), ("embed_bwd", 3, f32(9, 8)),
+       ("embed_bwd", 0, ids(3, 5)), ("embed_bwd", 4, torch.zeros(128, dtype=torch.uint8)[::2]),
+       ("layer_norm_fwd", 1, f32(16)), ("layer_norm_fwd", 2, bf16(15)), ("layer_norm_fwd", 2, bf16(32)[::2]), ("layer_norm_fwd", 4, bf16(2, 6, 16)),
+       ("layer_norm_fwd", 4, f32(2, 5, 16)), ("layer_norm_fwd", 5, f32(2, 6)), ("layer_norm_fwd", 5, bf16(2, 5)), ("layer_norm_fwd", 6, f32(5, 2).t()),
+       ("layer_norm_bwd", 0, bf16(1, 5, 16)), ("layer_norm_bwd", 5, bf16(2, 5, 32)[..., :16]), ("layer_norm_bwd", 5, f32(2, 5, 16)),
+       ("layer_norm_bwd", 6, bf16(16)), ("layer_norm_bwd", 7, f32(17)), ("layer_norm_bwd", 3, f32(10)),
+       ("token_loss_fwd", 1, f32(9, 16)), ("token_loss_fwd", 1, bf16(9, 17)), ("token_loss_fwd", 2, ids(2, 6)), ("token_loss_fwd", 2, f32(2, 5)),
+       ("token_loss_fwd", 3, bf16(2, 5)), ("token_loss_fwd", 4, f32(5, 2)), ("token_loss_bwd", 0, bf16(2, 5)), ("token_loss_bwd", 4, f32(2, 4)),
+       ("token_loss_bwd", 5, bf16(2, 6, 16)), ("token_loss_bwd", 5, bf16(2, 10, 16)[:, ::2]), ("token_loss_bwd", 6, f32(8, 16)),
+       ("token_loss_bwd", 6, f32(9, 16).half()), ("token_loss_bwd", 6, f32(16, 9).t())]
+
+
+@pytest.mark.parametrize("name,at,bad", BAD)
+def test_tensors_that_do_not_fit_are_refused(library, name, at, bad):
+    args = good()[name]
+    args[at] = bad
+    with pytest.raises((TypeError, ValueError)):
+        getattr(s1f, name)(*args)
+    assert library.calls == []
+
+
+def test_strides_of_single_rows_and_batches_do_not_matter(library):
+    """torch gives a dimension of one element any stride."""
+    x = torch.zeros((1, 1, 16), dtype=torch.bfloat16).as_strided((1, 1, 16), (3, 5, 1))
+    s1f.layer_norm_fwd(x, bf16(16), bf16(16), 1e-5, bf16(1, 1, 16), f32(1, 1), f32(1, 1))
+    s1f.layer_norm_bwd(bf16(1, 1, 16), x, bf16(16), f32(1, 1), f32(1, 1), bf16(1, 1, 16), f32(16), f32(16), torch.zeros(64))
+    assert library.calls == ["s1f_layer_norm_fwd", "s1f_layer_norm_bwd"]
+
+
+def test_tensors_outside_device_memory_are_refused():
+    for name, args in good().items():
+        with pytest.raises(ValueError):
+            getattr(s1f, name)(*args)
