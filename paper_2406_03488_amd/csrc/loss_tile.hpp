@@ -26,7 +26,8 @@ template <int R, bool TR, int NW> struct Side {
   static constexpr int ROW = TR ? 2 * R : 128, CHUNKS = ROW / 16, RPP = 1024 / ROW;   // bytes and chunks of a row, rows per piece
   S1F_DEV static int h(int k) { return R >= 128 ? (k & 3) | ((k >> 3) & 1) << 2 : ((k >> 1) & 1) | ((k >> 3) & 1) << 1; }
 
-  const char *base;         // of the stage that is copied next (uniform)
+  static constexpr int BIAS = 1024 * (PER_WAVE - 1);
+  const char *next;         // of the stage that is copied next, less BIAS (uniform)
   int64_t step;             // bytes to the next stage
   unsigned voff[PER_WAVE];  // of the lane's chunk in each of the wave's pieces
   int row_bytes;
@@ -38,10 +39,10 @@ template <int R, bool TR, int NW> struct Side {
     chunk = TR ? ((((c >> 1) ^ h(row)) << 1) | (c & 1)) : (c ^ ((row >> 1) & 7));
   }
   // m0: first row (column) of the tile; limit: rows (columns) that there are; those behind are copies of the last (columns: first)
-  S1F_DEV void init(const bf16_t *data, int64_t ld, int64_t m0, int64_t limit, int wave, int lane) {
+  S1F_DEV void init(const bf16_t *data, int64_t ld, int64_t m0, int64_t limit, int k_stage, int wave, int lane) {
     row_bytes = (int)(ld * 2);
-    base = reinterpret_cast<const char *>(TR ? data + m0 : data + m0 * ld);
     step = TR ? kDepth * ld * 2 : kDepth * 2;
+    next = reinterpret_cast<const char *>(TR ? data + m0 : data + m0 * ld) + k_stage * step - BIAS;
 #pragma unroll
     for (int i = 0; i < PER_WAVE; ++i) {
       int r, c;
@@ -51,16 +52,16 @@ template <int R, bool TR, int NW> struct Side {
       } else {
         if (m0 + r >= limit) r = (int)(limit - 1 - m0);
       }
-      voff[i] = (unsigned)(r * row_bytes + 16 * c);
+      // (the immediate offset of a copy instruction counts for its address in memory as well as in LDS)
+      voff[i] = (unsigned)(r * row_bytes + 16 * c) + (unsigned)(BIAS - 1024 * i);
     }
   }
-  // Copies a stage to LDS address `dst`.  left: contraction that the operand has from this stage on; where it is less than a stage, what
-  // is behind is read from the stage's beginning and overwritten by clear_tail.
-  S1F_DEV void issue(const char *from, lds_addr dst, int left, int wave, int lane) const {
+  // Copies a stage at `from` to LDS address `dst`.
+  template <bool TAIL> S1F_DEV void issue(const char *from, lds_addr dst, int left, int wave, int lane) const {
     unsigned off[PER_WAVE];
 #pragma unroll
     for (int i = 0; i < PER_WAVE; ++i) off[i] = voff[i];
-    if (left < kDepth) {
+    if constexpr (TAIL) {   // `left` of the stage's contraction are there: what is behind is read from its beginning, and cleared by clear_tail
 #pragma unroll
       for (int i = 0; i < PER_WAVE; ++i) {
         int r, c;
@@ -79,15 +80,14 @@ template <int R, bool TR, int NW> struct Side {
     const unsigned to = __builtin_amdgcn_readfirstlane(dst + (unsigned)(wave * PER_WAVE * 1024));
     if constexpr (PER_WAVE == 4)
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\t"
-                   "global_load_lds_dwordx4 %2, %6 offset:1024\n\t"
-                   "global_load_lds_dwordx4 %3, %7 offset:2048\n\t"
-                   "global_load_lds_dwordx4 %4, %8 offset:3072"
-                   : : "s"(to), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(b), "s"(b - 1024), "s"(b - 2048), "s"(b - 3072)
-                   : "m0");
+                   "global_load_lds_dwordx4 %2, %5 offset:1024\n\t"
+                   "global_load_lds_dwordx4 %3, %5 offset:2048\n\t"
+                   "global_load_lds_dwordx4 %4, %5 offset:3072"
+                   : : "s"(to), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(b) : "m0");
     else if constexpr (PER_WAVE == 2)
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\t"
-                   "global_load_lds_dwordx4 %2, %4 offset:1024"
-                   : : "s"(to), "v"(off[0]), "v"(off[1]), "s"(b), "s"(b - 1024) : "m0");
+                   "global_load_lds_dwordx4 %2, %3 offset:1024"
+                   : : "s"(to), "v"(off[0]), "v"(off[1]), "s"(b) : "m0");
     else {
       static_assert(PER_WAVE == 1, "one, two or four pieces");
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(off[0]), "s"(b) : "m0");
@@ -105,29 +105,30 @@ template <int R, bool TR, int NW> struct Side {
   }
   // Operand of one matrix instruction: rows (columns) 16 * block .. +15 of the tile, contraction 32 * half .. +31; of the latter
   // lane (n, j) holds 8j .. 8j+7, whichever way the operand is stored.
-  struct At {
-    lds_addr a;
-  };
-  S1F_DEV static At at(lds_addr stage, int lane) {
+  // at(): the lane's address for the wave's first block; operand(): its block number `block`.
+  S1F_DEV static lds_addr at(int first_block, int lane) {
     const int n = lane & 15, j = lane >> 4;
     if constexpr (TR) {
       const int k = 8 * j + (n >> 2);
-      return At{opaque(stage + (unsigned)(k * ROW + h(k) * 32 + (n & 3) * 8))};
+      return (unsigned)(k * ROW + (n & 3) * 8) + ((unsigned)(h(k) * 32) ^ (unsigned)(first_block * 32));
     } else {
-      return At{opaque(stage + (unsigned)(n * 128 + 16 * (j ^ ((n >> 1) & 7))))};
+      return (unsigned)(first_block * 2048 + n * 128 + 16 * (j ^ ((n >> 1) & 7)));
     }
   }
-  S1F_DEV static bf16x8 operand(At x, int block, int half) {
+  // (what has to be added to the address of a stage's half is a constant; see opaque)
+  S1F_DEV static lds_addr half_of(lds_addr a, int half) { return opaque(TR ? a : a ^ (unsigned)(half * 64)); }
+  S1F_DEV static bf16x8 operand(lds_addr a, int block, int half) {
     if constexpr (TR) {
-      const lds_addr p = (x.a ^ (unsigned)((block * 32) & (ROW - 1))) + (unsigned)(half * 32 * ROW);
-      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<__attribute__((address_space(3))) s16x4 *>((uintptr_t)p));
+      const lds_addr p = a ^ (unsigned)(block * 32);
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          reinterpret_cast<__attribute__((address_space(3))) s16x4 *>((uintptr_t)(p + (unsigned)(half * 32 * ROW))));
       const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-          reinterpret_cast<__attribute__((address_space(3))) s16x4 *>((uintptr_t)(p + (unsigned)(4 * ROW))));
+          reinterpret_cast<__attribute__((address_space(3))) s16x4 *>((uintptr_t)(p + (unsigned)(half * 32 * ROW + 4 * ROW))));
       typedef short s16x8 __attribute__((ext_vector_type(8)));
       s16x8 r = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
       return __builtin_bit_cast(bf16x8, r);
     } else {
-      return lds_load<bf16x8>((x.a ^ (unsigned)(half * 64)) + (unsigned)(block * 2048));
+      return lds_load<bf16x8>(a + (unsigned)(block * 2048));
     }
   }
 };
@@ -141,81 +142,110 @@ struct Matrix {
 
 // The main loop: acc[mb][nb] = the block of rows 16 * (MB * wave_m + mb) and columns 16 * (NB * wave_n + nb), as the matrix
 // instruction leaves it with the operands in this order: lane (n, j) holds row n, columns 4j .. 4j+3 of the block.
-template <int BM, int BN, int WM, int WN, bool TRA, bool TRB> struct Product {
+// PAIRS: 1, or 6 products of planes for each.
+template <int BM, int BN, int WM, int WN, bool TRA, bool TRB, int PAIRS> struct Product {
   static constexpr int NW = WM * WN, THREADS = 64 * NW, MB = BM / WM / 16, NB = BN / WN / 16;
   typedef Side<BM, TRA, NW> SA;
   typedef Side<BN, TRB, NW> SB;
   static constexpr int STAGE = SA::BYTES + SB::BYTES, LDS_BYTES = 2 * STAGE;
 
-  // k: contraction of one product of planes; stages [begin, end) of all of them, counted k-stage by k-stage, plane by plane within
+  // k: contraction; stages [begin, end) of it, counted in stages of a product of planes, the PAIRS of each one after the other
   S1F_DEV static void run(f32x4 (&acc)[MB][NB], const Matrix &a, const Matrix &b, int64_t m0, int64_t m_limit, int64_t n0, int64_t n_limit,
-                          int64_t k, int pairs, int begin, int end, lds_addr lds) {
+                          int64_t k, int begin, int end, lds_addr lds) {
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
-    SA sa;
-    SB sb;
-    sa.init(a.data, a.ld, m0, m_limit, wave, lane);
-    sb.init(b.data, b.ld, n0, n_limit, wave, lane);
-    int pair = begin % pairs;                      // of the stage that is copied next
-    int kt = begin / pairs;
-    // copies the next stage to `dst`
-    auto issue = [&](lds_addr dst) {
-      // (2,0) (0,2) (1,1) (1,0) (0,1) (0,0): smallest products first
-      const int of_a = pairs == 1 ? 0 : (int)((0x001102u >> (4 * pair)) & 3u), of_b = pairs == 1 ? 0 : (int)((0x010120u >> (4 * pair)) & 3u);
-      const int64_t rest = k - (int64_t)kt * kDepth;
-      const int left = rest < kDepth ? (int)rest : kDepth;
-      sa.issue(sa.base + kt * sa.step + of_a * a.plane * 2, dst, left, wave, lane);
-      sb.issue(sb.base + kt * sb.step + of_b * b.plane * 2, dst + SA::BYTES, left, wave, lane);
-      if (++pair == pairs) {
-        pair = 0;
-        ++kt;
-      }
-    };
-    // contraction left from stage t on
-    auto left_at = [&](int t) -> int {
-      const int64_t rest = k - (int64_t)(t / pairs) * kDepth;
-      return rest < kDepth ? (int)rest : kDepth;
-    };
-    auto landed = [&](lds_addr at, int t) {        // this wave's copies of stage t are there
-      const int left = left_at(t);
-      if (left < kDepth) {
-        sa.clear_tail(at, left, wave, lane);
-        sb.clear_tail(at + SA::BYTES, left, wave, lane);
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      }
-    };
 #pragma unroll
     for (int i = 0; i < MB; ++i)
 #pragma unroll
       for (int j = 0; j < NB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (begin >= end) return;
-    lds_addr cur = lds, next = lds + STAGE;
-    issue(cur);
-    if (begin + 1 < end) issue(next);
-    for (int t = begin; t < end; ++t) {
-      if (t + 1 < end) wait_async_tiles_but_last<SA::PER_WAVE + SB::PER_WAVE>();
-      else wait_async_tiles();
-      landed(cur, t);
-      __syncthreads();
-      const typename SA::At xa = SA::at(cur, lane);
-      const typename SB::At xb = SB::at(cur + SA::BYTES, lane);
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        bf16x8 fa[MB], fb[NB];
-#pragma unroll
-        for (int i = 0; i < MB; ++i) fa[i] = SA::operand(xa, wm * MB + i, half);
-#pragma unroll
-        for (int j = 0; j < NB; ++j) fb[j] = SB::operand(xb, wn * NB + j, half);
-#pragma unroll
-        for (int i = 0; i < MB; ++i)
-#pragma unroll
-          for (int j = 0; j < NB; ++j) acc[i][j] = mma16(fb[j], fa[i], acc[i][j]);
+    SA sa;
+    SB sb;
+    sa.init(a.data, a.ld, m0, m_limit, begin / PAIRS, wave, lane);
+    sb.init(b.data, b.ld, n0, n_limit, begin / PAIRS, wave, lane);
+    int pair = begin % PAIRS;                       // of the stage that is copied next
+    const int left = (int)((k - 1) % kDepth) + 1;   // contraction of the last stage
+    const int tail = left < kDepth ? (int)((k - 1) / kDepth) * PAIRS : 0x7fffffff;   // first stage that is not whole
+    // copies stage t to `dst`
+    auto issue = [&](int t, lds_addr dst) {
+      const char *from_a = sa.next, *from_b = sb.next;
+      if constexpr (PAIRS == 6) {   // (2,0) (0,2) (1,1) (1,0) (0,1) (0,0): smallest products first
+        from_a += (int64_t)((0x001102u >> (4 * pair)) & 3u) * a.plane * 2;
+        from_b += (int64_t)((0x010120u >> (4 * pair)) & 3u) * b.plane * 2;
       }
+      if (t < tail) {
+        sa.template issue<false>(from_a, dst, kDepth, wave, lane);
+        sb.template issue<false>(from_b, dst + SA::BYTES, kDepth, wave, lane);
+      } else {
+        sa.template issue<true>(from_a, dst, left, wave, lane);
+        sb.template issue<true>(from_b, dst + SA::BYTES, left, wave, lane);
+      }
+      if (PAIRS == 1 || ++pair == PAIRS) {
+        pair = 0;
+        sa.next += sa.step;
+        sb.next += sb.step;
+      }
+    };
+    auto landed = [&](int t, lds_addr at) {        // this wave's copies of stage t are there
+      if (t >= tail) {
+        sa.clear_tail(at, left, wave, lane);
+        sb.clear_tail(at + SA::BYTES, left, wave, lane);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      }
+    };
+    lds_addr cur = lds, next = lds + STAGE;
+    issue(begin, cur);
+    if (begin + 1 < end) {
+      issue(begin + 1, next);
+      wait_async_tiles_but_last<SA::PER_WAVE + SB::PER_WAVE>();
+    } else {
+      wait_async_tiles();
+    }
+    landed(begin, cur);
+    __syncthreads();
+    // Operands are read half a stage ahead of the products that take them.  When the products of a stage's first half are through,
+    // nobody reads that stage any more and the next one has been on its way for a whole stage: one barrier per stage does for both.
+    bf16x8 fa[2][MB], fb[2][NB];
+    const lds_addr lane_a = SA::at(wm * MB, lane), lane_b = SA::BYTES + SB::at(wn * NB, lane);
+    constexpr int OPERANDS = MB + NB, PER_SLOT = (OPERANDS * 4 + 3 * MB - 1) / (3 * MB);   // read in the first three quarters of the products
+    // Products of one half, and the reads of the operands of the next: a slot for each row of blocks, nothing moves across its end.
+    auto half_stage = [&](bf16x8 (&ra)[MB], bf16x8 (&rb)[NB], const bf16x8 (&xa)[MB], const bf16x8 (&xb)[NB], lds_addr at, int half, auto between) {
+      const lds_addr pa = SA::half_of(at + lane_a, half), pb = SB::half_of(at + lane_b, half);
+#pragma unroll
+      for (int i = 0; i < MB; ++i) {
+#pragma unroll
+        for (int r = 0; r < PER_SLOT; ++r) {
+          const int o = i * PER_SLOT + r;
+          if (o < NB) rb[o] = SB::operand(pb, o, half);
+          else if (o < OPERANDS) ra[o - NB] = SA::operand(pa, o - NB, half);
+        }
+#pragma unroll
+        for (int j = 0; j < NB; ++j) acc[i][j] = mma16(xb[j], xa[i], acc[i][j]);
+        if (i == 0) between();
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    auto nothing = [] {};
+    {
+      const lds_addr pa = SA::half_of(cur + lane_a, 0), pb = SB::half_of(cur + lane_b, 0);
+#pragma unroll
+      for (int j = 0; j < NB; ++j) fb[0][j] = SB::operand(pb, j, 0);
+#pragma unroll
+      for (int i = 0; i < MB; ++i) fa[0][i] = SA::operand(pa, i, 0);
+    }
+    for (int t = begin; t < end; ++t) {
+      __builtin_amdgcn_sched_barrier(0);
+      half_stage(fa[1], fb[1], fa[0], fb[0], cur, 1, nothing);
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+      landed(t + 1, next);   // (behind the last stage: clears what nobody reads)
       __syncthreads();
-      if (t + 2 < end) issue(cur);
+      __builtin_amdgcn_sched_barrier(0);
+      // (behind the last stage: reads what an earlier one has left, and nothing uses it)
+      half_stage(fa[0], fb[0], fa[1], fb[1], next, 0, [&] { if (t + 2 < end) issue(t + 2, cur); });
       const lds_addr was = cur;
       cur = next;
       next = was;
     }
+    __syncthreads();
   }
 };
 

@@ -38,7 +38,7 @@ struct LossArgs {
   int64_t rows_plane, packed_plane, dz_plane, dz_ld;
   float *part;                                     // dx in parts: [part][slot][width]
   // piece of the vocabulary, and of the launch
-  int32_t first, piece, direct, pairs, splits, add, parts, wide;
+  int32_t first, piece, direct, splits, add, parts, wide;
   int32_t tiles_m, tiles_n;
   Divisor by_group, by_n, by_tiles, by_row;
 };
@@ -160,15 +160,16 @@ S1F_DEV Matrix weight_matrix(const LossArgs &a) {
 template <typename T, int BM, int BN, int WM, int WN, bool STATS>
 __global__ void __launch_bounds__(64 * WM * WN) loss_scores_kernel(const LossArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
-  typedef Product<BM, BN, WM, WN, false, false> P;
+  constexpr int PAIRS = sizeof(T) == 4 ? 6 : 1;
+  typedef Product<BM, BN, WM, WN, false, false, PAIRS> P;
   const int count = *a.count;
   int tm, tn;
   decode_tile(a, blockIdx.x, tm, tn);
   const int m0 = tm * BM, n0 = tn * BN;
   if (m0 >= count) return;
   f32x4 acc[P::MB][P::NB];
-  const int stages = ((a.width + kDepth - 1) / kDepth) * a.pairs;
-  P::run(acc, Matrix{a.rows, a.width, a.rows_plane}, weight_matrix(a), m0, count, n0, a.piece, a.width, a.pairs, 0, stages, to_lds_addr(smem));
+  P::run(acc, Matrix{a.rows, a.width, a.rows_plane}, weight_matrix(a), m0, count, n0, a.piece, a.width, 0,
+         (a.width + kDepth - 1) / kDepth * PAIRS, to_lds_addr(smem));
   const int lane = lane_id(), n = lane & 15, j = lane >> 4, wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
   if constexpr (STATS) {
     float *red = reinterpret_cast<float *>(smem);     // [WN][BM][maximum, sum]
@@ -273,18 +274,18 @@ __global__ void __launch_bounds__(256) loss_join_kernel(const LossArgs a) {
 }
 
 // dx = dz W over a piece of the vocabulary, in `splits` parts of it that run side by side.
-template <int BM, int BN, int WM, int WN> __global__ void __launch_bounds__(64 * WM * WN) loss_dx_kernel(const LossArgs a) {
+template <int PAIRS, int BM, int BN, int WM, int WN> __global__ void __launch_bounds__(64 * WM * WN) loss_dx_kernel(const LossArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
-  typedef Product<BM, BN, WM, WN, false, true> P;
+  typedef Product<BM, BN, WM, WN, false, true, PAIRS> P;
   const int count = *a.count;
   int part, tile, tm, tn;
   div_mod(blockIdx.x, a.by_tiles, part, tile);
   decode_tile(a, tile, tm, tn);
   const int m0 = tm * BM, n0 = tn * BN;
   if (m0 >= count) return;
-  const int64_t stages = (int64_t)((a.piece + kDepth - 1) / kDepth) * a.pairs;
+  const int64_t stages = (int64_t)((a.piece + kDepth - 1) / kDepth) * PAIRS;
   f32x4 acc[P::MB][P::NB];
-  P::run(acc, Matrix{a.dz, a.dz_ld, a.dz_plane}, weight_matrix(a), m0, count, n0, a.width, a.piece, a.pairs, (int)(stages * part / a.splits),
+  P::run(acc, Matrix{a.dz, a.dz_ld, a.dz_plane}, weight_matrix(a), m0, count, n0, a.width, a.piece, (int)(stages * part / a.splits),
          (int)(stages * (part + 1) / a.splits), to_lds_addr(smem));
   const int lane = lane_id(), n = lane & 15, j = lane >> 4, wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
 #pragma unroll
@@ -323,15 +324,15 @@ template <typename T, bool WIDE> __global__ void __launch_bounds__(256) loss_dx_
 }
 
 // dW of a piece of the vocabulary: added into fp32 accumulators (ADD), or written in bf16.
-template <int BM, int BN, int WM, int WN, bool ADD> __global__ void __launch_bounds__(64 * WM * WN) loss_dw_kernel(const LossArgs a) {
+template <int PAIRS, int BM, int BN, int WM, int WN, bool ADD> __global__ void __launch_bounds__(64 * WM * WN) loss_dw_kernel(const LossArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
-  typedef Product<BM, BN, WM, WN, true, true> P;
+  typedef Product<BM, BN, WM, WN, true, true, PAIRS> P;
   int tm, tn;
   decode_tile(a, blockIdx.x, tm, tn);
   const int m0 = tm * BM, n0 = tn * BN, count = *a.count;
   f32x4 acc[P::MB][P::NB];
-  P::run(acc, Matrix{a.dz, a.dz_ld, a.dz_plane}, Matrix{a.rows, a.width, a.rows_plane}, m0, a.dz_ld, n0, a.width, count, a.pairs, 0,
-         ((count + kDepth - 1) / kDepth) * a.pairs, to_lds_addr(smem));
+  P::run(acc, Matrix{a.dz, a.dz_ld, a.dz_plane}, Matrix{a.rows, a.width, a.rows_plane}, m0, a.dz_ld, n0, a.width, count, 0,
+         (count + kDepth - 1) / kDepth * PAIRS, to_lds_addr(smem));
   const int lane = lane_id(), n = lane & 15, j = lane >> 4, wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
 #pragma unroll
   for (int mb = 0; mb < P::MB; ++mb) {
@@ -483,7 +484,6 @@ LossArgs args_of(const s1f_rows *d, const LossPlan &p, const int64_t *targets, i
   a.dz_plane = p.n * a.dz_ld;
   a.part = reinterpret_cast<float *>(ws + p.part);
   a.direct = p.direct;
-  a.pairs = p.planes == 3 ? 6 : 1;
   a.splits = p.splits;
   return a;
 }
@@ -500,11 +500,11 @@ template <typename T> int forward(const s1f_rows *d, LossArgs a, const LossPlan 
     if (!p.direct) e = pack<T>(a, false, wide_weight(d, a.weight_stride), a.piece, st);
     if (e != S1F_OK) break;
     if (small) {
-      typedef Product<64, 128, 1, 4, false, false> P;
+      typedef Product<64, 128, 1, 4, false, false, 1> P;   // (sizes do not depend on the last)
       tiles_of(a, p.n, a.piece, 64, 128);
       e = launch_tiles<&loss_scores_kernel<T, 64, 128, 1, 4, true>>(P::LDS_BYTES, P::THREADS, (int64_t)a.tiles_m * a.tiles_n, a, st);
     } else {
-      typedef Product<256, 256, 2, 4, false, false> P;
+      typedef Product<256, 256, 2, 4, false, false, 1> P;
       tiles_of(a, p.n, a.piece, 256, 256);
       e = launch_tiles<&loss_scores_kernel<T, 256, 256, 2, 4, true>>(P::LDS_BYTES, P::THREADS, (int64_t)a.tiles_m * a.tiles_n, a, st);
     }
@@ -515,6 +515,7 @@ template <typename T> int forward(const s1f_rows *d, LossArgs a, const LossPlan 
 }
 
 template <typename T, bool ADD> int backward(const s1f_rows *d, LossArgs a, const LossPlan &p, hipStream_t st) {
+  constexpr int PAIRS = sizeof(T) == 4 ? 6 : 1;
   int e = launch_rows_kernel(&loss_rows_kernel<false>, 1, 1024, a, st);
   if (e == S1F_OK) e = pack<T>(a, true, wide_x(d, a.x), p.n, st);
   for (int64_t at = 0; at < a.vocab && e == S1F_OK; at += p.piece) {
@@ -524,22 +525,22 @@ template <typename T, bool ADD> int backward(const s1f_rows *d, LossArgs a, cons
     if (!p.direct) e = pack<T>(a, false, wide_weight(d, a.weight_stride), a.piece, st);
     if (e != S1F_OK) break;
     {
-      typedef Product<256, 256, 2, 4, false, false> P;
+      typedef Product<256, 256, 2, 4, false, false, 1> P;
       tiles_of(a, p.n, a.piece, 256, 256);
       e = launch_tiles<&loss_scores_kernel<T, 256, 256, 2, 4, false>>(P::LDS_BYTES, P::THREADS, (int64_t)a.tiles_m * a.tiles_n, a, st);
     }
     if (e != S1F_OK) break;
     {
-      typedef Product<256, 256, 2, 4, false, true> P;
+      typedef Product<256, 256, 2, 4, false, true, 1> P;
       tiles_of(a, p.n, a.width, 256, 256);
-      e = launch_tiles<&loss_dx_kernel<256, 256, 2, 4>>(P::LDS_BYTES, P::THREADS, (int64_t)a.tiles_m * a.tiles_n * a.splits, a, st);
+      e = launch_tiles<&loss_dx_kernel<PAIRS, 256, 256, 2, 4>>(P::LDS_BYTES, P::THREADS, (int64_t)a.tiles_m * a.tiles_n * a.splits, a, st);
     }
     if (e != S1F_OK) break;
     {
-      typedef Product<256, 256, 2, 4, true, true> P;
+      typedef Product<256, 256, 2, 4, true, true, 1> P;
       tiles_of(a, a.piece, a.width, 256, 256);
       a.wide = on16(a.dweight) && a.dweight_stride % 4 == 0;
-      e = launch_tiles<&loss_dw_kernel<256, 256, 2, 4, ADD>>(P::LDS_BYTES, P::THREADS, (int64_t)a.tiles_m * a.tiles_n, a, st);
+      e = launch_tiles<&loss_dw_kernel<PAIRS, 256, 256, 2, 4, ADD>>(P::LDS_BYTES, P::THREADS, (int64_t)a.tiles_m * a.tiles_n, a, st);
     }
   }
   if (e != S1F_OK) return e;
