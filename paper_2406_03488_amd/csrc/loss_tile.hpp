@@ -19,14 +19,29 @@ namespace s1f {
 
 constexpr int kDepth = 64;   // contraction per stage
 
+template <int N> struct Int {
+  static constexpr int value = N;
+};
+template <int N, int I = 0, typename F> S1F_DEV void for_each(F &&f) {   // f(Int<0>{}) .. f(Int<N - 1>{})
+  if constexpr (I < N) {
+    f(Int<I>{});
+    for_each<N, I + 1>(f);
+  }
+}
+S1F_DEV const char *uniform_pointer(const char *p) {
+  const uint64_t bits = reinterpret_cast<uint64_t>(p);
+  return reinterpret_cast<const char *>(((uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(bits >> 32)) << 32) |
+                                        (uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)bits));
+}
+
 // R: rows of C (or columns of C, for the other operand) in the tile; TR: stored by columns; NW: waves that copy.
 template <int R, bool TR, int NW> struct Side {
   static constexpr int BYTES = R * kDepth * 2, PIECES = BYTES / 1024, PER_WAVE = PIECES / NW;
-  static_assert(PIECES % NW == 0 && PER_WAVE <= 4, "pieces of a wave share one M0");
+  static_assert(PIECES % NW == 0 && (PER_WAVE <= 4 || PER_WAVE == 8), "up to four pieces share one M0");
   static constexpr int ROW = TR ? 2 * R : 128, CHUNKS = ROW / 16, RPP = 1024 / ROW;   // bytes and chunks of a row, rows per piece
   S1F_DEV static int h(int k) { return R >= 128 ? (k & 3) | ((k >> 3) & 1) << 2 : ((k >> 1) & 1) | ((k >> 3) & 1) << 1; }
 
-  static constexpr int BIAS = 1024 * (PER_WAVE - 1);
+  static constexpr int GROUP = PER_WAVE < 4 ? PER_WAVE : 4, BIAS = 1024 * (GROUP - 1);
   const char *next;         // of the stage that is copied next, less BIAS (uniform)
   int64_t step;             // bytes to the next stage
   unsigned voff[PER_WAVE];  // of the lane's chunk in each of the wave's pieces
@@ -53,45 +68,26 @@ template <int R, bool TR, int NW> struct Side {
         if (m0 + r >= limit) r = (int)(limit - 1 - m0);
       }
       // (the immediate offset of a copy instruction counts for its address in memory as well as in LDS)
-      voff[i] = (unsigned)(r * row_bytes + 16 * c) + (unsigned)(BIAS - 1024 * i);
+      voff[i] = (unsigned)(r * row_bytes + 16 * c) + (unsigned)(BIAS - 1024 * (i % GROUP));
     }
   }
-  // Copies a stage at `from` to LDS address `dst`.
-  template <bool TAIL> S1F_DEV void issue(const char *from, lds_addr dst, int left, int wave, int lane) const {
-    unsigned off[PER_WAVE];
+  // From here on stages hold `left` of their contraction: what is behind is read from the stage's beginning, and cleared by clear_tail.
+  S1F_DEV void shorten(int left, int wave, int lane) {
 #pragma unroll
-    for (int i = 0; i < PER_WAVE; ++i) off[i] = voff[i];
-    if constexpr (TAIL) {   // `left` of the stage's contraction are there: what is behind is read from its beginning, and cleared by clear_tail
-#pragma unroll
-      for (int i = 0; i < PER_WAVE; ++i) {
-        int r, c;
-        slot(wave * PER_WAVE + i, lane, r, c);
-        if (TR) {
-          if (r >= left) off[i] -= (unsigned)(r * row_bytes);
-        } else {
-          if (8 * c >= left) off[i] -= (unsigned)(16 * c);
-        }
+    for (int i = 0; i < PER_WAVE; ++i) {
+      int r, c;
+      slot(wave * PER_WAVE + i, lane, r, c);
+      if (TR) {
+        if (r >= left) voff[i] -= (unsigned)(r * row_bytes);
+      } else {
+        if (8 * c >= left) voff[i] -= (unsigned)(16 * c);
       }
     }
-    const uint64_t bits = reinterpret_cast<uint64_t>(from);
-    const char *b = reinterpret_cast<const char *>(
-        ((uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(bits >> 32)) << 32) |
-        (uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)bits));
-    const unsigned to = __builtin_amdgcn_readfirstlane(dst + (unsigned)(wave * PER_WAVE * 1024));
-    if constexpr (PER_WAVE == 4)
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\t"
-                   "global_load_lds_dwordx4 %2, %5 offset:1024\n\t"
-                   "global_load_lds_dwordx4 %3, %5 offset:2048\n\t"
-                   "global_load_lds_dwordx4 %4, %5 offset:3072"
-                   : : "s"(to), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(b) : "m0");
-    else if constexpr (PER_WAVE == 2)
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\t"
-                   "global_load_lds_dwordx4 %2, %3 offset:1024"
-                   : : "s"(to), "v"(off[0]), "v"(off[1]), "s"(b) : "m0");
-    else {
-      static_assert(PER_WAVE == 1, "one, two or four pieces");
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(off[0]), "s"(b) : "m0");
-    }
+  }
+  // Copies piece I of the wave's pieces of a stage at `from` (uniform) to LDS address `dst` (of the wave's first piece; uniform).
+  template <int I> S1F_DEV void copy(const char *from, unsigned dst) const {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 offset:%3"
+                 : : "s"(dst + 1024 * (I / GROUP * GROUP)), "v"(voff[I]), "s"(from), "n"(1024 * (I % GROUP)) : "m0");
   }
   // Zeros in the wave's own slots behind the end of the contraction, once its copies have landed.
   S1F_DEV void clear_tail(lds_addr at, int left, int wave, int lane) const {
@@ -165,25 +161,39 @@ template <int BM, int BN, int WM, int WN, bool TRA, bool TRB, int PAIRS> struct 
     int pair = begin % PAIRS;                       // of the stage that is copied next
     const int left = (int)((k - 1) % kDepth) + 1;   // contraction of the last stage
     const int tail = left < kDepth ? (int)((k - 1) / kDepth) * PAIRS : 0x7fffffff;   // first stage that is not whole
-    // copies stage t to `dst`
-    auto issue = [&](int t, lds_addr dst) {
-      const char *from_a = sa.next, *from_b = sb.next;
+    // Where stage t is copied from; the pieces of A come first.
+    const char *from_a, *from_b;
+    unsigned to;
+    auto begin_copy = [&](int t, lds_addr dst) {
+      if (t == tail || (t == begin && t > tail)) {
+        sa.shorten(left, wave, lane);
+        sb.shorten(left, wave, lane);
+      }
+      from_a = sa.next;
+      from_b = sb.next;
       if constexpr (PAIRS == 6) {   // (2,0) (0,2) (1,1) (1,0) (0,1) (0,0): smallest products first
         from_a += (int64_t)((0x001102u >> (4 * pair)) & 3u) * a.plane * 2;
         from_b += (int64_t)((0x010120u >> (4 * pair)) & 3u) * b.plane * 2;
       }
-      if (t < tail) {
-        sa.template issue<false>(from_a, dst, kDepth, wave, lane);
-        sb.template issue<false>(from_b, dst + SA::BYTES, kDepth, wave, lane);
-      } else {
-        sa.template issue<true>(from_a, dst, left, wave, lane);
-        sb.template issue<true>(from_b, dst + SA::BYTES, left, wave, lane);
-      }
+      from_a = uniform_pointer(from_a);
+      from_b = uniform_pointer(from_b);
+      to = __builtin_amdgcn_readfirstlane(dst);
       if (PAIRS == 1 || ++pair == PAIRS) {
         pair = 0;
         sa.next += sa.step;
         sb.next += sb.step;
       }
+    };
+    const unsigned to_a = wave * SA::PER_WAVE * 1024, to_b = SA::BYTES + wave * SB::PER_WAVE * 1024;
+    auto copy_piece = [&](auto i) {
+      constexpr int I = decltype(i)::value;
+      if constexpr (I < SA::PER_WAVE) sa.template copy<I>(from_a, to + to_a);
+      else sb.template copy<I - SA::PER_WAVE>(from_b, to + to_b);
+    };
+    constexpr int PIECES = SA::PER_WAVE + SB::PER_WAVE;
+    auto issue = [&](int t, lds_addr dst) {
+      begin_copy(t, dst);
+      for_each<PIECES>(copy_piece);
     };
     auto landed = [&](int t, lds_addr at) {        // this wave's copies of stage t are there
       if (t >= tail) {
@@ -207,24 +217,30 @@ template <int BM, int BN, int WM, int WN, bool TRA, bool TRB, int PAIRS> struct 
     bf16x8 fa[2][MB], fb[2][NB];
     const lds_addr lane_a = SA::at(wm * MB, lane), lane_b = SA::BYTES + SB::at(wn * NB, lane);
     constexpr int OPERANDS = MB + NB, PER_SLOT = (OPERANDS * 4 + 3 * MB - 1) / (3 * MB);   // read in the first three quarters of the products
-    // Products of one half, and the reads of the operands of the next: a slot for each row of blocks, nothing moves across its end.
-    auto half_stage = [&](bf16x8 (&ra)[MB], bf16x8 (&rb)[NB], const bf16x8 (&xa)[MB], const bf16x8 (&xb)[NB], lds_addr at, int half, auto between) {
-      const lds_addr pa = SA::half_of(at + lane_a, half), pb = SB::half_of(at + lane_b, half);
-#pragma unroll
-      for (int i = 0; i < MB; ++i) {
+    // Products of one half, and the reads of the operands of the next: a slot for each row of blocks, nothing moves across its end.  COPY: and the
+    // wave's copies, spread over the slots: a wave issues in order, and copies of all waves one right behind the other fill the queues
+    // of the memory pipe, in front of which they then wait with their products behind them (scores of 6144 x 7168 x 100003 6.6 ms so).
+    auto half_stage = [&](bf16x8 (&ra)[MB], bf16x8 (&rb)[NB], const bf16x8 (&xa)[MB], const bf16x8 (&xb)[NB], lds_addr at, auto second, auto copies) {
+      constexpr int HALF = decltype(second)::value;
+      constexpr bool COPY = decltype(copies)::value != 0;
+      const lds_addr pa = SA::half_of(at + lane_a, HALF), pb = SB::half_of(at + lane_b, HALF);
+      for_each<MB>([&](auto slot) {
+        constexpr int i = decltype(slot)::value;
 #pragma unroll
         for (int r = 0; r < PER_SLOT; ++r) {
           const int o = i * PER_SLOT + r;
-          if (o < NB) rb[o] = SB::operand(pb, o, half);
-          else if (o < OPERANDS) ra[o - NB] = SA::operand(pa, o - NB, half);
+          if (o < NB) rb[o] = SB::operand(pb, o, HALF);
+          else if (o < OPERANDS) ra[o - NB] = SA::operand(pa, o - NB, HALF);
         }
 #pragma unroll
         for (int j = 0; j < NB; ++j) acc[i][j] = mma16(xb[j], xa[i], acc[i][j]);
-        if (i == 0) between();
+        if constexpr (COPY) {
+          constexpr int FIRST = i * PIECES / MB, COUNT = (i + 1) * PIECES / MB - FIRST;
+          for_each<COUNT>([&](auto p) { copy_piece(Int<FIRST + decltype(p)::value>{}); });
+        }
         __builtin_amdgcn_sched_barrier(0);
-      }
+      });
     };
-    auto nothing = [] {};
     {
       const lds_addr pa = SA::half_of(cur + lane_a, 0), pb = SB::half_of(cur + lane_b, 0);
 #pragma unroll
@@ -232,19 +248,23 @@ template <int BM, int BN, int WM, int WN, bool TRA, bool TRB, int PAIRS> struct 
 #pragma unroll
       for (int i = 0; i < MB; ++i) fa[0][i] = SA::operand(pa, i, 0);
     }
-    for (int t = begin; t < end; ++t) {
+    int t = begin;
+    auto step = [&](auto copies) {
       __builtin_amdgcn_sched_barrier(0);
-      half_stage(fa[1], fb[1], fa[0], fb[0], cur, 1, nothing);
+      half_stage(fa[1], fb[1], fa[0], fb[0], cur, Int<1>{}, Int<0>{});
       asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
       landed(t + 1, next);   // (behind the last stage: clears what nobody reads)
       __syncthreads();
       __builtin_amdgcn_sched_barrier(0);
-      // (behind the last stage: reads what an earlier one has left, and nothing uses it)
-      half_stage(fa[0], fb[0], fa[1], fb[1], next, 0, [&] { if (t + 2 < end) issue(t + 2, cur); });
+      if constexpr (decltype(copies)::value != 0) begin_copy(t + 2, cur);
+      half_stage(fa[0], fb[0], fa[1], fb[1], next, Int<0>{}, copies);   // (behind the last stage: reads what is left there, and nothing uses it)
       const lds_addr was = cur;
       cur = next;
       next = was;
-    }
+      ++t;
+    };
+    while (t + 2 < end) step(Int<1>{});
+    while (t < end) step(Int<0>{});
     __syncthreads();
   }
 };
