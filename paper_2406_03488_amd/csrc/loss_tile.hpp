@@ -143,7 +143,7 @@ template <int BM, int BN, int WM, int WN, bool TRA, bool TRB, int PAIRS> struct 
   static constexpr int NW = WM * WN, THREADS = 64 * NW, MB = BM / WM / 16, NB = BN / WN / 16;
   typedef Side<BM, TRA, NW> SA;
   typedef Side<BN, TRB, NW> SB;
-  static constexpr int STAGE = SA::BYTES + SB::BYTES, LDS_BYTES = 2 * STAGE;
+  static constexpr int LDS_BYTES = 3 * SA::BYTES + 2 * SB::BYTES;
 
   // k: contraction; stages [begin, end) of it, counted in stages of a product of planes, the PAIRS of each one after the other
   S1F_DEV static void run(f32x4 (&acc)[MB][NB], const Matrix &a, const Matrix &b, int64_t m0, int64_t m_limit, int64_t n0, int64_t n_limit,
@@ -158,72 +158,66 @@ template <int BM, int BN, int WM, int WN, bool TRA, bool TRB, int PAIRS> struct 
     SB sb;
     sa.init(a.data, a.ld, m0, m_limit, begin / PAIRS, wave, lane);
     sb.init(b.data, b.ld, n0, n_limit, begin / PAIRS, wave, lane);
-    int pair = begin % PAIRS;                       // of the stage that is copied next
     const int left = (int)((k - 1) % kDepth) + 1;   // contraction of the last stage
     const int tail = left < kDepth ? (int)((k - 1) / kDepth) * PAIRS : 0x7fffffff;   // first stage that is not whole
-    // Where stage t is copied from; the pieces of A come first.
+    // Where a side's stage t is copied from, and to.  Calls are for consecutive stages.
     const char *from_a, *from_b;
-    unsigned to;
-    auto begin_copy = [&](int t, lds_addr dst) {
-      if (t == tail || (t == begin && t > tail)) {
-        sa.shorten(left, wave, lane);
-        sb.shorten(left, wave, lane);
-      }
-      from_a = sa.next;
-      from_b = sb.next;
-      if constexpr (PAIRS == 6) {   // (2,0) (0,2) (1,1) (1,0) (0,1) (0,0): smallest products first
-        from_a += (int64_t)((0x001102u >> (4 * pair)) & 3u) * a.plane * 2;
-        from_b += (int64_t)((0x010120u >> (4 * pair)) & 3u) * b.plane * 2;
-      }
-      from_a = uniform_pointer(from_a);
-      from_b = uniform_pointer(from_b);
-      to = __builtin_amdgcn_readfirstlane(dst);
+    unsigned to_a, to_b;
+    int pair_a = begin % PAIRS, pair_b = pair_a;
+    auto begin_copy = [&](auto &side, const Matrix &m, unsigned order, int &pair, const char *&from, unsigned &to, int t, lds_addr dst) {
+      if (t == tail || (t == begin && t > tail)) side.shorten(left, wave, lane);
+      from = side.next;
+      if constexpr (PAIRS == 6) from += (int64_t)((order >> (4 * pair)) & 3u) * m.plane * 2;
+      from = uniform_pointer(from);
+      to = __builtin_amdgcn_readfirstlane(dst + (unsigned)(wave * side.PER_WAVE * 1024));
       if (PAIRS == 1 || ++pair == PAIRS) {
         pair = 0;
-        sa.next += sa.step;
-        sb.next += sb.step;
+        side.next += side.step;
       }
     };
-    const unsigned to_a = wave * SA::PER_WAVE * 1024, to_b = SA::BYTES + wave * SB::PER_WAVE * 1024;
-    auto copy_piece = [&](auto i) {
-      constexpr int I = decltype(i)::value;
-      if constexpr (I < SA::PER_WAVE) sa.template copy<I>(from_a, to + to_a);
-      else sb.template copy<I - SA::PER_WAVE>(from_b, to + to_b);
-    };
-    constexpr int PIECES = SA::PER_WAVE + SB::PER_WAVE;
-    auto issue = [&](int t, lds_addr dst) {
-      begin_copy(t, dst);
-      for_each<PIECES>(copy_piece);
-    };
-    auto landed = [&](int t, lds_addr at) {        // this wave's copies of stage t are there
+    // planes of the pairs: (2,0) (0,2) (1,1) (1,0) (0,1) (0,0), smallest products first
+    auto begin_a = [&](int t, lds_addr dst) { begin_copy(sa, a, 0x001102u, pair_a, from_a, to_a, t, dst); };
+    auto begin_b = [&](int t, lds_addr dst) { begin_copy(sb, b, 0x010120u, pair_b, from_b, to_b, t, dst); };
+    auto piece_a = [&](auto i) { sa.template copy<decltype(i)::value>(from_a, to_a); };
+    auto piece_b = [&](auto i) { sb.template copy<decltype(i)::value>(from_b, to_b); };
+    constexpr int PA = SA::PER_WAVE, PB = SB::PER_WAVE;
+    auto landed = [&](int t, lds_addr at_a, lds_addr at_b) {        // this wave's copies of stage t are there
       if (t >= tail) {
-        sa.clear_tail(at, left, wave, lane);
-        sb.clear_tail(at + SA::BYTES, left, wave, lane);
+        sa.clear_tail(at_a, left, wave, lane);
+        sb.clear_tail(at_b, left, wave, lane);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       }
     };
-    lds_addr cur = lds, next = lds + STAGE;
-    issue(begin, cur);
+    // Three places for stages of A, two for those of B: all that LDS holds of 256 x 256 tiles.
+    lds_addr a0 = lds, a1 = lds + SA::BYTES, a2 = a1 + SA::BYTES, b0 = a2 + SA::BYTES, b1 = b0 + SB::BYTES;
+    begin_a(begin, a0);
+    for_each<PA>(piece_a);
+    begin_b(begin, b0);
+    for_each<PB>(piece_b);
     if (begin + 1 < end) {
-      issue(begin + 1, next);
-      wait_async_tiles_but_last<SA::PER_WAVE + SB::PER_WAVE>();
+      begin_a(begin + 1, a1);
+      for_each<PA>(piece_a);
+      begin_b(begin + 1, b1);
+      for_each<PB>(piece_b);
+      wait_async_tiles_but_last<PA + PB>();
     } else {
       wait_async_tiles();
     }
-    landed(begin, cur);
+    landed(begin, a0, b0);
     __syncthreads();
     // Operands are read half a stage ahead of the products that take them.  When the products of a stage's first half are through,
-    // nobody reads that stage any more and the next one has been on its way for a whole stage: one barrier per stage does for both.
+    // nobody reads that stage any more: one barrier per stage says so, and that the next one has landed.  Behind it B's stage after the next is
+    // copied into the place that has become free, and under the first half of the next stage A's stage after that.
     bf16x8 fa[2][MB], fb[2][NB];
-    const lds_addr lane_a = SA::at(wm * MB, lane), lane_b = SA::BYTES + SB::at(wn * NB, lane);
+    const lds_addr lane_a = SA::at(wm * MB, lane), lane_b = SB::at(wn * NB, lane);
     constexpr int OPERANDS = MB + NB, PER_SLOT = (OPERANDS * 4 + 3 * MB - 1) / (3 * MB);   // read in the first three quarters of the products
-    // Products of one half, and the reads of the operands of the next: a slot for each row of blocks, nothing moves across its end.  COPY: and the
-    // wave's copies, spread over the slots: a wave issues in order, and copies of all waves one right behind the other fill the queues
-    // of the memory pipe, in front of which they then wait with their products behind them (scores of 6144 x 7168 x 100003 6.6 ms so).
-    auto half_stage = [&](bf16x8 (&ra)[MB], bf16x8 (&rb)[NB], const bf16x8 (&xa)[MB], const bf16x8 (&xb)[NB], lds_addr at, auto second, auto copies) {
-      constexpr int HALF = decltype(second)::value;
-      constexpr bool COPY = decltype(copies)::value != 0;
-      const lds_addr pa = SA::half_of(at + lane_a, HALF), pb = SB::half_of(at + lane_b, HALF);
+    // Products of one half, and the reads of the operands of the next: a slot for each row of blocks, nothing moves across its end.  The wave's copies
+    // are spread over the slots: a wave issues in order, and copies of all waves one right behind the other fill the queues of the memory
+    // pipe, in front of which they then wait with their products behind them.
+    auto half_stage = [&](bf16x8 (&ra)[MB], bf16x8 (&rb)[NB], const bf16x8 (&xa)[MB], const bf16x8 (&xb)[NB], lds_addr at_a, lds_addr at_b, auto second,
+                          auto pieces, auto piece) {
+      constexpr int HALF = decltype(second)::value, PIECES = decltype(pieces)::value;
+      const lds_addr pa = SA::half_of(at_a + lane_a, HALF), pb = SB::half_of(at_b + lane_b, HALF);
       for_each<MB>([&](auto slot) {
         constexpr int i = decltype(slot)::value;
 #pragma unroll
@@ -234,33 +228,37 @@ template <int BM, int BN, int WM, int WN, bool TRA, bool TRB, int PAIRS> struct 
         }
 #pragma unroll
         for (int j = 0; j < NB; ++j) acc[i][j] = mma16(xb[j], xa[i], acc[i][j]);
-        if constexpr (COPY) {
-          constexpr int FIRST = i * PIECES / MB, COUNT = (i + 1) * PIECES / MB - FIRST;
-          for_each<COUNT>([&](auto p) { copy_piece(Int<FIRST + decltype(p)::value>{}); });
-        }
+        constexpr int FIRST = i * PIECES / MB, COUNT = (i + 1) * PIECES / MB - FIRST;
+        for_each<COUNT>([&](auto p) { piece(Int<FIRST + decltype(p)::value>{}); });
         __builtin_amdgcn_sched_barrier(0);
       });
     };
     {
-      const lds_addr pa = SA::half_of(cur + lane_a, 0), pb = SB::half_of(cur + lane_b, 0);
+      const lds_addr pa = SA::half_of(a0 + lane_a, 0), pb = SB::half_of(b0 + lane_b, 0);
 #pragma unroll
       for (int j = 0; j < NB; ++j) fb[0][j] = SB::operand(pb, j, 0);
 #pragma unroll
       for (int i = 0; i < MB; ++i) fa[0][i] = SA::operand(pa, i, 0);
     }
     int t = begin;
-    auto step = [&](auto copies) {
+    auto step = [&](auto copies) {   // copies: whether there is a stage t + 2
+      constexpr int C = decltype(copies)::value;
+      if constexpr (C) begin_a(t + 2, a2);
       __builtin_amdgcn_sched_barrier(0);
-      half_stage(fa[1], fb[1], fa[0], fb[0], cur, Int<1>{}, Int<0>{});
-      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-      landed(t + 1, next);   // (behind the last stage: clears what nobody reads)
+      half_stage(fa[1], fb[1], fa[0], fb[0], a0, b0, Int<1>{}, Int<C * PA>{}, piece_a);
+      if constexpr (C) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(PA) : "memory");
+      else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+      landed(t + 1, a1, b1);   // (behind the last stage: clears what nobody reads)
       __syncthreads();
+      if constexpr (C) begin_b(t + 2, b0);
       __builtin_amdgcn_sched_barrier(0);
-      if constexpr (decltype(copies)::value != 0) begin_copy(t + 2, cur);
-      half_stage(fa[0], fb[0], fa[1], fb[1], next, Int<0>{}, copies);   // (behind the last stage: reads what is left there, and nothing uses it)
-      const lds_addr was = cur;
-      cur = next;
-      next = was;
+      half_stage(fa[0], fb[0], fa[1], fb[1], a1, b1, Int<0>{}, Int<C * PB>{}, piece_b);   // (behind the last stage: reads that nothing uses)
+      const lds_addr was_a = a0, was_b = b0;
+      a0 = a1;
+      a1 = a2;
+      a2 = was_a;
+      b0 = b1;
+      b1 = was_b;
       ++t;
     };
     while (t + 2 < end) step(Int<1>{});
