@@ -33,6 +33,7 @@ struct LossArgs {
   // workspace
   int32_t *count, *row_of, *slot_of, *target_of;   // counted rows; their numbers; a row's place among them (-1: none); targets
   float *target_score;                             // [slot]
+  float *of_row;                                   // [slot][lse, dloss]
   float *stats;                                    // [tile of the vocabulary][slot][maximum, sum]
   bf16_t *rows, *packed, *dz;                      // counted rows; a piece of the weight; dz of the piece: planes of [.][width] or [.][dz_ld]
   int64_t rows_plane, packed_plane, dz_plane, dz_ld;
@@ -104,6 +105,10 @@ template <typename T, bool WIDE, bool ROWS> __global__ void __launch_bounds__(25
   const int c = (int)(id - row64 * per_row);
   if (row64 >= (ROWS ? *a.count : a.piece)) return;
   const int row = (int)row64;
+  if (ROWS && c == 0 && a.dloss) {   // (backward)
+    a.of_row[2 * row] = a.lse_in[a.row_of[row]];
+    a.of_row[2 * row + 1] = a.dloss[a.row_of[row]];
+  }
   const T *from = ROWS ? reinterpret_cast<const T *>(a.x) + a.xs.offset(a.row_of[row])
                        : reinterpret_cast<const T *>(a.weight) + (a.first + row) * a.weight_stride;
   float v[8];
@@ -171,29 +176,50 @@ __global__ void __launch_bounds__(64 * WM * WN) loss_scores_kernel(const LossArg
   P::run(acc, Matrix{a.rows, a.width, a.rows_plane}, weight_matrix(a), m0, count, n0, a.piece, a.width, 0,
          (a.width + kDepth - 1) / kDepth * PAIRS, to_lds_addr(smem));
   const int lane = lane_id(), n = lane & 15, j = lane >> 4, wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
+  // A tile's results cost the vector unit about as long as four stages of products the matrix unit, so nothing is asked per element that can be
+  // asked per tile or per 16 rows: whether the vocabulary ends in it, and whether a lane holds its row's target (one tile in hundreds).
+  const int col0 = 16 * wn * P::NB + 4 * j;   // the lane's columns of the tile: col0 + 16 * nb + e
+  const bool edge = n0 + BN > a.piece;
+  int target[P::MB];                          // the lane's element 4 * nb + e that is its row's target, or none
+#pragma unroll
+  for (int mb = 0; mb < P::MB; ++mb) {
+    const int slot = m0 + 16 * (wm * P::MB + mb) + n, t = (slot < count ? a.target_of[slot] : -1) - a.first - n0 - col0;
+    target[mb] = t >= 0 && t < 16 * P::NB && (t & 15) < 4 ? (t >> 4) * 4 + (t & 3) : -1;
+  }
   if constexpr (STATS) {
     float *red = reinterpret_cast<float *>(smem);     // [WN][BM][maximum, sum]
+    if (edge) {
+#pragma unroll
+      for (int nb = 0; nb < P::NB; ++nb)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (n0 + col0 + 16 * nb + e >= a.piece) {
+#pragma unroll
+            for (int mb = 0; mb < P::MB; ++mb) acc[mb][nb][e] = -INFINITY;
+          }
+    }
 #pragma unroll
     for (int mb = 0; mb < P::MB; ++mb) {
-      const int in_tile = 16 * (wm * P::MB + mb) + n, slot = m0 + in_tile;
-      const int target = (slot < count ? a.target_of[slot] : -1) - a.first;
+      const int in_tile = 16 * (wm * P::MB + mb) + n;
+      if (target[mb] >= 0) {
+#pragma unroll
+        for (int nb = 0; nb < P::NB; ++nb)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (target[mb] == 4 * nb + e) a.target_score[m0 + in_tile] = acc[mb][nb][e];
+      }
       float most = -INFINITY;
 #pragma unroll
       for (int nb = 0; nb < P::NB; ++nb)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int col = n0 + 16 * (wn * P::NB + nb) + 4 * j + e;
-          if (col == target) a.target_score[slot] = acc[mb][nb][e];
-          if (col >= a.piece) acc[mb][nb][e] = -INFINITY;
-          most = fmaxf(most, acc[mb][nb][e]);
-        }
+        for (int e = 0; e < 4; ++e) most = fmaxf(most, acc[mb][nb][e]);
       most = max_over_rows(most);
-      const float from = most == -INFINITY ? 0.f : most;
+      const float from = most == -INFINITY ? 0.f : most * kLog2e;
       float sum = 0.f;
 #pragma unroll
       for (int nb = 0; nb < P::NB; ++nb)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum += exp2_fast((acc[mb][nb][e] - from) * kLog2e);
+        for (int e = 0; e < 4; ++e) sum += exp2_fast(fmaf(acc[mb][nb][e], kLog2e, -from));
       sum = sum_over_rows(sum);
       if (j == 0) {
         red[2 * (wn * BM + in_tile)] = most;
@@ -205,37 +231,54 @@ __global__ void __launch_bounds__(64 * WM * WN) loss_scores_kernel(const LossArg
       float most = red[2 * r], sum = 0.f;
 #pragma unroll
       for (int w = 1; w < WN; ++w) most = fmaxf(most, red[2 * (w * BM + r)]);
-      const float from = most == -INFINITY ? 0.f : most;
+      const float from = most == -INFINITY ? 0.f : most * kLog2e;
 #pragma unroll
-      for (int w = 0; w < WN; ++w) sum += red[2 * (w * BM + r) + 1] * exp2_fast((red[2 * (w * BM + r)] - from) * kLog2e);
+      for (int w = 0; w < WN; ++w) sum += red[2 * (w * BM + r) + 1] * exp2_fast(fmaf(red[2 * (w * BM + r)], kLog2e, -from));
       float *to = a.stats + 2 * ((int64_t)(a.first / BN + tn) * a.n + m0 + r);
       to[0] = most;
       to[1] = sum;
     }
   } else {
+    float lse[P::MB], g[P::MB];
+#pragma unroll
+    for (int mb = 0; mb < P::MB; ++mb) {
+      const int slot = m0 + 16 * (wm * P::MB + mb) + n, at = slot < count ? slot : count - 1;
+      lse[mb] = a.of_row[2 * at];
+      g[mb] = a.of_row[2 * at + 1];
+    }
 #pragma unroll
     for (int mb = 0; mb < P::MB; ++mb) {
       const int slot = m0 + 16 * (wm * P::MB + mb) + n;
+      // exp((z - lse) log2 e) as two roundings: the difference, which is exact or small, first
+#pragma unroll
+      for (int nb = 0; nb < P::NB; ++nb)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[mb][nb][e] = exp2_fast((acc[mb][nb][e] - lse[mb]) * kLog2e);
+      if (target[mb] >= 0) {
+#pragma unroll
+        for (int nb = 0; nb < P::NB; ++nb)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (target[mb] == 4 * nb + e) acc[mb][nb][e] -= 1.f;
+      }
       if (slot >= count) continue;
-      const int target = a.target_of[slot] - a.first, row = a.row_of[slot];
-      const float lse = a.lse_in[row], g = a.dloss[row];
 #pragma unroll
       for (int nb = 0; nb < P::NB; ++nb) {
-        const int col = n0 + 16 * (wn * P::NB + nb) + 4 * j;
-        f32x4 d;
+        const int col = n0 + col0 + 16 * nb;
+        f32x4 d = acc[mb][nb] * g[mb];
+        if (edge) {
+          if (col >= a.dz_ld) continue;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float p = exp2_fast((acc[mb][nb][e] - lse) * kLog2e) - (col + e == target ? 1.f : 0.f);
-          d[e] = col + e < a.piece ? p * g : 0.f;
+          for (int e = 0; e < 4; ++e)
+            if (col + e >= a.piece) d[e] = 0.f;
         }
-        if (col >= a.dz_ld) continue;
         bf16_t *to = a.dz + (int64_t)slot * a.dz_ld + col;
         if constexpr (sizeof(T) == 4) {
           typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-          const Planes p = split3(d, f32x4{0.f, 0.f, 0.f, 0.f});
+          const Planes q = split3(d, f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
           for (int i = 0; i < 3; ++i) {
-            const u32x4 v = __builtin_bit_cast(u32x4, p.p[i]);
+            const u32x4 v = __builtin_bit_cast(u32x4, q.p[i]);
             *reinterpret_cast<u32x2 *>(to + i * a.dz_plane) = u32x2{v[0], v[1]};
           }
         } else {
@@ -377,7 +420,7 @@ struct LossPlan {
   int64_t n, width, planes, piece;
   bool direct;
   int splits;
-  int64_t count, row_of, slot_of, target_of, target_score, stats, rows, packed, dz, part, bytes;   // offsets
+  int64_t count, row_of, slot_of, target_of, target_score, of_row, stats, rows, packed, dz, part, bytes;   // offsets
 };
 
 int check_loss(const s1f_rows *d, int64_t vocab, int64_t weight_stride) {
@@ -424,6 +467,7 @@ LossPlan plan_of(const s1f_rows *d, int64_t vocab, int64_t weight_stride, bool b
   if (backward) {
     const int64_t pairs = p.planes == 3 ? 6 : 1;
     p.splits = splits_for((p.n + kTileBig - 1) / kTileBig * ((p.width + kTileBig - 1) / kTileBig), (p.piece + kDepth - 1) / kDepth * pairs);
+    p.of_row = take(8 * p.n);
     p.dz = take(p.planes * 2 * p.n * up_to(p.piece, 64));
     p.part = take(4 * (int64_t)p.splits * p.n * p.width);
   } else {
@@ -474,6 +518,7 @@ LossArgs args_of(const s1f_rows *d, const LossPlan &p, const int64_t *targets, i
   a.slot_of = reinterpret_cast<int32_t *>(ws + p.slot_of);
   a.target_of = reinterpret_cast<int32_t *>(ws + p.target_of);
   a.target_score = reinterpret_cast<float *>(ws + p.target_score);
+  a.of_row = reinterpret_cast<float *>(ws + p.of_row);
   a.stats = reinterpret_cast<float *>(ws + p.stats);
   a.rows = reinterpret_cast<bf16_t *>(ws + p.rows);
   a.rows_plane = p.n * p.width;
