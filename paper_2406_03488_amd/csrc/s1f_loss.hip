@@ -37,25 +37,30 @@ struct LossArgs {
   float *stats;                                    // [tile of the vocabulary][slot][maximum, sum]
   bf16_t *rows, *packed, *dz;                      // counted rows; a piece of the weight; dz of the piece: planes of [.][width] or [.][dz_ld]
   int64_t rows_plane, packed_plane, dz_plane, dz_ld;
-  float *part;                                     // dx in parts: [part][slot][width]
+  float *sum, *part;                               // dx: [slot][width]; what the parts of a cut tile but the first add: [part - 1][tile][row][column]
   // piece of the vocabulary, and of the launch
-  int32_t first, piece, direct, splits, add, parts, wide;
-  int32_t tiles_m, tiles_n;
-  Divisor by_group, by_n, by_tiles, by_row;
+  int32_t first, piece, direct, add, parts, wide;
+  // tiles of the launch: their grid; the first one; whether a workgroup takes a quarter of one
+  int32_t tiles_m, tiles_n, tile0, quarters;
+  Divisor by_group;                                // 4 * tiles_m
+  // dx: the tiles from `whole` on, `rest` of them, are cut into `splits` parts along the vocabulary
+  int32_t whole, rest, splits;
 };
 
 // ---- rows that count -------------------------------------------------------------------------------------------------------------------
 
-// One workgroup walks the targets, 8 of them per thread at a time.
+// One workgroup walks the targets, 8192 of them at a time: wave w has rows 1024 * e + 64 * w + lane, so that lanes read neighbours and a ballot numbers
+// the rows of a wave (8 neighbours to a thread instead, added up over lanes: 10 us for 4099 rows).
 template <bool FWD> __global__ void __launch_bounds__(1024) loss_rows_kernel(const LossArgs a) {
-  __shared__ int of_wave[16];
+  __shared__ int counted[8][16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int carry = 0;
   for (int at = 0; at < a.n; at += 8192) {
-    int t[8], own = 0;
+    int t[8];
+    uint64_t has[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const int row = at + 8 * threadIdx.x + e;
+      const int row = at + 1024 * e + threadIdx.x;
       t[e] = -1;
       if (row < a.n) {
         int b, r;
@@ -63,32 +68,33 @@ template <bool FWD> __global__ void __launch_bounds__(1024) loss_rows_kernel(con
         const int64_t id = a.targets[b * a.targets_sb + r];
         if (id >= 0 && id < a.vocab) t[e] = (int)id;
       }
-      own += t[e] >= 0;
-    }
-    int x = own;
-    for (int s = 1; s < 64; s *= 2) {
-      const int y = __shfl_up(x, s);
-      if (lane >= s) x += y;
-    }
-    if (lane == 63) of_wave[wave] = x;
-    __syncthreads();
-    int before = carry + x - own;
-    for (int w = 0; w < 16; ++w) {
-      if (w < wave) before += of_wave[w];
-      carry += of_wave[w];
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const int row = at + 8 * threadIdx.x + e;
-      if (row >= a.n) break;
-      a.slot_of[row] = t[e] >= 0 ? before : -1;
-      if (t[e] >= 0) {
-        a.row_of[before] = row;
-        a.target_of[before] = t[e];
-        ++before;
-      } else if (FWD) {
-        a.loss[row] = 0.f;
-        a.lse[row] = 0.f;
+      has[e] = __ballot(t[e] >= 0);
+      if (lane == 0) counted[e][wave] = __builtin_popcountll(has[e]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      int before = carry;
+#pragma unroll
+      for (int w = 0; w < 16; ++w) {
+        const int c = counted[e][w];
+        carry += c;
+        if (w < wave) before += c;
+      }
+      const int row = at + 1024 * e + threadIdx.x;
+      if (row < a.n) {
+        before += __builtin_popcountll(has[e] & ((uint64_t(1) << lane) - 1));
+        a.slot_of[row] = t[e] >= 0 ? before : -1;
+        if (t[e] >= 0) {
+          a.row_of[before] = row;
+          a.target_of[before] = t[e];
+        } else if (FWD) {
+          a.loss[row] = 0.f;
+          a.lse[row] = 0.f;
+        }
       }
     }
     __syncthreads();
@@ -139,7 +145,7 @@ template <typename T, bool WIDE, bool ROWS> __global__ void __launch_bounds__(25
 
 // ---- products --------------------------------------------------------------------------------------------------------------------------
 
-// Workgroup -> tile.  The hardware hands workgroups to the 8 XCDs in turn; each takes consecutive tiles, in blocks of four columns of tiles
+// Number of a tile -> its place.  The hardware hands workgroups to the 8 XCDs in turn; each takes consecutive tiles, in blocks of four columns of tiles
 // walked down the rows, so that the 32 workgroups that an XCD runs side by side share eight row and four column panels in its L2.
 S1F_DEV void decode_tile(const LossArgs &a, int tile, int &tm, int &tn) {
   const int tiles = a.tiles_m * a.tiles_n, per = tiles >> 3;
@@ -155,6 +161,19 @@ S1F_DEV void decode_tile(const LossArgs &a, int tile, int &tm, int &tn) {
     tn = 4 * group + in % left;
   }
 }
+// The number of the tile at a place.
+S1F_DEV int encode_tile(const LossArgs &a, int tm, int tn) {
+  const int tiles = a.tiles_m * a.tiles_n, per = tiles >> 3, group = tn >> 2, left = a.tiles_n - 4 * group;
+  const int tile = 4 * group * a.tiles_m + tm * (left < 4 ? left : 4) + (tn & 3);
+  return tile < per * 8 ? (tile % per) * 8 + tile / per : tile;
+}
+// Workgroup -> tile, or quarter of a tile.
+S1F_DEV void own_tile(const LossArgs &a, int &tm, int &tn) {
+  if (!a.quarters) return decode_tile(a, a.tile0 + blockIdx.x, tm, tn);
+  decode_tile(a, a.tile0 + (blockIdx.x >> 2), tm, tn);
+  tm = 2 * tm + ((blockIdx.x >> 1) & 1);
+  tn = 2 * tn + (blockIdx.x & 1);
+}
 
 S1F_DEV Matrix weight_matrix(const LossArgs &a) {
   return a.direct ? Matrix{reinterpret_cast<const bf16_t *>(a.weight) + a.first * a.weight_stride, a.weight_stride, 0}
@@ -163,15 +182,15 @@ S1F_DEV Matrix weight_matrix(const LossArgs &a) {
 
 // Scores of a tile of rows and vocabulary: STATS: maximum and sum of exponentials of each row (forward); else dz (backward).
 template <typename T, int BM, int BN, int WM, int WN, bool STATS>
-__global__ void __launch_bounds__(64 * WM * WN) loss_scores_kernel(const LossArgs a) {
+__global__ void __launch_bounds__(64 * WM * WN, 2) loss_scores_kernel(const LossArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   constexpr int PAIRS = sizeof(T) == 4 ? 6 : 1;
   typedef Product<BM, BN, WM, WN, false, false, PAIRS> P;
   const int count = *a.count;
   int tm, tn;
-  decode_tile(a, blockIdx.x, tm, tn);
+  own_tile(a, tm, tn);
   const int m0 = tm * BM, n0 = tn * BN;
-  if (m0 >= count) return;
+  if (m0 >= count || n0 >= a.piece) return;
   f32x4 acc[P::MB][P::NB];
   P::run(acc, Matrix{a.rows, a.width, a.rows_plane}, weight_matrix(a), m0, count, n0, a.piece, a.width, 0,
          (a.width + kDepth - 1) / kDepth * PAIRS, to_lds_addr(smem));
@@ -227,14 +246,19 @@ __global__ void __launch_bounds__(64 * WM * WN) loss_scores_kernel(const LossArg
       }
     }
     __syncthreads();
-    for (int r = threadIdx.x; r < BM && m0 + r < count; r += P::THREADS) {
-      float most = red[2 * r], sum = 0.f;
+    // statistics are kept for every 128 columns, whatever tile they come from
+    constexpr int PER = BN / 128, WAVES = WN / PER;
+    for (int r = threadIdx.x; r < BM * PER; r += P::THREADS) {
+      const int row = r % BM, part = r / BM;
+      if (m0 + row >= count || n0 + 128 * part >= a.piece) continue;
+      const float *in = red + 2 * (part * WAVES * BM + row);
+      float most = in[0], sum = 0.f;
 #pragma unroll
-      for (int w = 1; w < WN; ++w) most = fmaxf(most, red[2 * (w * BM + r)]);
+      for (int w = 1; w < WAVES; ++w) most = fmaxf(most, in[2 * w * BM]);
       const float from = most == -INFINITY ? 0.f : most * kLog2e;
 #pragma unroll
-      for (int w = 0; w < WN; ++w) sum += red[2 * (w * BM + r) + 1] * exp2_fast(fmaf(red[2 * (w * BM + r)], kLog2e, -from));
-      float *to = a.stats + 2 * ((int64_t)(a.first / BN + tn) * a.n + m0 + r);
+      for (int w = 0; w < WAVES; ++w) sum += in[2 * w * BM + 1] * exp2_fast(fmaf(in[2 * w * BM], kLog2e, -from));
+      float *to = a.stats + 2 * ((int64_t)((a.first + n0) / 128 + part) * a.n + m0 + row);
       to[0] = most;
       to[1] = sum;
     }
@@ -289,90 +313,119 @@ __global__ void __launch_bounds__(64 * WM * WN) loss_scores_kernel(const LossArg
   }
 }
 
-// The forward's statistics of each row joined: 64 rows per workgroup, its waves a quarter of the vocabulary's tiles each.
-__global__ void __launch_bounds__(256) loss_join_kernel(const LossArgs a) {
-  __shared__ float red[4][64][2];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, slot = blockIdx.x * 64 + lane, count = *a.count;
-  if ((int)blockIdx.x * 64 >= count) return;
+// The forward's statistics of each row joined: 16 rows per workgroup, for each of which 64 lanes share the vocabulary's tiles.  Bound by latency: 4 lanes to a
+// row took 28 us for 4099 rows and 196 tiles, 16 lanes 15.
+__global__ void __launch_bounds__(1024) loss_join_kernel(const LossArgs a) {
+  constexpr int SHARES = 64;
+  __shared__ float red[SHARES][16][2];
+  const int in = threadIdx.x & 15, share = threadIdx.x >> 4, slot = blockIdx.x * 16 + in, count = *a.count;
+  if ((int)blockIdx.x * 16 >= count) return;
   float most = -INFINITY, sum = 0.f;
   if (slot < count)
-    for (int t = a.parts * wave / 4; t < a.parts * (wave + 1) / 4; ++t) {
-      const float *s = a.stats + 2 * ((int64_t)t * a.n + slot);
-      const float m = fmaxf(most, s[0]), from = m == -INFINITY ? 0.f : m;
-      sum = sum * exp2_fast((most - from) * kLog2e) + s[1] * exp2_fast((s[0] - from) * kLog2e);
-      most = m;
+    for (int t = share; t < a.parts; t += SHARES * 4) {   // four at a time, asked for together
+      float m[4], x[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const bool is = t + SHARES * u < a.parts;
+        const float *s = a.stats + 2 * ((int64_t)(is ? t + SHARES * u : t) * a.n + slot);
+        m[u] = s[0];
+        x[u] = is ? s[1] : 0.f;
+      }
+      const float now = fmaxf(fmaxf(most, fmaxf(m[0], m[1])), fmaxf(m[2], m[3])), from = now == -INFINITY ? 0.f : now * kLog2e;
+      sum *= exp2_fast(fmaf(most, kLog2e, -from));
+#pragma unroll
+      for (int u = 0; u < 4; ++u) sum += x[u] * exp2_fast(fmaf(m[u], kLog2e, -from));
+      most = now;
     }
-  red[wave][lane][0] = most;
-  red[wave][lane][1] = sum;
-  __syncthreads();
-  if (wave > 0 || slot >= count) return;
-  for (int w = 1; w < 4; ++w) most = fmaxf(most, red[w][lane][0]);
-  const float from = most == -INFINITY ? 0.f : most;
-  sum = 0.f;
-  for (int w = 0; w < 4; ++w) sum += red[w][lane][1] * exp2_fast((red[w][lane][0] - from) * kLog2e);
+  red[share][in][0] = most;
+  red[share][in][1] = sum;
+  for (int half = SHARES / 2; half > 0; half /= 2) {
+    __syncthreads();
+    if (share < half) {
+      const float m = red[share + half][in][0], now = fmaxf(most, m), from = now == -INFINITY ? 0.f : now * kLog2e;
+      sum = sum * exp2_fast(fmaf(most, kLog2e, -from)) + red[share + half][in][1] * exp2_fast(fmaf(m, kLog2e, -from));
+      most = now;
+      red[share][in][0] = most;
+      red[share][in][1] = sum;
+    }
+  }
+  if (share > 0 || slot >= count) return;
   const int row = a.row_of[slot];
   const float lse = most + logf(sum);
   a.lse[row] = lse;
   a.loss[row] = lse - a.target_score[slot];
 }
 
-// dx = dz W over a piece of the vocabulary, in `splits` parts of it that run side by side.
-template <int PAIRS, int BM, int BN, int WM, int WN> __global__ void __launch_bounds__(64 * WM * WN) loss_dx_kernel(const LossArgs a) {
+// dx = dz W over a piece of the vocabulary.  Tiles that do not fill a round of workgroups are cut along the vocabulary.
+template <int PAIRS, int BM, int BN, int WM, int WN> __global__ void __launch_bounds__(64 * WM * WN, 2) loss_dx_kernel(const LossArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   typedef Product<BM, BN, WM, WN, false, true, PAIRS> P;
   const int count = *a.count;
-  int part, tile, tm, tn;
-  div_mod(blockIdx.x, a.by_tiles, part, tile);
+  int tile = blockIdx.x, part = 0, parts = 1, tm, tn;
+  if (tile >= a.whole) {
+    part = (tile - a.whole) / a.rest;
+    tile -= part * a.rest;
+    parts = a.splits;
+  }
   decode_tile(a, tile, tm, tn);
   const int m0 = tm * BM, n0 = tn * BN;
   if (m0 >= count) return;
   const int64_t stages = (int64_t)((a.piece + kDepth - 1) / kDepth) * PAIRS;
   f32x4 acc[P::MB][P::NB];
-  P::run(acc, Matrix{a.dz, a.dz_ld, a.dz_plane}, weight_matrix(a), m0, count, n0, a.width, a.piece, (int)(stages * part / a.splits),
-         (int)(stages * (part + 1) / a.splits), to_lds_addr(smem));
+  P::run(acc, Matrix{a.dz, a.dz_ld, a.dz_plane}, weight_matrix(a), m0, count, n0, a.width, a.piece, (int)(stages * part / parts),
+         (int)(stages * (part + 1) / parts), to_lds_addr(smem));
   const int lane = lane_id(), n = lane & 15, j = lane >> 4, wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
+  float *to = part == 0 ? a.sum + (int64_t)m0 * a.width + n0 : a.part + ((int64_t)(part - 1) * a.rest + tile - a.whole) * (BM * BN);
+  const int stride = part == 0 ? a.width : BN;
 #pragma unroll
   for (int mb = 0; mb < P::MB; ++mb) {
-    const int slot = m0 + 16 * (wm * P::MB + mb) + n;
-    if (slot >= count) continue;
+    const int row = 16 * (wm * P::MB + mb) + n;
+    if (m0 + row >= count) continue;
 #pragma unroll
     for (int nb = 0; nb < P::NB; ++nb) {
-      const int col = n0 + 16 * (wn * P::NB + nb) + 4 * j;
-      if (col >= a.width) continue;
-      f32x4 *to = reinterpret_cast<f32x4 *>(a.part + ((int64_t)part * a.n + slot) * a.width + col);
-      *to = a.add ? *to + acc[mb][nb] : acc[mb][nb];
+      const int col = 16 * (wn * P::NB + nb) + 4 * j;
+      if (n0 + col >= a.width) continue;
+      f32x4 *at = reinterpret_cast<f32x4 *>(to + (int64_t)row * stride + col);
+      *at = a.add ? *at + acc[mb][nb] : acc[mb][nb];
     }
   }
 }
 
-// Parts of dx added up in their order, rounded, and put where the rows of x lie; zeros for rows without a target.
-template <typename T, bool WIDE> __global__ void __launch_bounds__(256) loss_dx_join_kernel(const LossArgs a) {
+// dx rounded and put where the rows of x lie, parts of cut tiles (of TILE x TILE) added up in their order; zeros for rows without a target.
+template <typename T, bool WIDE, int TILE> __global__ void __launch_bounds__(256) loss_dx_join_kernel(const LossArgs a) {
   typedef Piece<T, WIDE> P;
   const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int per_row = a.hidden / P::N;
   const int64_t row = id / per_row;
-  const int c = (int)(id - row * per_row);
+  const int col = (int)(id - row * per_row) * P::N;
   if (row >= a.n) return;
   const int slot = a.slot_of[row];
   float v[P::N], more[P::N];
 #pragma unroll
   for (int e = 0; e < P::N; ++e) v[e] = 0.f;
-  if (slot >= 0)
-    for (int p = 0; p < a.parts; ++p) {
-      load_f32<P::N>(a.part + ((int64_t)p * a.n + slot) * a.width + c * P::N, more);
+  if (slot >= 0) {
+    load_f32<P::N>(a.sum + (int64_t)slot * a.width + col, v);
+    if (a.splits > 1) {
+      const int tile = encode_tile(a, slot / TILE, col / TILE);
+      if (tile >= a.whole)
+        for (int p = 0; p + 1 < a.splits; ++p) {
+          load_f32<P::N>(a.part + (((int64_t)p * a.rest + tile - a.whole) * TILE + slot % TILE) * TILE + col % TILE, more);
 #pragma unroll
-      for (int e = 0; e < P::N; ++e) v[e] += more[e];
+          for (int e = 0; e < P::N; ++e) v[e] += more[e];
+        }
     }
-  P::store(reinterpret_cast<T *>(a.dx) + a.xs.offset((int)row) + c * P::N, v);
+  }
+  P::store(reinterpret_cast<T *>(a.dx) + a.xs.offset((int)row) + col, v);
 }
 
 // dW of a piece of the vocabulary: added into fp32 accumulators (ADD), or written in bf16.
-template <int PAIRS, int BM, int BN, int WM, int WN, bool ADD> __global__ void __launch_bounds__(64 * WM * WN) loss_dw_kernel(const LossArgs a) {
+template <int PAIRS, int BM, int BN, int WM, int WN, bool ADD> __global__ void __launch_bounds__(64 * WM * WN, 2) loss_dw_kernel(const LossArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   typedef Product<BM, BN, WM, WN, true, true, PAIRS> P;
   int tm, tn;
-  decode_tile(a, blockIdx.x, tm, tn);
+  own_tile(a, tm, tn);
   const int m0 = tm * BM, n0 = tn * BN, count = *a.count;
+  if (m0 >= a.piece || n0 >= a.width) return;
   f32x4 acc[P::MB][P::NB];
   P::run(acc, Matrix{a.dz, a.dz_ld, a.dz_plane}, Matrix{a.rows, a.width, a.rows_plane}, m0, a.dz_ld, n0, a.width, count, 0,
          (count + kDepth - 1) / kDepth * PAIRS, to_lds_addr(smem));
@@ -413,14 +466,75 @@ template <int PAIRS, int BM, int BN, int WM, int WN, bool ADD> __global__ void _
 
 constexpr int64_t kMostLossRows = int64_t(1) << 20, kMostLossVocab = int64_t(1) << 24, kMostWeightStride = int64_t(1) << 22;
 constexpr int64_t kMostPacked = int64_t(1) << 28, kMostDz = int64_t(1) << 30;   // bytes of a piece of the weight, of its dz
-constexpr int kTileBig = 256, kMostSplits = 16;
 int64_t up_to(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
+
+// Tiles of 256 x 256 (eight waves, one workgroup to a compute unit), 128 x 128 (four, two to a unit) or 64 x 128 (four, two to a unit).
+enum Tile { kBig, kMiddle, kLow };
+constexpr int kUnits = 256;   // compute units
+
+// Predicted microseconds of a launch of tiles of so many stages of products, from launches of 1 to 4099 rows over 800 to 50021 tokens with 256 to 4096
+// elements: a tile's beginning and end, and its stages: alone on a compute unit, or beside another one.  Rounds of big tiles count whole, those of
+// the others overlap.
+double tiles_us(Tile tile, int64_t tiles, double stages) {
+  if (tile == kBig) return (double)((tiles + kUnits - 1) / kUnits) * (8.0 + 1.45 * stages);
+  if (tiles <= kUnits) return tile == kMiddle ? 5.0 + 0.55 * stages : 4.5 + 0.40 * stages;
+  const double rounds = std::max(1.0, (double)tiles / (2 * kUnits) + 0.25);
+  return rounds * (tile == kMiddle ? 6.0 + 0.90 * stages : 5.0 + 0.60 * stages);
+}
+int64_t grid_of(int64_t m, int64_t n, int bm, int bn) { return (m + bm - 1) / bm * ((n + bn - 1) / bn); }
+
+// How the tiles of a product [m, n] are taken: big ones up to `whole`, their rest in quarters (the last round of big tiles may be one of a few: forward of
+// 4099 rows over 50021 tokens, 3332 tiles); or all in one of the other sizes.
+struct Cut {
+  Tile tile;
+  int64_t whole;
+};
+Cut cut_for(int64_t m, int64_t n, int64_t stages, bool low) {
+  const int64_t big = grid_of(m, n, 256, 256), rounds = big / kUnits * kUnits;
+  Cut best = {kBig, big};
+  double least = tiles_us(kBig, big, (double)stages);
+  auto offer = [&](Cut c, double us) {
+    if (us < least) {
+      least = us;
+      best = c;
+    }
+  };
+  if (rounds > 0 && rounds < big) offer({kBig, rounds}, tiles_us(kBig, rounds, (double)stages) + 3.0 + tiles_us(kMiddle, 4 * (big - rounds), (double)stages));
+  offer({kMiddle, 0}, tiles_us(kMiddle, grid_of(m, n, 128, 128), (double)stages));
+  if (low) offer({kLow, 0}, tiles_us(kLow, grid_of(m, n, 64, 128), (double)stages));
+  return best;
+}
+// dx: the big tiles behind the last full round, or all middle tiles, cut into parts along the vocabulary, each of which but the first
+// is written and read once more (4 TB/s).
+struct DxCut {
+  Tile tile;
+  int64_t whole, rest;
+  int splits;
+};
+DxCut dx_cut_for(int64_t m, int64_t n, int64_t stages) {
+  DxCut best = {};
+  double least = 1e30;
+  for (Tile tile : {kBig, kMiddle}) {
+    const int side = tile == kBig ? 256 : 128;
+    const int64_t tiles = grid_of(m, n, side, side), whole = tile == kBig ? tiles / kUnits * kUnits : 0, rest = tiles - whole;
+    for (int splits = 1; splits <= 32 && (splits == 1 || (rest > 0 && stages / splits >= 4 && rest * splits <= 4 * kUnits)); ++splits) {
+      const double us = (whole ? tiles_us(tile, whole, (double)stages) : 0.0) + (rest ? tiles_us(tile, rest * splits, (double)stages / splits) : 0.0) +
+                        (double)(splits - 1) * rest * side * side * 8 / 4e6;
+      if (us < 0.98 * least) {
+        least = us;
+        best = {tile, whole, rest, splits};
+      }
+    }
+  }
+  return best;
+}
 
 struct LossPlan {
   int64_t n, width, planes, piece;
   bool direct;
-  int splits;
-  int64_t count, row_of, slot_of, target_of, target_score, of_row, stats, rows, packed, dz, part, bytes;   // offsets
+  Cut scores, dw;
+  DxCut dx;
+  int64_t count, row_of, slot_of, target_of, target_score, of_row, stats, rows, packed, dz, sum, part, bytes;   // offsets
 };
 
 int check_loss(const s1f_rows *d, int64_t vocab, int64_t weight_stride) {
@@ -429,21 +543,6 @@ int check_loss(const s1f_rows *d, int64_t vocab, int64_t weight_stride) {
   if (vocab < 1 || weight_stride < d->hidden) return S1F_EINVAL;
   if (vocab > kMostLossVocab || weight_stride >= kMostWeightStride || d->batch * d->rows > kMostLossRows) return S1F_EUNSUPPORTED;
   return S1F_OK;
-}
-
-// Parts into which the products of dx are cut along the vocabulary: the rounds of workgroups that the parts take on 256 compute units,
-// in the length of a part.
-int splits_for(int64_t tiles, int64_t stages) {
-  int best = 1;
-  double least = 1e30;
-  for (int s = 1; s <= kMostSplits && (s == 1 || stages / s >= 8); ++s) {
-    const double rounds = (double)((tiles * s + 255) / 256), time = rounds * ((double)stages / s + 8.0);
-    if (time < 0.95 * least) {
-      least = time;
-      best = s;
-    }
-  }
-  return best;
 }
 
 LossPlan plan_of(const s1f_rows *d, int64_t vocab, int64_t weight_stride, bool backward) {
@@ -455,7 +554,7 @@ LossPlan plan_of(const s1f_rows *d, int64_t vocab, int64_t weight_stride, bool b
   int64_t piece = vocab;
   if (!p.direct) piece = std::min(piece, kMostPacked / (p.planes * 2 * p.width));
   if (backward) piece = std::min(piece, kMostDz / (p.planes * 2 * p.n));
-  p.piece = piece < vocab ? std::max<int64_t>(kTileBig, piece / kTileBig * kTileBig) : vocab;
+  p.piece = piece < vocab ? std::max<int64_t>(256, piece / 256 * 256) : vocab;
   int64_t at = 0;
   auto take = [&at](int64_t bytes) { const int64_t was = at; at += up_to(bytes, 256); return was; };
   p.count = take(4);
@@ -464,15 +563,19 @@ LossPlan plan_of(const s1f_rows *d, int64_t vocab, int64_t weight_stride, bool b
   p.target_of = take(4 * p.n);
   p.rows = take(p.planes * 2 * p.n * p.width);
   if (!p.direct) p.packed = take(p.planes * 2 * p.piece * p.width);
+  const int64_t pairs = p.planes == 3 ? 6 : 1, stages = (p.width + kDepth - 1) / kDepth * pairs;
+  p.scores = cut_for(p.n, p.piece, stages, true);
   if (backward) {
-    const int64_t pairs = p.planes == 3 ? 6 : 1;
-    p.splits = splits_for((p.n + kTileBig - 1) / kTileBig * ((p.width + kTileBig - 1) / kTileBig), (p.piece + kDepth - 1) / kDepth * pairs);
+    p.dx = dx_cut_for(p.n, p.width, (p.piece + kDepth - 1) / kDepth * pairs);
+    p.dw = cut_for(p.piece, p.width, (p.n + kDepth - 1) / kDepth * pairs, false);
+    const int64_t side = p.dx.tile == kBig ? 256 : 128;
     p.of_row = take(8 * p.n);
     p.dz = take(p.planes * 2 * p.n * up_to(p.piece, 64));
-    p.part = take(4 * (int64_t)p.splits * p.n * p.width);
+    p.sum = take(4 * p.n * p.width);
+    p.part = take(4 * (p.dx.splits - 1) * p.dx.rest * side * side);
   } else {
     p.target_score = take(4 * p.n);
-    p.stats = take(8 * p.n * ((vocab + 63) / 64));
+    p.stats = take(8 * p.n * ((vocab + 127) / 128));
   }
   p.bytes = at;
   return p;
@@ -495,7 +598,6 @@ void tiles_of(LossArgs &a, int64_t m, int64_t n, int bm, int bn) {
   a.tiles_m = (int32_t)((m + bm - 1) / bm);
   a.tiles_n = (int32_t)((n + bn - 1) / bn);
   a.by_group = Divisor::of(4 * a.tiles_m);
-  a.by_tiles = Divisor::of((int64_t)a.tiles_m * a.tiles_n);
 }
 
 template <typename T> int pack(const LossArgs &a, bool rows, bool wide, int64_t most, hipStream_t st) {
@@ -527,73 +629,101 @@ LossArgs args_of(const s1f_rows *d, const LossPlan &p, const int64_t *targets, i
   a.dz = reinterpret_cast<bf16_t *>(ws + p.dz);
   a.dz_ld = up_to(p.piece, 64);
   a.dz_plane = p.n * a.dz_ld;
+  a.sum = reinterpret_cast<float *>(ws + p.sum);
   a.part = reinterpret_cast<float *>(ws + p.part);
   a.direct = p.direct;
-  a.splits = p.splits;
+  a.whole = (int32_t)p.dx.whole;
+  a.rest = (int32_t)p.dx.rest;
+  a.splits = p.dx.splits;
   return a;
 }
 bool wide_weight(const s1f_rows *d, int64_t stride) { return d->hidden % 8 == 0 && stride % elements_of_16_bytes(d->dtype) == 0; }
 bool wide_x(const s1f_rows *d, const void *p) { return on16(p) && d->hidden % 8 == 0 && wide_rows(d, d->x_stride_b, d->x_stride_s); }
 
+// Launches `kernel`, made for the tile size that it is given, over the tiles of a product [m, n] as `cut` says.  KERNELS<tile>: the kernel, its LDS and threads.
+template <template <Tile> class KERNELS> int launch_cut(const Cut &cut, int64_t m, int64_t n, LossArgs a, hipStream_t st) {
+  auto go = [&](auto kernels, int64_t grid) {
+    typedef decltype(kernels) K;
+    return launch_tiles<K::kernel>(K::P::LDS_BYTES, K::P::THREADS, grid, a, st);
+  };
+  if (cut.tile == kMiddle) {
+    tiles_of(a, m, n, 128, 128);
+    return go(KERNELS<kMiddle>{}, (int64_t)a.tiles_m * a.tiles_n);
+  }
+  if (cut.tile == kLow) {
+    tiles_of(a, m, n, 64, 128);
+    return go(KERNELS<kLow>{}, (int64_t)a.tiles_m * a.tiles_n);
+  }
+  tiles_of(a, m, n, 256, 256);
+  const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n, whole = std::min(cut.whole, tiles);   // (the last piece may have fewer)
+  const int e = go(KERNELS<kBig>{}, whole);
+  if (e != S1F_OK || whole == tiles) return e;
+  a.tile0 = (int32_t)whole;
+  a.quarters = 1;
+  return go(KERNELS<kMiddle>{}, 4 * (tiles - whole));
+}
+template <Tile TILE> struct Shape {
+  static constexpr int BM = TILE == kBig ? 256 : TILE == kMiddle ? 128 : 64, BN = TILE == kBig ? 256 : 128, WM = TILE == kLow ? 1 : 2,
+                       WN = TILE == kMiddle ? 2 : 4;
+};
+// (sizes of a product do not depend on its number of planes)
+template <typename T, bool STATS> struct Scores {
+  template <Tile TILE> struct Of : Shape<TILE> {
+    typedef Shape<TILE> S;
+    typedef Product<S::BM, S::BN, S::WM, S::WN, false, false, 1> P;
+    static constexpr auto kernel = &loss_scores_kernel<T, S::BM, S::BN, S::WM, S::WN, STATS>;
+  };
+};
+template <int PAIRS, bool ADD> struct Dw {
+  template <Tile TILE> struct Of : Shape<TILE == kLow ? kMiddle : TILE> {
+    typedef Shape<TILE == kLow ? kMiddle : TILE> S;
+    typedef Product<S::BM, S::BN, S::WM, S::WN, true, true, 1> P;
+    static constexpr auto kernel = &loss_dw_kernel<PAIRS, S::BM, S::BN, S::WM, S::WN, ADD>;
+  };
+};
+template <int PAIRS, Tile TILE> int launch_dx(const LossPlan &p, LossArgs a, hipStream_t st) {
+  typedef Shape<TILE> S;
+  typedef Product<S::BM, S::BN, S::WM, S::WN, false, true, 1> P;
+  tiles_of(a, p.n, a.width, S::BM, S::BN);
+  return launch_tiles<&loss_dx_kernel<PAIRS, S::BM, S::BN, S::WM, S::WN>>(P::LDS_BYTES, P::THREADS, a.whole + (int64_t)a.rest * a.splits, a, st);
+}
+
 template <typename T> int forward(const s1f_rows *d, LossArgs a, const LossPlan &p, hipStream_t st) {
   int e = launch_rows_kernel(&loss_rows_kernel<true>, 1, 1024, a, st);
   if (e == S1F_OK) e = pack<T>(a, true, wide_x(d, a.x), p.n, st);
-  const bool small = p.n <= 128;
   for (int64_t at = 0; at < a.vocab && e == S1F_OK; at += p.piece) {
     a.first = (int32_t)at;
     a.piece = (int32_t)std::min(p.piece, a.vocab - at);
     if (!p.direct) e = pack<T>(a, false, wide_weight(d, a.weight_stride), a.piece, st);
-    if (e != S1F_OK) break;
-    if (small) {
-      typedef Product<64, 128, 1, 4, false, false, 1> P;   // (sizes do not depend on the last)
-      tiles_of(a, p.n, a.piece, 64, 128);
-      e = launch_tiles<&loss_scores_kernel<T, 64, 128, 1, 4, true>>(P::LDS_BYTES, P::THREADS, (int64_t)a.tiles_m * a.tiles_n, a, st);
-    } else {
-      typedef Product<256, 256, 2, 4, false, false, 1> P;
-      tiles_of(a, p.n, a.piece, 256, 256);
-      e = launch_tiles<&loss_scores_kernel<T, 256, 256, 2, 4, true>>(P::LDS_BYTES, P::THREADS, (int64_t)a.tiles_m * a.tiles_n, a, st);
-    }
+    if (e == S1F_OK) e = launch_cut<Scores<T, true>::template Of>(p.scores, p.n, a.piece, a, st);
   }
   if (e != S1F_OK) return e;
-  a.parts = (int32_t)((a.vocab + (small ? 127 : 255)) / (small ? 128 : 256));
-  return launch_rows_kernel(&loss_join_kernel, (p.n + 63) / 64, 256, a, st);
+  a.parts = (a.vocab + 127) / 128;
+  return launch_rows_kernel(&loss_join_kernel, (p.n + 15) / 16, 1024, a, st);
 }
 
 template <typename T, bool ADD> int backward(const s1f_rows *d, LossArgs a, const LossPlan &p, hipStream_t st) {
   constexpr int PAIRS = sizeof(T) == 4 ? 6 : 1;
   int e = launch_rows_kernel(&loss_rows_kernel<false>, 1, 1024, a, st);
   if (e == S1F_OK) e = pack<T>(a, true, wide_x(d, a.x), p.n, st);
+  a.wide = on16(a.dweight) && a.dweight_stride % 4 == 0;
   for (int64_t at = 0; at < a.vocab && e == S1F_OK; at += p.piece) {
     a.first = (int32_t)at;
     a.piece = (int32_t)std::min(p.piece, a.vocab - at);
     a.add = at > 0;
     if (!p.direct) e = pack<T>(a, false, wide_weight(d, a.weight_stride), a.piece, st);
-    if (e != S1F_OK) break;
-    {
-      typedef Product<256, 256, 2, 4, false, false, 1> P;
-      tiles_of(a, p.n, a.piece, 256, 256);
-      e = launch_tiles<&loss_scores_kernel<T, 256, 256, 2, 4, false>>(P::LDS_BYTES, P::THREADS, (int64_t)a.tiles_m * a.tiles_n, a, st);
-    }
-    if (e != S1F_OK) break;
-    {
-      typedef Product<256, 256, 2, 4, false, true, 1> P;
-      tiles_of(a, p.n, a.width, 256, 256);
-      e = launch_tiles<&loss_dx_kernel<PAIRS, 256, 256, 2, 4>>(P::LDS_BYTES, P::THREADS, (int64_t)a.tiles_m * a.tiles_n * a.splits, a, st);
-    }
-    if (e != S1F_OK) break;
-    {
-      typedef Product<256, 256, 2, 4, true, true, 1> P;
-      tiles_of(a, a.piece, a.width, 256, 256);
-      a.wide = on16(a.dweight) && a.dweight_stride % 4 == 0;
-      e = launch_tiles<&loss_dw_kernel<PAIRS, 256, 256, 2, 4, ADD>>(P::LDS_BYTES, P::THREADS, (int64_t)a.tiles_m * a.tiles_n, a, st);
-    }
+    if (e == S1F_OK) e = launch_cut<Scores<T, false>::template Of>(p.scores, p.n, a.piece, a, st);
+    if (e == S1F_OK) e = p.dx.tile == kBig ? launch_dx<PAIRS, kBig>(p, a, st) : launch_dx<PAIRS, kMiddle>(p, a, st);
+    if (e == S1F_OK) e = launch_cut<Dw<PAIRS, ADD>::template Of>(p.dw, a.piece, a.width, a, st);
   }
   if (e != S1F_OK) return e;
-  a.parts = a.splits;
+  const int side = p.dx.tile == kBig ? 256 : 128;
+  tiles_of(a, p.n, a.width, side, side);
   const bool wide = wide_x(d, a.dx);
   const int64_t per_row = wide ? d->hidden / elements_of_16_bytes(d->dtype) : d->hidden, grid = (p.n * per_row + 255) / 256;
   if (grid * 256 >= (int64_t(1) << 32)) return S1F_EUNSUPPORTED;
-  return launch_rows_kernel(wide ? &loss_dx_join_kernel<T, true> : &loss_dx_join_kernel<T, false>, grid, 256, a, st);
+  if (side == 256) return launch_rows_kernel(wide ? &loss_dx_join_kernel<T, true, 256> : &loss_dx_join_kernel<T, false, 256>, grid, 256, a, st);
+  return launch_rows_kernel(wide ? &loss_dx_join_kernel<T, true, 128> : &loss_dx_join_kernel<T, false, 128>, grid, 256, a, st);
 }
 
 }  // namespace
