@@ -20,59 +20,64 @@ struct RowsOf {
   }
 };
 
-// A row's elements in pieces of N: 16 bytes where everything is aligned to them (WIDE), else single elements.
+// A row's elements in pieces of 16 bytes.  WIDE: rows start on 16 bytes and hold a whole number of pieces; else a piece lies wherever its elements do
+// (memory takes accesses of 16 bytes on any element: a layer norm gradient of 2714 rows of 2563 elements element by element took 40 us), and the last one may
+// be short: `left` elements of the row are there from the piece on.
 template <typename T, bool WIDE> struct Piece {
-  static constexpr int N = WIDE ? Elem<T>::CE : 1;
+  static constexpr int N = Elem<T>::CE;
+  typedef T Wide __attribute__((ext_vector_type(N)));
+  typedef T Loose __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+  typedef Wide Raw;
   typedef float Values[N];
-  S1F_DEV static void load(const T *p, Values &v) {
-    if constexpr (!WIDE) {
-      v[0] = (float)*p;
-    } else if constexpr (sizeof(T) == 4) {
-      const f32x4 x = *reinterpret_cast<const f32x4 *>(p);
-#pragma unroll
-      for (int e = 0; e < N; ++e) v[e] = x[e];
+  S1F_DEV static Raw get(const T *p, int left) {
+    if constexpr (WIDE) {
+      return *reinterpret_cast<const Wide *>(p);
     } else {
-      const bf16x8 x = *reinterpret_cast<const bf16x8 *>(p);
+      if (left >= N) return *reinterpret_cast<const Loose *>(p);
+      Raw r;
 #pragma unroll
-      for (int e = 0; e < N; ++e) v[e] = (float)x[e];
+      for (int e = 0; e < N; ++e) r[e] = e < left ? p[e] : (T)0.f;
+      return r;
     }
   }
-  S1F_DEV static void store(T *p, const Values &v) {
-    if constexpr (!WIDE) {
-      *p = (T)v[0];
-    } else if constexpr (sizeof(T) == 4) {
-      f32x4 x;
+  S1F_DEV static Raw none() {
+    Raw r;
 #pragma unroll
-      for (int e = 0; e < N; ++e) x[e] = v[e];
-      *reinterpret_cast<f32x4 *>(p) = x;
+    for (int e = 0; e < N; ++e) r[e] = (T)0.f;
+    return r;
+  }
+  S1F_DEV static void values(const Raw &r, Values &v) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = (float)r[e];
+  }
+  S1F_DEV static void load(const T *p, int left, Values &v) { values(get(p, left), v); }
+  S1F_DEV static void store(T *p, int left, const Values &v) {
+    Raw r;
+#pragma unroll
+    for (int e = 0; e < N; ++e) r[e] = (T)v[e];
+    if constexpr (WIDE) {
+      *reinterpret_cast<Wide *>(p) = r;
+    } else if (left >= N) {
+      *reinterpret_cast<Loose *>(p) = r;
     } else {
-      bf16x8 x;
 #pragma unroll
-      for (int e = 0; e < N; ++e) x[e] = (bf16_t)v[e];
-      *reinterpret_cast<bf16x8 *>(p) = x;
+      for (int e = 0; e < N; ++e)
+        if (e < left) p[e] = r[e];
     }
   }
 };
-// N consecutive fp32 values (N = 1, 4 or 8)
-template <int N> S1F_DEV void load_f32(const float *p, float (&v)[N]) {
-  if constexpr (N == 1) {
-    v[0] = *p;
-  } else {
+// The same for N consecutive fp32 values, N = 4 or 8.
+template <int N, bool WIDE> S1F_DEV void load_f32(const float *p, int left, float (&v)[N]) {
 #pragma unroll
-    for (int i = 0; i < N; i += 4) {
-      const f32x4 x = *reinterpret_cast<const f32x4 *>(p + i);
+  for (int i = 0; i < N; i += 4) {
+    const f32x4 x = Piece<float, WIDE>::get(p + i, left - i);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[i + e] = x[e];
-    }
+    for (int e = 0; e < 4; ++e) v[i + e] = x[e];
   }
 }
-template <int N> S1F_DEV void store_f32(float *p, const float (&v)[N]) {
-  if constexpr (N == 1) {
-    *p = v[0];
-  } else {
+template <int N, bool WIDE> S1F_DEV void store_f32(float *p, int left, const float (&v)[N]) {
 #pragma unroll
-    for (int i = 0; i < N; i += 4) *reinterpret_cast<f32x4 *>(p + i) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
-  }
+  for (int i = 0; i < N; i += 4) Piece<float, WIDE>::store(p + i, left - i, {v[i], v[i + 1], v[i + 2], v[i + 3]});
 }
 
 constexpr int64_t kMostRows = int64_t(1) << 24;   // batch * rows: numbers of rows are 32 bits, grids one launch

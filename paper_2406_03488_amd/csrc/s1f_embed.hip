@@ -23,12 +23,13 @@ struct EmbedArgs {
   int64_t acc_stride;
   RowsOf y;
   int32_t n, hidden, vocab, pieces;     // rows of all batch entries; pieces of a row
-  int32_t tpr_log2, chunk;              // threads that share a row; sorted rows per workgroup of the sums
+  int32_t tpr_log2, chunk, part_ld;     // threads that share a row; sorted rows per chunk of the sums; row length of their partial sums
   float scale;
   // workspace of the backward
   int32_t *row_of, *key_of;             // rows sorted by token, and their tokens (`vocab`: none)
   int32_t *row_from, *key_from, *count; // input of a sorting pass; rows of each tile with each digit
-  float *head, *tail;                   // [chunk][hidden]: sum of the run that reaches into the chunk, that leaves it
+  int32_t *long_runs;                   // number of runs that go on behind a chunk, and the chunks where they start
+  float *head, *tail;                   // [chunk][part_ld]: sum of the run that reaches into the chunk, that leaves it
   int32_t tiles, shift, bits, first_pass;
 };
 
@@ -48,127 +49,157 @@ template <typename T, bool WIDE> __global__ void __launch_bounds__(256) embed_fw
   const T *from = reinterpret_cast<const T *>(a.table) + (key < a.vocab ? key : 0) * a.table_stride;
   T *to = reinterpret_cast<T *>(a.out) + a.y.offset(row);
   for (int p = threadIdx.x & (step - 1); p < a.pieces; p += step) {
+    const int left = a.hidden - p * P::N;
     typename P::Values v;
-    P::load(from + p * P::N, v);
+    P::load(from + p * P::N, left, v);
 #pragma unroll
     for (int e = 0; e < P::N; ++e) v[e] = key < a.vocab ? v[e] * a.scale : 0.f;
-    P::store(to + p * P::N, v);
+    P::store(to + p * P::N, left, v);
   }
 }
 
 // Rows sorted by token by counting, for every row, the rows in front of it: n^2 comparisons, of 64 by one vector instruction, whose
-// result a scalar one counts.  A workgroup places 32 rows; its waves share the rows that they are compared with.
-__global__ void __launch_bounds__(256) embed_rank_kernel(const EmbedArgs a) {
-  __shared__ int counted[4][32];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, first = blockIdx.x * 32;
-  const int own_row = first + (lane & 31);
-  const int own = own_row < a.n ? key_at(a, own_row) : a.vocab;
-  int key[32], before[32];
+// result a scalar one counts.  A workgroup of 16 waves places 32 rows, two to a wave, out of all tokens in LDS: 5.8 us for 2714 rows (each wave reading them
+// from memory as it went 12, a chain of loads), 12 for 8192, 26 for 12000, 34 for 16384, where two sorting passes take 33.
+constexpr int32_t kMostRanked = 12288;    // rows up to which counting sorts them
+constexpr int kRanked = 32;               // rows per workgroup
+__global__ void __launch_bounds__(1024) embed_rank_kernel(const EmbedArgs a) {
+  extern __shared__ int tokens[];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, first = blockIdx.x * kRanked, blocks = (a.n + 63) >> 6;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.long_runs = 0;
+  for (int i = threadIdx.x; i < 64 * blocks; i += 1024) tokens[i] = i < a.n ? key_at(a, i) : 0x7fffffff;
+  __syncthreads();
+  constexpr int R = kRanked / 16;
+  int key[R], before[R];
 #pragma unroll
-  for (int i = 0; i < 32; ++i) {
-    key[i] = __builtin_amdgcn_readlane(own, i);
+  for (int i = 0; i < R; ++i) {
+    key[i] = __builtin_amdgcn_readfirstlane(tokens[first + R * wave + i]);
     before[i] = 0;
   }
-  const int blocks = (a.n + 63) >> 6, here = first >> 6;
-  for (int c = wave; c < blocks; c += 4) {
-    const int row = 64 * c + lane;
-    const int x = row < a.n ? key_at(a, row) : 0x7fffffff;
-    if (c == here) {
+  const int here = first >> 6;
+  // rows in front with the same token count, those behind do not
+  auto count = [&](int begin, int end, int equal) {
+#pragma unroll 4
+    for (int c = begin; c < end; ++c) {
+      const int x = tokens[64 * c + lane];
 #pragma unroll
-      for (int i = 0; i < 32; ++i) before[i] += __builtin_popcountll(__ballot(x < key[i] || (x == key[i] && row < first + i)));
-    } else {
-      const int equal = c < here ? 1 : 0;   // rows in front with the same token count, those behind do not
-#pragma unroll
-      for (int i = 0; i < 32; ++i) before[i] += __builtin_popcountll(__ballot(x < key[i] + equal));
+      for (int i = 0; i < R; ++i) before[i] += __builtin_popcountll(__ballot(x < key[i] + equal));
     }
-  }
-  if (lane == 0) {
+  };
+  count(0, here, 1);
+  count(here + 1, blocks, 0);
+  const int x = tokens[64 * here + lane];
 #pragma unroll
-    for (int i = 0; i < 32; ++i) counted[wave][i] = before[i];
-  }
-  __syncthreads();
-  if (threadIdx.x < 32 && own_row < a.n) {
-    const int at = counted[0][lane] + counted[1][lane] + counted[2][lane] + counted[3][lane];
-    a.row_of[at] = own_row;
-    a.key_of[at] = own;
+  for (int i = 0; i < R; ++i) {
+    const int row = first + R * wave + i;
+    before[i] += __builtin_popcountll(__ballot(x < key[i] || (x == key[i] && 64 * here + lane < row)));
+    if (lane == i && row < a.n) {
+      a.row_of[before[i]] = row;
+      a.key_of[before[i]] = key[i];
+    }
   }
 }
 
 // Sorting in passes over digits of at most 9 bits, the lowest first, each of which keeps the order of equal digits: count the digits of
-// every tile of 1024 rows, sum the counts up, and place the rows.  A wave has a tile to itself.
+// every tile of 1024 rows, sum the counts of each digit up over the tiles, and place the rows.
 constexpr int kTile = 1024, kDigits = 512;
 
 S1F_DEV int pass_key(const EmbedArgs &a, int i) { return a.first_pass ? key_at(a, i) : a.key_from[i]; }
 
 __global__ void __launch_bounds__(256) embed_count_kernel(const EmbedArgs a) {
-  __shared__ int counts[4][kDigits];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, tile = blockIdx.x * 4 + wave, digits = 1 << a.bits;
-  for (int d = lane; d < digits; d += 64) counts[wave][d] = 0;
+  __shared__ int counts[kDigits];
+  const int digits = 1 << a.bits;
+  for (int d = threadIdx.x; d < digits; d += 256) counts[d] = 0;
   __syncthreads();
-  for (int i = tile * kTile + lane; i < a.n && i < (tile + 1) * kTile; i += 64)
-    atomicAdd(&counts[wave][(pass_key(a, i) >> a.shift) & (digits - 1)], 1);   // (whole numbers: the same in any order)
+#pragma unroll
+  for (int u = 0; u < kTile / 256; ++u) {
+    const int i = blockIdx.x * kTile + 256 * u + threadIdx.x;
+    if (i < a.n) atomicAdd(&counts[(pass_key(a, i) >> a.shift) & (digits - 1)], 1);   // (whole numbers: the same in any order)
+  }
   __syncthreads();
-  if (tile < a.tiles)
-    for (int d = lane; d < digits; d += 64) a.count[d * a.tiles + tile] = counts[wave][d];
+  for (int d = threadIdx.x; d < digits; d += 256) a.count[d * a.tiles + blockIdx.x] = counts[d];
 }
 
-// Exclusive sums of `count` by one workgroup, 4 entries per thread at a time.
-__global__ void __launch_bounds__(1024) embed_scan_kernel(const EmbedArgs a) {
-  __shared__ int of_wave[16];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, total = a.tiles << a.bits;
-  int carry = 0;
-  for (int at = 0; at < total; at += 4096) {
-    const int i = at + 4 * threadIdx.x;
-    int v[4], own = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      v[e] = i + e < total ? a.count[i + e] : 0;
-      own += v[e];
-    }
+// Exclusive sums over the tiles of one digit per wave; their total behind them.
+__global__ void __launch_bounds__(256) embed_scan_kernel(const EmbedArgs a) {
+  const int lane = threadIdx.x & 63, digit = blockIdx.x * 4 + (threadIdx.x >> 6), digits = 1 << a.bits;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.long_runs = 0;
+  if (digit >= digits) return;
+  int *count = a.count + digit * a.tiles, carry = 0;
+  for (int at = 0; at < a.tiles; at += 64) {
+    const int own = at + lane < a.tiles ? count[at + lane] : 0;
     int x = own;
+#pragma unroll
     for (int s = 1; s < 64; s *= 2) {
       const int y = __shfl_up(x, s);
       if (lane >= s) x += y;
     }
-    if (lane == 63) of_wave[wave] = x;
-    __syncthreads();
-    int before = carry, all = 0;
-    for (int w = 0; w < 16; ++w) {
-      if (w < wave) before += of_wave[w];
-      all += of_wave[w];
-    }
-    before += x - own;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if (i + e < total) a.count[i + e] = before;
-      before += v[e];
-    }
-    carry += all;
-    __syncthreads();
+    if (at + lane < a.tiles) count[at + lane] = carry + x - own;
+    carry += __shfl(x, 63);
   }
+  if (lane == 0) a.count[digits * a.tiles + digit] = carry;
 }
 
+// A wave places 256 rows of the tile, 64 at a time.  next[wave][digit]: where its next row with that digit goes.
 __global__ void __launch_bounds__(256) embed_place_kernel(const EmbedArgs a) {
-  __shared__ int next[4][kDigits];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, tile = blockIdx.x * 4 + wave, digits = 1 << a.bits;
-  if (tile < a.tiles)
-    for (int d = lane; d < digits; d += 64) next[wave][d] = a.count[d * a.tiles + tile];
+  __shared__ int next[4][kDigits], of_wave[4];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, digits = 1 << a.bits;
+  for (int d = threadIdx.x; d < 4 * kDigits; d += 256) (&next[0][0])[d] = 0;
   __syncthreads();
-  if (tile >= a.tiles) return;   // (no barrier from here on)
-  const int end = (tile + 1) * kTile < a.n ? (tile + 1) * kTile : a.n;
-  for (int base = tile * kTile; base < end; base += 64) {
-    const int i = base + lane;
-    const bool is = i < end;
-    const int key = is ? pass_key(a, i) : 0, digit = (key >> a.shift) & (digits - 1);
+  constexpr int U = kTile / 256;
+  int key[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int i = blockIdx.x * kTile + 256 * wave + 64 * u + lane;
+    key[u] = i < a.n ? pass_key(a, i) : 0;
+    if (i < a.n) atomicAdd(&next[wave][(key[u] >> a.shift) & (digits - 1)], 1);
+  }
+  __syncthreads();
+  // rows with smaller digits (2 digits per thread), with this digit in tiles in front, in waves in front
+  int total[2], own = 0;
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const int d = 2 * threadIdx.x + e;
+    total[e] = d < digits ? a.count[digits * a.tiles + d] : 0;
+    own += total[e];
+  }
+  int x = own;
+#pragma unroll
+  for (int s = 1; s < 64; s *= 2) {
+    const int y = __shfl_up(x, s);
+    if (lane >= s) x += y;
+  }
+  if (lane == 63) of_wave[wave] = x;
+  __syncthreads();
+  int before = x - own;
+  for (int w = 0; w < wave; ++w) before += of_wave[w];
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const int d = 2 * threadIdx.x + e;
+    if (d < digits) {
+      int at = before + a.count[d * a.tiles + blockIdx.x];
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const int c = next[w][d];
+        next[w][d] = at;
+        at += c;
+      }
+    }
+    before += total[e];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int i = blockIdx.x * kTile + 256 * wave + 64 * u + lane, digit = (key[u] >> a.shift) & (digits - 1);
+    const bool is = i < a.n;
     uint64_t same = __ballot(is);
     for (int b = 0; b < a.bits; ++b) {
       const uint64_t ones = __ballot((digit >> b) & 1);
       same &= (digit >> b) & 1 ? ones : ~ones;
     }
     if (is) {
-      const int rank = __builtin_popcountll(same & ((uint64_t(1) << lane) - 1));
-      const int at = *(volatile int *)&next[wave][digit] + rank;
-      a.key_of[at] = key;
+      const int at = *(volatile int *)&next[wave][digit] + __builtin_popcountll(same & ((uint64_t(1) << lane) - 1));
+      a.key_of[at] = key[u];
       a.row_of[at] = a.first_pass ? i : a.row_from[i];
       if ((same >> lane) == 1) *(volatile int *)&next[wave][digit] = at + 1;   // the last lane of its digit
     }
@@ -176,95 +207,110 @@ __global__ void __launch_bounds__(256) embed_place_kernel(const EmbedArgs a) {
 }
 
 // Sums of the runs in one chunk of the sorted rows.  2^tpr_log2 threads share the columns of a row; the others of a workgroup take
-// other chunks.
-template <typename T, bool WIDE> struct RunSum {
-  typedef Piece<T, WIDE> P;
-  const EmbedArgs &a;
-  float sum[P::N];
-  int chunk, piece;
-  // at the end of a run: whether it reaches into the chunk from the one before, whether it goes on behind it
-  S1F_DEV void flush(int key, bool into, bool on) {
-    if (key < a.vocab) {
-      if (into || on) {
-        store_f32<P::N>((into ? a.head : a.tail) + (int64_t)chunk * a.hidden + piece * P::N, sum);
-      } else {
-        float *to = a.acc + key * a.acc_stride + piece * P::N;
-        float was[P::N];
-        load_f32<P::N>(to, was);
-#pragma unroll
-        for (int e = 0; e < P::N; ++e) was[e] += a.scale * sum[e];
-        store_f32<P::N>(to, was);
-      }
-    }
-#pragma unroll
-    for (int e = 0; e < P::N; ++e) sum[e] = 0.f;
-  }
-};
-
+// other chunks.  Of eight rows at a time everything is asked for together, the accumulators that their runs end in included.
 template <typename T, bool WIDE> __global__ void __launch_bounds__(256) embed_sum_kernel(const EmbedArgs a) {
   typedef Piece<T, WIDE> P;
   const int tpr = 1 << a.tpr_log2;
-  RunSum<T, WIDE> s{a, {}, (int)(blockIdx.x << (8 - a.tpr_log2)) + (int)(threadIdx.x >> a.tpr_log2),
-                    (int)(blockIdx.y * tpr + (threadIdx.x & (tpr - 1)))};
-  const int begin = s.chunk * a.chunk, end = begin + a.chunk < a.n ? begin + a.chunk : a.n;
-  if (begin >= a.n || s.piece >= a.pieces) return;
-  const T *dout = reinterpret_cast<const T *>(a.dout) + s.piece * P::N;
+  const int chunk = (int)(blockIdx.x << (8 - a.tpr_log2)) + (int)(threadIdx.x >> a.tpr_log2);
+  const int piece = blockIdx.y * tpr + (threadIdx.x & (tpr - 1));
+  const int begin = chunk * a.chunk, end = begin + a.chunk < a.n ? begin + a.chunk : a.n;
+  if (begin >= a.n || piece >= a.pieces) return;
+  const T *dout = reinterpret_cast<const T *>(a.dout) + piece * P::N;
+  const int64_t part = (int64_t)chunk * a.part_ld + piece * P::N;
+  const int left = a.hidden - piece * P::N;
   int key = a.key_of[begin];
-  bool into = begin > 0 && a.key_of[begin - 1] == key;
-  constexpr int U = 8;   // rows asked for together
+  bool into = begin > 0 && a.key_of[begin - 1] == key;   // the run reaches into the chunk from the one before
+  float sum[P::N];
+#pragma unroll
+  for (int e = 0; e < P::N; ++e) sum[e] = 0.f;
+  constexpr int U = 8;
   for (int i = begin; i < end && key < a.vocab; i += U) {
-    int k[U];
+    int k[U + 1];
     typename P::Values v[U];
+    float was[U][P::N];
+#pragma unroll
+    for (int u = 0; u <= U; ++u) k[u] = i + u < a.n ? a.key_of[i + u] : a.vocab;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int at = i + u < end ? i + u : end - 1;
-      k[u] = a.key_of[at];
-      P::load(dout + a.y.offset(a.row_of[at]), v[u]);
+      P::load(dout + a.y.offset(a.row_of[at]), left, v[u]);
+      if (k[u] != k[u + 1] && k[u] < a.vocab && i + u < end) load_f32<P::N, WIDE>(a.acc + k[u] * a.acc_stride + piece * P::N, left, was[u]);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (i + u >= end) break;
-      if (k[u] != key) {
-        s.flush(key, into, false);
-        into = false;
-        key = k[u];
-      }
+      if (i + u >= end || k[u] >= a.vocab) break;
 #pragma unroll
-      for (int e = 0; e < P::N; ++e) s.sum[e] += v[u][e];
+      for (int e = 0; e < P::N; ++e) sum[e] += v[u][e];
+      if (k[u] != k[u + 1]) {   // the run ends
+        if (into) {
+          store_f32<P::N, true>(a.head + part, P::N, sum);
+        } else {
+#pragma unroll
+          for (int e = 0; e < P::N; ++e) was[u][e] += a.scale * sum[e];
+          store_f32<P::N, WIDE>(a.acc + k[u] * a.acc_stride + piece * P::N, left, was[u]);
+        }
+        into = false;
+#pragma unroll
+        for (int e = 0; e < P::N; ++e) sum[e] = 0.f;
+      } else if (i + u + 1 == end) {   // it goes on behind the chunk
+        store_f32<P::N, true>((into ? a.head : a.tail) + part, P::N, sum);
+        if (!into && piece == 0) a.long_runs[1 + atomicAdd(a.long_runs, 1)] = chunk;
+      }
     }
+    key = k[U];
   }
-  s.flush(key, into, end < a.n && a.key_of[end] == key);
 }
 
-// Runs longer than a chunk: the threads of the chunk in which one starts add up what it has left there and in the chunks behind.
-template <int N> __global__ void __launch_bounds__(256) embed_join_kernel(const EmbedArgs a) {
-  const int tpr = 1 << a.tpr_log2;
-  const int chunk = (int)(blockIdx.x << (8 - a.tpr_log2)) + (int)(threadIdx.x >> a.tpr_log2);
-  const int piece = blockIdx.y * tpr + (threadIdx.x & (tpr - 1));
-  const int begin = chunk * a.chunk;
-  int end = begin + a.chunk;
-  if (end >= a.n || piece >= a.pieces) return;
-  const int key = a.key_of[end - 1];
-  if (key >= a.vocab || a.key_of[end] != key) return;
-  if (begin > 0 && a.key_of[begin - 1] == key) return;   // it has started further in front
-  float sum[N], more[N];
-  load_f32<N>(a.tail + (int64_t)chunk * a.hidden + piece * N, sum);
-  for (int c = chunk + 1;; ++c) {
-    load_f32<N>(a.head + (int64_t)c * a.hidden + piece * N, more);
+// Runs longer than a chunk, which the sums have listed by the chunk in which each starts (in any order: no result depends on it).  A workgroup takes 64
+// pieces of the columns of one and adds up what it has left there and in the chunks behind, its waves an eighth of them each.  (One thread one after the
+// other: 48 us for the 2100 rows of the most frequent of 50021 tokens; a workgroup for every chunk, most of which end at once: 17 to 60.)
+template <int N> __global__ void __launch_bounds__(512) embed_join_kernel(const EmbedArgs a) {
+  constexpr int SHARES = 8;
+  __shared__ __attribute__((aligned(16))) float meet[SHARES][64 * N];
+  const int lane = threadIdx.x & 63, share = threadIdx.x >> 6, blocks = (a.pieces + 63) / 64, units = *a.long_runs * blocks;
+  for (int unit = blockIdx.x; unit < units; unit += gridDim.x) {
+    const int chunk = a.long_runs[1 + unit / blocks], piece = unit % blocks * 64 + lane;
+    const int key = a.key_of[(chunk + 1) * a.chunk];
+    // last chunk that begins within the run: 64 of them are asked at a time
+    const int all = (a.n + a.chunk - 1) / a.chunk;
+    int last = chunk;
+    for (int more = 64; more == 64; last += more) {
+      const int c = last + 1 + lane;
+      const uint64_t on = __ballot(c < all && a.key_of[(c < all ? c : 0) * a.chunk] == key);
+      more = ~on ? __builtin_ctzll(~on) : 64;
+    }
+    const int chunks = last - chunk, stop = chunk + 1 + chunks * (share + 1) / SHARES;
+    const bool is = piece < a.pieces;
+    const float *head = a.head + (is ? piece : 0) * N;
+    float sum[N];
 #pragma unroll
-    for (int e = 0; e < N; ++e) sum[e] += more[e];
-    end += a.chunk;
-    if (end >= a.n || a.key_of[end] != key || a.key_of[end - 1] != key) break;
+    for (int e = 0; e < N; ++e) sum[e] = 0.f;
+    constexpr int U = 4;
+    for (int c = chunk + 1 + chunks * share / SHARES; c < stop; c += U) {
+      float more[U][N];
+#pragma unroll
+      for (int u = 0; u < U; ++u) load_f32<N, true>(head + (int64_t)(c + u < stop ? c + u : c) * a.part_ld, N, more[u]);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int e = 0; e < N; ++e) sum[e] += c + u < stop ? more[u][e] : 0.f;
+    }
+    __syncthreads();   // (the sums of the unit before have been read)
+    store_f32<N, true>(&meet[share][lane * N], N, sum);
+    __syncthreads();
+    const int col = (unit % blocks) * 64 * N + threadIdx.x;
+    static_assert(64 * N <= 64 * SHARES, "a column to a thread");
+    if ((int)threadIdx.x < 64 * N && col < a.hidden) {
+      float *to = a.acc + key * a.acc_stride + col, total = a.tail[(int64_t)chunk * a.part_ld + col];
+      const float was = *to;
+#pragma unroll
+      for (int w = 0; w < SHARES; ++w) total += meet[w][threadIdx.x];
+      *to = was + a.scale * total;
+    }
   }
-  float *to = a.acc + key * a.acc_stride + piece * N;
-  load_f32<N>(to, more);
-#pragma unroll
-  for (int e = 0; e < N; ++e) more[e] += a.scale * sum[e];
-  store_f32<N>(to, more);
 }
 
 constexpr int32_t kMostVocab = 1 << 26;   // three sorting passes
-constexpr int32_t kMostRanked = 16384;    // rows up to which counting sorts them
 
 int threads_per_row_log2(int64_t pieces) {
   int t = 3;
@@ -278,12 +324,15 @@ int check(const s1f_rows *d, int64_t vocab, int64_t stride) {
   return vocab > kMostVocab ? S1F_EUNSUPPORTED : S1F_OK;
 }
 int64_t up(int64_t x) { return (x + 255) / 256 * 256; }
+int64_t part_ld_of(const s1f_rows *d) { return (d->hidden + 7) / 8 * 8; }
+int32_t pieces_of(const s1f_rows *d) { return (int32_t)((d->hidden + elements_of_16_bytes(d->dtype) - 1) / elements_of_16_bytes(d->dtype)); }
 struct EmbedSpace {
-  int64_t rows, keys, rows2, keys2, count, head, tail, bytes;
+  int64_t rows, keys, rows2, keys2, count, long_runs, head, tail, bytes;
 };
-constexpr int kChunk = 32;
+// Sorted rows per chunk: a chunk is a chain of a few loads, so that few rows take short ones; a long one leaves fewer partial sums.
+int chunk_of(int64_t n) { return n < 8192 ? 8 : n < 32768 ? 16 : 32; }
 EmbedSpace space_of(const s1f_rows *d) {
-  const int64_t n = d->batch * d->rows, chunks = (n + kChunk - 1) / kChunk;
+  const int64_t n = d->batch * d->rows, chunks = (n + chunk_of(n) - 1) / chunk_of(n);
   EmbedSpace s = {};
   int64_t at = 0;
   auto take = [&at](int64_t bytes) { const int64_t was = at; at += up(bytes); return was; };
@@ -292,11 +341,12 @@ EmbedSpace space_of(const s1f_rows *d) {
   if (n > kMostRanked) {
     s.rows2 = take(4 * n);
     s.keys2 = take(4 * n);
-    s.count = take(4 * kDigits * ((n + kTile - 1) / kTile));
+    s.count = take(4 * kDigits * ((n + kTile - 1) / kTile + 1));
   }
+  s.long_runs = take(4 * (chunks + 1));
   if (chunks > 1) {
-    s.head = take(4 * chunks * d->hidden);
-    s.tail = take(4 * chunks * d->hidden);
+    s.head = take(4 * chunks * part_ld_of(d));
+    s.tail = take(4 * chunks * part_ld_of(d));
   }
   s.bytes = at;
   return s;
@@ -310,8 +360,9 @@ template <typename T> int sums(const EmbedArgs &a, bool wide, hipStream_t st) {
   const void *sum = wide ? reinterpret_cast<const void *>(&embed_sum_kernel<T, true>) : reinterpret_cast<const void *>(&embed_sum_kernel<T, false>);
   if (hipLaunchKernel(sum, grid, dim3(256), params, 0, st) != hipSuccess) return S1F_EDEVICE;
   if (chunks == 1) return S1F_OK;
-  const void *join = wide ? reinterpret_cast<const void *>(&embed_join_kernel<Elem<T>::CE>) : reinterpret_cast<const void *>(&embed_join_kernel<1>);
-  return hipLaunchKernel(join, grid, dim3(256), params, 0, st) == hipSuccess ? S1F_OK : S1F_EDEVICE;
+  const void *join = reinterpret_cast<const void *>(&embed_join_kernel<Elem<T>::CE>);
+  const int64_t units = chunks * ((a.pieces + 63) / 64);
+  return hipLaunchKernel(join, dim3((unsigned)(units < 2048 ? units : 2048)), dim3(512), params, 0, st) == hipSuccess ? S1F_OK : S1F_EDEVICE;
 }
 
 }  // namespace
@@ -331,7 +382,7 @@ extern "C" int s1f_embed_fwd(const s1f_rows *desc, const int64_t *ids, int64_t i
   a.table = table; a.table_stride = table_stride;
   a.out = out; a.y = y_rows(desc);
   a.n = (int32_t)(desc->batch * desc->rows); a.hidden = desc->hidden; a.vocab = (int32_t)vocab; a.scale = scale;
-  a.pieces = wide ? desc->hidden / (int32_t)elements_of_16_bytes(desc->dtype) : desc->hidden;
+  a.pieces = pieces_of(desc);
   a.tpr_log2 = threads_per_row_log2(a.pieces);
   const int64_t groups = 256 >> a.tpr_log2, grid = (a.n + groups - 1) / groups;
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
@@ -359,17 +410,19 @@ extern "C" int s1f_embed_bwd(const s1f_rows *desc, const int64_t *ids, int64_t i
   a.dout = dout; a.y = y_rows(desc);
   a.acc = dtable_acc; a.acc_stride = acc_stride;
   a.n = (int32_t)(desc->batch * desc->rows); a.hidden = desc->hidden; a.vocab = (int32_t)vocab; a.scale = scale;
-  a.pieces = wide ? desc->hidden / (int32_t)elements_of_16_bytes(desc->dtype) : desc->hidden;
+  a.pieces = pieces_of(desc);
   a.tpr_log2 = threads_per_row_log2(a.pieces);
-  a.chunk = kChunk;
+  a.chunk = chunk_of(a.n);
+  a.part_ld = (int32_t)part_ld_of(desc);
   a.row_of = reinterpret_cast<int32_t *>(ws + space.rows);
   a.key_of = reinterpret_cast<int32_t *>(ws + space.keys);
+  a.long_runs = reinterpret_cast<int32_t *>(ws + space.long_runs);
   a.head = reinterpret_cast<float *>(ws + space.head);
   a.tail = reinterpret_cast<float *>(ws + space.tail);
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
   int e = S1F_OK;
   if (a.n <= kMostRanked) {
-    e = launch_rows_kernel(&embed_rank_kernel, (a.n + 31) / 32, 256, a, st);
+    e = launch_rows_kernel(&embed_rank_kernel, (a.n + kRanked - 1) / kRanked, 1024, a, st, 4 * 64 * ((a.n + 63) / 64));
   } else {
     int all = 1;
     while ((int64_t(1) << all) <= vocab) ++all;   // bits of 0 .. vocab
@@ -385,9 +438,9 @@ extern "C" int s1f_embed_bwd(const s1f_rows *desc, const int64_t *ids, int64_t i
       pass.first_pass = p == 0;
       pass.shift = all * p / passes;
       pass.bits = all * (p + 1) / passes - pass.shift;
-      e = launch_rows_kernel(&embed_count_kernel, (a.tiles + 3) / 4, 256, pass, st);
-      if (e == S1F_OK) e = launch_rows_kernel(&embed_scan_kernel, 1, 1024, pass, st);
-      if (e == S1F_OK) e = launch_rows_kernel(&embed_place_kernel, (a.tiles + 3) / 4, 256, pass, st);
+      e = launch_rows_kernel(&embed_count_kernel, a.tiles, 256, pass, st);
+      if (e == S1F_OK) e = launch_rows_kernel(&embed_scan_kernel, ((1 << pass.bits) + 3) / 4, 256, pass, st);
+      if (e == S1F_OK) e = launch_rows_kernel(&embed_place_kernel, a.tiles, 256, pass, st);
     }
   }
   if (e != S1F_OK) return e;

@@ -118,17 +118,12 @@ template <typename T, bool WIDE, bool ROWS> __global__ void __launch_bounds__(25
   const T *from = ROWS ? reinterpret_cast<const T *>(a.x) + a.xs.offset(a.row_of[row])
                        : reinterpret_cast<const T *>(a.weight) + (a.first + row) * a.weight_stride;
   float v[8];
-  if constexpr (WIDE) {
 #pragma unroll
-    for (int i = 0; i < 8; i += Piece<T, true>::N) {
-      typename Piece<T, true>::Values p;
-      Piece<T, true>::load(from + 8 * c + i, p);
+  for (int i = 0; i < 8; i += Piece<T, WIDE>::N) {
+    typename Piece<T, WIDE>::Values p;
+    Piece<T, WIDE>::load(from + 8 * c + i, a.hidden - 8 * c - i, p);
 #pragma unroll
-      for (int e = 0; e < Piece<T, true>::N; ++e) v[i + e] = p[e];
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = 8 * c + e < a.hidden ? (float)from[8 * c + e] : 0.f;
+    for (int e = 0; e < Piece<T, WIDE>::N; ++e) v[i + e] = p[e];
   }
   bf16_t *to = (ROWS ? a.rows : a.packed) + row64 * a.width + 8 * c;
   if constexpr (sizeof(T) == 4) {
@@ -395,7 +390,7 @@ template <int PAIRS, int BM, int BN, int WM, int WN> __global__ void __launch_bo
 template <typename T, bool WIDE, int TILE> __global__ void __launch_bounds__(256) loss_dx_join_kernel(const LossArgs a) {
   typedef Piece<T, WIDE> P;
   const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int per_row = a.hidden / P::N;
+  const int per_row = (a.hidden + P::N - 1) / P::N;
   const int64_t row = id / per_row;
   const int col = (int)(id - row * per_row) * P::N;
   if (row >= a.n) return;
@@ -404,18 +399,18 @@ template <typename T, bool WIDE, int TILE> __global__ void __launch_bounds__(256
 #pragma unroll
   for (int e = 0; e < P::N; ++e) v[e] = 0.f;
   if (slot >= 0) {
-    load_f32<P::N>(a.sum + (int64_t)slot * a.width + col, v);
+    load_f32<P::N, true>(a.sum + (int64_t)slot * a.width + col, P::N, v);
     if (a.splits > 1) {
       const int tile = encode_tile(a, slot / TILE, col / TILE);
       if (tile >= a.whole)
         for (int p = 0; p + 1 < a.splits; ++p) {
-          load_f32<P::N>(a.part + (((int64_t)p * a.rest + tile - a.whole) * TILE + slot % TILE) * TILE + col % TILE, more);
+          load_f32<P::N, true>(a.part + (((int64_t)p * a.rest + tile - a.whole) * TILE + slot % TILE) * TILE + col % TILE, P::N, more);
 #pragma unroll
           for (int e = 0; e < P::N; ++e) v[e] += more[e];
         }
     }
   }
-  P::store(reinterpret_cast<T *>(a.dx) + a.xs.offset((int)row) + col, v);
+  P::store(reinterpret_cast<T *>(a.dx) + a.xs.offset((int)row) + col, a.hidden - col, v);
 }
 
 // dW of a piece of the vocabulary: added into fp32 accumulators (ADD), or written in bf16.
@@ -720,7 +715,7 @@ template <typename T, bool ADD> int backward(const s1f_rows *d, LossArgs a, cons
   const int side = p.dx.tile == kBig ? 256 : 128;
   tiles_of(a, p.n, a.width, side, side);
   const bool wide = wide_x(d, a.dx);
-  const int64_t per_row = wide ? d->hidden / elements_of_16_bytes(d->dtype) : d->hidden, grid = (p.n * per_row + 255) / 256;
+  const int64_t per_row = (d->hidden + elements_of_16_bytes(d->dtype) - 1) / elements_of_16_bytes(d->dtype), grid = (p.n * per_row + 255) / 256;
   if (grid * 256 >= (int64_t(1) << 32)) return S1F_EUNSUPPORTED;
   if (side == 256) return launch_rows_kernel(wide ? &loss_dx_join_kernel<T, true, 256> : &loss_dx_join_kernel<T, false, 256>, grid, 256, a, st);
   return launch_rows_kernel(wide ? &loss_dx_join_kernel<T, true, 128> : &loss_dx_join_kernel<T, false, 128>, grid, 256, a, st);

@@ -18,14 +18,14 @@ struct NormArgs {
   const float *mean_in, *rstd_in;
   void *y, *dx;
   float *mean, *rstd;
-  float *part;                    // [workgroup][dgamma, dbeta][hidden]
+  float *part;                    // [workgroup][dgamma, dbeta][part_ld]
   float *dgamma, *dbeta;
   RowsOf xs, ys;
-  int32_t n, hidden, pieces, parts;
+  int32_t n, hidden, pieces, part_ld, parts;
   float eps, inv_hidden;
 };
 
-// Sum over the TPR threads that share a row (64, 256 or 1024); every one of them gets it.  `lds`: a float per wave, not written
+// Sum over the TPR threads that share a row (64, 256, 512 or 1024); every one of them gets it.  `lds`: a float per wave, not written
 // before all have read the sum before the last.
 S1F_DEV float wave_sum(float x) {
 #pragma unroll
@@ -59,45 +59,45 @@ template <typename T, bool WIDE, int TPR, int E> __global__ void __launch_bounds
   const int row = blockIdx.x * (THREADS / TPR) + threadIdx.x / TPR, t = threadIdx.x % TPR;
   if (row >= a.n) return;   // (whole waves; with more threads to a row there is one row to a workgroup)
   const T *x = reinterpret_cast<const T *>(a.x) + a.xs.offset(row);
+  typename P::Raw raw[NP];
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    const int p = t + i * TPR;
+    raw[i] = p < a.pieces ? P::get(x + p * P::N, a.hidden - p * P::N) : P::none();
+  }
   typename P::Values v[NP];
   float s[1] = {0.f};
 #pragma unroll
   for (int i = 0; i < NP; ++i) {
-    const int p = t + i * TPR;
-    if (p < a.pieces) {
-      P::load(x + p * P::N, v[i]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < P::N; ++e) v[i][e] = 0.f;
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < NP; ++i)
+    P::values(raw[i], v[i]);
 #pragma unroll
     for (int e = 0; e < P::N; ++e) s[0] += v[i][e];
+  }
   row_sums<TPR>(s, lds[0]);
   const float mean = s[0] * a.inv_hidden;
   s[0] = 0.f;
 #pragma unroll
-  for (int i = 0; i < NP; ++i)
+  for (int i = 0; i < NP; ++i) {
+    const int left = a.hidden - (t + i * TPR) * P::N;
 #pragma unroll
     for (int e = 0; e < P::N; ++e) {
       v[i][e] -= mean;
-      if (t + i * TPR < a.pieces) s[0] += v[i][e] * v[i][e];
+      if (WIDE ? left > 0 : e < left) s[0] += v[i][e] * v[i][e];
     }
+  }
   row_sums<TPR>(s, lds[1]);
   const float rstd = 1.f / sqrtf(s[0] * a.inv_hidden + a.eps);
   T *y = reinterpret_cast<T *>(a.y) + a.ys.offset(row);
 #pragma unroll
   for (int i = 0; i < NP; ++i) {
-    const int p = t + i * TPR;
+    const int p = t + i * TPR, left = a.hidden - p * P::N;
     if (p >= a.pieces) break;
     typename P::Values g, b;
-    P::load(reinterpret_cast<const T *>(a.gamma) + p * P::N, g);
-    P::load(reinterpret_cast<const T *>(a.beta) + p * P::N, b);
+    P::load(reinterpret_cast<const T *>(a.gamma) + p * P::N, left, g);
+    P::load(reinterpret_cast<const T *>(a.beta) + p * P::N, left, b);
 #pragma unroll
     for (int e = 0; e < P::N; ++e) v[i][e] = v[i][e] * rstd * g[e] + b[e];
-    P::store(y + p * P::N, v[i]);
+    P::store(y + p * P::N, left, v[i]);
   }
   if (t == 0) {
     a.mean[row] = mean;
@@ -105,52 +105,60 @@ template <typename T, bool WIDE, int TPR, int E> __global__ void __launch_bounds
   }
 }
 
+// A workgroup's rows one after the other; the next one is asked for before the sums of this one, which a workgroup waits for together.  Rows stay as they
+// were loaded and are computed with twice, which takes half the registers of fp32 values.
 template <typename T, bool WIDE, int TPR, int E> __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_bwd_kernel(const NormArgs a) {
   typedef Piece<T, WIDE> P;
   constexpr int NP = E / P::N, THREADS = TPR < 256 ? 256 : TPR, R = THREADS / TPR;
   __shared__ float lds[2][2 * 16];
   __shared__ float other[R > 1 ? R - 1 : 1][R > 1 ? 2 * TPR * E : 1];
-  const int t = threadIdx.x % TPR, group = threadIdx.x / TPR;
+  const int t = threadIdx.x % TPR, group = threadIdx.x / TPR, step = gridDim.x * R;
   float dg[NP][P::N], db[NP][P::N];
-  typename P::Values gain[NP];
+  typename P::Raw gain[NP], x[NP], dy[NP], next_x[NP], next_dy[NP];
+  float mean = 0.f, rstd = 0.f, next_mean = 0.f, next_rstd = 0.f;
+  auto ask = [&](int row) {
+    const T *from_x = reinterpret_cast<const T *>(a.x) + a.xs.offset(row), *from_dy = reinterpret_cast<const T *>(a.dy) + a.ys.offset(row);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int p = t + i * TPR, left = a.hidden - p * P::N;
+      next_x[i] = p < a.pieces ? P::get(from_x + p * P::N, left) : P::none();
+      next_dy[i] = p < a.pieces ? P::get(from_dy + p * P::N, left) : P::none();
+    }
+    next_mean = a.mean_in[row];
+    next_rstd = a.rstd_in[row];
+  };
+  int row = blockIdx.x * R + group;
+  if (row < a.n) ask(row);
 #pragma unroll
   for (int i = 0; i < NP; ++i) {
     const int p = t + i * TPR;
-    if (p < a.pieces) P::load(reinterpret_cast<const T *>(a.gamma) + p * P::N, gain[i]);
+    gain[i] = p < a.pieces ? P::get(reinterpret_cast<const T *>(a.gamma) + p * P::N, a.hidden - p * P::N) : P::none();
 #pragma unroll
-    for (int e = 0; e < P::N; ++e) {
-      dg[i][e] = db[i][e] = 0.f;
-      if (p >= a.pieces) gain[i][e] = 0.f;
-    }
+    for (int e = 0; e < P::N; ++e) dg[i][e] = db[i][e] = 0.f;
   }
   int turn = 0;
   // (rows that share a workgroup never wait for each other: one row to a wave, or one to a workgroup)
-  for (int row = blockIdx.x * R + group; row < a.n; row += gridDim.x * R, turn ^= 1) {
-    const T *x = reinterpret_cast<const T *>(a.x) + a.xs.offset(row), *dy = reinterpret_cast<const T *>(a.dy) + a.ys.offset(row);
-    const float mean = a.mean_in[row], rstd = a.rstd_in[row];
-    typename P::Values xh[NP], d[NP];
+  for (; row < a.n; row += step, turn ^= 1) {
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      const int p = t + i * TPR;
-      if (p < a.pieces) {
-        P::load(x + p * P::N, xh[i]);
-        P::load(dy + p * P::N, d[i]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < P::N; ++e) xh[i][e] = d[i][e] = 0.f;
-      }
+      x[i] = next_x[i];
+      dy[i] = next_dy[i];
     }
+    mean = next_mean;
+    rstd = next_rstd;
+    if (row + step < a.n) ask(row + step);
     float s[2] = {0.f, 0.f};
+    // (behind the end of a row dy is 0)
 #pragma unroll
     for (int i = 0; i < NP; ++i)
 #pragma unroll
       for (int e = 0; e < P::N; ++e) {
-        xh[i][e] = t + i * TPR < a.pieces ? (xh[i][e] - mean) * rstd : 0.f;
-        dg[i][e] += d[i][e] * xh[i][e];
-        db[i][e] += d[i][e];
-        d[i][e] *= gain[i][e];
-        s[0] += d[i][e];
-        s[1] += d[i][e] * xh[i][e];
+        const float xh = ((float)x[i][e] - mean) * rstd, d = (float)dy[i][e], g = d * (float)gain[i][e];
+        const bool is = WIDE || e < a.hidden - (t + i * TPR) * P::N;
+        dg[i][e] += is ? d * xh : 0.f;
+        db[i][e] += d;
+        s[0] += g;
+        s[1] += is ? g * xh : 0.f;
       }
     row_sums<TPR>(s, lds[turn]);
     const float c0 = s[0] * a.inv_hidden, c1 = s[1] * a.inv_hidden;
@@ -159,9 +167,17 @@ template <typename T, bool WIDE, int TPR, int E> __global__ void __launch_bounds
     for (int i = 0; i < NP; ++i) {
       const int p = t + i * TPR;
       if (p >= a.pieces) break;
+      // (else the compiler keeps the fp32 values after all)
+      settle(x[i]);
+      settle(dy[i]);
+      settle(gain[i]);
+      typename P::Values o;
 #pragma unroll
-      for (int e = 0; e < P::N; ++e) d[i][e] = rstd * (d[i][e] - c0 - xh[i][e] * c1);
-      P::store(dx + p * P::N, d[i]);
+      for (int e = 0; e < P::N; ++e) {
+        const float xh = ((float)x[i][e] - mean) * rstd, g = (float)dy[i][e] * (float)gain[i][e];
+        o[e] = rstd * (g - c0 - xh * c1);
+      }
+      P::store(dx + p * P::N, a.hidden - p * P::N, o);
     }
   }
   if constexpr (R > 1) {   // the groups' sums meet in the first one
@@ -186,20 +202,20 @@ template <typename T, bool WIDE, int TPR, int E> __global__ void __launch_bounds
           db[i][e] += other[r][(2 * (i * P::N + e) + 1) * TPR + t];
         }
   }
-  float *part = a.part + (int64_t)blockIdx.x * 2 * a.hidden;
+  float *part = a.part + (int64_t)blockIdx.x * 2 * a.part_ld;
 #pragma unroll
   for (int i = 0; i < NP; ++i) {
     const int p = t + i * TPR;
     if (p >= a.pieces) break;
-    store_f32<P::N>(part + p * P::N, dg[i]);
-    store_f32<P::N>(part + a.hidden + p * P::N, db[i]);
+    store_f32<P::N, true>(part + p * P::N, P::N, dg[i]);
+    store_f32<P::N, true>(part + a.part_ld + p * P::N, P::N, db[i]);
   }
 }
 
 // Adds the workgroups' sums: 64 columns of [dgamma, dbeta] per workgroup, its four waves a quarter of the workgroups each.
 __global__ void __launch_bounds__(256) norm_join_kernel(const NormArgs a) {
   __shared__ float of_wave[4][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, width = 2 * a.hidden, c = blockIdx.x * 64 + lane;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, width = 2 * a.part_ld, c = blockIdx.x * 64 + lane, col = c < a.part_ld ? c : c - a.part_ld;
   float s = 0.f;
   if (c < width) {
     const int begin = a.parts * wave / 4, end = a.parts * (wave + 1) / 4;
@@ -208,9 +224,9 @@ __global__ void __launch_bounds__(256) norm_join_kernel(const NormArgs a) {
   }
   of_wave[wave][lane] = s;
   __syncthreads();
-  if (wave > 0 || c >= width) return;
+  if (wave > 0 || c >= width || col >= a.hidden) return;
   s = (of_wave[0][lane] + of_wave[1][lane]) + (of_wave[2][lane] + of_wave[3][lane]);
-  float *to = c < a.hidden ? a.dgamma + c : a.dbeta + (c - a.hidden);
+  float *to = (c < a.part_ld ? a.dgamma : a.dbeta) + col;
   *to += s;
 }
 
@@ -224,9 +240,10 @@ struct Shape {
 #define S1F_NORM_SHAPES(KERNEL)                                                                                  \
   template <typename T, bool WIDE> Shape KERNEL##_shape(int hidden) {                                            \
     if (hidden <= 64 * 8) return {&KERNEL##_kernel<T, WIDE, 64, 8>, 256, 4};                                     \
+    if (hidden <= 64 * 16) return {&KERNEL##_kernel<T, WIDE, 64, 16>, 256, 4};                                   \
     if (hidden <= 256 * 8) return {&KERNEL##_kernel<T, WIDE, 256, 8>, 256, 1};                                   \
     if (hidden <= 256 * 16) return {&KERNEL##_kernel<T, WIDE, 256, 16>, 256, 1};                                 \
-    if (hidden <= 256 * 32) return {&KERNEL##_kernel<T, WIDE, 256, 32>, 256, 1};                                 \
+    if (hidden <= 512 * 16) return {&KERNEL##_kernel<T, WIDE, 512, 16>, 512, 1};                                 \
     return {&KERNEL##_kernel<T, WIDE, 1024, 16>, 1024, 1};                                                       \
   }
 S1F_NORM_SHAPES(norm_fwd)
@@ -237,11 +254,13 @@ static_assert(kMostHidden <= 1024 * 16, "a row stays in registers");
   ((dtype) == S1F_BF16 ? ((wide) ? SHAPE<bf16_t, true>(hidden) : SHAPE<bf16_t, false>(hidden))             \
                        : ((wide) ? SHAPE<float, true>(hidden) : SHAPE<float, false>(hidden)))
 
-NormArgs args_of(const s1f_rows *d, bool wide) {
+int32_t part_ld_of(const s1f_rows *d) { return (d->hidden + 7) / 8 * 8; }
+NormArgs args_of(const s1f_rows *d) {
   NormArgs a = {};
   a.xs = x_rows(d); a.ys = y_rows(d);
   a.n = (int32_t)(d->batch * d->rows); a.hidden = d->hidden;
-  a.pieces = wide ? d->hidden / (int32_t)elements_of_16_bytes(d->dtype) : d->hidden;
+  a.pieces = (int32_t)((d->hidden + elements_of_16_bytes(d->dtype) - 1) / elements_of_16_bytes(d->dtype));
+  a.part_ld = part_ld_of(d);
   a.inv_hidden = 1.f / (float)d->hidden;
   return a;
 }
@@ -261,7 +280,7 @@ extern "C" int s1f_layer_norm_fwd(const s1f_rows *desc, const void *x, const voi
     if (!on_element(p, desc->dtype)) return S1F_EINVAL;
   if (!on4(mean) || !on4(rstd)) return S1F_EINVAL;
   const bool wide = wide_call(desc) && on16(x) && on16(gamma) && on16(beta) && on16(y);
-  NormArgs a = args_of(desc, wide);
+  NormArgs a = args_of(desc);
   a.x = x; a.gamma = gamma; a.beta = beta; a.y = y; a.mean = mean; a.rstd = rstd; a.eps = eps;
   const Shape s = S1F_BY_TYPE(norm_fwd_shape, desc->dtype, wide, desc->hidden);
   return launch_rows_kernel(s.kernel, (a.n + s.rows - 1) / s.rows, s.threads, a, reinterpret_cast<hipStream_t>(hip_stream));
@@ -270,7 +289,7 @@ extern "C" int s1f_layer_norm_fwd(const s1f_rows *desc, const void *x, const voi
 extern "C" size_t s1f_layer_norm_bwd_workspace_bytes(const s1f_rows *desc) {
   if (check_rows(desc, true, true) != S1F_OK) return 0;
   const int64_t n = desc->batch * desc->rows;
-  return (size_t)((n < kParts ? n : kParts) * 2 * desc->hidden * 4);
+  return (size_t)((n < kParts ? n : kParts) * 2 * part_ld_of(desc) * 4);
 }
 
 extern "C" int s1f_layer_norm_bwd(const s1f_rows *desc, const void *dy, const void *x, const void *gamma, const float *mean, const float *rstd,
@@ -283,7 +302,7 @@ extern "C" int s1f_layer_norm_bwd(const s1f_rows *desc, const void *dy, const vo
   if (!on4(mean) || !on4(rstd) || !on4(dgamma_acc) || !on4(dbeta_acc)) return S1F_EINVAL;
   if (workspace_bytes < s1f_layer_norm_bwd_workspace_bytes(desc)) return S1F_EINVAL;
   const bool wide = wide_call(desc) && on16(dy) && on16(x) && on16(gamma) && on16(dx);
-  NormArgs a = args_of(desc, wide);
+  NormArgs a = args_of(desc);
   a.x = x; a.dy = dy; a.gamma = gamma; a.mean_in = mean; a.rstd_in = rstd; a.dx = dx;
   a.dgamma = dgamma_acc; a.dbeta = dbeta_acc; a.part = reinterpret_cast<float *>(workspace);
   const Shape s = S1F_BY_TYPE(norm_bwd_shape, desc->dtype, wide, desc->hidden);
@@ -292,5 +311,5 @@ extern "C" int s1f_layer_norm_bwd(const s1f_rows *desc, const void *dy, const vo
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
   const int e = launch_rows_kernel(s.kernel, a.parts, s.threads, a, st);
   if (e != S1F_OK) return e;
-  return launch_rows_kernel(&norm_join_kernel, (2 * a.hidden + 63) / 64, 256, a, st);
+  return launch_rows_kernel(&norm_join_kernel, (2 * a.part_ld + 63) / 64, 256, a, st);
 }
