@@ -299,6 +299,7 @@ _calls, _calls_of = None, None
 class _PythonForms:
     """In place of the compiled forms where they cannot be loaded: every call is left to the Python code."""
     fwd = fwd_ws = bwd = bwd_noalloc = append = emit = staticmethod(lambda *args: -1)
+    embed_fwd = embed_bwd = layer_norm_fwd = layer_norm_bwd = token_loss_fwd = token_loss_bwd = fwd
 
 
 def _load_calls():
@@ -328,7 +329,8 @@ def _native():
             _calls, _calls_of = _PythonForms, lib
             return _calls
         entry = (lib.s1f_seg_attn_fwd, lib.s1f_seg_attn_fwd_ws, lib.s1f_seg_attn_bwd, lib.s1f_seg_attn_bwd_noalloc,
-                 lib.s1f_kv_append, lib.s1f_kv_grad_emit)
+                 lib.s1f_kv_append, lib.s1f_kv_grad_emit, lib.s1f_embed_fwd, lib.s1f_embed_bwd, lib.s1f_layer_norm_fwd,
+                 lib.s1f_layer_norm_bwd, lib.s1f_token_loss_fwd, lib.s1f_token_loss_bwd)
         _torch_calls.bind(*[ctypes.cast(f, ctypes.c_void_p).value for f in entry], torch.cuda.current_device,
                           getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
                               lambda device: torch.cuda.current_stream(device).cuda_stream))
@@ -688,6 +690,8 @@ def embed_fwd(ids, table, scale: float, out):
 
     ids [B, rows] int64; table [vocab, hidden]; out [B, rows, hidden] of the table's type.  Enqueued on torch's current stream.
     """
+    if _done(_native().embed_fwd(ids, table, scale, out), "s1f_embed_fwd"):
+        return
     _check_device(out, ids, table)
     desc = _rows_desc(y=out)
     at, ids_sb = _tokens(ids, out)
@@ -703,6 +707,8 @@ def embed_bwd_workspace_bytes(ids, dout, dtable_acc) -> int:
 def embed_bwd(ids, dout, scale: float, dtable_acc, workspace):
     """s1f_embed_bwd on torch device tensors: adds scale times the rows of dout to the fp32 rows of dtable_acc [vocab, hidden] that
     their tokens name; workspace is any device tensor of at least embed_bwd_workspace_bytes(...) bytes."""
+    if _done(_native().embed_bwd(ids, dout, scale, dtable_acc, workspace), "s1f_embed_bwd"):
+        return
     import torch
     _check_device(dout, ids, dtable_acc, workspace)
     desc = _rows_desc(y=dout)
@@ -715,6 +721,8 @@ def embed_bwd(ids, dout, scale: float, dtable_acc, workspace):
 def layer_norm_fwd(x, gamma, beta, eps: float, y, mean, rstd):
     """s1f_layer_norm_fwd on torch device tensors: x, y [B, rows, hidden]; gamma, beta [hidden] of their type; mean, rstd
     [B, rows] fp32, overwritten.  Enqueued on torch's current stream."""
+    if _done(_native().layer_norm_fwd(x, gamma, beta, eps, y, mean, rstd), "s1f_layer_norm_fwd"):
+        return
     _check_device(x, gamma, beta, y, mean, rstd)
     desc = _rows_desc(x, y)
     _vectors(x.shape[2], x.dtype, gamma, beta)
@@ -730,6 +738,8 @@ def layer_norm_bwd_workspace_bytes(dy, x) -> int:
 def layer_norm_bwd(dy, x, gamma, mean, rstd, dx, dgamma_acc, dbeta_acc, workspace):
     """s1f_layer_norm_bwd on torch device tensors: dx, with the shape and strides of x, is overwritten; dgamma_acc and dbeta_acc
     [hidden] fp32 are added to; workspace is any device tensor of at least layer_norm_bwd_workspace_bytes(...) bytes."""
+    if _done(_native().layer_norm_bwd(dy, x, gamma, mean, rstd, dx, dgamma_acc, dbeta_acc, workspace), "s1f_layer_norm_bwd"):
+        return
     import torch
     _check_device(dy, x, gamma, mean, rstd, dx, dgamma_acc, dbeta_acc, workspace)
     desc = _rows_desc(x, dy)
@@ -754,6 +764,8 @@ def token_loss_fwd(x, weight, targets, loss, lse, workspace):
     targets [B, rows] int64 (outside [0, vocab): the row takes no part); loss, lse [B, rows] fp32, overwritten; workspace is any device
     tensor of at least token_loss_fwd_workspace_bytes(...) bytes.  Enqueued on torch's current stream.
     """
+    if _done(_native().token_loss_fwd(x, weight, targets, loss, lse, workspace), "s1f_token_loss_fwd"):
+        return
     _check_device(x, weight, targets, loss, lse, workspace)
     desc = _rows_desc(x)
     stride = _matrix(weight, x.shape[2], x.dtype, "weight")
@@ -774,6 +786,8 @@ def token_loss_bwd(dloss, x, weight, targets, lse, dx, dweight, workspace):
     dloss, lse [B, rows] fp32; dx, with the shape and strides of x, is overwritten; dweight [vocab, hidden] is added to if it is fp32 and
     overwritten if it is bf16 (bf16 rows only); workspace is any device tensor of at least token_loss_bwd_workspace_bytes(...) bytes.
     """
+    if _done(_native().token_loss_bwd(dloss, x, weight, targets, lse, dx, dweight, workspace), "s1f_token_loss_bwd"):
+        return
     _check_device(dloss, x, weight, targets, lse, dx, dweight, workspace)
     desc = _rows_desc(x)
     _same_rows(x, dx)

@@ -23,6 +23,12 @@ struct Api {
   decltype(&s1f_seg_attn_bwd_noalloc) bwd_noalloc;
   decltype(&s1f_kv_append) append;
   decltype(&s1f_kv_grad_emit) emit;
+  decltype(&s1f_embed_fwd) embed_fwd;
+  decltype(&s1f_embed_bwd) embed_bwd;
+  decltype(&s1f_layer_norm_fwd) layer_norm_fwd;
+  decltype(&s1f_layer_norm_bwd) layer_norm_bwd;
+  decltype(&s1f_token_loss_fwd) token_loss_fwd;
+  decltype(&s1f_token_loss_bwd) token_loss_bwd;
 };
 Api api = {};
 PyObject *get_device = nullptr, *get_stream = nullptr;
@@ -205,14 +211,195 @@ PyObject *emit(PyObject *, PyObject *const *args, Py_ssize_t n) {
                     ks->stride(1), ks->stride(2), x.stream);
   });
 }
-// (addresses of the six entry points, torch's functions for the current device and for a device's stream)
+// ---- rows of hidden states: embedding, layer norm, token loss --------------------------------------------------------------------------
+
+// Plain tensors of the current device, number `real_at` a float, number `optional` maybe None; and the device's stream.
+struct RowArgs {
+  const at::Tensor *t[10];
+  double real = 0.0;
+  void *stream = nullptr;
+  bool read(PyObject *const *args, Py_ssize_t n, Py_ssize_t want, Py_ssize_t real_at, Py_ssize_t optional) {
+    if (n != want || get_device == nullptr || at::impl::PythonTorchFunctionTLS::stack_len() > 0) return false;
+    int64_t device = -1;
+    for (Py_ssize_t i = 0, k = 0; i < n; ++i) {
+      if (i == real_at) {
+        if (!PyFloat_CheckExact(args[i])) return false;
+        real = PyFloat_AS_DOUBLE(args[i]);
+        continue;
+      }
+      t[k] = i == optional && args[i] == Py_None ? nullptr : plain(args[i]);
+      if (t[k] == nullptr && !(i == optional && args[i] == Py_None)) return false;
+      if (t[k] != nullptr) {
+        if (device >= 0 && t[k]->get_device() != device) return false;
+        device = t[k]->get_device();
+      }
+      ++k;
+    }
+    PyObject *dev = PyObject_CallNoArgs(get_device);
+    const long current = dev ? PyLong_AsLong(dev) : -1;
+    PyObject *st = dev ? PyObject_CallOneArg(get_stream, dev) : nullptr;
+    Py_XDECREF(dev);
+    if (st == nullptr || current != device) {
+      Py_XDECREF(st);
+      return PyErr_Clear(), false;
+    }
+    stream = PyLong_AsVoidPtr(st);
+    Py_DECREF(st);
+    return PyErr_Occurred() == nullptr || (PyErr_Clear(), false);
+  }
+};
+
+bool hidden_ok(const at::Tensor &t) { return t.dim() == 3 && (t.stride(2) == 1 || t.size(2) <= 1); }
+int64_t stride_of(const at::Tensor &t, int i) { return t.size(i) > 1 ? t.stride(i) : 0; }
+// x, y: tensors on either side of a call, or null
+bool rows_desc_of(const at::Tensor *x, const at::Tensor *y, s1f_rows *d) {
+  *d = {};
+  const at::Tensor &a = x ? *x : *y;
+  if (!hidden_ok(a) || !dtype_of(a, &d->dtype) || !fits(a.size(0)) || !fits(a.size(2))) return false;
+  if (x && y && (!hidden_ok(*y) || y->sizes() != x->sizes() || y->scalar_type() != x->scalar_type())) return false;
+  d->batch = (int32_t)a.size(0); d->hidden = (int32_t)a.size(2); d->rows = a.size(1);
+  if (x) { d->x_stride_b = stride_of(*x, 0); d->x_stride_s = stride_of(*x, 1); }
+  if (y) { d->y_stride_b = stride_of(*y, 0); d->y_stride_s = stride_of(*y, 1); }
+  return true;
+}
+bool same_rows(const at::Tensor &a, const at::Tensor &b) {
+  return hidden_ok(b) && b.sizes() == a.sizes() && stride_of(a, 0) == stride_of(b, 0) && stride_of(a, 1) == stride_of(b, 1) &&
+         b.scalar_type() == a.scalar_type();
+}
+bool tokens_ok(const at::Tensor &t, const at::Tensor &like) {
+  return t.scalar_type() == at::kLong && t.sizes() == like.sizes().slice(0, 2) && (t.size(1) <= 1 || t.stride(1) == 1);
+}
+bool row_values_ok(const at::Tensor &v, const at::Tensor &like) {
+  return v.scalar_type() == at::kFloat && v.is_contiguous() && v.sizes() == like.sizes().slice(0, 2);
+}
+bool matrix_ok(const at::Tensor &t, int64_t hidden, at::ScalarType type) {
+  return t.scalar_type() == type && t.dim() == 2 && t.size(1) == hidden && (t.stride(1) == 1 || hidden <= 1);
+}
+int64_t matrix_stride(const at::Tensor &t) { return t.size(0) > 1 ? t.stride(0) : t.size(1); }
+bool vector_ok(const at::Tensor &t, int64_t hidden, at::ScalarType type) {
+  return t.scalar_type() == type && t.dim() == 1 && t.size(0) == hidden && t.is_contiguous();
+}
+bool space_ok(const at::Tensor *ws) { return ws == nullptr || ws->is_contiguous(); }
+const int64_t *tokens_of(const at::Tensor *t) { return static_cast<const int64_t *>(t->data_ptr()); }
+const float *values_of(const at::Tensor *t) { return static_cast<const float *>(t->data_ptr()); }
+
+// (ids, table, scale, out)
+PyObject *embed_fwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  return call([&]() -> int {
+    RowArgs x;
+    s1f_rows d;
+    if (!x.read(args, n, 4, 2, -1)) return kPython;
+    auto &[ids, table, out] = reinterpret_cast<const at::Tensor *(&)[3]>(x.t);
+    if (!rows_desc_of(nullptr, out, &d) || !tokens_ok(*ids, *out) || !matrix_ok(*table, out->size(2), out->scalar_type())) return kPython;
+    const int64_t *i = tokens_of(ids);
+    void *const p[] = {ptr(table), ptr(out)};
+    Unlocked u;
+    return api.embed_fwd(&d, i, stride_of(*ids, 0), p[0], matrix_stride(*table), table->size(0), (float)x.real, p[1], x.stream);
+  });
+}
+// (ids, dout, scale, dtable_acc, workspace)
+PyObject *embed_bwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  return call([&]() -> int {
+    RowArgs x;
+    s1f_rows d;
+    if (!x.read(args, n, 5, 2, 4)) return kPython;
+    auto &[ids, dout, acc, ws] = reinterpret_cast<const at::Tensor *(&)[4]>(x.t);
+    if (!rows_desc_of(nullptr, dout, &d) || !tokens_ok(*ids, *dout) || !matrix_ok(*acc, dout->size(2), at::kFloat) || !space_ok(ws)) return kPython;
+    const int64_t *i = tokens_of(ids);
+    void *const p[] = {ptr(dout), ptr(acc), ws ? ptr(ws) : nullptr};
+    Unlocked u;
+    return api.embed_bwd(&d, i, stride_of(*ids, 0), p[0], acc->size(0), (float)x.real, static_cast<float *>(p[1]), matrix_stride(*acc), p[2],
+                         bytes(ws), x.stream);
+  });
+}
+// (x, gamma, beta, eps, y, mean, rstd)
+PyObject *layer_norm_fwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  return call([&]() -> int {
+    RowArgs a;
+    s1f_rows d;
+    if (!a.read(args, n, 7, 3, -1)) return kPython;
+    auto &[x, gamma, beta, y, mean, rstd] = reinterpret_cast<const at::Tensor *(&)[6]>(a.t);
+    if (!rows_desc_of(x, y, &d) || !vector_ok(*gamma, x->size(2), x->scalar_type()) || !vector_ok(*beta, x->size(2), x->scalar_type()) ||
+        !row_values_ok(*mean, *x) || !row_values_ok(*rstd, *x))
+      return kPython;
+    void *const p[] = {ptr(x), ptr(gamma), ptr(beta), ptr(y), ptr(mean), ptr(rstd)};
+    Unlocked u;
+    return api.layer_norm_fwd(&d, p[0], p[1], p[2], (float)a.real, p[3], static_cast<float *>(p[4]), static_cast<float *>(p[5]), a.stream);
+  });
+}
+// (dy, x, gamma, mean, rstd, dx, dgamma_acc, dbeta_acc, workspace)
+PyObject *layer_norm_bwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  return call([&]() -> int {
+    RowArgs a;
+    s1f_rows d;
+    if (!a.read(args, n, 9, -1, 8)) return kPython;
+    auto &[dy, x, gamma, mean, rstd, dx, dg, db, ws] = reinterpret_cast<const at::Tensor *(&)[9]>(a.t);
+    if (!rows_desc_of(x, dy, &d) || !same_rows(*x, *dx) || !vector_ok(*gamma, x->size(2), x->scalar_type()) ||
+        !vector_ok(*dg, x->size(2), at::kFloat) || !vector_ok(*db, x->size(2), at::kFloat) || !row_values_ok(*mean, *x) ||
+        !row_values_ok(*rstd, *x) || !space_ok(ws))
+      return kPython;
+    void *const p[] = {ptr(dy), ptr(x), ptr(gamma), ptr(dx), ptr(dg), ptr(db), ws ? ptr(ws) : nullptr};
+    const float *m = values_of(mean), *r = values_of(rstd);
+    Unlocked u;
+    return api.layer_norm_bwd(&d, p[0], p[1], p[2], m, r, p[3], static_cast<float *>(p[4]), static_cast<float *>(p[5]), p[6], bytes(ws), a.stream);
+  });
+}
+// (x, weight, targets, loss, lse, workspace)
+PyObject *token_loss_fwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  return call([&]() -> int {
+    RowArgs a;
+    s1f_rows d;
+    if (!a.read(args, n, 6, -1, 5)) return kPython;
+    auto &[x, weight, targets, loss, lse, ws] = reinterpret_cast<const at::Tensor *(&)[6]>(a.t);
+    if (!rows_desc_of(x, nullptr, &d) || !matrix_ok(*weight, x->size(2), x->scalar_type()) || !tokens_ok(*targets, *x) ||
+        !row_values_ok(*loss, *x) || !row_values_ok(*lse, *x) || !space_ok(ws))
+      return kPython;
+    const int64_t *i = tokens_of(targets);
+    void *const p[] = {ptr(x), ptr(weight), ptr(loss), ptr(lse), ws ? ptr(ws) : nullptr};
+    Unlocked u;
+    return api.token_loss_fwd(&d, p[0], p[1], matrix_stride(*weight), weight->size(0), i, stride_of(*targets, 0), static_cast<float *>(p[2]),
+                              static_cast<float *>(p[3]), p[4], bytes(ws), a.stream);
+  });
+}
+// (dloss, x, weight, targets, lse, dx, dweight, workspace)
+PyObject *token_loss_bwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  return call([&]() -> int {
+    RowArgs a;
+    s1f_rows d;
+    int32_t code;
+    if (!a.read(args, n, 8, -1, 7)) return kPython;
+    auto &[dloss, x, weight, targets, lse, dx, dw, ws] = reinterpret_cast<const at::Tensor *(&)[8]>(a.t);
+    if (!rows_desc_of(x, nullptr, &d) || !same_rows(*x, *dx) || !matrix_ok(*weight, x->size(2), x->scalar_type()) || !dtype_of(*dw, &code) ||
+        !matrix_ok(*dw, x->size(2), dw->scalar_type()) || dw->sizes() != weight->sizes() || !tokens_ok(*targets, *x) ||
+        !row_values_ok(*dloss, *x) || !row_values_ok(*lse, *x) || !space_ok(ws))
+      return kPython;
+    const int64_t *i = tokens_of(targets);
+    const float *g = values_of(dloss), *l = values_of(lse);
+    void *const p[] = {ptr(x), ptr(weight), ptr(dx), ptr(dw), ws ? ptr(ws) : nullptr};
+    Unlocked u;
+    return api.token_loss_bwd(&d, g, p[0], p[1], matrix_stride(*weight), weight->size(0), i, stride_of(*targets, 0), l, p[2], p[3],
+                              matrix_stride(*dw), code, p[4], bytes(ws), a.stream);
+  });
+}
+
+// (addresses of the twelve entry points, torch's functions for the current device and for a device's stream)
 PyObject *bind(PyObject *, PyObject *args) {
-  unsigned long long a[6];
+  unsigned long long a[12];
   PyObject *dev, *st;
-  if (!PyArg_ParseTuple(args, "KKKKKKOO", &a[0], &a[1], &a[2], &a[3], &a[4], &a[5], &dev, &st)) return nullptr;
-  api = Api{reinterpret_cast<decltype(api.fwd)>(a[0]),         reinterpret_cast<decltype(api.fwd_ws)>(a[1]),
-            reinterpret_cast<decltype(api.bwd)>(a[2]),         reinterpret_cast<decltype(api.bwd_noalloc)>(a[3]),
-            reinterpret_cast<decltype(api.append)>(a[4]),      reinterpret_cast<decltype(api.emit)>(a[5])};
+  if (!PyArg_ParseTuple(args, "KKKKKKKKKKKKOO", &a[0], &a[1], &a[2], &a[3], &a[4], &a[5], &a[6], &a[7], &a[8], &a[9], &a[10], &a[11], &dev, &st))
+    return nullptr;
+  api = Api{reinterpret_cast<decltype(api.fwd)>(a[0]),
+            reinterpret_cast<decltype(api.fwd_ws)>(a[1]),
+            reinterpret_cast<decltype(api.bwd)>(a[2]),
+            reinterpret_cast<decltype(api.bwd_noalloc)>(a[3]),
+            reinterpret_cast<decltype(api.append)>(a[4]),
+            reinterpret_cast<decltype(api.emit)>(a[5]),
+            reinterpret_cast<decltype(api.embed_fwd)>(a[6]),
+            reinterpret_cast<decltype(api.embed_bwd)>(a[7]),
+            reinterpret_cast<decltype(api.layer_norm_fwd)>(a[8]),
+            reinterpret_cast<decltype(api.layer_norm_bwd)>(a[9]),
+            reinterpret_cast<decltype(api.token_loss_fwd)>(a[10]),
+            reinterpret_cast<decltype(api.token_loss_bwd)>(a[11])};
   Py_INCREF(dev);
   Py_INCREF(st);
   Py_XDECREF(get_device);
@@ -230,6 +417,12 @@ PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, nullptr},
                          {"bwd_noalloc", S1F_METHOD(bwd_noalloc), METH_FASTCALL, nullptr},
                          {"append", S1F_METHOD(append), METH_FASTCALL, nullptr},
                          {"emit", S1F_METHOD(emit), METH_FASTCALL, nullptr},
+                         {"embed_fwd", S1F_METHOD(embed_fwd), METH_FASTCALL, nullptr},
+                         {"embed_bwd", S1F_METHOD(embed_bwd), METH_FASTCALL, nullptr},
+                         {"layer_norm_fwd", S1F_METHOD(layer_norm_fwd), METH_FASTCALL, nullptr},
+                         {"layer_norm_bwd", S1F_METHOD(layer_norm_bwd), METH_FASTCALL, nullptr},
+                         {"token_loss_fwd", S1F_METHOD(token_loss_fwd), METH_FASTCALL, nullptr},
+                         {"token_loss_bwd", S1F_METHOD(token_loss_bwd), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_torch_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

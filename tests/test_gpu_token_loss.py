@@ -174,3 +174,35 @@ def test_gradient_is_the_same_every_time():
         dw = torch.zeros((3001, 264), device="cuda")
         runs.append((backward(dloss, x, w, targets, lse, dw), dw))
     assert all(torch.equal(a, b) for r in runs[1:] for a, b in zip(r, runs[0]))
+
+
+# Products of more tiles than a round of workgroups holds (tests/test_host_ends.py: these are cut as they are there for): rows, hidden, vocabulary
+CUTS = [(1040, 512, 16384), (2304, 8192, 2304), (700, 128, 130), (130, 2000, 9000)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,h,v", CUTS)
+def test_cut_products(n, h, v, dtype):
+    """Checked on the device in 64 bits, norm-wise: bf16 results and dz are off by at most 2^-8 of themselves each; fp32 ones by the roundings of sums of as many terms as
+    the longest one has, which in the worst case is k U of the terms' magnitudes, sqrt(k) or so times the norm of the result."""
+    rng = np.random.default_rng(n + v)
+    x, w, targets = make(rng, 1, n, h, v, 0.1, "dense", 0, dtype)
+    loss, lse = forward(x, w, targets)
+    known = (targets[0] >= 0) & (targets[0] < v)
+    x64, w64, t = x[0, known].double(), w.double(), targets[0, known]
+    z = x64 @ w64.T
+    want = torch.logsumexp(z, 1)
+    size = (x64.abs() @ w64.abs().T).max().item()
+    bound = (6 * h if dtype == "f32" else h) * U * size + 2.0 ** -20 + v * U
+    assert (lse[0, known].double() - want).abs().max() <= bound
+    assert (loss[0, known].double() - (want - z.gather(1, t[:, None])[:, 0])).abs().max() <= 2 * bound
+    dloss = torch.rand((1, n), device="cuda") / n
+    dw = torch.zeros((v, h), device="cuda")
+    dx = backward(dloss, x, w, targets, lse, dw)
+    z.sub_(lse[0, known].double()[:, None]).exp_()
+    z[torch.arange(len(t), device="cuda"), t] -= 1
+    z *= dloss[0, known].double()[:, None]
+    for got, w_ in ((dx[0, known], z @ w64), (dw, z.T @ x64)):
+        off = (got.double() - w_).norm() / w_.norm()
+        assert off <= (2.0 ** -7 if dtype == "bf16" else 4 * bound), off
+    assert not dx[0, ~known].any()

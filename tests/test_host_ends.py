@@ -1,6 +1,9 @@
 """What the calls of embedding, layer norm and token loss refuse: the C entry points before anything is launched, and their Python forms before the
 library is called.  No device."""
 import ctypes
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -119,6 +122,7 @@ def library(monkeypatch):
     monkeypatch.setattr(binding, "load_library", lambda: lib)
     monkeypatch.setattr(binding, "_stream_ptr", lambda: 0)
     monkeypatch.setattr(binding, "_check_device", lambda *t: None)
+    monkeypatch.setattr(binding, "_native", lambda: binding._PythonForms)
     return lib
 
 
@@ -181,7 +185,63 @@ def test_strides_of_single_rows_and_batches_do_not_matter(library):
     assert library.calls == ["s1f_layer_norm_fwd", "s1f_layer_norm_bwd"]
 
 
-def test_tensors_outside_device_memory_are_refused():
+def test_tensors_outside_device_memory_are_refused(monkeypatch):
+    monkeypatch.setattr(binding, "_native", lambda: binding._PythonForms)
     for name, args in good().items():
         with pytest.raises(ValueError):
             getattr(s1f, name)(*args)
+
+
+DRIVER = """
+import ctypes, sys
+ctypes.CDLL(sys.argv[1], mode=ctypes.RTLD_GLOBAL)
+import paper_2406_03488_amd as s1f
+from paper_2406_03488_amd.binding import Rows
+lib = s1f.load_library()
+p, big = 4096, 1 << 45   # (no address is looked at)
+for n, h, v, dtype in eval(sys.argv[2]):
+    d = ctypes.byref(Rows(1, h, dtype, 0, n, 0, h, 0, h))
+    assert lib.s1f_token_loss_fwd(d, p, p, h, v, p, 0, p, p, p, big, None) == 0
+    assert lib.s1f_token_loss_bwd(d, p, p, p, h, v, p, 0, p, p, p, h, 0, p, big, None) == 0
+    assert lib.s1f_embed_bwd(d, p, 0, p, v, 1.0, p, h, p, big, None) == 0
+"""
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+def launches(tmp_path, shapes):
+    so = str(tmp_path / "recording.so")
+    subprocess.run(["gcc", "-O1", "-shared", "-fPIC", "-Wall", "-Werror", "-o", so, os.path.join(ROOT, "tests", "recording_runtime.c")], check=True)
+    record = str(tmp_path / "record")
+    run = subprocess.run([sys.executable, "-c", DRIVER, so, repr(shapes)], env=dict(os.environ, RECORD=record, PYTHONPATH=ROOT), capture_output=True, text=True,
+                         cwd=ROOT)
+    assert run.returncode == 0, run.stderr
+    lines = [line.split() for line in open(record)]
+    told = {name: int(rest[1]) for what, name, *rest in lines if what == "attribute"}
+    done = [(name, int(rest[0]), int(rest[2])) for what, name, *rest in lines if what == "launch"]
+    assert all(lds <= 64 * 1024 or told.get(name, 0) >= lds for name, _, lds in done)
+    assert all(lds <= 160 * 1024 for _, _, lds in done)
+    return done
+
+
+def test_products_are_cut_as_the_gpu_tests_presume(tmp_path):
+    """tests/test_gpu_token_loss.py checks these shapes: big tiles with their rest in quarters, all sizes of tiles, dx in parts behind whole tiles."""
+    of = lambda shape, dtype=1: [(name.split("loss_")[1], grid) for name, grid, _ in launches(tmp_path, [(*shape, dtype)]) if "loss_" in name]
+    first = of((1040, 512, 16384))
+    scores = [(name, grid) for name, grid in first if name.startswith("scores")]
+    assert [grid for _, grid in scores] == [256, 256] * 2                     # 320 big tiles: a round of them, 64 in quarters, in both directions
+    assert "Li256ELi256" in scores[0][0] and "Li128ELi128" in scores[1][0]
+    second = of((2304, 8192, 2304))
+    dx = [grid for name, grid in second if name.startswith("dx_kernel")]
+    assert dx[0] > 256 and (dx[0] - 256) % 32 == 0 and dx[0] > 256 + 32       # 288 big tiles: 32 of them in parts
+    dw = [(name, grid) for name, grid in second if name.startswith("dw_kernel")]
+    assert [grid for _, grid in dw] == [256, 128] and "Li128ELi128" in dw[1][0]
+    assert any("scores" in name and "Li128ELi128" in name for name, _ in second)
+    assert any("scores" in name and "Li64ELi128" in name for name, _ in of((130, 2000, 9000)) + of((700, 128, 130)) + of((5, 64, 129)))
+
+
+def test_sorting_paths(tmp_path):
+    """Few rows are ranked, more take two or three passes over their tokens' digits."""
+    names = lambda n, v: [name for name, *_ in launches(tmp_path, [(n, 64, v, 0)]) if "embed_" in name]
+    assert sum("rank" in x for x in names(12288, 600)) == 1 and not any("place" in x for x in names(12288, 600))
+    assert sum("place" in x for x in names(12289, 600)) == 2 and sum("place" in x for x in names(12289, 300)) == 1
+    assert sum("place" in x for x in names(20000, 600000)) == 3
