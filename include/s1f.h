@@ -265,9 +265,9 @@ int s1f_kv_grad_emit(const s1f_desc *desc, const float *dk_prefix_acc, const flo
  *   - Per-row values (mean, rstd, loss, lse, dloss) are dense fp32 arrays [batch, rows].  Tokens and targets are int64 [batch, rows], rows
  *     contiguous, batch entries `*_stride_b` apart.
  *   - Pointers are aligned to their element; where rows also start on 16 bytes and hold a whole number of them, calls are faster.
- *   - The same arguments give the same bits: no atomics.
+ *   - The same arguments give the same bits: sums are taken in a fixed order, without atomics.
  * Errors as for the attention calls: S1F_EINVAL (null or misaligned pointer, bad size or stride, workspace too small), S1F_EUNSUPPORTED (dtype, or
- * sizes beyond a limit: hidden <= 16384, batch * rows <= 2^24), S1F_ERANGE (rows < 1), S1F_EDEVICE. */
+ * sizes beyond a limit: hidden <= 16384, batch * rows <= 2^21), S1F_ERANGE (rows < 1), S1F_EDEVICE. */
 typedef struct {
   int32_t batch;
   int32_t hidden;
@@ -308,8 +308,9 @@ size_t s1f_layer_norm_bwd_workspace_bytes(const s1f_rows *desc);
  *   dweight_dtype S1F_F32   added to fp32 accumulators
  *   dweight_dtype S1F_BF16  (bf16 rows only) overwritten, rounded once: the gradient of this call alone
  * bf16: dz is rounded to bf16 before its products, like the score gradients of the attention; sums are fp32.  fp32: products to fp32 precision (operands as
- * three exact bf16 parts each); a score that an infinity or NaN, or an operand from 2^127 on, takes part in is NaN.
- * y_stride_* are not used.  weight is 16-byte aligned; vocab <= 2^24, weight_stride < 2^22, batch * rows <= 2^20.  workspace: device
+ * three exact bf16 parts each); a score that an infinity or NaN, or an operand from 2^127 on, takes part in is NaN; gradients
+ * of single elements below 2^-110 keep 8 bits at least, not 24.
+ * y_stride_* are not used.  weight is 16-byte aligned; vocab <= 2^24, weight_stride < 2^22, batch * rows <= 2^20, batch * rows * hidden <= 2^33.  workspace: device
  * memory, 16-byte aligned, of at least s1f_token_loss_*_workspace_bytes(desc, vocab, weight_stride) bytes (0: invalid arguments); contents
  * undefined afterwards. */
 int s1f_token_loss_fwd(const s1f_rows *desc, const void *x, const void *weight, int64_t weight_stride, int64_t vocab, const int64_t *targets,

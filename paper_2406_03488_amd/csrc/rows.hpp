@@ -80,7 +80,7 @@ template <int N, bool WIDE> S1F_DEV void store_f32(float *p, int left, const flo
   for (int i = 0; i < N; i += 4) Piece<float, WIDE>::store(p + i, left - i, {v[i], v[i + 1], v[i + 2], v[i + 3]});
 }
 
-constexpr int64_t kMostRows = int64_t(1) << 24;   // batch * rows: numbers of rows are 32 bits, grids one launch
+constexpr int64_t kMostRows = int64_t(1) << 21;   // batch * rows: a launch of 1024 threads for each holds fewer than 2^32, more would not all run
 constexpr int32_t kMostHidden = 16384;
 
 inline bool on16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }

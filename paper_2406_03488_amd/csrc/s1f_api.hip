@@ -1212,7 +1212,7 @@ extern "C" const char *s1f_strerror(int status) {
   switch (status) {
     case S1F_OK: return "ok";
     case S1F_EINVAL: return "invalid argument (null or misaligned pointer, bad size or stride, workspace too small)";
-    case S1F_EUNSUPPORTED: return "unsupported dtype or head_dim (supported: f32/bf16 with head_dim 64, 80, 128)";
+    case S1F_EUNSUPPORTED: return "unsupported dtype, head_dim (attention: f32/bf16 with head_dim 64, 80, 128) or size";
     case S1F_ERANGE: return "segment out of range (seg_off < 0, seg_len < 1 or seg_off + seg_len > kv_capacity)";
     case S1F_EDEVICE: return "HIP runtime error at kernel launch";
     case S1F_ESCRATCH:
@@ -1222,4 +1222,4 @@ extern "C" const char *s1f_strerror(int status) {
   }
 }
 
-extern "C" int s1f_version(void) { return 200; }
+extern "C" int s1f_version(void) { return 300; }

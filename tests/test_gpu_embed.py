@@ -48,7 +48,7 @@ def test_forward_bit_for_bit(case, dtype):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("case", CASES + [(1, 12288, 24, 300, 0.1, "dense"), (1, 12289, 24, 300, 0.1, "dense"), (1, 16384, 24, 300, 0.1, "dense"), (1, 16385, 24, 300, 0.1, "dense"),
-                                          (1, 8191, 40, 30, 0.0, "dense"), (1, 8193, 40, 30, 0.0, "odd"), (1, 33000, 2056, 7, 0.1, "dense"), (2, 9999, 17, 70000, 0.3, "view"),
+                                          (1, 8191, 40, 30, 0.0, "dense"), (1, 8193, 40, 30, 0.0, "odd"), (1, 33000, 2056, 7, 0.1, "dense"), (1, 65536, 8, 900, 0.1, "dense"), (1, 65537, 8, 900, 0.1, "dense"), (3, 40000, 8, 100003, 0.0, "seq"), (2, 9999, 17, 70000, 0.3, "view"),
                                           (1, 40000, 8, 1, 0.0, "dense"), (1, 17000, 8, 600000, 0.9, "dense"), (1, 20480, 8, 511, 1.0, "dense")])
 def test_gradient(case, dtype):
     b, n, h, v, blank, layout = case

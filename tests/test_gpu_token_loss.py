@@ -177,7 +177,7 @@ def test_gradient_is_the_same_every_time():
 
 
 # Products of more tiles than a round of workgroups holds (tests/test_host_ends.py: these are cut as they are there for): rows, hidden, vocabulary
-CUTS = [(1040, 512, 16384), (2304, 8192, 2304), (700, 128, 130), (130, 2000, 9000)]
+CUTS = [(1040, 512, 16384), (2304, 8192, 2304), (700, 128, 130), (130, 2000, 9000), (2048, 72, 300), (2049, 72, 300), (9000, 64, 257)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])

@@ -55,7 +55,7 @@ def test_descriptors_refused(call):
     assert call(None) == 1
     for bad in (dict(batch=0), dict(batch=-1), dict(hidden=0), dict(reserved=1)):
         assert call(rows(**bad)) == 1, bad
-    for bad in (dict(dtype=2), dict(dtype=-1), dict(hidden=16385), dict(rows=(1 << 24) + 1), dict(batch=1 << 20, rows=1 << 20),
+    for bad in (dict(dtype=2), dict(dtype=-1), dict(hidden=16385), dict(rows=(1 << 21) + 1), dict(batch=1 << 20, rows=1 << 20),
                 dict(batch=1 << 30, rows=1 << 34)):
         h = bad.get("hidden", 64)
         d = rows(**{"x_stride_s": h, "y_stride_s": h, "x_stride_b": 1 << 40, "y_stride_b": 1 << 40, **bad})
@@ -90,6 +90,7 @@ def test_pointers_and_sizes_refused(call):
         assert call(rows(), weight=OFF) == 1
         assert call(rows(), vocab=(1 << 24) + 1) == 2 and call(rows(), stride=1 << 22) == 2
         assert call(rows(batch=1, rows=(1 << 20) + 1)) == 2
+        assert call(rows(batch=1, rows=1 << 20, hidden=8200, x_stride_s=8200), stride=8200) == 2
     if call is loss_bwd:
         assert call(rows(), into=63) == 1 and call(rows(), code=2) == 2 and call(rows(dtype=0), code=1) == 2
 
@@ -245,3 +246,33 @@ def test_sorting_paths(tmp_path):
     assert sum("rank" in x for x in names(12288, 600)) == 1 and not any("place" in x for x in names(12288, 600))
     assert sum("place" in x for x in names(12289, 600)) == 2 and sum("place" in x for x in names(12289, 300)) == 1
     assert sum("place" in x for x in names(20000, 600000)) == 3
+
+
+LARGEST = """
+import ctypes, sys
+ctypes.CDLL(sys.argv[1], mode=ctypes.RTLD_GLOBAL)
+import paper_2406_03488_amd as s1f
+from paper_2406_03488_amd.binding import Rows
+lib = s1f.load_library()
+p, big = 4096, 1 << 60   # (no address is looked at)
+for n, h, v, dtype in eval(sys.argv[2]):
+    d = ctypes.byref(Rows(1, h, dtype, 0, n, 0, h, 0, h))
+    if v <= 1 << 24 and n <= 1 << 20:
+        assert lib.s1f_token_loss_fwd(d, p, p, h, v, p, 0, p, p, p, big, None) == 0
+        assert lib.s1f_token_loss_bwd(d, p, p, p, h, v, p, 0, p, p, p, h, 0, p, big, None) == 0
+    assert lib.s1f_embed_fwd(d, p, 0, p, h, v, 1.0, p, None) == 0 and lib.s1f_embed_bwd(d, p, 0, p, v, 1.0, p, h, p, big, None) == 0
+    assert lib.s1f_layer_norm_fwd(d, p, p, p, 1e-5, p, p, p, None) == 0 and lib.s1f_layer_norm_bwd(d, p, p, p, p, p, p, p, p, p, big, None) == 0
+"""
+
+
+def test_the_largest_calls_fit_a_launch(tmp_path, monkeypatch):
+    """The runtime takes launches of 2^32 threads and more, and runs fewer workgroups."""
+    monkeypatch.setattr(sys.modules[__name__], "DRIVER", LARGEST)
+    shapes = [(1 << 21, 16384, 1 << 26), (1 << 20, 8192, 300), (1 << 19, 16384, 1 << 17), (1, 16384, 1 << 24), (64, 1, 1 << 24), (1 << 20, 64, 1 << 16), (1 << 20, 1, 1)]
+    done = launches(tmp_path, [(*s, dtype) for s in shapes for dtype in (0, 1)])
+    assert len(done) > 100 and all(0 < grid <= (1 << 31) - 1 for _, grid, _ in done)
+    assert all(grid * threads < 1 << 32 for _, grid, threads in threads_of(tmp_path))
+
+
+def threads_of(tmp_path):
+    return [(line.split()[1], int(line.split()[2]), int(line.split()[3])) for line in open(tmp_path / "record") if line.startswith("launch")]
