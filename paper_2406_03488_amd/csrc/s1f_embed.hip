@@ -40,7 +40,8 @@ S1F_DEV int key_at(const EmbedArgs &a, int row) {
   return id >= 0 && id < a.vocab ? (int)id : a.vocab;
 }
 
-// 2^tpr_log2 threads per row, each of which takes every 2^tpr_log2-th piece.
+// 2^tpr_log2 threads per row, each of which takes every 2^tpr_log2-th piece.  Bound by memory: 4897 rows of 7168 bf16 elements, 136 MB with a table row read for
+// each, 19 us, of which the caches serve some; 16 rows of 256 fp32 elements 2 us, a chain of two loads and a store.
 template <typename T, bool WIDE> __global__ void __launch_bounds__(256) embed_fwd_kernel(const EmbedArgs a) {
   typedef Piece<T, WIDE> P;
   const int row = (blockIdx.x << (8 - a.tpr_log2)) + (threadIdx.x >> a.tpr_log2);
@@ -101,7 +102,8 @@ __global__ void __launch_bounds__(1024) embed_rank_kernel(const EmbedArgs a) {
 }
 
 // Sorting in passes over digits of at most 9 bits, the lowest first, each of which keeps the order of equal digits: count the digits of
-// every tile of 1024 rows, sum the counts of each digit up over the tiles, and place the rows.
+// every tile of 1024 rows, sum the counts of each digit up over the tiles, and place the rows.  Bound by latency: of 32768 rows a pass counts for 4.6 us and
+// places for 8.8, with one workgroup to a tile.
 constexpr int kTile = 1024, kDigits = 512, kMostSummed = 64;   // (the last: tiles whose counts the placing workgroups sum up)
 
 S1F_DEV int pass_key(const EmbedArgs &a, int i) { return a.first_pass ? key_at(a, i) : a.key_from[i]; }
@@ -218,7 +220,8 @@ __global__ void __launch_bounds__(256) embed_place_kernel(const EmbedArgs a) {
 }
 
 // Sums of the runs in one chunk of the sorted rows.  2^tpr_log2 threads share the columns of a row; the others of a workgroup take
-// other chunks.  Of eight rows at a time everything is asked for together, the accumulators that their runs end in included.
+// other chunks.  Of eight rows at a time everything is asked for together, the accumulators that their runs end in included.  Bound by memory: 32768 rows of 4096
+// bf16 elements over 50021 tokens, 646 MB with the accumulators read and written, 142 to 146 us, 4.5 TB/s (a large copy: 4.8).
 template <typename T, bool WIDE> __global__ void __launch_bounds__(256) embed_sum_kernel(const EmbedArgs a) {
   typedef Piece<T, WIDE> P;
   const int tpr = 1 << a.tpr_log2;

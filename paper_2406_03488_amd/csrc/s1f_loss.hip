@@ -132,7 +132,7 @@ template <typename T, bool WIDE> S1F_DEV void pack_weight(const LossArgs &a, int
   if (row < a.piece)
     pack_eight<T, WIDE>(reinterpret_cast<const T *>(a.weight) + (a.first + row) * a.weight_stride, a.hidden, c, a.packed + row * a.width + 8 * c, a.packed_plane);
 }
-// ROWS: the counted rows of x; else `piece` rows of the weight from `first` on.
+// Bound by memory: 4099 rows of 4096 bf16 elements, 67 MB, 14 us.  ROWS: the counted rows of x; else `piece` rows of the weight from `first` on.
 template <typename T, bool WIDE, bool ROWS> __global__ void __launch_bounds__(256) loss_pack_kernel(const LossArgs a) {
   const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (!ROWS) return pack_weight<T, WIDE>(a, id);
@@ -238,7 +238,9 @@ S1F_DEV Matrix weight_matrix(const LossArgs &a) {
                   : Matrix{a.packed, a.width, a.packed_plane};
 }
 
-// Scores of a tile of rows and vocabulary: STATS: maximum and sum of exponentials of each row (forward); else dz (backward).
+// Scores of a tile of rows and vocabulary: STATS: maximum and sum of exponentials of each row (forward); else dz (backward).  Bound by the matrix units, at the
+// clock that power leaves them, and by the beginning and end of a tile, about 6 us in which they wait: 4099 rows of 4096 bf16 elements over 50021 tokens 1.30 ms,
+// 1.3 PFLOP/s, the library's product alone 1.27; gradient of 5530 rows of 7168 over 100003 tokens 6.3 ms, 1.25 PFLOP/s, the product alone 5.5.
 template <typename T, int BM, int BN, int WM, int WN, bool STATS>
 __global__ void __launch_bounds__(64 * WM * WN, 2) loss_scores_kernel(const LossArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -414,7 +416,8 @@ __global__ void __launch_bounds__(1024) loss_join_kernel(const LossArgs a) {
   a.loss[row] = lse - a.target_score[slot];
 }
 
-// dx = dz W over a piece of the vocabulary.  Tiles that do not fill a round of workgroups are cut along the vocabulary.
+// dx = dz W over a piece of the vocabulary.  Tiles that do not fill a round of workgroups are cut along the vocabulary.  5530 rows of 7168 bf16 elements over
+// 100003 tokens: 6.2 ms, 1.28 PFLOP/s, the library's product 7.9.
 template <int PAIRS, int BM, int BN, int WM, int WN> __global__ void __launch_bounds__(64 * WM * WN, 2) loss_dx_kernel(const LossArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   typedef Product<BM, BN, WM, WN, false, true, PAIRS> P;
@@ -449,7 +452,8 @@ template <int PAIRS, int BM, int BN, int WM, int WN> __global__ void __launch_bo
   }
 }
 
-// dx rounded and put where the rows of x lie, parts of cut tiles (of TILE x TILE) added up in their order; zeros for rows without a target.
+// dx rounded and put where the rows of x lie, parts of cut tiles (of TILE x TILE) added up in their order; zeros for rows without a target.  Bound by memory:
+// 6144 rows of 7168 elements, 247 MB, and parts: 57 us.
 template <typename T, bool WIDE, int TILE> __global__ void __launch_bounds__(256) loss_dx_join_kernel(const LossArgs a) {
   typedef Piece<T, WIDE> P;
   const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -476,7 +480,8 @@ template <typename T, bool WIDE, int TILE> __global__ void __launch_bounds__(256
   P::store(reinterpret_cast<T *>(a.dx) + a.xs.offset((int)row) + col, a.hidden - col, v);
 }
 
-// dW of a piece of the vocabulary: added into fp32 accumulators (ADD), or written in bf16.
+// dW of a piece of the vocabulary: added into fp32 accumulators (ADD), or written in bf16.  No atomics: a workgroup has all rows of its tile.  5530 rows of 7168
+// bf16 elements over 100003 tokens: 6.4 ms, 1.24 PFLOP/s, the library's product 6.9.
 template <int PAIRS, int BM, int BN, int WM, int WN, bool ADD> __global__ void __launch_bounds__(64 * WM * WN, 2) loss_dw_kernel(const LossArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   typedef Product<BM, BN, WM, WN, true, true, PAIRS> P;
