@@ -42,9 +42,8 @@ struct LossArgs {
   int32_t first, piece, direct, add, parts, wide, row_groups;
   // tiles of the launch: their grid; the first one; whether a workgroup takes a quarter of one
   int32_t tiles_m, tiles_n, tile0, quarters;
-  Divisor by_group;                                // 4 * tiles_m
-  // dx: the tiles from `whole` on, `rest` of them, are cut into `splits` parts along the vocabulary
-  int32_t whole, rest, splits;
+  // dx: the tiles from `whole` on, `rest` of them, are cut into `splits` parts along the vocabulary (see DxParts)
+  int32_t whole, rest, splits, most_splits;
 };
 
 // ---- rows that count -------------------------------------------------------------------------------------------------------------------
@@ -205,12 +204,10 @@ template <typename T, bool WIDE_X, bool WIDE_W, bool FWD> __global__ void __laun
 
 // Number of a tile -> its place.  The hardware hands workgroups to the 8 XCDs in turn; each takes consecutive tiles, in blocks of four columns of tiles
 // walked down the rows, so that the 32 workgroups that an XCD runs side by side share eight row and four column panels in its L2.
-S1F_DEV void decode_tile(const LossArgs &a, int tile, int &tm, int &tn) {
-  const int tiles = a.tiles_m * a.tiles_n, per = tiles >> 3;
+S1F_DEV void decode_tile(int tiles_m, int tiles_n, int tile, int &tm, int &tn) {
+  const int per = tiles_m * tiles_n >> 3;
   if (tile < per * 8) tile = (tile & 7) * per + (tile >> 3);
-  int group, in;
-  div_mod(tile, a.by_group, group, in);               // 4 * tiles_m to a group
-  const int left = a.tiles_n - 4 * group;
+  const int group = tile / (4 * tiles_m), in = tile - group * 4 * tiles_m, left = tiles_n - 4 * group;
   if (left >= 4) {
     tm = in >> 2;
     tn = 4 * group + (in & 3);
@@ -220,15 +217,15 @@ S1F_DEV void decode_tile(const LossArgs &a, int tile, int &tm, int &tn) {
   }
 }
 // The number of the tile at a place.
-S1F_DEV int encode_tile(const LossArgs &a, int tm, int tn) {
-  const int tiles = a.tiles_m * a.tiles_n, per = tiles >> 3, group = tn >> 2, left = a.tiles_n - 4 * group;
-  const int tile = 4 * group * a.tiles_m + tm * (left < 4 ? left : 4) + (tn & 3);
+S1F_DEV int encode_tile(int tiles_m, int tiles_n, int tm, int tn) {
+  const int per = tiles_m * tiles_n >> 3, group = tn >> 2, left = tiles_n - 4 * group;
+  const int tile = 4 * group * tiles_m + tm * (left < 4 ? left : 4) + (tn & 3);
   return tile < per * 8 ? (tile % per) * 8 + tile / per : tile;
 }
 // Workgroup -> tile, or quarter of a tile.
 S1F_DEV void own_tile(const LossArgs &a, int &tm, int &tn) {
-  if (!a.quarters) return decode_tile(a, a.tile0 + blockIdx.x, tm, tn);
-  decode_tile(a, a.tile0 + (blockIdx.x >> 2), tm, tn);
+  if (!a.quarters) return decode_tile(a.tiles_m, a.tiles_n, a.tile0 + blockIdx.x, tm, tn);
+  decode_tile(a.tiles_m, a.tiles_n, a.tile0 + (blockIdx.x >> 2), tm, tn);
   tm = 2 * tm + ((blockIdx.x >> 1) & 1);
   tn = 2 * tn + (blockIdx.x & 1);
 }
@@ -416,19 +413,41 @@ __global__ void __launch_bounds__(1024) loss_join_kernel(const LossArgs a) {
   a.loss[row] = lse - a.target_score[slot];
 }
 
+// How dx's tiles are cut.  The host plans for all rows; where it cuts every tile and fewer count, the workgroups and the room for parts that the plan has are shared
+// out among the tiles that there are (the same in every launch of a call): gradient of half of 1024 rows of 2048 bf16 elements over 32000 tokens 397 -> 366 us, of
+// 0.6 * 2048 rows of 2560 over 50021 1176 -> 1096, of 0.7 * 682 rows of 1280 fp32 elements over 20011 587 -> 575.
+struct DxParts {
+  int tiles_m, whole, rest, splits;
+  S1F_DEV DxParts(const LossArgs &a, int count, int tile) {
+    tiles_m = a.tiles_m;
+    whole = a.whole;
+    rest = a.rest;
+    splits = a.splits;
+    const int there = (count + tile - 1) / tile;
+    if (whole == 0 && splits > 1 && there < tiles_m && there > 0) {
+      const int planned = rest * (splits - 1);   // parts that there is room for behind every tile's first
+      tiles_m = there;
+      rest = there * a.tiles_n;
+      splits = planned / rest + 1 < a.most_splits ? planned / rest + 1 : a.most_splits;
+    }
+  }
+};
+
 // dx = dz W over a piece of the vocabulary.  Tiles that do not fill a round of workgroups are cut along the vocabulary.  5530 rows of 7168 bf16 elements over
 // 100003 tokens: 6.2 ms, 1.28 PFLOP/s, the library's product 7.9.
 template <int PAIRS, int BM, int BN, int WM, int WN> __global__ void __launch_bounds__(64 * WM * WN, 2) loss_dx_kernel(const LossArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   typedef Product<BM, BN, WM, WN, false, true, PAIRS> P;
   const int count = *a.count;
+  const DxParts cut(a, count, BM);
   int tile = blockIdx.x, part = 0, parts = 1, tm, tn;
-  if (tile >= a.whole) {
-    part = (tile - a.whole) / a.rest;
-    tile -= part * a.rest;
-    parts = a.splits;
+  if (tile >= cut.whole) {
+    part = (tile - cut.whole) / cut.rest;
+    tile -= part * cut.rest;
+    parts = cut.splits;
   }
-  decode_tile(a, tile, tm, tn);
+  if (part >= parts) return;
+  decode_tile(cut.tiles_m, a.tiles_n, tile, tm, tn);
   const int m0 = tm * BM, n0 = tn * BN;
   if (m0 >= count) return;
   const int64_t stages = (int64_t)((a.piece + kDepth - 1) / kDepth) * PAIRS;
@@ -436,7 +455,7 @@ template <int PAIRS, int BM, int BN, int WM, int WN> __global__ void __launch_bo
   P::run(acc, Matrix{a.dz, a.dz_ld, a.dz_plane}, weight_matrix(a), m0, count, n0, a.width, a.piece, (int)(stages * part / parts),
          (int)(stages * (part + 1) / parts), to_lds_addr(smem));
   const int lane = lane_id(), n = lane & 15, j = lane >> 4, wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
-  float *to = part == 0 ? a.sum + (int64_t)m0 * a.width + n0 : a.part + ((int64_t)(part - 1) * a.rest + tile - a.whole) * (BM * BN);
+  float *to = part == 0 ? a.sum + (int64_t)m0 * a.width + n0 : a.part + ((int64_t)(part - 1) * cut.rest + tile - cut.whole) * (BM * BN);
   const int stride = part == 0 ? a.width : BN;
 #pragma unroll
   for (int mb = 0; mb < P::MB; ++mb) {
@@ -468,10 +487,11 @@ template <typename T, bool WIDE, int TILE> __global__ void __launch_bounds__(256
   if (slot >= 0) {
     load_f32<P::N, true>(a.sum + (int64_t)slot * a.width + col, P::N, v);
     if (a.splits > 1) {
-      const int tile = encode_tile(a, slot / TILE, col / TILE);
-      if (tile >= a.whole)
-        for (int p = 0; p + 1 < a.splits; ++p) {
-          load_f32<P::N, true>(a.part + (((int64_t)p * a.rest + tile - a.whole) * TILE + slot % TILE) * TILE + col % TILE, P::N, more);
+      const DxParts cut(a, *a.count, TILE);
+      const int tile = encode_tile(cut.tiles_m, a.tiles_n, slot / TILE, col / TILE);
+      if (tile >= cut.whole)
+        for (int p = 0; p + 1 < cut.splits; ++p) {
+          load_f32<P::N, true>(a.part + (((int64_t)p * cut.rest + tile - cut.whole) * TILE + slot % TILE) * TILE + col % TILE, P::N, more);
 #pragma unroll
           for (int e = 0; e < P::N; ++e) v[e] += more[e];
         }
@@ -573,7 +593,7 @@ Cut cut_for(int64_t m, int64_t n, int64_t stages, bool low) {
 struct DxCut {
   Tile tile;
   int64_t whole, rest;
-  int splits;
+  int splits, most_splits;   // (the most if fewer rows count)
 };
 DxCut dx_cut_for(int64_t m, int64_t n, int64_t stages) {
   DxCut best = {};
@@ -586,7 +606,7 @@ DxCut dx_cut_for(int64_t m, int64_t n, int64_t stages) {
                         (double)(splits - 1) * rest * side * side * 8 / 4e6;
       if (us < 0.98 * least) {
         least = us;
-        best = {tile, whole, rest, splits};
+        best = {tile, whole, rest, splits, (int)std::max<int64_t>(splits, std::min<int64_t>(64, stages / 4))};
       }
     }
   }
@@ -662,7 +682,6 @@ template <auto KERNEL> int launch_tiles(int lds, int threads, int64_t grid, Loss
 void tiles_of(LossArgs &a, int64_t m, int64_t n, int bm, int bn) {
   a.tiles_m = (int32_t)((m + bm - 1) / bm);
   a.tiles_n = (int32_t)((n + bn - 1) / bn);
-  a.by_group = Divisor::of(4 * a.tiles_m);
 }
 
 template <typename T> int pack_weight_piece(const LossArgs &a, bool wide, hipStream_t st) {
@@ -716,6 +735,7 @@ LossArgs args_of(const s1f_rows *d, const LossPlan &p, const int64_t *targets, i
   a.whole = (int32_t)p.dx.whole;
   a.rest = (int32_t)p.dx.rest;
   a.splits = p.dx.splits;
+  a.most_splits = p.dx.most_splits;
   return a;
 }
 bool wide_weight(const s1f_rows *d, int64_t stride) { return d->hidden % 8 == 0 && stride % elements_of_16_bytes(d->dtype) == 0; }

@@ -180,13 +180,11 @@ def test_gradient_is_the_same_every_time():
 CUTS = [(1040, 512, 16384), (2304, 8192, 2304), (700, 128, 130), (130, 2000, 9000), (2048, 72, 300), (2049, 72, 300), (9000, 64, 257)]
 
 
-@pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("n,h,v", CUTS)
-def test_cut_products(n, h, v, dtype):
+def check_in_norm(n, h, v, blank, dtype):
     """Checked on the device in 64 bits, norm-wise: bf16 results and dz are off by at most 2^-8 of themselves each; fp32 ones by the roundings of sums of as many terms as
     the longest one has, which in the worst case is k U of the terms' magnitudes, sqrt(k) or so times the norm of the result."""
     rng = np.random.default_rng(n + v)
-    x, w, targets = make(rng, 1, n, h, v, 0.1, "dense", 0, dtype)
+    x, w, targets = make(rng, 1, n, h, v, blank, "dense", 0, dtype)
     loss, lse = forward(x, w, targets)
     known = (targets[0] >= 0) & (targets[0] < v)
     x64, w64, t = x[0, known].double(), w.double(), targets[0, known]
@@ -206,3 +204,20 @@ def test_cut_products(n, h, v, dtype):
         off = (got.double() - w_).norm() / w_.norm()
         assert off <= (2.0 ** -7 if dtype == "bf16" else 4 * bound), off
     assert not dx[0, ~known].any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,h,v", CUTS)
+def test_cut_products(n, h, v, dtype):
+    check_in_norm(n, h, v, 0.1, dtype)
+
+
+# dx in parts whose number follows the rows that count, the last one over two pieces of the vocabulary (tests/test_host_ends.py): rows, hidden, vocabulary
+PARTS = [(700, 264, 9001), (1500, 72, 2000), (700, 264, 180000)]
+
+
+@pytest.mark.parametrize("blank", [0.5, 0.8, 0.99])
+@pytest.mark.parametrize("n,h,v", PARTS)
+def test_parts_of_fewer_rows(n, h, v, blank):
+    for dtype in ("f32",) if v > 9001 else ("f32", "bf16"):
+        check_in_norm(n, h, v, blank, dtype)

@@ -237,6 +237,12 @@ def test_products_are_cut_as_the_gpu_tests_presume(tmp_path):
     dw = [(name, grid) for name, grid in second if name.startswith("dw_kernel")]
     assert [grid for _, grid in dw] == [256, 128] and "Li128ELi128" in dw[1][0]
     assert any("scores" in name and "Li128ELi128" in name for name, _ in second)
+    for shape, dtypes in (((700, 264, 9001), (0, 1)), ((1500, 72, 2000), (0, 1)), ((700, 264, 180000), (0,))):
+        for dtype in dtypes:                                                  # no whole tiles, more workgroups than tiles: each in parts
+            parts = [(grid, 128 if "Li128ELi128" in name else 256) for name, grid in of(shape, dtype) if name.startswith("dx_kernel")]
+            assert len(parts) == (2 if shape[2] > 9001 else 1)
+            tiles = -(-shape[0] // parts[0][1]) * -(-shape[1] // parts[0][1])
+            assert all(grid % tiles == 0 and 2 * tiles <= grid <= 1024 for grid, _ in parts), (shape, dtype, parts)
     assert any("scores" in name and "Li64ELi128" in name for name, _ in of((130, 2000, 9000)) + of((700, 128, 130)) + of((5, 64, 129)))
 
 
