@@ -221,3 +221,18 @@ PARTS = [(700, 264, 9001), (1500, 72, 2000), (700, 264, 180000)]
 def test_parts_of_fewer_rows(n, h, v, blank):
     for dtype in ("f32",) if v > 9001 else ("f32", "bf16"):
         check_in_norm(n, h, v, blank, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("h,more", [(72, 8), (200, 56), (8, 8), (100, 5)])
+def test_what_lies_between_rows_is_not_read(h, more, dtype):
+    """NaN between the rows of x and of the weight: whole stages of a product would read them."""
+    rng = np.random.default_rng(h)
+    b, n, v = 2, 70, 300
+    x = torch.full((b, n + 1, h + more), float("nan"), dtype=TYPES[dtype], device="cuda")[:, :n, :h]
+    w = torch.full((v, h + more), float("nan"), dtype=TYPES[dtype], device="cuda")[:, :h]
+    x.copy_(normal(rng, (b, n, h), dtype))
+    w.copy_(normal(rng, (v, h), dtype, 2 / np.sqrt(h)))
+    dw = torch.full((v, h + more), float("nan"), device="cuda")[:, :h]
+    dw.zero_()
+    check(x, w, tokens_of(rng, b, n, v, 0.1), dtype, dw, rng)
