@@ -17,6 +17,8 @@
 // power leaves them; operands that are constant take 15 % less.  Eight waves of 128 x 64 read 192 KiB of operands per stage out of LDS, which takes about as long
 // as their products; four waves of 128 x 128 read 128 KiB but have nobody to take turns with on their unit's four matrix pipes: no faster.
 #pragma once
+#include <type_traits>
+
 #include "attn_tile.hpp"
 
 namespace s1f {
@@ -268,6 +270,81 @@ template <int BM, int BN, int WM, int WN, bool TRA, bool TRB, int PAIRS> struct 
     while (t + 2 < end) step(Int<1>{});
     while (t < end) step(Int<0>{});
     __syncthreads();
+  }
+
+  // The same for operands of three planes and tiles small enough that LDS holds all planes of two stages: each is copied once for the six products, and read
+  // once into registers.  A call of few tiles is a chain of stages, of which there are then a sixth: scores of 256 rows of 256 elements over 5003 tokens 15.1 -> 11.2 us,
+  // loss of 64 rows of 4096 over 30000, which reads 740 MB of planes, 865 -> 570.  Eight waves of 32 x 32, two to a SIMD, so that one's reads pass under the other's
+  // products: 1.35 us per stage, four of 64 x 32 1.5.
+  static constexpr int PLANES_LDS_BYTES = 2 * 3 * (SA::BYTES + SB::BYTES);
+  S1F_DEV static void run_planes(f32x4 (&acc)[MB][NB], const Matrix &a, const Matrix &b, int64_t m0, int64_t m_limit, int64_t n0, int64_t n_limit,
+                                 int64_t k, lds_addr lds) {
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    SA sa;
+    SB sb;
+    sa.init(a.data, a.ld, m0, m_limit, 0, wave, lane);
+    sb.init(b.data, b.ld, n0, n_limit, 0, wave, lane);
+    const int stages = (int)((k + kDepth - 1) / kDepth), left = (int)((k - 1) % kDepth) + 1;
+    constexpr int COPIES = 3 * (SA::PER_WAVE + SB::PER_WAVE);
+    auto copy_side = [&](auto &side, const Matrix &m, lds_addr at, int bytes) {
+      for_each<3>([&](auto plane) {
+        constexpr int p = decltype(plane)::value;
+        const char *from = uniform_pointer(side.next + p * m.plane * 2);
+        const unsigned to = __builtin_amdgcn_readfirstlane(at + (unsigned)(p * bytes + wave * side.PER_WAVE * 1024));
+        for_each<std::remove_reference_t<decltype(side)>::PER_WAVE>([&](auto i) { side.template copy<decltype(i)::value>(from, to); });
+      });
+      side.next += side.step;
+    };
+    auto copy_stage = [&](int t, lds_addr place) {
+      if (t + 1 == stages && left < kDepth) {
+        sa.shorten(left, wave, lane);
+        sb.shorten(left, wave, lane);
+      }
+      copy_side(sa, a, place, SA::BYTES);
+      copy_side(sb, b, place + 3 * SA::BYTES, SB::BYTES);
+    };
+    const lds_addr places[2] = {lds, lds + 3 * (SA::BYTES + SB::BYTES)};
+    copy_stage(0, places[0]);
+    if (stages > 1) copy_stage(1, places[1]);
+    const lds_addr lane_a = SA::at(wm * MB, lane), lane_b = SB::at(wn * NB, lane);
+    for (int t = 0; t < stages; ++t) {
+      const lds_addr at_a = places[t & 1], at_b = at_a + 3 * SA::BYTES;
+      if (t + 1 < stages) wait_async_tiles_but_last<COPIES>();
+      else wait_async_tiles();
+      if (t + 1 == stages && left < kDepth) {
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+          sa.clear_tail(at_a + p * SA::BYTES, left, wave, lane);
+          sb.clear_tail(at_b + p * SB::BYTES, left, wave, lane);
+        }
+      }
+      __syncthreads();
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        bf16x8 fa[3][MB], fb[3][NB];
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+          const lds_addr pa = SA::half_of(at_a + p * SA::BYTES + lane_a, half), pb = SB::half_of(at_b + p * SB::BYTES + lane_b, half);
+#pragma unroll
+          for (int j = 0; j < NB; ++j) fb[p][j] = SB::operand(pb, j, half);
+#pragma unroll
+          for (int i = 0; i < MB; ++i) fa[p][i] = SA::operand(pa, i, half);
+        }
+        for_each<6>([&](auto pair) {   // (as above, smallest products first)
+          constexpr int P = decltype(pair)::value, PA = (0x001102 >> (4 * P)) & 3, PB = (0x010120 >> (4 * P)) & 3;
+#pragma unroll
+          for (int i = 0; i < MB; ++i)
+#pragma unroll
+            for (int j = 0; j < NB; ++j) acc[i][j] = mma16(fb[PB][j], fa[PA][i], acc[i][j]);
+        });
+      }
+      __syncthreads();
+      if (t + 2 < stages) copy_stage(t + 2, at_a);
+    }
   }
 };
 

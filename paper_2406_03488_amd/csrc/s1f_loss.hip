@@ -249,8 +249,9 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) loss_scores_kernel(const Loss
   const int m0 = tm * BM, n0 = tn * BN;
   if (m0 >= count || n0 >= a.piece) return;
   f32x4 acc[P::MB][P::NB];
-  P::run(acc, Matrix{a.rows, a.width, a.rows_plane}, weight_matrix(a), m0, count, n0, a.piece, a.width, 0,
-         (a.width + kDepth - 1) / kDepth * PAIRS, to_lds_addr(smem));
+  const Matrix rows = {a.rows, a.width, a.rows_plane};
+  if constexpr (PAIRS == 6 && BM == 64) P::run_planes(acc, rows, weight_matrix(a), m0, count, n0, a.piece, a.width, to_lds_addr(smem));
+  else P::run(acc, rows, weight_matrix(a), m0, count, n0, a.piece, a.width, 0, (a.width + kDepth - 1) / kDepth * PAIRS, to_lds_addr(smem));
   const int lane = lane_id(), n = lane & 15, j = lane >> 4, wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
   // A tile's results cost the vector unit about as long as four stages of products the matrix unit, so nothing is asked per element that can be
   // asked per tile or per 16 rows: whether the vocabulary ends in it, and whether a lane holds its row's target (one tile in hundreds).
@@ -552,13 +553,14 @@ constexpr int64_t kMostElements = int64_t(1) << 33;                             
 constexpr int64_t kMostPacked = int64_t(1) << 28, kMostDz = int64_t(1) << 30;   // bytes of a piece of the weight, of its dz
 int64_t up_to(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
-// Tiles of 256 x 256 (eight waves, one workgroup to a compute unit), 128 x 128 (four, two to a unit) or 64 x 128 (four, two to a unit).
+// Tiles of 256 x 256 (eight waves, one workgroup to a compute unit), 128 x 128 (four, two to a unit) or 64 x 128 (four, two to a unit; scores in fp32: eight, one to
+// a unit, see run_planes).
 enum Tile { kBig, kMiddle, kLow };
 constexpr int kUnits = 256;   // compute units
 
 // Predicted microseconds of a launch of tiles of so many stages of products, from launches of 1 to 4099 rows over 800 to 50021 tokens with 256 to 4096
 // elements: a tile's beginning and end, and its stages: alone on a compute unit, or beside another one.  Rounds of big tiles count whole, those of
-// the others overlap.
+// the others overlap.  (fp32 scores in 64 x 128 tiles take less, 5.5 us and 0.23 per stage a round; where either size would do, they and 128 x 128 are within 4 %.)
 double tiles_us(Tile tile, int64_t tiles, double stages) {
   if (tile == kBig) return (double)((tiles + kUnits - 1) / kUnits) * (8.0 + 1.45 * stages);
   if (tiles <= kUnits) return tile == kMiddle ? 5.0 + 0.55 * stages : 4.5 + 0.40 * stages;
@@ -745,7 +747,7 @@ bool wide_x(const s1f_rows *d, const void *p) { return on16(p) && d->hidden % 8 
 template <template <Tile> class KERNELS> int launch_cut(const Cut &cut, int64_t m, int64_t n, LossArgs a, hipStream_t st) {
   auto go = [&](auto kernels, int64_t grid) {
     typedef decltype(kernels) K;
-    return launch_tiles<K::kernel>(K::P::LDS_BYTES, K::P::THREADS, grid, a, st);
+    return launch_tiles<K::kernel>(K::LDS_BYTES, K::P::THREADS, grid, a, st);
   };
   if (cut.tile == kMiddle) {
     tiles_of(a, m, n, 128, 128);
@@ -771,14 +773,17 @@ template <Tile TILE> struct Shape {
 template <typename T, bool STATS> struct Scores {
   template <Tile TILE> struct Of : Shape<TILE> {
     typedef Shape<TILE> S;
-    typedef Product<S::BM, S::BN, S::WM, S::WN, false, false, 1> P;
-    static constexpr auto kernel = &loss_scores_kernel<T, S::BM, S::BN, S::WM, S::WN, STATS>;
+    static constexpr int WM = sizeof(T) == 4 && TILE == kLow ? 2 : S::WM;   // (one workgroup to a unit)
+    typedef Product<S::BM, S::BN, WM, S::WN, false, false, 1> P;
+    static constexpr int LDS_BYTES = sizeof(T) == 4 && TILE == kLow ? P::PLANES_LDS_BYTES : P::LDS_BYTES;
+    static constexpr auto kernel = &loss_scores_kernel<T, S::BM, S::BN, WM, S::WN, STATS>;
   };
 };
 template <int PAIRS, bool ADD> struct Dw {
   template <Tile TILE> struct Of : Shape<TILE == kLow ? kMiddle : TILE> {
     typedef Shape<TILE == kLow ? kMiddle : TILE> S;
     typedef Product<S::BM, S::BN, S::WM, S::WN, true, true, 1> P;
+    static constexpr int LDS_BYTES = P::LDS_BYTES;
     static constexpr auto kernel = &loss_dw_kernel<PAIRS, S::BM, S::BN, S::WM, S::WN, ADD>;
   };
 };
