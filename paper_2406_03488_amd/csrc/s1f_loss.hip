@@ -550,7 +550,8 @@ template <int PAIRS, int BM, int BN, int WM, int WN, bool ADD> __global__ void _
 
 constexpr int64_t kMostLossRows = int64_t(1) << 20, kMostLossVocab = int64_t(1) << 24, kMostWeightStride = int64_t(1) << 22;
 constexpr int64_t kMostElements = int64_t(1) << 33;                             // of x: threads of the launch that writes dx
-constexpr int64_t kMostPacked = int64_t(1) << 28, kMostDz = int64_t(1) << 30;   // bytes of a piece of the weight, of its dz
+// bytes of a piece of the weight, and of its dz (of more, up to 1.5 GiB, where 2^30 bytes hold less than 256 tokens: fp32 calls of more than 699050 rows)
+constexpr int64_t kMostPacked = int64_t(1) << 28, kMostDz = int64_t(1) << 30;
 int64_t up_to(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
 // Tiles of 256 x 256 (eight waves, one workgroup to a compute unit), 128 x 128 (four, two to a unit) or 64 x 128 (four, two to a unit; scores in fp32: eight, one to
@@ -642,7 +643,8 @@ LossPlan plan_of(const s1f_rows *d, int64_t vocab, int64_t weight_stride, bool b
   int64_t piece = std::min({vocab, (int64_t(1) << 35) / p.n, (int64_t(1) << 36) / p.width});
   if (!p.direct) piece = std::min(piece, kMostPacked / (p.planes * 2 * p.width));
   if (backward) piece = std::min(piece, kMostDz / (p.planes * 2 * p.n));
-  p.piece = piece < vocab ? std::max<int64_t>(256, piece / 256 * 256) : vocab;
+  // (and never longer than the vocabulary: with enough rows `piece` is below 256, and a vocabulary may lie between)
+  p.piece = std::min(vocab, piece < vocab ? std::max<int64_t>(256, piece / 256 * 256) : vocab);
   int64_t at = 0;
   auto take = [&at](int64_t bytes) { const int64_t was = at; at += up_to(bytes, 256); return was; };
   p.count = take(4);

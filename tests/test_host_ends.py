@@ -282,3 +282,16 @@ def test_the_largest_calls_fit_a_launch(tmp_path, monkeypatch):
 
 def threads_of(tmp_path):
     return [(line.split()[1], int(line.split()[2]), int(line.split()[3])) for line in open(tmp_path / "record") if line.startswith("launch")]
+
+
+@pytest.mark.parametrize("n,v", [(1 << 20, 200), (1 << 20, 171), (1 << 20, 255), (700000, 255), (1 << 20, 300), (699050, 255), (3000, 200), (2048, 200)])
+def test_no_more_of_the_weight_is_packed_than_there_is(tmp_path, n, v):
+    """fp32 calls whose rows leave room for fewer than 256 tokens a piece: a launch that packs the weight has a workgroup (or a
+    quarter of one) for each of its rows."""
+    h = 2048
+    done = launches(tmp_path, [(n, h, v, 0)])
+    grids = [(name, grid) for name, grid, _ in done if "loss_prepare" in name or ("loss_pack" in name and name.split("loss_pack_kernel")[1].split("EE")[0].endswith("Lb0"))]
+    assert grids
+    for name, grid in grids:
+        threads, rows = (1024, (n + 7) // 8) if "loss_prepare" in name else (256, 0)
+        assert grid <= rows + -(-v * (h // 8) // threads), (name, grid)
