@@ -235,6 +235,11 @@ S1F_DEV Matrix weight_matrix(const LossArgs &a) {
                   : Matrix{a.packed, a.width, a.packed_plane};
 }
 
+// Exponentials of scores relative to a maximum.  The difference is taken first: exact or small, then its product with log2 e rounded; and a maximum times log2 e is
+// infinite from 2.36e38 on, where masks of the type's lowest value lie.  Where there is no score above -infinity, relative to 0: all of them 0.
+S1F_DEV float above(float most) { return most == -INFINITY ? 0.f : most; }
+S1F_DEV float exp_of(float x) { return exp2_fast(x * kLog2e); }
+
 // Scores of a tile of rows and vocabulary: STATS: maximum and sum of exponentials of each row (forward); else dz (backward).  Bound by the matrix units, at the
 // clock that power leaves them, and by the beginning and end of a tile, about 6 us in which they wait: 4099 rows of 4096 bf16 elements over 50021 tokens 1.30 ms,
 // 1.3 PFLOP/s, the library's product alone 1.27; gradient of 5530 rows of 7168 over 100003 tokens 6.3 ms, 1.25 PFLOP/s, the product alone 5.5.
@@ -291,12 +296,12 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) loss_scores_kernel(const Loss
 #pragma unroll
         for (int e = 0; e < 4; ++e) most = fmaxf(most, acc[mb][nb][e]);
       most = max_over_rows(most);
-      const float from = most == -INFINITY ? 0.f : most * kLog2e;
+      const float from = above(most);
       float sum = 0.f;
 #pragma unroll
       for (int nb = 0; nb < P::NB; ++nb)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum += exp2_fast(fmaf(acc[mb][nb][e], kLog2e, -from));
+        for (int e = 0; e < 4; ++e) sum += exp_of(acc[mb][nb][e] - from);
       sum = sum_over_rows(sum);
       if (j == 0) {
         red[2 * (wn * BM + in_tile)] = most;
@@ -313,9 +318,9 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) loss_scores_kernel(const Loss
       float most = in[0], sum = 0.f;
 #pragma unroll
       for (int w = 1; w < WAVES; ++w) most = fmaxf(most, in[2 * w * BM]);
-      const float from = most == -INFINITY ? 0.f : most * kLog2e;
+      const float from = above(most);
 #pragma unroll
-      for (int w = 0; w < WAVES; ++w) sum += in[2 * w * BM + 1] * exp2_fast(fmaf(in[2 * w * BM], kLog2e, -from));
+      for (int w = 0; w < WAVES; ++w) sum += in[2 * w * BM + 1] * exp_of(in[2 * w * BM] - from);
       float *to = a.stats + 2 * ((int64_t)((a.first + n0) / 128 + part) * a.n + m0 + row);
       to[0] = most;
       to[1] = sum;
@@ -331,11 +336,10 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) loss_scores_kernel(const Loss
 #pragma unroll
     for (int mb = 0; mb < P::MB; ++mb) {
       const int slot = m0 + 16 * (wm * P::MB + mb) + n;
-      // exp((z - lse) log2 e) as two roundings: the difference, which is exact or small, first
 #pragma unroll
       for (int nb = 0; nb < P::NB; ++nb)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[mb][nb][e] = exp2_fast((acc[mb][nb][e] - lse[mb]) * kLog2e);
+        for (int e = 0; e < 4; ++e) acc[mb][nb][e] = exp_of(acc[mb][nb][e] - lse[mb]);
       if (target[mb] >= 0) {
 #pragma unroll
         for (int nb = 0; nb < P::NB; ++nb)
@@ -389,10 +393,10 @@ __global__ void __launch_bounds__(1024) loss_join_kernel(const LossArgs a) {
         m[u] = s[0];
         x[u] = is ? s[1] : 0.f;
       }
-      const float now = fmaxf(fmaxf(most, fmaxf(m[0], m[1])), fmaxf(m[2], m[3])), from = now == -INFINITY ? 0.f : now * kLog2e;
-      sum *= exp2_fast(fmaf(most, kLog2e, -from));
+      const float now = fmaxf(fmaxf(most, fmaxf(m[0], m[1])), fmaxf(m[2], m[3])), from = above(now);
+      sum *= exp_of(most - from);
 #pragma unroll
-      for (int u = 0; u < 4; ++u) sum += x[u] * exp2_fast(fmaf(m[u], kLog2e, -from));
+      for (int u = 0; u < 4; ++u) sum += x[u] * exp_of(m[u] - from);
       most = now;
     }
   red[share][in][0] = most;
@@ -400,8 +404,8 @@ __global__ void __launch_bounds__(1024) loss_join_kernel(const LossArgs a) {
   for (int half = SHARES / 2; half > 0; half /= 2) {
     __syncthreads();
     if (share < half) {
-      const float m = red[share + half][in][0], now = fmaxf(most, m), from = now == -INFINITY ? 0.f : now * kLog2e;
-      sum = sum * exp2_fast(fmaf(most, kLog2e, -from)) + red[share + half][in][1] * exp2_fast(fmaf(m, kLog2e, -from));
+      const float m = red[share + half][in][0], now = fmaxf(most, m), from = above(now);
+      sum = sum * exp_of(most - from) + red[share + half][in][1] * exp_of(m - from);
       most = now;
       red[share][in][0] = most;
       red[share][in][1] = sum;
