@@ -13,6 +13,7 @@
 #include <algorithm>
 #include <atomic>
 
+#include "attn_plain.hpp"
 #include "loss_tile.hpp"
 #include "rows.hpp"
 
@@ -101,6 +102,32 @@ template <bool FWD> __global__ void __launch_bounds__(1024) loss_rows_kernel(con
   if (threadIdx.x == 0) *a.count = carry;
 }
 
+// Planes of fp32 operands, of the largest ones too: past the largest bf16 number the first plane is that number, which rounding would take to infinity, and
+// the others have what is left, exactly.  A mask of the type's lowest value has planes, then, and takes no part in a gradient as zero times it is zero.  The planes
+// of infinities and NaN are such: see scores_plain.
+S1F_DEV Planes planes_of(f32x4 lo, f32x4 hi) {
+  constexpr float kMost = 0x1.fep127f;
+  f32x4 l, h;
+  bool all = true;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    l[e] = __builtin_amdgcn_fmed3f(lo[e], -kMost, kMost);
+    h[e] = __builtin_amdgcn_fmed3f(hi[e], -kMost, kMost);
+    all = all && l[e] == lo[e] && h[e] == hi[e];
+  }
+  Planes p = split3(l, h);
+  if (!all) {
+    const Planes rest = split3(lo - l, hi - h);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float x = e < 4 ? lo[e] : hi[e - 4], c = e < 4 ? l[e] : h[e - 4];
+      if (x == c) continue;
+      p.p[1][e] = rest.p[0][e];
+      p.p[2][e] = rest.p[1][e];
+    }
+  }
+  return p;
+}
 // Eight elements of a row as the products read them: bf16, zeros behind `hidden`; fp32 ones as three planes, `plane` elements apart.  (Planes not
 // 2^16 times as large, see kUp: what lies below 2^-110 is nothing beside a row's other scores.)
 template <typename T, bool WIDE> S1F_DEV void pack_eight(const T *from, int hidden, int c, bf16_t *to, int64_t plane) {
@@ -114,7 +141,7 @@ template <typename T, bool WIDE> S1F_DEV void pack_eight(const T *from, int hidd
     for (int e = 0; e < P::N; ++e) v[i + e] = p[e];
   }
   if constexpr (sizeof(T) == 4) {
-    const Planes p = split3(f32x4{v[0], v[1], v[2], v[3]}, f32x4{v[4], v[5], v[6], v[7]});
+    const Planes p = planes_of(f32x4{v[0], v[1], v[2], v[3]}, f32x4{v[4], v[5], v[6], v[7]});
 #pragma unroll
     for (int i = 0; i < 3; ++i) *reinterpret_cast<bf16x8 *>(to + i * plane) = p.p[i];
   } else {
@@ -235,6 +262,50 @@ S1F_DEV Matrix weight_matrix(const LossArgs &a) {
                   : Matrix{a.packed, a.width, a.packed_plane};
 }
 
+// fp32 scores that the products of planes cannot give: where an operand is not finite, or a score or one of its terms passes the largest float, there is a NaN or an infinity
+// among them.  A wave computes the 16 rows' blocks in which that happens again, from the operands in memory, with the fp32 matrix instructions: what fp32 arithmetic gives, in which a score
+// of minus infinity has weight zero and leaves its row's others alone.  What is finite pays one instruction per score; one weight of minus infinity in 20011 rows of 1280: loss of 682 rows 234 -> 880 us, an infinity in each of
+// 4099 rows of 1024 over 20000 tokens 832 -> 3736.  slot0, col0: of the wave's first block; lanes
+// as in the epilogue below.
+template <int MB, int NB> S1F_DEV void scores_plain(f32x4 (&acc)[MB][NB], const LossArgs &a, int count, int slot0, int col0) {
+  typedef Piece<float, false> P;
+  const int lane = lane_id(), n = lane & 15, j = lane >> 4;
+#pragma unroll
+  for (int mb = 0; mb < MB; ++mb) {
+    float bad = 0.f;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) bad = add_if_not_finite(acc[mb][nb], bad);
+    if (!any_not_finite(bad)) continue;
+    const int slot = slot0 + 16 * mb + n;
+    const float *x = reinterpret_cast<const float *>(a.x) + a.xs.offset(a.row_of[slot < count ? slot : count - 1]), *w[NB];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const int v = col0 + 16 * nb + n;
+      w[nb] = reinterpret_cast<const float *>(a.weight) + (a.first + (v < a.piece ? v : a.piece - 1)) * a.weight_stride;
+      acc[mb][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    // four steps of four at a time, of which lane (n, j) holds elements 4j .. 4j+3: in either operand, so that any order does
+#pragma unroll 1
+    for (int k0 = 0; k0 < a.hidden; k0 += 16) {
+      const int k = k0 + 4 * j;
+      const f32x4 fx = P::get(x + k, a.hidden - k);
+      f32x4 fw[NB];
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) fw[nb] = P::get(w[nb] + k, a.hidden - k);
+      bool numbers = false;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[mb][nb] = __builtin_amdgcn_mfma_f32_16x16x4f32(fw[nb][e], fx[e], acc[mb][nb], 0, 0, 0);
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) numbers = numbers || acc[mb][nb][e] == acc[mb][nb][e];
+      if (__builtin_amdgcn_ballot_w64(numbers) == 0) break;   // (NaN throughout, and stays so)
+    }
+  }
+}
+
 // Exponentials of scores relative to a maximum.  The difference is taken first: exact or small, then its product with log2 e rounded; and a maximum times log2 e is
 // infinite from 2.36e38 on, where masks of the type's lowest value lie.  Where there is no score above -infinity, relative to 0: all of them 0.
 S1F_DEV float above(float most) { return most == -INFINITY ? 0.f : most; }
@@ -258,6 +329,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) loss_scores_kernel(const Loss
   if constexpr (PAIRS == 6 && BM == 64) P::run_planes(acc, rows, weight_matrix(a), m0, count, n0, a.piece, a.width, to_lds_addr(smem));
   else P::run(acc, rows, weight_matrix(a), m0, count, n0, a.piece, a.width, 0, (a.width + kDepth - 1) / kDepth * PAIRS, to_lds_addr(smem));
   const int lane = lane_id(), n = lane & 15, j = lane >> 4, wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
+  if constexpr (sizeof(T) == 4) scores_plain(acc, a, count, m0 + 16 * wm * P::MB, n0 + 16 * wn * P::NB);
   // A tile's results cost the vector unit about as long as four stages of products the matrix unit, so nothing is asked per element that can be
   // asked per tile or per 16 rows: whether the vocabulary ends in it, and whether a lane holds its row's target (one tile in hundreds).
   const int col0 = 16 * wn * P::NB + 4 * j;   // the lane's columns of the tile: col0 + 16 * nb + e

@@ -7,6 +7,7 @@ import paper_2406_03488_amd as s1f
 from ends_harness import HALF, U, TYPES, f64, loss_tolerances, normal, row_values, space, untouched, within
 from oracle import ends as E
 
+LOWEST = torch.finfo(torch.float32).min
 pytestmark = pytest.mark.gpu
 
 
@@ -112,3 +113,72 @@ def test_one_score_far_above_the_others(dtype):
     want = torch.zeros(v, device="cuda")
     want[300], want[17] = n / 2, -n / 2
     assert torch.equal(dw[:, 3], want)
+
+
+@pytest.mark.parametrize("element,mask", [(1.0, LOWEST), (1.0, -1.5 * 2.0 ** 127), (0.5, LOWEST), (1.25, LOWEST), (2.0 ** 100, LOWEST)])
+@pytest.mark.parametrize("case", MASKED)
+def test_masked_tokens_of_fp32(case, element, mask):
+    """Masks past the largest bf16 number, of which the last two give scores of minus infinity: weight zero, and gradients of zero times a finite number."""
+    n, h, v, spans = case
+    rng = np.random.default_rng(n + v)
+    x, w, on = masked_call(rng, n, h, v, spans, "f32", element, mask)
+    check_against_the_others(x, w, on, "f32", rng)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("case", MASKED)
+def test_masks_of_minus_infinity(case, dtype):
+    """As above, but for the mask's own column of dx, in which zero times infinity is NaN."""
+    n, h, v, spans = case
+    rng = np.random.default_rng(n + v)
+    x, w, on = masked_call(rng, n, h, v, spans, dtype, 1.0, float("-inf"))
+    finite = w.clone()
+    finite[:, -1] = 0.0
+    finite[on, -1] = w[on, -1]
+    targets = torch.from_numpy(on[rng.integers(0, len(on), n)])[None].cuda()
+    loss, lse = forward(x, w, targets)
+    x64, w64, at = f64(x)[0], f64(w)[on], np.searchsorted(on, targets[0].cpu().numpy())
+    want_loss, want_lse = E.token_loss(x64, w64, at)
+    e_loss, e_lse = loss_tolerances(x64, w64, at, want_lse, None, dtype, np.arange(n))
+    within(f64(lse)[0], want_lse, e_lse, "lse")
+    within(f64(loss)[0], want_loss, e_loss, "loss")
+    g = torch.rand((1, n), device="cuda") + 0.5
+    dx, dw = backward(g, x, w, targets, lse)
+    assert torch.isnan(dx[..., -1]).all()
+    lse64, g64 = f64(lse)[0], f64(g)[0]
+    want_dx, want_dw, _, _ = E.token_loss_grad(g64, x64, w64, at, lse64)
+    _, _, e_dx, e_dw = loss_tolerances(x64, w64, at, lse64, g64, dtype, np.arange(n))
+    within(f64(dx)[0, :, :-1], want_dx[:, :-1], (e_dx * (1 + HALF[dtype]) + HALF[dtype] * np.abs(want_dx))[:, :-1], "dx")
+    got = f64(dw)
+    within(got[on], want_dw, e_dw * (1 + U) + U * np.abs(want_dw), "dweight")
+    got[on] = 0
+    assert not got.any()
+
+
+@pytest.mark.parametrize("n,h,v", [(1, 1, 1), (70, 72, 300), (130, 67, 700), (300, 136, 2055), (1040, 64, 16384)])
+def test_fp32_scores_that_are_not_finite_are_what_fp32_arithmetic_gives(n, h, v):
+    """Infinities and NaN in rows and weights, and sums that pass the largest float, against the formula in fp32 on the CPU: what is NaN, infinite and finite is the same; rows
+    without any are as without them."""
+    rng = np.random.default_rng(n)
+    x, w = normal(rng, (1, n, h), "f32"), normal(rng, (v, h), "f32", 2 / np.sqrt(h))
+    targets = torch.from_numpy(rng.integers(0, v, (1, n)))
+    x[0, :, 0] = x[0, :, 0].abs() + 0.1
+    w[v // 2, 0] = float("-inf")                              # a score of minus infinity for every row
+    kinds = [float("inf"), float("-inf"), float("nan"), 3e38, -3e38]
+    for i, r in enumerate(range(0, n, 11)):
+        x[0, r, (i * 7) % h] = kinds[i % 5]
+    if v > 20:
+        w[v - 1, h - 1], w[v - 2, h - 1] = 3e38, 3.4e38       # with rows whose last element is above 1: infinite
+    z = x[0] @ w.T
+    most = z.max(1).values
+    lse = torch.where(most == float("-inf"), most, most + (z - most[:, None]).exp().sum(1).log())     # (of nothing but masked tokens: log 0)
+    loss = lse - z.gather(1, targets[0][:, None])[:, 0]
+    got_loss, got_lse = forward(x.cuda(), w.cuda(), targets.cuda())
+    for got, want in ((got_loss, loss), (got_lse, lse)):
+        got = got[0].cpu()
+        assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(torch.isinf(got), torch.isinf(want))
+        there = torch.isfinite(want)
+        assert torch.equal(got.sign()[torch.isinf(want)], want.sign()[torch.isinf(want)])
+        # fp32 sums of h terms on both sides, of magnitudes that stay below 60, or one term and what is nothing beside it
+        off = (got[there].double() - want[there].double()).abs() / want[there].double().abs().clamp(min=1.0)
+        assert there.sum() == 0 or off.max() <= (16 * h + 64) * U * 60
