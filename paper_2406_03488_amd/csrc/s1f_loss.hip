@@ -129,7 +129,8 @@ S1F_DEV Planes planes_of(f32x4 lo, f32x4 hi) {
   return p;
 }
 // Eight elements of a row as the products read them: bf16, zeros behind `hidden`; fp32 ones as three planes, `plane` elements apart.  (Planes not
-// 2^16 times as large, see kUp: what lies below 2^-110 is nothing beside a row's other scores.)
+// 2^16 times as large, see kUp: the largest floats would have none, and what lies below 2^-110 is nothing beside a row's other scores; to gradients of nothing but
+// such elements it leaves 8 bits.)
 template <typename T, bool WIDE> S1F_DEV void pack_eight(const T *from, int hidden, int c, bf16_t *to, int64_t plane) {
   typedef Piece<T, WIDE> P;
   float v[8];
@@ -433,7 +434,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) loss_scores_kernel(const Loss
         bf16_t *to = a.dz + (int64_t)slot * a.dz_ld + col;
         if constexpr (sizeof(T) == 4) {
           typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-          const Planes q = split3(d, f32x4{0.f, 0.f, 0.f, 0.f});
+          const Planes q = split3(d * kUp, f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
           for (int i = 0; i < 3; ++i) {
             const u32x4 v = __builtin_bit_cast(u32x4, q.p[i]);
@@ -510,6 +511,10 @@ struct DxParts {
   }
 };
 
+// fp32 dz are split 2^16 times as large as they are, and what comes of them divided: most tokens have next to no probability, and the last plane of a value below 2^-110
+// would lie under the smallest bf16 number (see kUp).
+template <int PAIRS> constexpr float kOfDz = PAIRS == 6 ? 1.f / kUp : 1.f;
+
 // dx = dz W over a piece of the vocabulary.  Tiles that do not fill a round of workgroups are cut along the vocabulary.  5530 rows of 7168 bf16 elements over
 // 100003 tokens: 6.2 ms, 1.28 PFLOP/s, the library's product 7.9.
 template <int PAIRS, int BM, int BN, int WM, int WN> __global__ void __launch_bounds__(64 * WM * WN, 2) loss_dx_kernel(const LossArgs a) {
@@ -543,7 +548,8 @@ template <int PAIRS, int BM, int BN, int WM, int WN> __global__ void __launch_bo
       const int col = 16 * (wn * P::NB + nb) + 4 * j;
       if (n0 + col >= a.width) continue;
       f32x4 *at = reinterpret_cast<f32x4 *>(to + (int64_t)row * stride + col);
-      *at = a.add ? *at + acc[mb][nb] : acc[mb][nb];
+      const f32x4 d = acc[mb][nb] * kOfDz<PAIRS>;
+      *at = a.add ? *at + d : d;
     }
   }
 }
@@ -598,7 +604,7 @@ template <int PAIRS, int BM, int BN, int WM, int WN, bool ADD> __global__ void _
     for (int nb = 0; nb < P::NB; ++nb) {
       const int col = n0 + 16 * (wn * P::NB + nb) + 4 * j;
       const int64_t at = (a.first + v) * a.dweight_stride + col;
-      const f32x4 d = acc[mb][nb];
+      const f32x4 d = acc[mb][nb] * kOfDz<PAIRS>;
       if constexpr (ADD) {
         float *to = reinterpret_cast<float *>(a.dweight) + at;
         if (a.wide && col + 4 <= a.hidden) {

@@ -182,3 +182,19 @@ def test_fp32_scores_that_are_not_finite_are_what_fp32_arithmetic_gives(n, h, v)
         # fp32 sums of h terms on both sides, of magnitudes that stay below 60, or one term and what is nothing beside it
         off = (got[there].double() - want[there].double()).abs() / want[there].double().abs().clamp(min=1.0)
         assert there.sum() == 0 or off.max() <= (16 * h + 64) * U * 60
+
+
+@pytest.mark.parametrize("n,h,v", [(70, 72, 300), (300, 136, 2055)])
+@pytest.mark.parametrize("power", [-116, -100, 60])
+def test_fp32_gradients_of_small_and_large_size(n, h, v, power):
+    """Gradients scale with dloss.  At 2^-116 numbers below 2^-126 are among them: dz is off by 2^-150, and by as much where its last plane ends; in dx that makes up to v 2^-149 |w| < 2^-139
+    beside elements of 2^-116 |w| > 2^-119, in dweight n 2^-149 |x| < 2^-138 beside 2^-116."""
+    rng = np.random.default_rng(power + 200)
+    x, w = normal(rng, (1, n, h), "f32").cuda(), normal(rng, (v, h), "f32", 0.1).cuda()
+    targets = torch.from_numpy(rng.integers(0, v, (1, n))).cuda()
+    _, lse = forward(x, w, targets)
+    g = torch.rand((1, n), device="cuda") + 0.5
+    ones, many = backward(g, x, w, targets, lse), backward(g * 2.0 ** power, x, w, targets, lse)
+    for a, b in zip(ones, many):
+        off = (b.double() * 2.0 ** -power - a.double()).abs().amax()
+        assert off <= (2.0 ** -20 * a.double().abs().amax() if power < -100 else 0), off
