@@ -1,0 +1,69 @@
+"""The token loss's products element by element, in calls of every instance of its kernels and every way they are cut (exact_products.py): whole numbers have to be
+equal, single products of full operands right to the roundings of one."""
+import pytest
+import torch
+
+import paper_2406_03488_amd as s1f
+from ends_harness import row_values, space, untouched
+from exact_products import ONE_PRODUCT, PIECES, SHAPES, TYPES, WHOLE, backward_case, scores_case
+
+pytestmark = pytest.mark.gpu
+
+
+def check(kind, n, h, v, dtype, into, blank=0.0, seed=0):
+    """into: type of dweight.  fp32: added to what is there."""
+    x, w, t, lse, g, dx, dw = (a.cuda() for a in backward_case(kind, n, h, v, dtype, blank, seed))
+    got_dx = torch.full_like(x, float("nan"))
+    start = torch.zeros((v, h), device="cuda") if kind == "one" else torch.arange(v, device="cuda").remainder(7).float()[:, None].expand(v, h).contiguous()
+    got_dw = start.clone() if into == "f32" else torch.full((v, h), float("nan"), dtype=TYPES[into], device="cuda")
+    size = s1f.token_loss_bwd_workspace_bytes(x, w)
+    ws, buffer = space(size)
+    s1f.token_loss_bwd(g, x, w, t, lse, got_dx, got_dw, ws)
+    assert untouched(buffer, size)
+    want_dw = dw + start.double() if into == "f32" else dw
+    for what, got, want in (("dx", got_dx[0], dx), ("dweight", got_dw, want_dw)):
+        if kind == "one" and dtype == "f32":
+            off = (got.double() - want).abs() - ONE_PRODUCT * want.abs()
+            bad = ~(off <= 0)
+        else:
+            bad = got != want.to(torch.float32).to(got.dtype)      # (exact in fp32: rounded once)
+        assert not bad.any(), f"{what}: {int(bad.sum())} of {bad.numel()} elements are wrong, the first at {torch.nonzero(bad)[0].tolist()}"
+
+
+KINDS = ["one", "all dx", "all dw", "some"]
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("types", ["f32 f32", "bf16 f32", "bf16 bf16"])
+@pytest.mark.parametrize("n,h,v", SHAPES + WHOLE)
+def test_gradient(n, h, v, types, kind):
+    check(kind, n, h, v, *types.split())
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("types", ["f32 f32", "bf16 f32", "bf16 bf16"])
+def test_gradient_over_several_pieces(types, kind):
+    dtype, into = types.split()
+    check(kind, *PIECES[dtype], dtype, into)
+
+
+@pytest.mark.parametrize("kind", ["one", "all dx", "some"])
+@pytest.mark.parametrize("types", ["f32 f32", "bf16 bf16"])
+@pytest.mark.parametrize("blank", [0.5, 0.95, 1.0])
+@pytest.mark.parametrize("n,h,v", WHOLE + [(1040, 512, 16384), (2304, 8192, 2304), (700, 264, 9001)])
+def test_gradient_of_fewer_rows(n, h, v, blank, types, kind):
+    """Most rows out, behind whole rounds of tiles and where all are in parts."""
+    check(kind, n, h, v, *types.split(), blank=blank, seed=1)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,h,v", SHAPES + WHOLE)
+def test_scores(n, h, v, dtype):
+    x, w, t, want = (a.cuda() for a in scores_case(n, h, v, dtype))
+    loss, lse = row_values(1, n), row_values(1, n)
+    size = s1f.token_loss_fwd_workspace_bytes(x, w)
+    ws, buffer = space(size)
+    s1f.token_loss_fwd(x, w, t, loss, lse, ws)
+    assert untouched(buffer, size)
+    assert (loss == 0).all()
+    assert ((lse[0].double() - want).abs() <= (ONE_PRODUCT if dtype == "f32" else 0) * want).all()
