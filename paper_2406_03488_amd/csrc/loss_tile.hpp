@@ -43,11 +43,12 @@ S1F_DEV const char *uniform_pointer(const char *p) {
 // R: rows of C (or columns of C, for the other operand) in the tile; TR: stored by columns; NW: waves that copy.
 template <int R, bool TR, int NW> struct Side {
   static constexpr int BYTES = R * kDepth * 2, PIECES = BYTES / 1024, PER_WAVE = PIECES / NW;
-  static_assert(PIECES % NW == 0 && (PER_WAVE <= 4 || PER_WAVE == 8), "up to four pieces share one M0");
+  static_assert(PIECES % NW == 0 && PER_WAVE <= 4, "a wave's pieces share one M0: the offset of a copy instruction reaches four");
+  static_assert(!TR || R >= 128, "a unit has eight slots");
   static constexpr int ROW = TR ? 2 * R : 128, CHUNKS = ROW / 16, RPP = 1024 / ROW;   // bytes and chunks of a row, rows per piece
-  S1F_DEV static int h(int k) { return R >= 128 ? (k & 3) | ((k >> 3) & 1) << 2 : ((k >> 1) & 1) | ((k >> 3) & 1) << 1; }
+  S1F_DEV static int h(int k) { return (k & 3) | ((k >> 3) & 1) << 2; }
 
-  static constexpr int GROUP = PER_WAVE < 4 ? PER_WAVE : 4, BIAS = 1024 * (GROUP - 1);
+  static constexpr int BIAS = 1024 * (PER_WAVE - 1);
   const char *next;         // of the stage that is copied next, less BIAS (uniform)
   int64_t step;             // bytes to the next stage
   unsigned voff[PER_WAVE];  // of the lane's chunk in each of the wave's pieces
@@ -74,7 +75,7 @@ template <int R, bool TR, int NW> struct Side {
         if (m0 + r >= limit) r = (int)(limit - 1 - m0);
       }
       // (the immediate offset of a copy instruction counts for its address in memory as well as in LDS)
-      voff[i] = (unsigned)(r * row_bytes + 16 * c) + (unsigned)(BIAS - 1024 * (i % GROUP));
+      voff[i] = (unsigned)(r * row_bytes + 16 * c) + (unsigned)(BIAS - 1024 * i);
     }
   }
   // From here on stages hold `left` of their contraction: what is behind is read from the stage's beginning, and cleared by clear_tail.
@@ -93,7 +94,7 @@ template <int R, bool TR, int NW> struct Side {
   // Copies piece I of the wave's pieces of a stage at `from` (uniform) to LDS address `dst` (of the wave's first piece; uniform).
   template <int I> S1F_DEV void copy(const char *from, unsigned dst) const {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 offset:%3"
-                 : : "s"(dst + 1024 * (I / GROUP * GROUP)), "v"(voff[I]), "s"(from), "n"(1024 * (I % GROUP)) : "m0");
+                 : : "s"(dst), "v"(voff[I]), "s"(from), "n"(1024 * I) : "m0");
   }
   // Zeros in the wave's own slots behind the end of the contraction, once its copies have landed.
   S1F_DEV void clear_tail(lds_addr at, int left, int wave, int lane) const {

@@ -721,7 +721,7 @@ LossPlan plan_of(const s1f_rows *d, int64_t vocab, int64_t weight_stride, bool b
   p.width = up_to(d->hidden, 8);
   p.planes = d->dtype == S1F_F32 ? 3 : 1;
   p.direct = d->dtype == S1F_BF16 && d->hidden % 8 == 0 && weight_stride % 8 == 0;
-  // (of either product over the vocabulary a launch holds fewer than 2^32 threads: 256 for 64 x 128 scores or 128 x 128 of dW)
+  // (of either product over the vocabulary a launch holds fewer than 2^32 threads: up to 512 for 64 x 128 scores, 256 for 128 x 128 of dW)
   int64_t piece = std::min({vocab, (int64_t(1) << 35) / p.n, (int64_t(1) << 36) / p.width});
   if (!p.direct) piece = std::min(piece, kMostPacked / (p.planes * 2 * p.width));
   if (backward) piece = std::min(piece, kMostDz / (p.planes * 2 * p.n));
