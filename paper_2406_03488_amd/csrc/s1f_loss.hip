@@ -45,6 +45,9 @@ struct LossArgs {
   int32_t tiles_m, tiles_n, tile0, quarters;
   // dx: the tiles from `whole` on, `rest` of them, are cut into `splits` parts along the vocabulary (see DxParts)
   int32_t whole, rest, splits, most_splits;
+  // dW: fp32 sums over more than kMostSummed rows are cut into parts of so many; what all but the first add: [part - 1][tile][row][column]
+  int32_t dw_parts;
+  float *dw_part;
 };
 
 // ---- rows that count -------------------------------------------------------------------------------------------------------------------
@@ -227,6 +230,11 @@ template <typename T, bool WIDE_X, bool WIDE_W, bool FWD> __global__ void __laun
     pack_eight<T, WIDE_X>(reinterpret_cast<const T *>(a.x) + a.xs.offset(first + r), a.hidden, c, a.rows + (int64_t)slots[r] * a.width + 8 * c, a.rows_plane);
   }
 }
+
+// Rows that one fp32 sum of dW runs over, six products for each.  Error of dW relative to its norm, 64 elements over 300 tokens: of 8192 rows in one sum 1.0e-6, of 16384 in one 1.4e-6 and in
+// parts 0.8e-6, of 131072 5.0e-6 and 0.5e-6 (the library's product of 32-bit dz: 1.5e-6 to 1.9e-6); these calls take 444 us, 850 and 462, 7830 and 854.  Parts cost room for a
+// tile each, written and read once.  bf16 sums are six times as short, and their dz is rounded.
+constexpr int kMostSummed = 8192;
 
 // ---- products --------------------------------------------------------------------------------------------------------------------------
 
@@ -583,19 +591,39 @@ template <typename T, bool WIDE, int TILE> __global__ void __launch_bounds__(256
   P::store(reinterpret_cast<T *>(a.dx) + a.xs.offset((int)row) + col, a.hidden - col, v);
 }
 
-// dW of a piece of the vocabulary: added into fp32 accumulators (ADD), or written in bf16.  No atomics: a workgroup has all rows of its tile.  5530 rows of 7168
-// bf16 elements over 100003 tokens: 6.4 ms, 1.24 PFLOP/s, the library's product 6.9.
+// dW of a piece of the vocabulary: added into fp32 accumulators (ADD), or written in bf16.  No atomics: a workgroup has all rows of its tile, or in fp32, whose six products make a sum
+// over as many rows six times as long, those of a part (see kMostSummed).  5530 rows of 7168 bf16 elements over 100003 tokens: 6.4 ms, 1.24 PFLOP/s, the library's product 6.9.
 template <int PAIRS, int BM, int BN, int WM, int WN, bool ADD> __global__ void __launch_bounds__(64 * WM * WN, 2) loss_dw_kernel(const LossArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   typedef Product<BM, BN, WM, WN, true, true, PAIRS> P;
-  int tm, tn;
-  own_tile(a, tm, tn);
+  int tm, tn, part = 0;
+  if (PAIRS == 1 || a.dw_parts == 1) {
+    own_tile(a, tm, tn);
+  } else {
+    part = blockIdx.x / (a.tiles_m * a.tiles_n);
+    decode_tile(a.tiles_m, a.tiles_n, blockIdx.x - part * (a.tiles_m * a.tiles_n), tm, tn);
+  }
   const int m0 = tm * BM, n0 = tn * BN, count = *a.count;
   if (m0 >= a.piece || n0 >= a.width) return;
+  int begin = 0, end = (count + kDepth - 1) / kDepth;
+  if (PAIRS == 6 && a.dw_parts > 1) {
+    begin = part * (kMostSummed / kDepth);
+    end = end < begin + kMostSummed / kDepth ? end : begin + kMostSummed / kDepth;
+    if (part > 0 && begin >= end) return;
+  }
   f32x4 acc[P::MB][P::NB];
-  P::run(acc, Matrix{a.dz, a.dz_ld, a.dz_plane}, Matrix{a.rows, a.width, a.rows_plane}, m0, a.dz_ld, n0, a.width, count, 0,
-         (count + kDepth - 1) / kDepth * PAIRS, to_lds_addr(smem));
+  P::run(acc, Matrix{a.dz, a.dz_ld, a.dz_plane}, Matrix{a.rows, a.width, a.rows_plane}, m0, a.dz_ld, n0, a.width, count, begin * PAIRS, end * PAIRS,
+         to_lds_addr(smem));
   const int lane = lane_id(), n = lane & 15, j = lane >> 4, wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
+  if (PAIRS == 6 && part > 0) {
+    float *to = a.dw_part + ((int64_t)(part - 1) * a.tiles_m * a.tiles_n + tm * a.tiles_n + tn) * (BM * BN);
+#pragma unroll
+    for (int mb = 0; mb < P::MB; ++mb)
+#pragma unroll
+      for (int nb = 0; nb < P::NB; ++nb)
+        *reinterpret_cast<f32x4 *>(to + (16 * (wm * P::MB + mb) + n) * BN + 16 * (wn * P::NB + nb) + 4 * j) = acc[mb][nb] * kOfDz<PAIRS>;
+    return;
+  }
 #pragma unroll
   for (int mb = 0; mb < P::MB; ++mb) {
     const int v = m0 + 16 * (wm * P::MB + mb) + n;
@@ -626,6 +654,23 @@ template <int PAIRS, int BM, int BN, int WM, int WN, bool ADD> __global__ void _
       }
     }
   }
+}
+
+// The parts of dW behind the first (of tiles of TILE x TILE), added up in their order.  Bound by memory.
+template <int TILE> __global__ void __launch_bounds__(256) loss_dw_join_kernel(const LossArgs a) {
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int per_row = (a.hidden + 3) / 4;
+  const int64_t v = id / per_row;
+  const int col = (int)(id - v * per_row) * 4, parts = (*a.count + kMostSummed - 1) / kMostSummed;
+  if (v >= a.piece || parts <= 1) return;
+  const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n;
+  const float *from = a.dw_part + (v / TILE * a.tiles_n + col / TILE) * (TILE * TILE) + (v % TILE) * TILE + col % TILE;
+  f32x4 sum = *reinterpret_cast<const f32x4 *>(from);
+  for (int p = 2; p < parts; ++p) sum += *reinterpret_cast<const f32x4 *>(from + (p - 1) * tiles * (TILE * TILE));
+  float *to = reinterpret_cast<float *>(a.dweight) + (a.first + v) * a.dweight_stride + col;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (col + e < a.hidden) to[e] += sum[e];
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------------------------
@@ -703,7 +748,8 @@ struct LossPlan {
   bool direct;
   Cut scores, dw;
   DxCut dx;
-  int64_t count, row_of, slot_of, target_of, target_score, of_row, stats, rows, packed, dz, sum, part, bytes;   // offsets
+  int dw_parts;
+  int64_t count, row_of, slot_of, target_of, target_score, of_row, stats, rows, packed, dz, sum, part, dw_part, bytes;   // offsets
 };
 
 int check_loss(const s1f_rows *d, int64_t vocab, int64_t weight_stride) {
@@ -740,11 +786,18 @@ LossPlan plan_of(const s1f_rows *d, int64_t vocab, int64_t weight_stride, bool b
   if (backward) {
     p.dx = dx_cut_for(p.n, p.width, (p.piece + kDepth - 1) / kDepth * pairs);
     p.dw = cut_for(p.piece, p.width, (p.n + kDepth - 1) / kDepth * pairs, false);
-    const int64_t side = p.dx.tile == kBig ? 256 : 128;
+    p.dw_parts = p.planes == 3 ? (int)((p.n + kMostSummed - 1) / kMostSummed) : 1;
+    if (p.dw_parts > 1) {   // of whole tiles
+      const int64_t big = grid_of(p.piece, p.width, 256, 256), middle = grid_of(p.piece, p.width, 128, 128);
+      const double stages = (double)(kMostSummed / kDepth * pairs);
+      p.dw = tiles_us(kBig, big * p.dw_parts, stages) < tiles_us(kMiddle, middle * p.dw_parts, stages) ? Cut{kBig, big} : Cut{kMiddle, 0};
+    }
+    const int64_t side = p.dx.tile == kBig ? 256 : 128, dw_side = p.dw.tile == kBig ? 256 : 128;
     p.of_row = take(8 * p.n);
     p.dz = take(p.planes * 2 * p.n * up_to(p.piece, 64));
     p.sum = take(4 * p.n * p.width);
     p.part = take(4 * (p.dx.splits - 1) * p.dx.rest * side * side);
+    p.dw_part = take(4 * (p.dw_parts - 1) * grid_of(p.piece, p.width, (int)dw_side, (int)dw_side) * dw_side * dw_side);
   } else {
     p.target_score = take(4 * p.n);
     p.stats = take(8 * p.n * ((vocab + 127) / 128));
@@ -817,6 +870,8 @@ LossArgs args_of(const s1f_rows *d, const LossPlan &p, const int64_t *targets, i
   a.dz_plane = p.n * a.dz_ld;
   a.sum = reinterpret_cast<float *>(ws + p.sum);
   a.part = reinterpret_cast<float *>(ws + p.part);
+  a.dw_part = reinterpret_cast<float *>(ws + p.dw_part);
+  a.dw_parts = p.dw_parts;
   a.direct = p.direct;
   a.whole = (int32_t)p.dx.whole;
   a.rest = (int32_t)p.dx.rest;
@@ -878,6 +933,16 @@ template <int PAIRS, Tile TILE> int launch_dx(const LossPlan &p, LossArgs a, hip
   return launch_tiles<&loss_dx_kernel<PAIRS, S::BM, S::BN, S::WM, S::WN>>(P::LDS_BYTES, P::THREADS, a.whole + (int64_t)a.rest * a.splits, a, st);
 }
 
+// dW in parts, and their join.
+template <Tile TILE> int launch_dw_parts(const LossPlan &p, LossArgs a, hipStream_t st) {
+  typedef typename Dw<6, true>::template Of<TILE> K;
+  constexpr int SIDE = TILE == kBig ? 256 : 128;
+  tiles_of(a, a.piece, a.width, SIDE, SIDE);
+  const int e = launch_tiles<K::kernel>(K::LDS_BYTES, K::P::THREADS, (int64_t)a.tiles_m * a.tiles_n * p.dw_parts, a, st);
+  if (e != S1F_OK) return e;
+  return launch_rows_kernel(&loss_dw_join_kernel<SIDE>, ((int64_t)a.piece * ((a.hidden + 3) / 4) + 255) / 256, 256, a, st);
+}
+
 template <typename T> int forward(const s1f_rows *d, LossArgs a, const LossPlan &p, hipStream_t st) {
   const bool wide_w = wide_weight(d, a.weight_stride);
   a.piece = (int32_t)p.piece;
@@ -906,7 +971,9 @@ template <typename T, bool ADD> int backward(const s1f_rows *d, LossArgs a, cons
     if (!p.direct && at > 0) e = pack_weight_piece<T>(a, wide_w, st);
     if (e == S1F_OK) e = launch_cut<Scores<T, false>::template Of>(p.scores, p.n, a.piece, a, st);
     if (e == S1F_OK) e = p.dx.tile == kBig ? launch_dx<PAIRS, kBig>(p, a, st) : launch_dx<PAIRS, kMiddle>(p, a, st);
-    if (e == S1F_OK) e = launch_cut<Dw<PAIRS, ADD>::template Of>(p.dw, a.piece, a.width, a, st);
+    if (e != S1F_OK) continue;
+    if (PAIRS == 1 || p.dw_parts == 1) e = launch_cut<Dw<PAIRS, ADD>::template Of>(p.dw, a.piece, a.width, a, st);
+    else e = p.dw.tile == kBig ? launch_dw_parts<kBig>(p, a, st) : launch_dw_parts<kMiddle>(p, a, st);
   }
   if (e != S1F_OK) return e;
   const int side = p.dx.tile == kBig ? 256 : 128;

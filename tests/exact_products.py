@@ -20,6 +20,8 @@ ONE_PRODUCT = (1 + 2.0 ** -9 + 5 * 2) * 2.0 ** -24
 SHAPES = [(1040, 512, 16384), (2304, 8192, 2304), (700, 128, 130), (130, 2000, 9000), (300, 1280, 20011), (700, 264, 9001), (5, 64, 129), (3000, 72, 2000)]
 # whole rounds of big tiles of dx, with a rest in parts behind them or without one
 WHOLE = [(2049, 8192, 1000), (4096, 4096, 700)]
+# fp32 calls of so many rows that dweight's sums over them are cut into parts: middle and big tiles, the last part short
+LONG = [(24577, 136, 515), (16391, 2048, 4100)]
 # several pieces of the vocabulary, the last one short
 PIECES = {"f32": (700, 264, 180000), "bf16": (1100, 64, 600011)}
 

@@ -7,7 +7,7 @@ import sys
 import numpy as np
 import pytest
 
-from exact_products import ONE_PRODUCT, PIECES, SHAPES, WHOLE, backward_case, scores_case
+from exact_products import LONG, ONE_PRODUCT, PIECES, SHAPES, WHOLE, backward_case, scores_case
 from oracle import ends as E
 from test_host_fp32_planes import SIX, product
 
@@ -62,6 +62,16 @@ def test_whole_rounds_of_dx(tmp_path, code):
     assert dx[0] > 256 and (dx[0] - 256) % 32 == 0 and dx[1] == 256
 
 
+@pytest.mark.parametrize("shape,tile", zip(LONG, (128, 256)))
+def test_long_sums_are_cut(tmp_path, shape, tile):
+    """dweight of more than 8192 fp32 rows: as many workgroups for a tile as there are parts, and a join; of 8192, and of bf16 rows, as ever."""
+    n, h, v = shape
+    done = [(name, grid) for name, grid in launches(tmp_path, [(*shape, 0, 0)]) if name.startswith("dw")]
+    assert len(done) == 2 and f"Li{tile}ELi{tile}" in done[0][0] and done[1][0].startswith("dw_join")
+    assert done[0][1] == -(-v // tile) * -(-h // tile) * -(-n // 8192) and done[1][1] == -(-v * (h // 4) // 256)
+    assert not any(name.startswith("dw_join") for name, _ in launches(tmp_path, [(8192, h, v, 0, 0), (n, h, v, 1, 0), (n, h, v, 1, 1)]))
+
+
 @pytest.mark.parametrize("dtype,code", [("f32", 0), ("bf16", 1)])
 def test_pieces(tmp_path, dtype, code):
     n = sum(name.startswith("dx_kernel") for name, _ in launches(tmp_path, [(*PIECES[dtype], code, 0)]))
@@ -89,7 +99,7 @@ def test_expected_scores(n, h, v):
 
 def test_sums_stay_whole_in_fp32():
     """Whatever the order: fewer than 2^24 / 400 terms of at most 400, or 2^24 / 6 of at most 6."""
-    for n, h, v in SHAPES + WHOLE + list(PIECES.values()):
+    for n, h, v in SHAPES + WHOLE + LONG + list(PIECES.values()):
         assert 6 * max(n, v) < 2 ** 24 and 400 * max(v / h * 2 + 200, n / h * 2 + 200) < 2 ** 24
 
 
