@@ -13,8 +13,9 @@
 //            8j .. 8j+3 and 8j+8 .. 8j+11 together, which h spreads over all banks.
 // Both keep a wave's 64 lanes on whole lines of memory.
 //
-// Bound by power and LDS: in long walks a stage of a 256 x 256 tile takes 1.41 us, 1.48 PFLOP/s over 256 compute units, matrix units 64 % busy at the 1.8 GHz that
-// power leaves them; operands that are constant take 15 % less.  Eight waves of 128 x 64 read 192 KiB of operands per stage out of LDS, which takes about as long
+// Bound by power and LDS: a round of 256 x 256 tiles of 256 stages (4096 rows of 16384 elements over 4096 tokens) takes 385 us, 1.43 PFLOP/s, matrix units 65 % busy at 2.09 GHz, of which
+// a stage is 1.42 us (the difference to 128 stages), 1.52 PFLOP/s; in launches of milliseconds power leaves 1.8 GHz (4099 rows of 4096 over 50021 tokens: 70 % busy, 1.3 PFLOP/s).  Operands that
+// are constant take 15 % less.  Eight waves of 128 x 64 read 192 KiB of operands per stage out of LDS, which takes about as long
 // as their products; four waves of 128 x 128 read 128 KiB but have nobody to take turns with on their unit's four matrix pipes: no faster.
 #pragma once
 #include <type_traits>
