@@ -6,7 +6,8 @@
 //
 // Scores never exist in memory as a whole.  The forward's tiles of scores leave a maximum and a sum of exponentials per row; the
 // backward computes the scores of a piece of the vocabulary anew, writes that piece's dz in bf16 (rounded once, as the attention kernels round
-// their score gradients; fp32 calls: three bf16 planes of it, nothing rounded), and both products read it.
+// their score gradients; by which dx of 1000 x 512 over
+// 5000 tokens is 2.3e-3 off relative to its norm, 1.7e-3 of it the rounding of dx itself, and dW in fp32 1.5e-3; fp32 calls: in three bf16 planes that hold it whole), and both products read it.
 // Rows without a target take no part: the others are gathered into consecutive rows first, so nothing is computed for them and whatever
 // they hold, infinities and NaN included, stays theirs.  The number of rows that count is known on the device only; workgroups
 // behind them end at once.

@@ -64,6 +64,62 @@ def test_gradient_of_many_rows(n, h, v, blank, kind):
     check(kind, n, h, v, "f32", "f32", blank=blank, seed=2)
 
 
+@pytest.mark.parametrize("kind", ["all dx", "all dw", "some"])
+@pytest.mark.parametrize("v", [171, 200, 255, 300])
+def test_gradient_of_as_many_rows_as_there_may_be(v, kind):
+    """A piece of the vocabulary has 256 tokens then, or all that there are."""
+    check(kind, 1 << 20, 8, v, "f32", "f32", blank=0.3, seed=4)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_two_calls_at_once(dtype):
+    """On two streams, each with a workspace of its own, and captured into one graph as two branches of it that are replayed with other targets."""
+    n, h, v = 9000, 72, 700
+    calls = []
+    for seed in (5, 6):
+        x, w, t, lse, g, *_ = (a.cuda() for a in backward_case("some", n, h, v, dtype, 0.2, seed))
+        ws = torch.empty(max(s1f.token_loss_bwd_workspace_bytes(x, w), s1f.token_loss_fwd_workspace_bytes(x, w)), dtype=torch.uint8, device="cuda")
+        calls.append((x, w, t, lse, g, torch.empty_like(x), torch.zeros((v, h), device="cuda"), row_values(1, n), row_values(1, n), ws))
+
+    def run(x, w, t, lse, g, dx, dw, loss, made, ws):
+        dw.zero_()
+        s1f.token_loss_fwd(x, w, t, loss, made, ws)
+        s1f.token_loss_bwd(g, x, w, t, lse, dx, dw, ws)
+
+    outputs = lambda: [a.clone() for c in calls for a in c[5:9]]
+    sides = [torch.cuda.Stream() for _ in calls]
+
+    def both():
+        here = torch.cuda.current_stream()
+        for side, c in zip(sides, calls):
+            side.wait_stream(here)
+            with torch.cuda.stream(side):
+                run(*c)
+        for side in sides:
+            here.wait_stream(side)
+
+    for c in calls:
+        run(*c)
+    want = outputs()
+    both()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outputs(), want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both()
+    for turn in range(3):
+        for c in calls:
+            c[2].copy_(torch.where(torch.rand(c[2].shape, device="cuda") < 0.3 * turn, -1, torch.randint(0, v, c[2].shape, device="cuda")))
+            run(*c)
+        want = outputs()
+        for c in calls:
+            for a in c[5:9]:
+                a.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outputs(), want)), turn
+
+
 def test_long_sums_keep_their_bits():
     """dweight of 49152 fp32 rows over 300 tokens, relative to its norm: 1.5e-6 off with the library's products of 32-bit scores.  One sum over all rows, six products for each, was 2.6e-6 off.  Roundings
     are of either sign and follow the size of the sum so far: in six parts their squares are a sixth, 1.1e-6."""
