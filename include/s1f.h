@@ -309,7 +309,7 @@ size_t s1f_layer_norm_bwd_workspace_bytes(const s1f_rows *desc);
  *   dweight_dtype S1F_BF16  (bf16 rows only) overwritten, rounded once: the gradient of this call alone
  * bf16: dz is rounded to bf16 before its products, like the score gradients of the attention, which puts dx and dweight some 1.5e-3 of their norm off whatever dweight's type; sums are
  * fp32.  fp32: products to fp32 precision (operands as
- * three exact bf16 parts each, but for elements of x and weight below 2^-110, which keep 8 bits at least; dz below 2^112).
+ * three exact bf16 parts each, but for elements of x and weight below 2^-110, which keep 8 bits at least; dz, dx and dweight below 2^112).
  * A score of minus infinity or of the type's lowest value, as masks make it, has weight 0; where all of a row's are minus infinity lse is that, and loss NaN; one of plus
  * infinity or NaN makes lse and loss of its row NaN.  fp32 scores are what fp32 arithmetic gives, of any operands; calls in which some are not
  * finite take up to 5 times as long.  In gradients zero times infinity is NaN, and so may be in fp32 whatever an infinity takes part in or the largest float is passed in.

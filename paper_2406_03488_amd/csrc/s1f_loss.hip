@@ -46,7 +46,7 @@ struct LossArgs {
   int32_t tiles_m, tiles_n, tile0, quarters;
   // dx: the tiles from `whole` on, `rest` of them, are cut into `splits` parts along the vocabulary (see DxParts)
   int32_t whole, rest, splits, most_splits;
-  // dW: fp32 sums over more than kMostSummed rows are cut into parts of so many; what all but the first add: [part - 1][tile][row][column]
+  // dW: parts that fp32 sums are cut into if all rows count (see sums_of); what all but the first add: [part - 1][tile][row][column]
   int32_t dw_parts;
   float *dw_part;
 };
@@ -232,10 +232,12 @@ template <typename T, bool WIDE_X, bool WIDE_W, bool FWD> __global__ void __laun
   }
 }
 
-// Rows that one fp32 sum of dW runs over, six products for each.  Error of dW relative to its norm, 64 elements over 300 tokens: of 8192 rows in one sum 1.0e-6, of 16384 in one 1.4e-6 and in
-// parts 0.8e-6, of 131072 5.0e-6 and 0.5e-6 (the library's product of 32-bit dz: 1.5e-6 to 1.9e-6); these calls take 444 us, 850 and 462, 7830 and 854.  Parts cost room for a
-// tile each, written and read once.  bf16 sums are six times as short, and their dz is rounded.
-constexpr int kMostSummed = 8192;
+// Rows that one fp32 sum of dW runs over, up to half as many again, six products for each.  Error of dW relative to its norm, 64 elements over 300 tokens: of 8192 rows in one sum 1.0e-6,
+// of 12288 in one 1.2e-6 and in two 0.7e-6, of 16384 1.4e-6 and 0.8e-6, of 131072 5.0e-6 and 0.5e-6 (the library's product of 32-bit dz: 1.5e-6 to 1.9e-6); the last two calls take
+// 850 -> 462 us and 7830 -> 854.  A part but the first costs room for its tiles, written and read once: 8193 rows of 1024 over 32000 tokens in two parts 8.9 ms for 8.6, 16384 of 4096 over
+// 20000 36.7 for 37.0.  bf16 sums are six times as short, and their dz is rounded.
+constexpr int kSummed = 8192;
+__host__ __device__ __forceinline__ int sums_of(int rows) { return rows < kSummed ? 1 : (rows + kSummed / 2) / kSummed; }
 
 // ---- products --------------------------------------------------------------------------------------------------------------------------
 
@@ -593,7 +595,7 @@ template <typename T, bool WIDE, int TILE> __global__ void __launch_bounds__(256
 }
 
 // dW of a piece of the vocabulary: added into fp32 accumulators (ADD), or written in bf16.  No atomics: a workgroup has all rows of its tile, or in fp32, whose six products make a sum
-// over as many rows six times as long, those of a part (see kMostSummed).  5530 rows of 7168 bf16 elements over 100003 tokens: 6.4 ms, 1.24 PFLOP/s, the library's product 6.9.
+// over as many rows six times as long, those of a part (see kSummed).  5530 rows of 7168 bf16 elements over 100003 tokens: 6.4 ms, 1.24 PFLOP/s, the library's product 6.9.
 template <int PAIRS, int BM, int BN, int WM, int WN, bool ADD> __global__ void __launch_bounds__(64 * WM * WN, 2) loss_dw_kernel(const LossArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   typedef Product<BM, BN, WM, WN, true, true, PAIRS> P;
@@ -608,9 +610,10 @@ template <int PAIRS, int BM, int BN, int WM, int WN, bool ADD> __global__ void _
   if (m0 >= a.piece || n0 >= a.width) return;
   int begin = 0, end = (count + kDepth - 1) / kDepth;
   if (PAIRS == 6 && a.dw_parts > 1) {
-    begin = part * (kMostSummed / kDepth);
-    end = end < begin + kMostSummed / kDepth ? end : begin + kMostSummed / kDepth;
-    if (part > 0 && begin >= end) return;
+    const int parts = sums_of(count);
+    if (part >= parts) return;
+    begin = (int)((int64_t)end * part / parts);
+    end = (int)((int64_t)end * (part + 1) / parts);
   }
   f32x4 acc[P::MB][P::NB];
   P::run(acc, Matrix{a.dz, a.dz_ld, a.dz_plane}, Matrix{a.rows, a.width, a.rows_plane}, m0, a.dz_ld, n0, a.width, count, begin * PAIRS, end * PAIRS,
@@ -662,8 +665,8 @@ template <int TILE> __global__ void __launch_bounds__(256) loss_dw_join_kernel(c
   const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int per_row = (a.hidden + 3) / 4;
   const int64_t v = id / per_row;
-  const int col = (int)(id - v * per_row) * 4, parts = (*a.count + kMostSummed - 1) / kMostSummed;
-  if (v >= a.piece || parts <= 1) return;
+  const int col = (int)(id - v * per_row) * 4, parts = sums_of(*a.count);
+  if (v >= a.piece || parts == 1) return;
   const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n;
   const float *from = a.dw_part + (v / TILE * a.tiles_n + col / TILE) * (TILE * TILE) + (v % TILE) * TILE + col % TILE;
   f32x4 sum = *reinterpret_cast<const f32x4 *>(from);
@@ -789,10 +792,10 @@ LossPlan plan_of(const s1f_rows *d, int64_t vocab, int64_t weight_stride, bool b
   if (backward) {
     p.dx = dx_cut_for(p.n, p.width, (p.piece + kDepth - 1) / kDepth * pairs);
     p.dw = cut_for(p.piece, p.width, (p.n + kDepth - 1) / kDepth * pairs, false);
-    p.dw_parts = p.planes == 3 ? (int)((p.n + kMostSummed - 1) / kMostSummed) : 1;
+    p.dw_parts = p.planes == 3 ? sums_of((int)p.n) : 1;
     if (p.dw_parts > 1) {   // of whole tiles
       const int64_t big = grid_of(p.piece, p.width, 256, 256), middle = grid_of(p.piece, p.width, 128, 128);
-      const double stages = (double)(kMostSummed / kDepth * pairs);
+      const double stages = (double)(kSummed / kDepth * pairs);
       p.dw = tiles_us(kBig, big * p.dw_parts, stages) < tiles_us(kMiddle, middle * p.dw_parts, stages) ? Cut{kBig, big} : Cut{kMiddle, 0};
     }
     const int64_t side = p.dx.tile == kBig ? 256 : 128, dw_side = p.dw.tile == kBig ? 256 : 128;

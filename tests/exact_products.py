@@ -21,7 +21,7 @@ SHAPES = [(1040, 512, 16384), (2304, 8192, 2304), (700, 128, 130), (130, 2000, 9
 # whole rounds of big tiles of dx, with a rest in parts behind them or without one
 WHOLE = [(2049, 8192, 1000), (4096, 4096, 700)]
 # fp32 calls of so many rows that dweight's sums over them are cut into parts: middle and big tiles, the last part short
-LONG = [(24577, 136, 515), (16391, 2048, 4100)]
+LONG = [(24577, 136, 515), (24581, 2048, 4100)]
 # several pieces of the vocabulary, the last one short
 PIECES = {"f32": (700, 264, 180000), "bf16": (1100, 64, 600011)}
 

@@ -60,7 +60,7 @@ def test_gradient_of_fewer_rows(n, h, v, blank, types, kind):
 @pytest.mark.parametrize("blank", [0.0, 0.5, 0.95, 1.0])
 @pytest.mark.parametrize("n,h,v", LONG)
 def test_gradient_of_many_rows(n, h, v, blank, kind):
-    """dweight's sums in parts of 8192 rows that count."""
+    """dweight's sums in parts of about 8192 rows that count."""
     check(kind, n, h, v, "f32", "f32", blank=blank, seed=2)
 
 

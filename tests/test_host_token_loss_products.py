@@ -64,12 +64,12 @@ def test_whole_rounds_of_dx(tmp_path, code):
 
 @pytest.mark.parametrize("shape,tile", zip(LONG, (128, 256)))
 def test_long_sums_are_cut(tmp_path, shape, tile):
-    """dweight of more than 8192 fp32 rows: as many workgroups for a tile as there are parts, and a join; of 8192, and of bf16 rows, as ever."""
+    """dweight of 12288 fp32 rows and more: as many workgroups for a tile as there are parts, and a join; of fewer, and of bf16 rows, one for a tile."""
     n, h, v = shape
     done = [(name, grid) for name, grid in launches(tmp_path, [(*shape, 0, 0)]) if name.startswith("dw")]
     assert len(done) == 2 and f"Li{tile}ELi{tile}" in done[0][0] and done[1][0].startswith("dw_join")
-    assert done[0][1] == -(-v // tile) * -(-h // tile) * -(-n // 8192) and done[1][1] == -(-v * (h // 4) // 256)
-    assert not any(name.startswith("dw_join") for name, _ in launches(tmp_path, [(8192, h, v, 0, 0), (n, h, v, 1, 0), (n, h, v, 1, 1)]))
+    assert done[0][1] == -(-v // tile) * -(-h // tile) * ((n + 4096) // 8192) and done[1][1] == -(-v * (h // 4) // 256)
+    assert not any(name.startswith("dw_join") for name, _ in launches(tmp_path, [(12287, h, v, 0, 0), (n, h, v, 1, 0), (n, h, v, 1, 1)]))
 
 
 @pytest.mark.parametrize("dtype,code", [("f32", 0), ("bf16", 1)])
