@@ -255,6 +255,66 @@ int s1f_kv_grad_emit(const s1f_desc *desc, const float *dk_prefix_acc, const flo
                      int64_t seg_len, void *dk_seg, void *dv_seg, int64_t seg_stride_b, int64_t seg_stride_h,
                      int64_t seg_stride_s, void *hip_stream);
 
+/* What turns a segment's projections into operands of its attention: queries and keys rotated by their positions (arXiv 2104.09864), keys and values put into
+ * the caches, in one launch (in the place of s1f_kv_append); with s1f_qk_norm_rope_* every head of queries and keys is normed first.  And the way back,
+ * from dq and the final rows of the fp32 accumulators of dK/dV (in the place of s1f_kv_grad_emit).
+ *   - q, k, v  [batch, heads, rows, head_dim] as the projections made them (q_stride_*, kv_stride_*; parts of one projection's rows as well), and their
+ *     gradients dq, dk, dv; q_rot and its gradient dq_rot (rot_stride_*); caches k_cache, v_cache and accumulators dk_prefix_acc, dv_prefix_acc
+ *     [batch, n_kv_heads, cache_capacity, head_dim] (cache_stride_*), of which rows [seg_off, seg_off + rows) are written, or read.  head_dim is contiguous.
+ *   - The first rotary_dim elements of a head are rotated, in pairs (i, i + rotary_dim / 2), or (2i, 2i + 1) if interleaved: pair i of the token at position p
+ *     by p * freqs[i] radians, an angle that is computed in 64 bits, and scaled by `magnitude`.  The others stay as they are.  rotary_dim 0: freqs may be NULL.
+ *   - positions int64 [batch, rows], rows contiguous, batch entries positions_stride_b apart, of any order and sign; NULL: row r has first_position + r.
+ *   - v, v_cache (dv, dv_prefix_acc) may both be NULL.
+ *   - q_rot may be q, k_cache + seg_off rows k, v_cache so v, dq dq_rot, where their strides are the same; dq may not be q.
+ * Computed in fp32, rounded once.  Pointers are aligned to their element; calls are faster where rows, and half of rotary_dim unless interleaved, are made of 16 bytes.
+ * Errors as for the attention calls: S1F_EINVAL, S1F_EUNSUPPORTED (dtype; head_dim odd or above 256; batch * rows > 2^26; more than 2^16 heads), S1F_ERANGE (rows < 1,
+ * rows outside [0, cache_capacity)), S1F_EDEVICE. */
+typedef struct {
+  int32_t batch;
+  int32_t n_q_heads;
+  int32_t n_kv_heads;
+  int32_t head_dim;    /* even, <= 256 */
+  int32_t dtype;       /* s1f_dtype; accumulators are always fp32 */
+  int32_t rotary_dim;  /* even, <= head_dim */
+  int32_t interleaved; /* 0 or 1 */
+  int32_t reserved;    /* must be 0 */
+  int64_t rows;        /* per batch entry: the tokens of the segment */
+  int64_t q_stride_b, q_stride_h, q_stride_s; /* elements */
+  int64_t kv_stride_b, kv_stride_h, kv_stride_s;
+  int64_t rot_stride_b, rot_stride_h, rot_stride_s;
+  int64_t cache_stride_b, cache_stride_h, cache_stride_s;
+  int64_t cache_capacity;
+} s1f_heads;
+int s1f_rope_fwd(const s1f_heads *desc, const void *q, const void *k, const void *v, const double *freqs, float magnitude, const int64_t *positions,
+                 int64_t positions_stride_b, int64_t first_position, int64_t seg_off, void *q_rot, void *k_cache, void *v_cache, void *hip_stream);
+int s1f_rope_bwd(const s1f_heads *desc, const void *dq_rot, const float *dk_prefix_acc, const float *dv_prefix_acc, const double *freqs, float magnitude,
+                 const int64_t *positions, int64_t positions_stride_b, int64_t first_position, int64_t seg_off, void *dq, void *dk, void *dv, void *hip_stream);
+
+/* The same behind a norm of every head of q and k: x / sqrt(sum(x^2) / head_dim + eps) * gain, gains [head_dim] in the element type, eps >= 0.  The backward
+ * takes q and k, and adds the gradients of the gains, sums over all rows and heads, to the fp32 accumulators dq_gain_acc, dk_gain_acc [head_dim]; the same arguments give
+ * the same bits.  workspace: device memory, 16-byte aligned, of at least s1f_qk_norm_rope_bwd_workspace_bytes(desc) bytes (0: invalid arguments); contents
+ * undefined afterwards. */
+int s1f_qk_norm_rope_fwd(const s1f_heads *desc, const void *q, const void *k, const void *v, const void *q_gain, const void *k_gain, float eps,
+                         const double *freqs, float magnitude, const int64_t *positions, int64_t positions_stride_b, int64_t first_position, int64_t seg_off,
+                         void *q_rot, void *k_cache, void *v_cache, void *hip_stream);
+int s1f_qk_norm_rope_bwd(const s1f_heads *desc, const void *dq_rot, const float *dk_prefix_acc, const float *dv_prefix_acc, const void *q, const void *k,
+                         const void *q_gain, const void *k_gain, float eps, const double *freqs, float magnitude, const int64_t *positions,
+                         int64_t positions_stride_b, int64_t first_position, int64_t seg_off, void *dq, void *dk, void *dv, float *dq_gain_acc,
+                         float *dk_gain_acc, void *workspace, size_t workspace_bytes, void *hip_stream);
+size_t s1f_qk_norm_rope_bwd_workspace_bytes(const s1f_heads *desc);
+
+/* Frequencies of the rotation, in radians per token, of the rotary_dim / 2 pairs, and the magnitude that goes with them: f_i = base^(-2i / rotary_dim), scaled for
+ * contexts `factor` times as long as the trained one:
+ *   S1F_ROPE_LINEAR  f_i / factor: positions interpolated (arXiv 2306.15595)
+ *   S1F_ROPE_BASE    base * factor^(rotary_dim / (rotary_dim - 2)): the slowest pair as above, the fastest as it is
+ *   S1F_ROPE_PARTS   by the turns that a pair makes over trained_rows tokens: from fast_turns on f_i, up to slow_turns f_i / factor, between them a share of either that is linear
+ *                    in the turns; magnitude 0.1 ln(factor) + 1 (arXiv 2309.00071)
+ * HOST function; freqs [rotary_dim / 2] and magnitude are caller-owned HOST memory; what a scaling does not name is not read.  Errors: S1F_EINVAL for rotary_dim odd or < 2, base <= 0, factor <= 0
+ * (S1F_ROPE_PARTS: < 1), an unknown scaling, S1F_ROPE_BASE with rotary_dim 2, S1F_ROPE_PARTS with trained_rows < 1 or not 0 <= slow_turns < fast_turns, numbers that are not finite, null pointers. */
+typedef enum { S1F_ROPE_PLAIN = 0, S1F_ROPE_LINEAR = 1, S1F_ROPE_BASE = 2, S1F_ROPE_PARTS = 3 } s1f_rope_scaling;
+int s1f_rope_frequencies(int32_t rotary_dim, double base, int32_t scaling, double factor, int64_t trained_rows, double slow_turns, double fast_turns,
+                         double *freqs, float *magnitude);
+
 /* What a pipeline stage computes per segment beside attention, for the rows of hidden states [batch, rows, hidden] of a segment: the
  * first stage makes them out of tokens, every stage normalises them, the last stage turns them into a loss.  Like the attention
  * calls they run forward for the segments of a sequence in order and backward in reverse order, and the gradients of what all

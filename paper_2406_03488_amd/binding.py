@@ -34,6 +34,13 @@ class Rows(ctypes.Structure):
                 ("y_stride_b", ctypes.c_int64), ("y_stride_s", ctypes.c_int64)]
 
 
+class Heads(ctypes.Structure):
+    """Mirror of s1f_heads."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "n_q_heads", "n_kv_heads", "head_dim", "dtype", "rotary_dim", "interleaved", "reserved")] + [
+        (n, ctypes.c_int64) for n in ("rows", "q_stride_b", "q_stride_h", "q_stride_s", "kv_stride_b", "kv_stride_h", "kv_stride_s", "rot_stride_b",
+                                      "rot_stride_h", "rot_stride_s", "cache_stride_b", "cache_stride_h", "cache_stride_s", "cache_capacity")]
+
+
 class Pass(ctypes.Structure):
     _fields_ = [("micro_batch", ctypes.c_int32), ("segment", ctypes.c_int32), ("backward", ctypes.c_int32)]
 
@@ -115,6 +122,17 @@ def load_library():
     for f in (lib.s1f_embed_bwd_workspace_bytes, lib.s1f_layer_norm_bwd_workspace_bytes, lib.s1f_token_loss_fwd_workspace_bytes,
               lib.s1f_token_loss_bwd_workspace_bytes):
         f.restype = sz
+    hp, f64 = ctypes.POINTER(Heads), ctypes.c_double
+    turn = [vp, f32, vp, i64, i64, i64]                     # freqs, magnitude, positions, their stride, first_position, seg_off
+    lib.s1f_rope_frequencies.argtypes = [i32, f64, i32, f64, i64, f64, f64, ctypes.POINTER(f64), ctypes.POINTER(f32)]
+    lib.s1f_rope_fwd.argtypes = [hp, vp, vp, vp, *turn, vp, vp, vp, vp]
+    lib.s1f_rope_bwd.argtypes = [hp, vp, vp, vp, *turn, vp, vp, vp, vp]
+    lib.s1f_qk_norm_rope_fwd.argtypes = [hp, vp, vp, vp, vp, vp, f32, *turn, vp, vp, vp, vp]
+    lib.s1f_qk_norm_rope_bwd.argtypes = [hp, vp, vp, vp, vp, vp, vp, vp, f32, *turn, vp, vp, vp, vp, vp, vp, sz, vp]
+    for f in (lib.s1f_rope_frequencies, lib.s1f_rope_fwd, lib.s1f_rope_bwd, lib.s1f_qk_norm_rope_fwd, lib.s1f_qk_norm_rope_bwd):
+        f.restype = ctypes.c_int
+    lib.s1f_qk_norm_rope_bwd_workspace_bytes.argtypes = [hp]
+    lib.s1f_qk_norm_rope_bwd_workspace_bytes.restype = sz
     lib.s1f_seq1f1b_warmup.argtypes = [i32, i32, i32, i32, ctypes.POINTER(i64)]
     lib.s1f_seq1f1b_warmup.restype = ctypes.c_int
     lib.s1f_seq1f1b_order.argtypes = [i32, i32, i32, i32, ctypes.POINTER(Pass), i64, ctypes.POINTER(i64)]
@@ -300,6 +318,7 @@ class _PythonForms:
     """In place of the compiled forms where they cannot be loaded: every call is left to the Python code."""
     fwd = fwd_ws = bwd = bwd_noalloc = append = emit = staticmethod(lambda *args: -1)
     embed_fwd = embed_bwd = layer_norm_fwd = layer_norm_bwd = token_loss_fwd = token_loss_bwd = fwd
+    rope_fwd = rope_bwd = qk_norm_rope_fwd = qk_norm_rope_bwd = fwd
 
 
 def _load_calls():
@@ -330,8 +349,9 @@ def _native():
             return _calls
         entry = (lib.s1f_seg_attn_fwd, lib.s1f_seg_attn_fwd_ws, lib.s1f_seg_attn_bwd, lib.s1f_seg_attn_bwd_noalloc,
                  lib.s1f_kv_append, lib.s1f_kv_grad_emit, lib.s1f_embed_fwd, lib.s1f_embed_bwd, lib.s1f_layer_norm_fwd,
-                 lib.s1f_layer_norm_bwd, lib.s1f_token_loss_fwd, lib.s1f_token_loss_bwd)
-        _torch_calls.bind(*[ctypes.cast(f, ctypes.c_void_p).value for f in entry], torch.cuda.current_device,
+                 lib.s1f_layer_norm_bwd, lib.s1f_token_loss_fwd, lib.s1f_token_loss_bwd, lib.s1f_rope_fwd, lib.s1f_rope_bwd,
+                 lib.s1f_qk_norm_rope_fwd, lib.s1f_qk_norm_rope_bwd)
+        _torch_calls.bind(tuple(ctypes.cast(f, ctypes.c_void_p).value for f in entry), torch.cuda.current_device,
                           getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
                               lambda device: torch.cuda.current_stream(device).cuda_stream))
         _calls, _calls_of = _torch_calls, lib
@@ -587,6 +607,162 @@ def kv_grad_emit(dk_prefix_acc, dv_prefix_acc, seg_off: int, dk_seg, dv_seg):
                               dk_seg.shape[2], dk_seg.data_ptr(), dv_seg.data_ptr(), s[0], s[1], s[2], _stream_ptr())
     if rc != 0:
         raise S1FError(rc, "s1f_kv_grad_emit")
+
+
+# ---- heads on their way from the projections to the attention, and back --------------------------------------------------------------
+
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_PARTS = range(4)
+
+
+def rope_frequencies(rotary_dim: int, base: float = 10000.0, scaling: int = ROPE_PLAIN, factor: float = 1.0, trained_rows: int = 0,
+                     slow_turns: float = 1.0, fast_turns: float = 32.0):
+    """s1f_rope_frequencies: (list of the rotary_dim / 2 frequencies in radians per token, magnitude).  The rotations take the
+    frequencies as an fp64 tensor on their device."""
+    out, magnitude = (ctypes.c_double * max(int(rotary_dim) // 2, 1))(), ctypes.c_float(0.0)
+    rc = load_library().s1f_rope_frequencies(int(rotary_dim), float(base), int(scaling), float(factor), int(trained_rows), float(slow_turns),
+                                             float(fast_turns), out, ctypes.byref(magnitude))
+    if rc != 0:
+        raise S1FError(rc, "s1f_rope_frequencies")
+    return list(out), float(magnitude.value)
+
+
+def _head_strides(t):
+    """(batch, head, row) strides of a [batch, heads, rows, head_dim] tensor, 0 where it has one of them."""
+    return tuple(t.stride(i) if t.shape[i] > 1 else 0 for i in range(3))
+
+
+def _head_shape(t, shape, dtype, what):
+    if t.dim() != 4 or (t.stride(3) != 1 and t.shape[3] > 1):
+        raise ValueError(f"{what}: expected [batch, heads, rows, head_dim] with contiguous head_dim")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what}: expected {tuple(shape)}, got {tuple(t.shape)}")
+    if t.dtype != dtype:
+        raise TypeError(f"{what}: expected {dtype}, got {t.dtype}")
+
+
+def _heads_desc(q, q_rot, kv, caches, gradients, freqs, interleaved) -> Heads:
+    """Descriptor of a call on q and kv (k and v, or their gradients; v may be None) on one side, q_rot and caches on the other; with
+    `gradients` the caches are fp32 accumulators."""
+    import torch
+    if q.dim() != 4 or kv[0].dim() != 4 or caches[0].dim() != 4:
+        raise ValueError("expected [batch, heads, rows, head_dim] tensors")
+    if (kv[1] is None) != (caches[1] is None):
+        raise ValueError("values need a place to go to, or neither is given")
+    b, hq, n, d = q.shape
+    hk, capacity = kv[0].shape[1], caches[0].shape[2]
+    _head_shape(q, q.shape, q.dtype, "queries")
+    _head_shape(q_rot, q.shape, q.dtype, "queries")
+    for t in kv:
+        if t is not None:
+            _head_shape(t, (b, hk, n, d), q.dtype, "keys and values")
+            if _head_strides(t) != _head_strides(kv[0]):
+                raise ValueError("keys and values must have identical strides")
+    for t in caches:
+        if t is not None:
+            _head_shape(t, (b, hk, capacity, d), torch.float32 if gradients else q.dtype, "accumulators" if gradients else "caches")
+            if _head_strides(t) != _head_strides(caches[0]):
+                raise ValueError("caches must have identical strides")
+    if freqs.dtype != torch.float64:
+        raise TypeError("frequencies are fp64")
+    if freqs.dim() != 1 or not freqs.is_contiguous() or 2 * freqs.shape[0] > d:
+        raise ValueError("frequencies must be a contiguous vector, one for each pair of a head")
+    return Heads(b, hq, hk, d, _dtype_code(q), 2 * freqs.shape[0], 1 if interleaved else 0, 0, n, *_head_strides(q), *_head_strides(kv[0]),
+                 *_head_strides(q_rot), *_head_strides(caches[0]), capacity)
+
+
+def _turn(q, freqs, magnitude, positions, seg_off):
+    """The arguments between a call's inputs and its outputs.  positions: [batch, rows] int64, or the first row's."""
+    import torch
+    if isinstance(positions, torch.Tensor):
+        if positions.dtype != torch.int64:
+            raise TypeError("positions are int64")
+        if positions.shape != (q.shape[0], q.shape[2]) or (positions.shape[1] > 1 and positions.stride(1) != 1):
+            raise ValueError("positions must be [batch, rows] with contiguous rows")
+        at, sb, first = positions.data_ptr(), positions.stride(0) if positions.shape[0] > 1 else 0, 0
+    else:
+        at, sb, first = None, 0, int(positions)
+        if not -2 ** 62 < first < 2 ** 62:
+            raise ValueError("position out of range")
+    return freqs.data_ptr() or None, float(magnitude), at, sb, first, int(seg_off)
+
+
+def _on_device(*tensors):
+    """The tensors among a call's arguments."""
+    import torch
+    _check_device(*[t for t in tensors if isinstance(t, torch.Tensor)])
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def rope_fwd(q, k, v, freqs, magnitude: float, interleaved: bool, positions, seg_off: int, q_rot, k_cache, v_cache):
+    """s1f_rope_fwd on torch device tensors: q rotated into q_rot, k rotated and v as it is into rows [seg_off, seg_off + rows) of the caches.
+
+    q, q_rot [B, Hq, rows, D]; k, v [B, Hkv, rows, D]; k_cache, v_cache [B, Hkv, capacity, D]; v and v_cache may both be None; freqs fp64, one
+    per pair (rope_frequencies); positions [B, rows] int64 on the device, or an integer: the first row's.  Enqueued on torch's current stream.
+    """
+    if _done(_native().rope_fwd(q, k, v, freqs, magnitude, interleaved, positions, seg_off, q_rot, k_cache, v_cache), "s1f_rope_fwd"):
+        return
+    _on_device(q, k, v, freqs, positions, q_rot, k_cache, v_cache)
+    desc = _heads_desc(q, q_rot, (k, v), (k_cache, v_cache), False, freqs, interleaved)
+    _checked(load_library().s1f_rope_fwd(ctypes.byref(desc), q.data_ptr(), k.data_ptr(), _ptr(v), *_turn(q, freqs, magnitude, positions, seg_off),
+                                         q_rot.data_ptr(), k_cache.data_ptr(), _ptr(v_cache), _stream_ptr()), "s1f_rope_fwd")
+
+
+def rope_bwd(dq_rot, dk_prefix_acc, dv_prefix_acc, freqs, magnitude: float, interleaved: bool, positions, seg_off: int, dq, dk, dv):
+    """s1f_rope_bwd on torch device tensors: dq_rot, and rows [seg_off, seg_off + rows) of the fp32 accumulators [B, Hkv, capacity, D], back to
+    dq, dk, dv (shaped like q, k, v; overwritten); dv_prefix_acc and dv may both be None."""
+    if _done(_native().rope_bwd(dq_rot, dk_prefix_acc, dv_prefix_acc, freqs, magnitude, interleaved, positions, seg_off, dq, dk, dv), "s1f_rope_bwd"):
+        return
+    _on_device(dq_rot, dk_prefix_acc, dv_prefix_acc, freqs, positions, dq, dk, dv)
+    desc = _heads_desc(dq, dq_rot, (dk, dv), (dk_prefix_acc, dv_prefix_acc), True, freqs, interleaved)
+    _checked(load_library().s1f_rope_bwd(ctypes.byref(desc), dq_rot.data_ptr(), dk_prefix_acc.data_ptr(), _ptr(dv_prefix_acc),
+                                         *_turn(dq, freqs, magnitude, positions, seg_off), dq.data_ptr(), dk.data_ptr(), _ptr(dv), _stream_ptr()),
+             "s1f_rope_bwd")
+
+
+def qk_norm_rope_fwd(q, k, v, q_gain, k_gain, eps: float, freqs, magnitude: float, interleaved: bool, positions, seg_off: int, q_rot, k_cache, v_cache):
+    """s1f_qk_norm_rope_fwd on torch device tensors: rope_fwd of q and k with every head divided by its root mean square and multiplied by q_gain or
+    k_gain [D], of the tensors' type."""
+    if _done(_native().qk_norm_rope_fwd(q, k, v, q_gain, k_gain, eps, freqs, magnitude, interleaved, positions, seg_off, q_rot, k_cache, v_cache),
+             "s1f_qk_norm_rope_fwd"):
+        return
+    _on_device(q, k, v, q_gain, k_gain, freqs, positions, q_rot, k_cache, v_cache)
+    desc = _heads_desc(q, q_rot, (k, v), (k_cache, v_cache), False, freqs, interleaved)
+    _vectors(q.shape[3], q.dtype, q_gain, k_gain)
+    _checked(load_library().s1f_qk_norm_rope_fwd(ctypes.byref(desc), q.data_ptr(), k.data_ptr(), _ptr(v), q_gain.data_ptr(), k_gain.data_ptr(), float(eps),
+                                                 *_turn(q, freqs, magnitude, positions, seg_off), q_rot.data_ptr(), k_cache.data_ptr(), _ptr(v_cache),
+                                                 _stream_ptr()), "s1f_qk_norm_rope_fwd")
+
+
+def qk_norm_rope_bwd_workspace_bytes(dq_rot, dk_prefix_acc) -> int:
+    b, hq, n, d = dq_rot.shape
+    desc = Heads(b, hq, dk_prefix_acc.shape[1], d, _dtype_code(dq_rot), 0, 0, 0, n, *[1 << 30] * 12, n)
+    return int(load_library().s1f_qk_norm_rope_bwd_workspace_bytes(ctypes.byref(desc)))
+
+
+def qk_norm_rope_bwd(dq_rot, dk_prefix_acc, dv_prefix_acc, q, k, q_gain, k_gain, eps: float, freqs, magnitude: float, interleaved: bool, positions,
+                     seg_off: int, dq, dk, dv, dq_gain_acc, dk_gain_acc, workspace):
+    """s1f_qk_norm_rope_bwd on torch device tensors: rope_bwd behind which the gradients pass the norm.  q, k as the forward took them, with the strides of
+    dq and dk; dq_gain_acc, dk_gain_acc [D] fp32 are added to; workspace is any device tensor of at least qk_norm_rope_bwd_workspace_bytes(...) bytes."""
+    if _done(_native().qk_norm_rope_bwd(dq_rot, dk_prefix_acc, dv_prefix_acc, q, k, q_gain, k_gain, eps, freqs, magnitude, interleaved, positions, seg_off,
+                                        dq, dk, dv, dq_gain_acc, dk_gain_acc, workspace), "s1f_qk_norm_rope_bwd"):
+        return
+    import torch
+    _on_device(dq_rot, dk_prefix_acc, dv_prefix_acc, q, k, q_gain, k_gain, freqs, positions, dq, dk, dv, dq_gain_acc, dk_gain_acc, workspace)
+    desc = _heads_desc(dq, dq_rot, (dk, dv), (dk_prefix_acc, dv_prefix_acc), True, freqs, interleaved)
+    for t, like in ((q, dq), (k, dk)):
+        _head_shape(t, like.shape, like.dtype, "queries and keys")
+        if _head_strides(t) != _head_strides(like):
+            raise ValueError("gradients must have the strides of what they are the gradients of")
+    _vectors(dq.shape[3], dq.dtype, q_gain, k_gain)
+    _vectors(dq.shape[3], torch.float32, dq_gain_acc, dk_gain_acc)
+    _checked(load_library().s1f_qk_norm_rope_bwd(ctypes.byref(desc), dq_rot.data_ptr(), dk_prefix_acc.data_ptr(), _ptr(dv_prefix_acc), q.data_ptr(),
+                                                 k.data_ptr(), q_gain.data_ptr(), k_gain.data_ptr(), float(eps),
+                                                 *_turn(dq, freqs, magnitude, positions, seg_off), dq.data_ptr(), dk.data_ptr(), _ptr(dv),
+                                                 dq_gain_acc.data_ptr(), dk_gain_acc.data_ptr(), *_space(workspace), _stream_ptr()),
+             "s1f_qk_norm_rope_bwd")
 
 
 # ---- rows of hidden states: embedding, layer norm, token loss ---------------------------------------------------------------------

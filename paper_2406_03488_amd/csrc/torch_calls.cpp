@@ -11,6 +11,8 @@
 #include <ATen/core/Tensor.h>
 #include <torch/version.h>
 
+#include <cstring>
+
 #include "s1f.h"
 
 namespace {
@@ -29,6 +31,10 @@ struct Api {
   decltype(&s1f_layer_norm_bwd) layer_norm_bwd;
   decltype(&s1f_token_loss_fwd) token_loss_fwd;
   decltype(&s1f_token_loss_bwd) token_loss_bwd;
+  decltype(&s1f_rope_fwd) rope_fwd;
+  decltype(&s1f_rope_bwd) rope_bwd;
+  decltype(&s1f_qk_norm_rope_fwd) qk_norm_rope_fwd;
+  decltype(&s1f_qk_norm_rope_bwd) qk_norm_rope_bwd;
 };
 Api api = {};
 PyObject *get_device = nullptr, *get_stream = nullptr;
@@ -382,24 +388,196 @@ PyObject *token_loss_bwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
   });
 }
 
-// (addresses of the twelve entry points, torch's functions for the current device and for a device's stream)
+// ---- heads on their way from the projections to the attention, and back ------------------------------------------------------------------
+
+// Arguments by kinds: t a plain tensor of the current device, o one or None, f a float, b a truth value, i an integer, p an integer or a
+// plain tensor; and the device's stream.
+struct MixedArgs {
+  const at::Tensor *t[18];
+  double real[2] = {0.0, 0.0};
+  int64_t whole[2] = {0, 0};
+  bool truth = false;
+  const at::Tensor *positions = nullptr;
+  int64_t first = 0;
+  void *stream = nullptr;
+  static bool integer(PyObject *x, int64_t *to) {
+    int overflow = 0;
+    if (!PyLong_CheckExact(x)) return false;
+    *to = PyLong_AsLongLongAndOverflow(x, &overflow);
+    return overflow == 0;
+  }
+  bool read(PyObject *const *args, Py_ssize_t n, const char *kinds) {
+    if (n != (Py_ssize_t)std::strlen(kinds) || get_device == nullptr || at::impl::PythonTorchFunctionTLS::stack_len() > 0) return false;
+    int64_t device = -1;
+    int tensors = 0, reals = 0, wholes = 0;
+    for (Py_ssize_t i = 0; i < n; ++i) {
+      const at::Tensor *x = nullptr;
+      switch (kinds[i]) {
+        case 'f':
+          if (!PyFloat_CheckExact(args[i])) return false;
+          real[reals++] = PyFloat_AS_DOUBLE(args[i]);
+          continue;
+        case 'b':
+          if (!PyBool_Check(args[i])) return false;
+          truth = args[i] == Py_True;
+          continue;
+        case 'i':
+          if (!integer(args[i], &whole[wholes++])) return false;
+          continue;
+        case 'p':
+          if (integer(args[i], &first)) {
+            if (first <= -(int64_t(1) << 62) || first >= int64_t(1) << 62) return false;
+            continue;
+          }
+          x = positions = plain(args[i]);
+          break;
+        default:
+          x = t[tensors++] = kinds[i] == 'o' && args[i] == Py_None ? nullptr : plain(args[i]);
+          if (x == nullptr && kinds[i] == 'o' && args[i] == Py_None) continue;
+      }
+      if (x == nullptr || (device >= 0 && x->get_device() != device)) return false;
+      device = x->get_device();
+    }
+    PyObject *dev = PyObject_CallNoArgs(get_device);
+    const long current = dev ? PyLong_AsLong(dev) : -1;
+    PyObject *st = dev ? PyObject_CallOneArg(get_stream, dev) : nullptr;
+    Py_XDECREF(dev);
+    if (st == nullptr || current != device) {
+      Py_XDECREF(st);
+      return PyErr_Clear(), false;
+    }
+    stream = PyLong_AsVoidPtr(st);
+    Py_DECREF(st);
+    return PyErr_Occurred() == nullptr || (PyErr_Clear(), false);
+  }
+};
+
+bool heads_ok(const at::Tensor &t, int64_t b, int64_t h, int64_t n, int64_t d, at::ScalarType type) {
+  return t.dim() == 4 && t.size(0) == b && t.size(1) == h && t.size(2) == n && t.size(3) == d && (t.stride(3) == 1 || d <= 1) && t.scalar_type() == type;
+}
+bool same_strides(const at::Tensor &a, const at::Tensor &b) {   // (of tensors of one shape)
+  return stride_of(a, 0) == stride_of(b, 0) && stride_of(a, 1) == stride_of(b, 1) && stride_of(a, 2) == stride_of(b, 2);
+}
+// q, k, v on one side, q_rot and the caches (of the type `cached`) on the other; v and v_cache: both or neither
+bool heads_desc_of(const MixedArgs &x, const at::Tensor &q, const at::Tensor &q_rot, const at::Tensor &k, const at::Tensor *v, const at::Tensor &k_cache,
+                   const at::Tensor *v_cache, bool gradients, const at::Tensor &freqs, s1f_heads *d) {
+  *d = {};
+  if (q.dim() != 4 || k.dim() != 4 || k_cache.dim() != 4 || (v == nullptr) != (v_cache == nullptr) || !dtype_of(q, &d->dtype)) return false;
+  const int64_t b = q.size(0), hq = q.size(1), n = q.size(2), dim = q.size(3), hk = k.size(1), capacity = k_cache.size(2);
+  const at::ScalarType type = q.scalar_type(), cached = gradients ? at::kFloat : type;
+  if (!fits(b) || !fits(hq) || !fits(hk) || !fits(dim) || !heads_ok(q, b, hq, n, dim, type) || !heads_ok(q_rot, b, hq, n, dim, type)) return false;
+  if (!heads_ok(k, b, hk, n, dim, type) || !heads_ok(k_cache, b, hk, capacity, dim, cached)) return false;
+  if (v && (!heads_ok(*v, b, hk, n, dim, type) || !same_strides(*v, k) || !heads_ok(*v_cache, b, hk, capacity, dim, cached) || !same_strides(*v_cache, k_cache)))
+    return false;
+  if (freqs.scalar_type() != at::kDouble || freqs.dim() != 1 || !freqs.is_contiguous() || 2 * freqs.size(0) > dim) return false;
+  if (x.positions && (x.positions->scalar_type() != at::kLong || x.positions->dim() != 2 || x.positions->size(0) != b || x.positions->size(1) != n ||
+                      (n > 1 && x.positions->stride(1) != 1)))
+    return false;
+  d->batch = (int32_t)b; d->n_q_heads = (int32_t)hq; d->n_kv_heads = (int32_t)hk; d->head_dim = (int32_t)dim;
+  d->rotary_dim = (int32_t)(2 * freqs.size(0)); d->interleaved = x.truth; d->rows = n;
+  d->q_stride_b = stride_of(q, 0); d->q_stride_h = stride_of(q, 1); d->q_stride_s = stride_of(q, 2);
+  d->kv_stride_b = stride_of(k, 0); d->kv_stride_h = stride_of(k, 1); d->kv_stride_s = stride_of(k, 2);
+  d->rot_stride_b = stride_of(q_rot, 0); d->rot_stride_h = stride_of(q_rot, 1); d->rot_stride_s = stride_of(q_rot, 2);
+  d->cache_stride_b = stride_of(k_cache, 0); d->cache_stride_h = stride_of(k_cache, 1); d->cache_stride_s = stride_of(k_cache, 2);
+  d->cache_capacity = capacity;
+  return true;
+}
+void *ptr_or_null(const at::Tensor *t) { return t ? ptr(t) : nullptr; }
+// What follows a call's inputs.
+struct Turn {
+  const double *freqs;
+  const int64_t *at = nullptr;
+  int64_t sb = 0;
+  Turn(const MixedArgs &x, const at::Tensor *f) : freqs(static_cast<const double *>(f->data_ptr())) {
+    if (x.positions) {
+      at = tokens_of(x.positions);
+      sb = stride_of(*x.positions, 0);
+    }
+  }
+};
+
+// (q, k, v or None[, q_gain, k_gain, eps], freqs, magnitude, interleaved, positions, seg_off, q_rot, k_cache, v_cache or None)
+PyObject *rope_fwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  return call([&]() -> int {
+    MixedArgs x;
+    s1f_heads d;
+    if (!x.read(args, n, "ttotfbpitto")) return kPython;
+    auto &[q, k, v, freqs, q_rot, kc, vc] = reinterpret_cast<const at::Tensor *(&)[7]>(x.t);
+    if (!heads_desc_of(x, *q, *q_rot, *k, v, *kc, vc, false, *freqs, &d)) return kPython;
+    const Turn turn(x, freqs);
+    void *const p[] = {ptr(q), ptr(k), ptr_or_null(v), ptr(q_rot), ptr(kc), ptr_or_null(vc)};
+    Unlocked u;
+    return api.rope_fwd(&d, p[0], p[1], p[2], turn.freqs, (float)x.real[0], turn.at, turn.sb, x.first, x.whole[0], p[3], p[4], p[5], x.stream);
+  });
+}
+PyObject *qk_norm_rope_fwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  return call([&]() -> int {
+    MixedArgs x;
+    s1f_heads d;
+    if (!x.read(args, n, "ttottftfbpitto")) return kPython;
+    auto &[q, k, v, q_gain, k_gain, freqs, q_rot, kc, vc] = reinterpret_cast<const at::Tensor *(&)[9]>(x.t);
+    if (!heads_desc_of(x, *q, *q_rot, *k, v, *kc, vc, false, *freqs, &d) || !vector_ok(*q_gain, d.head_dim, q->scalar_type()) ||
+        !vector_ok(*k_gain, d.head_dim, q->scalar_type()))
+      return kPython;
+    const Turn turn(x, freqs);
+    void *const p[] = {ptr(q), ptr(k), ptr_or_null(v), ptr(q_gain), ptr(k_gain), ptr(q_rot), ptr(kc), ptr_or_null(vc)};
+    Unlocked u;
+    return api.qk_norm_rope_fwd(&d, p[0], p[1], p[2], p[3], p[4], (float)x.real[0], turn.freqs, (float)x.real[1], turn.at, turn.sb, x.first, x.whole[0], p[5],
+                                p[6], p[7], x.stream);
+  });
+}
+// (dq_rot, dk_acc, dv_acc or None, freqs, magnitude, interleaved, positions, seg_off, dq, dk, dv or None)
+PyObject *rope_bwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  return call([&]() -> int {
+    MixedArgs x;
+    s1f_heads d;
+    if (!x.read(args, n, "ttotfbpitto")) return kPython;
+    auto &[dq_rot, dka, dva, freqs, dq, dk, dv] = reinterpret_cast<const at::Tensor *(&)[7]>(x.t);
+    if (!heads_desc_of(x, *dq, *dq_rot, *dk, dv, *dka, dva, true, *freqs, &d)) return kPython;
+    const Turn turn(x, freqs);
+    void *const p[] = {ptr(dq_rot), ptr(dka), ptr_or_null(dva), ptr(dq), ptr(dk), ptr_or_null(dv)};
+    Unlocked u;
+    return api.rope_bwd(&d, p[0], static_cast<const float *>(p[1]), static_cast<const float *>(p[2]), turn.freqs, (float)x.real[0], turn.at, turn.sb, x.first,
+                        x.whole[0], p[3], p[4], p[5], x.stream);
+  });
+}
+// (dq_rot, dk_acc, dv_acc or None, q, k, q_gain, k_gain, eps, freqs, magnitude, interleaved, positions, seg_off, dq, dk, dv or None, dq_gain_acc,
+// dk_gain_acc, workspace)
+PyObject *qk_norm_rope_bwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  return call([&]() -> int {
+    MixedArgs x;
+    s1f_heads d;
+    if (!x.read(args, n, "ttottttftfbpittotto")) return kPython;
+    auto &[dq_rot, dka, dva, q, k, q_gain, k_gain, freqs, dq, dk, dv, dqg, dkg, ws] = reinterpret_cast<const at::Tensor *(&)[14]>(x.t);
+    if (!heads_desc_of(x, *dq, *dq_rot, *dk, dv, *dka, dva, true, *freqs, &d)) return kPython;
+    if (!heads_ok(*q, d.batch, d.n_q_heads, d.rows, d.head_dim, dq->scalar_type()) || !same_strides(*q, *dq) ||
+        !heads_ok(*k, d.batch, d.n_kv_heads, d.rows, d.head_dim, dq->scalar_type()) || !same_strides(*k, *dk) ||
+        !vector_ok(*q_gain, d.head_dim, dq->scalar_type()) || !vector_ok(*k_gain, d.head_dim, dq->scalar_type()) ||
+        !vector_ok(*dqg, d.head_dim, at::kFloat) || !vector_ok(*dkg, d.head_dim, at::kFloat) || !space_ok(ws))
+      return kPython;
+    const Turn turn(x, freqs);
+    void *const p[] = {ptr(dq_rot), ptr(dka), ptr_or_null(dva), ptr(q), ptr(k), ptr(q_gain), ptr(k_gain), ptr(dq), ptr(dk), ptr_or_null(dv), ptr(dqg), ptr(dkg),
+                       ptr_or_null(ws)};
+    Unlocked u;
+    return api.qk_norm_rope_bwd(&d, p[0], static_cast<const float *>(p[1]), static_cast<const float *>(p[2]), p[3], p[4], p[5], p[6], (float)x.real[0],
+                                turn.freqs, (float)x.real[1], turn.at, turn.sb, x.first, x.whole[0], p[7], p[8], p[9], static_cast<float *>(p[10]),
+                                static_cast<float *>(p[11]), p[12], bytes(ws), x.stream);
+  });
+}
+
+// (addresses of the entry points in the order of Api, torch's functions for the current device and for a device's stream)
 PyObject *bind(PyObject *, PyObject *args) {
-  unsigned long long a[12];
-  PyObject *dev, *st;
-  if (!PyArg_ParseTuple(args, "KKKKKKKKKKKKOO", &a[0], &a[1], &a[2], &a[3], &a[4], &a[5], &a[6], &a[7], &a[8], &a[9], &a[10], &a[11], &dev, &st))
-    return nullptr;
-  api = Api{reinterpret_cast<decltype(api.fwd)>(a[0]),
-            reinterpret_cast<decltype(api.fwd_ws)>(a[1]),
-            reinterpret_cast<decltype(api.bwd)>(a[2]),
-            reinterpret_cast<decltype(api.bwd_noalloc)>(a[3]),
-            reinterpret_cast<decltype(api.append)>(a[4]),
-            reinterpret_cast<decltype(api.emit)>(a[5]),
-            reinterpret_cast<decltype(api.embed_fwd)>(a[6]),
-            reinterpret_cast<decltype(api.embed_bwd)>(a[7]),
-            reinterpret_cast<decltype(api.layer_norm_fwd)>(a[8]),
-            reinterpret_cast<decltype(api.layer_norm_bwd)>(a[9]),
-            reinterpret_cast<decltype(api.token_loss_fwd)>(a[10]),
-            reinterpret_cast<decltype(api.token_loss_bwd)>(a[11])};
+  PyObject *addresses, *dev, *st;
+  if (!PyArg_ParseTuple(args, "O!OO", &PyTuple_Type, &addresses, &dev, &st)) return nullptr;
+  constexpr Py_ssize_t kEntries = sizeof(Api) / sizeof(void *);
+  if (PyTuple_GET_SIZE(addresses) != kEntries) return PyErr_Format(PyExc_ValueError, "expected %zd entry points", kEntries);
+  void *at[kEntries];
+  for (Py_ssize_t i = 0; i < kEntries; ++i) {
+    at[i] = PyLong_AsVoidPtr(PyTuple_GET_ITEM(addresses, i));
+    if (PyErr_Occurred()) return nullptr;
+  }
+  static_assert(sizeof(at) == sizeof(Api), "an Api is its entry points");
+  std::memcpy(&api, at, sizeof(Api));
   Py_INCREF(dev);
   Py_INCREF(st);
   Py_XDECREF(get_device);
@@ -423,6 +601,10 @@ PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, nullptr},
                          {"layer_norm_bwd", S1F_METHOD(layer_norm_bwd), METH_FASTCALL, nullptr},
                          {"token_loss_fwd", S1F_METHOD(token_loss_fwd), METH_FASTCALL, nullptr},
                          {"token_loss_bwd", S1F_METHOD(token_loss_bwd), METH_FASTCALL, nullptr},
+                         {"rope_fwd", S1F_METHOD(rope_fwd), METH_FASTCALL, nullptr},
+                         {"rope_bwd", S1F_METHOD(rope_bwd), METH_FASTCALL, nullptr},
+                         {"qk_norm_rope_fwd", S1F_METHOD(qk_norm_rope_fwd), METH_FASTCALL, nullptr},
+                         {"qk_norm_rope_bwd", S1F_METHOD(qk_norm_rope_bwd), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_torch_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
