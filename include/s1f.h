@@ -384,6 +384,31 @@ int s1f_token_loss_bwd(const s1f_rows *desc, const float *dloss, const void *x, 
 size_t s1f_token_loss_fwd_workspace_bytes(const s1f_rows *desc, int64_t vocab, int64_t weight_stride);
 size_t s1f_token_loss_bwd_workspace_bytes(const s1f_rows *desc, int64_t vocab, int64_t weight_stride);
 
+/* Gated feed-forward block of every row: [gate | up] = x W_in^T, h = act(gate) * up, y = h W_out^T, with w_in [2 * inner, hidden] (gate's rows first) and
+ * w_out [hidden, inner], rows w_in_stride and w_out_stride elements apart.  x has x_stride_*, y y_stride_*.
+ *   act      S1F_SILU g / (1 + exp(-g)), S1F_GELU g * (1 + erf(g / sqrt 2)) / 2, S1F_GELU_TANH g * (1 + tanh(sqrt(2 / pi) * (g + 0.044715 g^3))) / 2
+ *   gate_up  [batch, rows, 2 * inner], dense, of the element type: [gate | up] of every row, rounded once, for the backward; NULL: not kept
+ * The backward takes gate_up and dy (y_stride_*): dh = dy W_out, dgate = dh * up * act'(gate), dup = dh * act(gate);
+ *   dx = [dgate | dup] W_in (x_stride_*, overwritten),  dw_in: [dgate | dup]^T x,  dw_out: dy^T h, with h as gate_up gives it
+ *   dweight_dtype S1F_F32   both added to fp32 accumulators
+ *   dweight_dtype S1F_BF16  (bf16 rows only) both overwritten, rounded once: the gradients of this call alone
+ * bf16: h, dgate and dup are rounded to bf16 before their products, like the probabilities and score gradients of the attention; sums are fp32.  fp32: products to fp32
+ * precision (operands as three exact bf16 parts each, but for elements below 2^-110, which keep 8 bits at least, and for dgate and dup below 2^-126), of finite numbers below 2^112; whatever an
+ * infinity or a NaN takes part in may be NaN.
+ * A row's y, gate_up and dx depend on that row alone.
+ * Weights and d; calls are faster where hidden and inner are multiples of 8 and all rows start on 16 bytes: other bf16 operands, and all fp32 ones,
+ * are laid out anew in the workspace first.  inner <= 2^17, strides of weights < 2^22, 2 * inner * w_in_stride and hidden * w_out_stride < 2^30, batch * rows * hidden and
+ * batch * rows * 2 * inner <= 2^33.  workspace: device memory, 16-byte aligned, of at least s1f_gated_ffn_*_workspace_bytes(...) bytes (0: invalid
+ * arguments); contents undefined afterwards. */
+typedef enum { S1F_SILU = 0, S1F_GELU = 1, S1F_GELU_TANH = 2 } s1f_activation;
+int s1f_gated_ffn_fwd(const s1f_rows *desc, const void *x, const void *w_in, int64_t w_in_stride, const void *w_out, int64_t w_out_stride, int64_t inner,
+                      int32_t act, void *y, void *gate_up, void *workspace, size_t workspace_bytes, void *hip_stream);
+int s1f_gated_ffn_bwd(const s1f_rows *desc, const void *dy, const void *x, const void *w_in, int64_t w_in_stride, const void *w_out, int64_t w_out_stride,
+                      int64_t inner, int32_t act, const void *gate_up, void *dx, void *dw_in, int64_t dw_in_stride, void *dw_out, int64_t dw_out_stride,
+                      int32_t dweight_dtype, void *workspace, size_t workspace_bytes, void *hip_stream);
+size_t s1f_gated_ffn_fwd_workspace_bytes(const s1f_rows *desc, int64_t inner, int64_t w_in_stride, int64_t w_out_stride);
+size_t s1f_gated_ffn_bwd_workspace_bytes(const s1f_rows *desc, int64_t inner, int64_t w_in_stride, int64_t w_out_stride);
+
 /* Order of passes of one pipeline device under the sequence-level 1F1B schedule (Section 3.2).  HOST
  * functions, no device work.
  *

@@ -40,20 +40,26 @@ def head_norm_grad(dy, x, gain, eps):
     return rstd * (g - xhat * (g * xhat).mean(-1, keepdims=True)), (dy * xhat).sum((0, 1, 2))
 
 
-_erf = np.vectorize(math.erf, otypes=[np.float64])
+_erfc = np.vectorize(math.erfc, otypes=[np.float64])
+
+
+def _sigmoid(x):
+    e = np.exp(-np.abs(x))
+    return np.where(x < 0, e, 1) / (1 + e)
 
 
 def activation(g, act):
-    """act(g) and its derivative; act: "silu", "gelu" or "gelu_tanh" """
+    """act(g) and its derivative; act: "silu", "gelu" or "gelu_tanh".  1 + erf(x) is erfc(-x), and (1 + tanh(x)) / 2 the sigmoid of 2x: with the
+    former, gates far below 0 would lose all digits of 64 bits, too."""
     if act == "silu":
-        s = 1 / (1 + np.exp(-g))
+        s = _sigmoid(g)
         return g * s, s + g * s * (1 - s)
     if act == "gelu":
-        p = (1 + _erf(g / math.sqrt(2))) / 2
+        p = _erfc(-g / math.sqrt(2)) / 2
         return g * p, p + g * np.exp(-g * g / 2) / math.sqrt(2 * math.pi)
-    k = math.sqrt(2 / math.pi)
-    t = np.tanh(k * (g + 0.044715 * g ** 3))
-    return g * (1 + t) / 2, (1 + t) / 2 + g / 2 * (1 - t * t) * k * (1 + 3 * 0.044715 * g * g)
+    k = 2 * math.sqrt(2 / math.pi)
+    s = _sigmoid(k * (g + 0.044715 * g ** 3))
+    return g * s, s + g * s * (1 - s) * k * (1 + 3 * 0.044715 * g * g)
 
 
 def gated_ffn(x, w_in, w_out, act):

@@ -133,6 +133,11 @@ def load_library():
         f.restype = ctypes.c_int
     lib.s1f_qk_norm_rope_bwd_workspace_bytes.argtypes = [hp]
     lib.s1f_qk_norm_rope_bwd_workspace_bytes.restype = sz
+    lib.s1f_gated_ffn_fwd.argtypes = [rp, vp, vp, i64, vp, i64, i64, i32, vp, vp, vp, sz, vp]
+    lib.s1f_gated_ffn_bwd.argtypes = [rp, vp, vp, vp, i64, vp, i64, i64, i32, vp, vp, vp, i64, vp, i64, i32, vp, sz, vp]
+    lib.s1f_gated_ffn_fwd.restype = lib.s1f_gated_ffn_bwd.restype = ctypes.c_int
+    for f in (lib.s1f_gated_ffn_fwd_workspace_bytes, lib.s1f_gated_ffn_bwd_workspace_bytes):
+        f.argtypes, f.restype = [rp, i64, i64, i64], sz
     lib.s1f_seq1f1b_warmup.argtypes = [i32, i32, i32, i32, ctypes.POINTER(i64)]
     lib.s1f_seq1f1b_warmup.restype = ctypes.c_int
     lib.s1f_seq1f1b_order.argtypes = [i32, i32, i32, i32, ctypes.POINTER(Pass), i64, ctypes.POINTER(i64)]
@@ -318,7 +323,7 @@ class _PythonForms:
     """In place of the compiled forms where they cannot be loaded: every call is left to the Python code."""
     fwd = fwd_ws = bwd = bwd_noalloc = append = emit = staticmethod(lambda *args: -1)
     embed_fwd = embed_bwd = layer_norm_fwd = layer_norm_bwd = token_loss_fwd = token_loss_bwd = fwd
-    rope_fwd = rope_bwd = qk_norm_rope_fwd = qk_norm_rope_bwd = fwd
+    rope_fwd = rope_bwd = qk_norm_rope_fwd = qk_norm_rope_bwd = gated_ffn_fwd = gated_ffn_bwd = fwd
 
 
 def _load_calls():
@@ -350,7 +355,7 @@ def _native():
         entry = (lib.s1f_seg_attn_fwd, lib.s1f_seg_attn_fwd_ws, lib.s1f_seg_attn_bwd, lib.s1f_seg_attn_bwd_noalloc,
                  lib.s1f_kv_append, lib.s1f_kv_grad_emit, lib.s1f_embed_fwd, lib.s1f_embed_bwd, lib.s1f_layer_norm_fwd,
                  lib.s1f_layer_norm_bwd, lib.s1f_token_loss_fwd, lib.s1f_token_loss_bwd, lib.s1f_rope_fwd, lib.s1f_rope_bwd,
-                 lib.s1f_qk_norm_rope_fwd, lib.s1f_qk_norm_rope_bwd)
+                 lib.s1f_qk_norm_rope_fwd, lib.s1f_qk_norm_rope_bwd, lib.s1f_gated_ffn_fwd, lib.s1f_gated_ffn_bwd)
         _torch_calls.bind(tuple(ctypes.cast(f, ctypes.c_void_p).value for f in entry), torch.cuda.current_device,
                           getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
                               lambda device: torch.cuda.current_stream(device).cuda_stream))
@@ -977,3 +982,73 @@ def token_loss_bwd(dloss, x, weight, targets, lse, dx, dweight, workspace):
     _checked(load_library().s1f_token_loss_bwd(ctypes.byref(desc), dloss.data_ptr(), x.data_ptr(), weight.data_ptr(), stride,
                                                weight.shape[0], at, targets_sb, lse.data_ptr(), dx.data_ptr(), dweight.data_ptr(), into,
                                                code, *_space(workspace), _stream_ptr()), "s1f_token_loss_bwd")
+
+
+SILU, GELU, GELU_TANH = range(3)
+
+
+def _ffn_weights(x, w_in, w_out, what=("w_in", "w_out"), dtype=None):
+    """(inner, row strides of w_in [2 * inner, hidden] and w_out [hidden, inner])"""
+    hidden, dtype = x.shape[2], dtype or x.dtype
+    in_stride = _matrix(w_in, hidden, dtype, what[0])
+    if w_in.shape[0] % 2 != 0:
+        raise ValueError(f"{what[0]} must be [2 * inner, hidden]")
+    inner = w_in.shape[0] // 2
+    if w_out.dim() != 2 or w_out.shape[0] != hidden:
+        raise ValueError(f"{what[1]} must be [hidden, inner]")
+    return inner, in_stride, _matrix(w_out, inner, dtype, what[1])
+
+
+def _check_gate_up(gate_up, x, inner):
+    if gate_up.dtype != x.dtype:
+        raise TypeError("gate_up must share the element type")
+    if not gate_up.is_contiguous() or gate_up.shape != (*x.shape[:2], 2 * inner):
+        raise ValueError("gate_up must be a contiguous [batch, rows, 2 * inner] tensor")
+
+
+def gated_ffn_fwd_workspace_bytes(x, w_in, w_out) -> int:
+    return int(load_library().s1f_gated_ffn_fwd_workspace_bytes(ctypes.byref(_rows_desc(x, x)), *_ffn_weights(x, w_in, w_out)))
+
+
+def gated_ffn_fwd(x, w_in, w_out, act: int, y, gate_up, workspace):
+    """s1f_gated_ffn_fwd on torch device tensors: y = (act(g) * u) w_out^T with [g | u] = x w_in^T.
+
+    x, y [B, rows, hidden]; w_in [2 * inner, hidden], g's rows first; w_out [hidden, inner]; act SILU, GELU or GELU_TANH; gate_up [B, rows, 2 * inner]
+    is overwritten with [g | u] for the backward, None: not kept; workspace is any device tensor of at least gated_ffn_fwd_workspace_bytes(...)
+    bytes.  Enqueued on torch's current stream.
+    """
+    if _done(_native().gated_ffn_fwd(x, w_in, w_out, act, y, gate_up, workspace), "s1f_gated_ffn_fwd"):
+        return
+    _on_device(x, w_in, w_out, y, gate_up, workspace)
+    desc = _rows_desc(x, y)
+    inner, in_stride, out_stride = _ffn_weights(x, w_in, w_out)
+    if gate_up is not None:
+        _check_gate_up(gate_up, x, inner)
+    _checked(load_library().s1f_gated_ffn_fwd(ctypes.byref(desc), x.data_ptr(), w_in.data_ptr(), in_stride, w_out.data_ptr(), out_stride, inner, int(act),
+                                              y.data_ptr(), _ptr(gate_up), *_space(workspace), _stream_ptr()), "s1f_gated_ffn_fwd")
+
+
+def gated_ffn_bwd_workspace_bytes(dy, x, w_in, w_out) -> int:
+    return int(load_library().s1f_gated_ffn_bwd_workspace_bytes(ctypes.byref(_rows_desc(x, dy)), *_ffn_weights(x, w_in, w_out)))
+
+
+def gated_ffn_bwd(dy, x, w_in, w_out, act: int, gate_up, dx, dw_in, dw_out, workspace):
+    """s1f_gated_ffn_bwd on torch device tensors, from the gate_up that the forward has kept.
+
+    dx, with the shape and strides of x, is overwritten; dw_in and dw_out, of one type, are added to if they are fp32 and overwritten if they are bf16 (bf16 rows only);
+    workspace is any device tensor of at least gated_ffn_bwd_workspace_bytes(...) bytes.
+    """
+    if _done(_native().gated_ffn_bwd(dy, x, w_in, w_out, act, gate_up, dx, dw_in, dw_out, workspace), "s1f_gated_ffn_bwd"):
+        return
+    _on_device(dy, x, w_in, w_out, gate_up, dx, dw_in, dw_out, workspace)
+    desc = _rows_desc(x, dy)
+    _same_rows(x, dx)
+    inner, in_stride, out_stride = _ffn_weights(x, w_in, w_out)
+    code = _dtype_code(dw_in)
+    into, dw_in_stride, dw_out_stride = _ffn_weights(x, dw_in, dw_out, ("dw_in", "dw_out"), dw_in.dtype)
+    if into != inner:
+        raise ValueError("dw_in and dw_out must have the shapes of w_in and w_out")
+    _check_gate_up(gate_up, x, inner)
+    _checked(load_library().s1f_gated_ffn_bwd(ctypes.byref(desc), dy.data_ptr(), x.data_ptr(), w_in.data_ptr(), in_stride, w_out.data_ptr(), out_stride, inner,
+                                              int(act), gate_up.data_ptr(), dx.data_ptr(), dw_in.data_ptr(), dw_in_stride, dw_out.data_ptr(),
+                                              dw_out_stride, code, *_space(workspace), _stream_ptr()), "s1f_gated_ffn_bwd")

@@ -1,4 +1,4 @@
-// Matrix products of the token loss (gfx950): C[m][n] = sum over k of A(m, k) * B(n, k), both operands bf16, sums fp32.
+// Matrix products of the token loss and of the gated feed-forward block (gfx950): C[m][n] = sum over k of A(m, k) * B(n, k), both operands bf16, sums fp32.
 //
 // A workgroup owns a BM x BN tile of C and walks k in stages of 64, which travel from memory to LDS by asynchronous copies and from
 // there into the registers of the matrix instructions.  An operand is stored either way around:
@@ -61,8 +61,10 @@ template <int R, bool TR, int NW> struct Side {
     const int c = lane % CHUNKS;
     chunk = TR ? ((((c >> 1) ^ h(row)) << 1) | (c & 1)) : (c ^ ((row >> 1) & 7));
   }
-  // m0: first row (column) of the tile; limit: rows (columns) that there are; those behind are copies of the last (columns: first)
-  S1F_DEV void init(const bf16_t *data, int64_t ld, int64_t m0, int64_t limit, int k_stage, int wave, int lane) {
+  // m0: first row (column) of the tile; limit: rows (columns) that there are; those behind are copies of the last (columns: first).
+  // apart: 0, or (rows) the tile's blocks of 16 are taken in turn from the rows from m0 on, R / 2 of them, and from those `apart` rows behind them: what belongs together
+  // of two products then lies in one wave's registers.
+  S1F_DEV void init(const bf16_t *data, int64_t ld, int64_t m0, int64_t limit, int64_t apart, int k_stage, int wave, int lane) {
     row_bytes = (int)(ld * 2);
     step = TR ? kDepth * ld * 2 : kDepth * 2;
     next = reinterpret_cast<const char *>(TR ? data + m0 : data + m0 * ld) + k_stage * step - BIAS;
@@ -73,7 +75,10 @@ template <int R, bool TR, int NW> struct Side {
       if (TR) {
         if (m0 + 8 * c >= limit) c = 0;
       } else {
+        const int second = apart ? (r >> 4) & 1 : 0;
+        if (apart) r = (r >> 5 << 4) + (r & 15);
         if (m0 + r >= limit) r = (int)(limit - 1 - m0);
+        r += second ? (int)apart : 0;
       }
       // (the immediate offset of a copy instruction counts for its address in memory as well as in LDS)
       voff[i] = (unsigned)(r * row_bytes + 16 * c) + (unsigned)(BIAS - 1024 * i);
@@ -154,8 +159,9 @@ template <int BM, int BN, int WM, int WN, bool TRA, bool TRB, int PAIRS> struct 
   static constexpr int LDS_BYTES = 3 * SA::BYTES + 2 * SB::BYTES;
 
   // k: contraction; stages [begin, end) of it, counted in stages of a product of planes, the PAIRS of each one after the other
+  // b_apart: see Side::init
   S1F_DEV static void run(f32x4 (&acc)[MB][NB], const Matrix &a, const Matrix &b, int64_t m0, int64_t m_limit, int64_t n0, int64_t n_limit,
-                          int64_t k, int begin, int end, lds_addr lds) {
+                          int64_t k, int begin, int end, lds_addr lds, int64_t b_apart = 0) {
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
 #pragma unroll
     for (int i = 0; i < MB; ++i)
@@ -164,8 +170,8 @@ template <int BM, int BN, int WM, int WN, bool TRA, bool TRB, int PAIRS> struct 
     if (begin >= end) return;
     SA sa;
     SB sb;
-    sa.init(a.data, a.ld, m0, m_limit, begin / PAIRS, wave, lane);
-    sb.init(b.data, b.ld, n0, n_limit, begin / PAIRS, wave, lane);
+    sa.init(a.data, a.ld, m0, m_limit, 0, begin / PAIRS, wave, lane);
+    sb.init(b.data, b.ld, n0, n_limit, b_apart, begin / PAIRS, wave, lane);
     const int left = (int)((k - 1) % kDepth) + 1;   // contraction of the last stage
     const int tail = left < kDepth ? (int)((k - 1) / kDepth) * PAIRS : 0x7fffffff;   // first stage that is not whole
     // Where a side's stage t is copied from, and to.  Calls are for consecutive stages.
@@ -274,22 +280,23 @@ template <int BM, int BN, int WM, int WN, bool TRA, bool TRB, int PAIRS> struct 
     __syncthreads();
   }
 
-  // The same for operands of three planes and tiles small enough that LDS holds all planes of two stages: each is copied once for the six products, and read
+  // The same (stages of all planes) for operands of three planes and tiles small enough that LDS holds all planes of two stages: each is copied once for the six products, and read
   // once into registers.  A call of few tiles is a chain of stages, of which there are then a sixth: scores of 256 rows of 256 elements over 5003 tokens 15.1 -> 11.2 us,
   // loss of 64 rows of 4096 over 30000, which reads 740 MB of planes, 865 -> 570.  Eight waves of 32 x 32, two to a SIMD, so that one's reads pass under the other's
   // products: 1.35 us per stage, four of 64 x 32 1.5.
   static constexpr int PLANES_LDS_BYTES = 2 * 3 * (SA::BYTES + SB::BYTES);
   S1F_DEV static void run_planes(f32x4 (&acc)[MB][NB], const Matrix &a, const Matrix &b, int64_t m0, int64_t m_limit, int64_t n0, int64_t n_limit,
-                                 int64_t k, lds_addr lds) {
+                                 int64_t k, int begin, int end, lds_addr lds, int64_t b_apart = 0) {
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
 #pragma unroll
     for (int i = 0; i < MB; ++i)
 #pragma unroll
       for (int j = 0; j < NB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (begin >= end) return;
     SA sa;
     SB sb;
-    sa.init(a.data, a.ld, m0, m_limit, 0, wave, lane);
-    sb.init(b.data, b.ld, n0, n_limit, 0, wave, lane);
+    sa.init(a.data, a.ld, m0, m_limit, 0, begin, wave, lane);
+    sb.init(b.data, b.ld, n0, n_limit, b_apart, begin, wave, lane);
     const int stages = (int)((k + kDepth - 1) / kDepth), left = (int)((k - 1) % kDepth) + 1;
     constexpr int COPIES = 3 * (SA::PER_WAVE + SB::PER_WAVE);
     auto copy_side = [&](auto &side, const Matrix &m, lds_addr at, int bytes) {
@@ -310,12 +317,12 @@ template <int BM, int BN, int WM, int WN, bool TRA, bool TRB, int PAIRS> struct 
       copy_side(sb, b, place + 3 * SA::BYTES, SB::BYTES);
     };
     const lds_addr places[2] = {lds, lds + 3 * (SA::BYTES + SB::BYTES)};
-    copy_stage(0, places[0]);
-    if (stages > 1) copy_stage(1, places[1]);
+    copy_stage(begin, places[0]);
+    if (begin + 1 < end) copy_stage(begin + 1, places[1]);
     const lds_addr lane_a = SA::at(wm * MB, lane), lane_b = SB::at(wn * NB, lane);
-    for (int t = 0; t < stages; ++t) {
-      const lds_addr at_a = places[t & 1], at_b = at_a + 3 * SA::BYTES;
-      if (t + 1 < stages) wait_async_tiles_but_last<COPIES>();
+    for (int t = begin; t < end; ++t) {
+      const lds_addr at_a = places[(t - begin) & 1], at_b = at_a + 3 * SA::BYTES;
+      if (t + 1 < end) wait_async_tiles_but_last<COPIES>();
       else wait_async_tiles();
       if (t + 1 == stages && left < kDepth) {
 #pragma unroll
@@ -345,7 +352,7 @@ template <int BM, int BN, int WM, int WN, bool TRA, bool TRB, int PAIRS> struct 
         });
       }
       __syncthreads();
-      if (t + 2 < stages) copy_stage(t + 2, at_a);
+      if (t + 2 < end) copy_stage(t + 2, at_a);
     }
   }
 };

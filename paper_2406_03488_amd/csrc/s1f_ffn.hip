@@ -1,0 +1,642 @@
+// The gated feed-forward block of a layer on the rows of a segment, and its gradient.  n rows of `hidden` elements, `inner` between the projections.
+//
+//   forward    [g | u] = x W_in^T,  h = act(g) * u,  y = h W_out^T
+//   backward   dh = dy W_out,  dg = dh * u * act'(g),  du = dh * act(g);  dx = [dg | du] W_in,  dW_in += [dg | du]^T x,  dW_out += dy^T h
+//
+// Bound by the matrix units: 6 n hidden inner operations and 12.  Nothing of it is a pass over memory of its own: a tile of x W_in^T holds the same columns of
+// both halves, in the same lanes, so that h is what its results leave in memory (and g and u, rounded, if the caller keeps them); dh stays in registers, and the tile
+// that computes it reads g and u and leaves dg, du and h.  h, dg and du are bf16 in memory, rounded once, as the attention kernels round their probabilities and score
+// gradients; fp32 calls: three bf16 planes that hold them whole, and fp32 operands are split into such planes first.
+#include <cmath>
+
+#include "product_launch.hpp"
+
+namespace s1f {
+namespace {
+
+// One operand laid out anew: rows of `hidden` elements as rows of `width` bf16 ones, zeros behind the end; fp32 ones as three planes.
+struct PackJob {
+  const void *from;
+  RowsOf rows;
+  int64_t n, plane;
+  bf16_t *to;
+  int32_t hidden, width, wide, up;   // up: times kUp
+  int64_t first_block;
+};
+constexpr int kMostJobs = 4;
+
+struct FfnArgs {
+  Matrix a, b;                    // operands of the launch
+  int32_t m, n, k;                // rows and columns of its product, and its contraction
+  int32_t m_limit, n_limit;       // what there is of either operand (columns: whole pieces of 8)
+  int32_t inner, act;
+  // where results go: h and [dg | du], planes of [.][ld]; rows of the call's tensors
+  bf16_t *h, *dz;
+  int64_t h_ld, h_plane, dz_ld, dz_plane;
+  void *gate_up;                  // [.][2 * inner]
+  int32_t wide_gate_up;
+  void *out;
+  RowsOf out_rows;
+  int32_t wide_out;
+  float scale;                    // of the results (see kUp)
+  // tiles (see Cuts)
+  int32_t tiles_m, tiles_n, tile0, quarters, whole, rest, splits;
+  float *part;                    // [part][tile][row][column]
+  PackJob jobs[kMostJobs];
+  int32_t n_jobs;
+};
+
+// ---- operands --------------------------------------------------------------------------------------------------------------------------
+
+// Bound by memory.  All of a call's operands in one launch.
+template <typename T> __global__ void __launch_bounds__(256) ffn_pack_kernel(const FfnArgs a) {
+  int j = 0;
+  while (j + 1 < a.n_jobs && (int64_t)blockIdx.x >= a.jobs[j + 1].first_block) ++j;
+  const PackJob &p = a.jobs[j];
+  const int64_t id = ((int64_t)blockIdx.x - p.first_block) * 256 + threadIdx.x;
+  const int per_row = p.width / 8;
+  const int64_t row = id / per_row;
+  const int c = (int)(id - row * per_row);
+  if (row >= p.n) return;
+  const T *from = reinterpret_cast<const T *>(p.from) + p.rows.offset((int)row);
+  bf16_t *to = p.to + row * p.width + 8 * c;
+  if (sizeof(T) == 4 && p.up) {
+    f32x4 v[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) v[i] = Piece<float, false>::get(reinterpret_cast<const float *>(from) + 8 * c + 4 * i, p.hidden - 8 * c - 4 * i) * kUp;
+    const Planes q = split3(v[0], v[1]);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) *reinterpret_cast<bf16x8 *>(to + i * p.plane) = q.p[i];
+  } else if (p.wide) {
+    pack_eight<T, true>(from, p.hidden, c, to, p.plane);
+  } else {
+    pack_eight<T, false>(from, p.hidden, c, to, p.plane);
+  }
+}
+
+// ---- activations -----------------------------------------------------------------------------------------------------------------------
+
+// 1 / (1 + exp(-x)).  bf16 calls: the unit's exponential and reciprocal, 2^-22 off or so.
+template <typename T> S1F_DEV float sigmoid(float x) {
+  if constexpr (sizeof(T) == 4) return 1.f / (1.f + expf(-x));
+  else return __builtin_amdgcn_rcpf(1.f + exp2_fast(x * -kLog2e));
+}
+// act(g), and act'(g).  The tanh form is g * sigmoid(2 sqrt(2 / pi) (g + 0.044715 g^3)), which keeps its digits where 1 + tanh would lose them, and erfc does
+// where 1 + erf would.
+template <typename T> S1F_DEV float activation(float g, int act) {
+  if (act == S1F_SILU) return g * sigmoid<T>(g);
+  if (act == S1F_GELU) return 0.5f * g * erfcf(g * -0.70710678f);
+  return g * sigmoid<T>(1.5957691216f * g * (1.f + 0.044715f * g * g));
+}
+template <typename T> S1F_DEV void activation(float g, int act, float &a, float &slope) {
+  if (act == S1F_GELU) {
+    const float p = 0.5f * erfcf(g * -0.70710678f);
+    a = g * p;
+    slope = p + g * 0.39894228f * expf(-0.5f * g * g);
+    return;
+  }
+  const bool silu = act == S1F_SILU;
+  const float s = sigmoid<T>(silu ? g : 1.5957691216f * g * (1.f + 0.044715f * g * g)), rest = s * (1.f - s);
+  a = g * s;
+  // (far out, where the sigmoid does not change any more, g^2 may be infinite)
+  const float inside = silu ? 1.f : 1.5957691216f * (1.f + 0.134145f * g * g);
+  slope = rest == 0.f ? s : s + g * rest * inside;
+}
+
+// ---- products --------------------------------------------------------------------------------------------------------------------------
+
+// Workgroup -> tile, or quarter of a tile; and which part of its contraction.
+S1F_DEV void ffn_tile(const FfnArgs &a, int &tm, int &tn, int &tile, int &part, int &parts) {
+  part = 0;
+  parts = 1;
+  if (a.quarters) {
+    tile = a.tile0 + (blockIdx.x >> 2);
+    decode_tile(a.tiles_m, a.tiles_n, tile, tm, tn);
+    tm = 2 * tm + ((blockIdx.x >> 1) & 1);
+    tn = 2 * tn + (blockIdx.x & 1);
+    return;
+  }
+  tile = blockIdx.x;
+  if (tile >= a.whole) {
+    part = (tile - a.whole) / a.rest;
+    tile -= part * a.rest;
+    parts = a.splits;
+  }
+  decode_tile(a.tiles_m, a.tiles_n, tile, tm, tn);
+}
+
+// (one workgroup to a unit where LDS holds all planes of two stages)
+template <int PAIRS, int BM> constexpr bool kAllPlanes = PAIRS == 6 && BM == 64;
+template <typename P, int PAIRS, int BM>
+S1F_DEV void ffn_product(f32x4 (&acc)[P::MB][P::NB], const FfnArgs &a, int m0, int n0, int part, int parts, lds_addr lds, int64_t b_apart = 0) {
+  const int64_t stages = (a.k + kDepth - 1) / kDepth * (kAllPlanes<PAIRS, BM> ? 1 : PAIRS);
+  const int begin = (int)(stages * part / parts), end = (int)(stages * (part + 1) / parts);
+  if constexpr (kAllPlanes<PAIRS, BM>) P::run_planes(acc, a.a, a.b, m0, a.m_limit, n0, a.n_limit, a.k, begin, end, lds, b_apart);
+  else P::run(acc, a.a, a.b, m0, a.m_limit, n0, a.n_limit, a.k, begin, end, lds, b_apart);
+}
+
+// Four values of a row of a bf16 matrix, or of its three planes; the first `there` of them if `some`.
+template <int PAIRS> S1F_DEV void put4(bf16_t *to, int64_t plane, f32x4 v, bool some, int there) {
+  if constexpr (PAIRS == 6) {
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    const Planes q = split3(v, f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      if (!some) {
+        const u32x4 w = __builtin_bit_cast(u32x4, q.p[i]);
+        *reinterpret_cast<u32x2 *>(to + i * plane) = u32x2{w[0], w[1]};
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (e < there) to[i * plane + e] = q.p[i][e];
+      }
+    }
+  } else {
+    if (!some) {
+      store4<bf16_t>(to, v[0], v[1], v[2], v[3]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (e < there) to[e] = (bf16_t)v[e];
+    }
+  }
+}
+template <typename T> S1F_DEV void put_values(T *to, f32x4 v, bool wide, int there) {
+  if (wide && there >= 4) {
+    store4<T>(to, v[0], v[1], v[2], v[3]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < there) to[e] = (T)v[e];
+  }
+}
+template <typename T> S1F_DEV f32x4 get_values(const T *from, bool wide, int there) {
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  if (wide && there >= 4) {
+    typedef T Four __attribute__((ext_vector_type(4)));
+    const Four x = *reinterpret_cast<const Four *>(from);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = (float)x[e];
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < there) v[e] = (float)from[e];
+  }
+  return v;
+}
+
+// h = act(g) * u of a tile of BM rows and BN / 2 columns.
+template <typename T, int BM, int BN, int WM, int WN> __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_up_kernel(const FfnArgs a) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  constexpr int PAIRS = sizeof(T) == 4 ? 6 : 1;
+  typedef Product<BM, BN, WM, WN, false, false, PAIRS> P;
+  int tm, tn, tile, part, parts;
+  ffn_tile(a, tm, tn, tile, part, parts);
+  const int m0 = tm * BM, n0 = tn * (BN / 2);
+  if (m0 >= a.m || n0 >= a.n) return;
+  f32x4 acc[P::MB][P::NB];
+  ffn_product<P, PAIRS, BM>(acc, a, m0, n0, 0, 1, to_lds_addr(smem), a.inner);
+  const int lane = lane_id(), n = lane & 15, j = lane >> 4, wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
+#pragma unroll
+  for (int mb = 0; mb < P::MB; ++mb) {
+    const int row = m0 + 16 * (wm * P::MB + mb) + n;
+    if (row >= a.m) continue;
+#pragma unroll
+    for (int p = 0; p < P::NB / 2; ++p) {
+      const int col = n0 + 16 * (wn * P::NB / 2 + p) + 4 * j, there = a.n - col;
+      if (col >= a.h_ld) continue;
+      const f32x4 g = acc[mb][2 * p], u = acc[mb][2 * p + 1];
+      if (a.gate_up) {
+        T *to = reinterpret_cast<T *>(a.gate_up) + (int64_t)row * 2 * a.inner + col;
+        put_values<T>(to, g, a.wide_gate_up, there);
+        put_values<T>(to + a.inner, u, a.wide_gate_up, there);
+      }
+      f32x4 h;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) h[e] = e < there ? activation<T>(g[e], a.act) * u[e] : 0.f;
+      put4<PAIRS>(a.h + (int64_t)row * a.h_ld + col, a.h_plane, h, false, 4);
+    }
+  }
+}
+
+// dh = dy W_out of a tile, and of it [dg | du] and h.
+template <typename T, int BM, int BN, int WM, int WN> __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_dh_kernel(const FfnArgs a) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  constexpr int PAIRS = sizeof(T) == 4 ? 6 : 1;
+  typedef Product<BM, BN, WM, WN, false, true, PAIRS> P;
+  int tm, tn, tile, part, parts;
+  ffn_tile(a, tm, tn, tile, part, parts);
+  const int m0 = tm * BM, n0 = tn * BN;
+  if (m0 >= a.m || n0 >= a.n) return;
+  f32x4 acc[P::MB][P::NB];
+  ffn_product<P, PAIRS, BM>(acc, a, m0, n0, 0, 1, to_lds_addr(smem));
+  const int lane = lane_id(), n = lane & 15, j = lane >> 4, wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
+  const bool some = a.inner % 4 != 0;   // (then du does not start where four elements do)
+#pragma unroll
+  for (int mb = 0; mb < P::MB; ++mb) {
+    const int row = m0 + 16 * (wm * P::MB + mb) + n;
+    if (row >= a.m) continue;
+#pragma unroll
+    for (int nb = 0; nb < P::NB; ++nb) {
+      const int col = n0 + 16 * (wn * P::NB + nb) + 4 * j, there = a.inner - col;
+      if (col >= a.h_ld) continue;
+      const T *from = reinterpret_cast<const T *>(a.gate_up) + (int64_t)row * 2 * a.inner + col;
+      const f32x4 g = get_values<T>(from, a.wide_gate_up, there), u = get_values<T>(from + a.inner, a.wide_gate_up, there);
+      f32x4 dg, du, h;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float act, slope;
+        activation<T>(g[e], a.act, act, slope);
+        const bool is = e < there;
+        h[e] = is ? act * u[e] : 0.f;
+        dg[e] = is ? acc[mb][nb][e] * u[e] * slope : 0.f;
+        du[e] = is ? acc[mb][nb][e] * act : 0.f;
+      }
+      put4<PAIRS>(a.h + (int64_t)row * a.h_ld + col, a.h_plane, h, false, 4);
+      if (there <= 0) continue;
+      bf16_t *to = a.dz + (int64_t)row * a.dz_ld + col;
+      put4<PAIRS>(to, a.dz_plane, dg, some, there);
+      put4<PAIRS>(to + a.inner, a.dz_plane, du, some, there);
+      if (there <= 4)   // zeros behind the end of du, where the products read whole pieces of 8
+        for (int c = 2 * a.inner; c < a.dz_ld; ++c)
+#pragma unroll
+          for (int i = 0; i < (PAIRS == 6 ? 3 : 1); ++i) a.dz[(int64_t)row * a.dz_ld + c + i * a.dz_plane] = (bf16_t)0.f;
+    }
+  }
+}
+
+enum Result { kStoreBf16, kStoreF32, kAddF32 };
+template <Result R> S1F_DEV void put_result(const FfnArgs &a, int row, int col, f32x4 v) {
+  const int64_t at = a.out_rows.offset(row) + col;
+  const int there = a.n - col;
+  if constexpr (R == kStoreBf16) {
+    put_values<bf16_t>(reinterpret_cast<bf16_t *>(a.out) + at, v, a.wide_out, there);
+  } else {
+    float *to = reinterpret_cast<float *>(a.out) + at;
+    if constexpr (R == kAddF32) v += get_values<float>(to, a.wide_out, there);
+    put_values<float>(to, v, a.wide_out, there);
+  }
+}
+
+// y, dx, dW_in and dW_out.  The tiles from `whole` on are cut along the contraction: their parts are added up by the join.
+template <int PAIRS, int BM, int BN, int WM, int WN, bool TRA, bool TRB, Result R> __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_product_kernel(const FfnArgs a) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  typedef Product<BM, BN, WM, WN, TRA, TRB, PAIRS> P;
+  int tm, tn, tile, part, parts;
+  ffn_tile(a, tm, tn, tile, part, parts);
+  const int m0 = tm * BM, n0 = tn * BN;
+  if (m0 >= a.m || n0 >= a.n) return;
+  f32x4 acc[P::MB][P::NB];
+  ffn_product<P, PAIRS, BM>(acc, a, m0, n0, part, parts, to_lds_addr(smem));
+  const int lane = lane_id(), n = lane & 15, j = lane >> 4, wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
+  float *to = a.part + ((int64_t)part * a.rest + tile - a.whole) * (BM * BN);
+#pragma unroll
+  for (int mb = 0; mb < P::MB; ++mb) {
+    const int row = 16 * (wm * P::MB + mb) + n;
+    if (m0 + row >= a.m) continue;
+#pragma unroll
+    for (int nb = 0; nb < P::NB; ++nb) {
+      const int col = 16 * (wn * P::NB + nb) + 4 * j;
+      if (n0 + col >= a.n) continue;
+      const f32x4 v = acc[mb][nb] * a.scale;
+      if (parts > 1) *reinterpret_cast<f32x4 *>(to + row * BN + col) = v;
+      else put_result<R>(a, m0 + row, n0 + col, v);
+    }
+  }
+}
+
+// The parts of cut tiles of BM x BN added up in their order.  Bound by memory.
+template <int BM, int BN, Result R> __global__ void __launch_bounds__(256) ffn_join_kernel(const FfnArgs a) {
+  constexpr int PER = BM * BN / 1024;   // workgroups to a tile
+  const int in = blockIdx.x / PER, at = (blockIdx.x % PER) * 1024 + threadIdx.x * 4, row = at / BN, col = at % BN;
+  int tm, tn;
+  decode_tile(a.tiles_m, a.tiles_n, a.whole + in, tm, tn);
+  if (tm * BM + row >= a.m || tn * BN + col >= a.n) return;
+  const float *from = a.part + (int64_t)in * (BM * BN) + at;
+  f32x4 v = *reinterpret_cast<const f32x4 *>(from);
+#pragma unroll 4
+  for (int p = 1; p < a.splits; ++p) v += *reinterpret_cast<const f32x4 *>(from + (int64_t)p * a.rest * (BM * BN));
+  put_result<R>(a, tm * BM + row, tn * BN + col, v);
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------------------------------
+
+constexpr int64_t kMostInner = int64_t(1) << 17, kMostStride = int64_t(1) << 22, kMostApart = int64_t(1) << 29, kMostElements = int64_t(1) << 33;
+constexpr int64_t kMostFfnRows = int64_t(1) << 20;
+
+// How the tiles of a product are taken: big ones up to `whole` and the rest in quarters (Cut); or those from `whole` on in parts along the contraction.
+struct Cuts {
+  Tile tile;
+  int64_t whole, rest;
+  int splits;
+  bool quarters;
+};
+constexpr int tile_m(Tile t) { return t == kBig ? 256 : t == kMiddle ? 128 : 64; }
+constexpr int tile_n(Tile t) { return t == kBig ? 256 : 128; }
+Cuts cuts_for(int64_t m, int64_t n, int64_t stages, bool low, bool split) {
+  Cuts best = {};
+  double best_us = 1e30;
+  auto offer = [&](const Cuts &c, double us) {
+    if (us < 0.98 * best_us) {
+      best_us = us;
+      best = c;
+    }
+  };
+  const Cut c = cut_for(m, n, stages, low);
+  const int64_t all = grid_of(m, n, tile_m(c.tile), tile_n(c.tile));
+  const bool quarters = c.tile == kBig && c.whole < all;
+  const int64_t at_once = c.tile == kBig ? c.whole : all;
+  offer(Cuts{c.tile, at_once, all - at_once, 1, quarters},
+        tiles_us(c.tile, at_once, (double)stages) + (quarters ? 3.0 + tiles_us(kMiddle, 4 * (all - at_once), (double)stages) : 0.0));
+  if (!split) return best;
+  for (Tile tile : {kBig, kMiddle, kLow}) {
+    if (tile == kLow && !low) continue;
+    const int64_t tiles = grid_of(m, n, tile_m(tile), tile_n(tile)), whole = tile == kBig ? tiles / kUnits * kUnits : 0, rest = tiles - whole;
+    if (rest == 0) continue;
+    for (int splits = 2; splits <= 32 && stages / splits >= 4 && rest * splits <= 4 * kUnits; ++splits)
+      offer(Cuts{tile, whole, rest, splits, false}, (whole ? tiles_us(tile, whole, (double)stages) : 0.0) + tiles_us(tile, rest * splits, (double)stages / splits) +
+                                                        3.0 + (double)splits * rest * tile_m(tile) * tile_n(tile) * 8 / 4e6);
+  }
+  return best;
+}
+int64_t part_bytes(const Cuts &c) { return c.splits > 1 ? 4 * c.splits * c.rest * tile_m(c.tile) * tile_n(c.tile) : 0; }
+
+struct FfnPlan {
+  int64_t n, planes, width, inner_width, dz_ld, turns, per_turn;   // dW's rows are taken per_turn at a time
+  bool direct_in, direct_out;     // weights as they are
+  Cuts up, down, dh, dx, dw_in, dw_out;
+  int64_t x, dy, w_in, w_out, h, dz, part, bytes;   // offsets
+};
+
+int check_ffn(const s1f_rows *d, int64_t inner, int64_t in_stride, int64_t out_stride) {
+  const int rc = check_rows(d, true, true);
+  if (rc != S1F_OK) return rc;
+  if (inner < 1 || in_stride < d->hidden || (d->hidden > 1 && out_stride < inner)) return S1F_EINVAL;
+  const int64_t n = d->batch * d->rows;
+  if (inner > kMostInner || in_stride >= kMostStride || out_stride >= kMostStride || inner * in_stride > kMostApart || n > kMostFfnRows || n * d->hidden > kMostElements ||
+      n * 2 * inner > kMostElements)
+    return S1F_EUNSUPPORTED;
+  return S1F_OK;
+}
+
+// Rows that one fp32 sum of a weight's gradient runs over, up to half as many again, six products for each: longer sums would be off by more than fp32 products are (the token
+// loss's, of 64 elements over 300 tokens: 8192 rows 1.0e-6 of the norm, 16384 1.4e-6, 131072 5.0e-6).  More rows take turns: each turn adds to the accumulators.
+constexpr int64_t kSummed = 8192;
+int64_t turns_of(int64_t n, int64_t planes) { return planes == 1 || n < kSummed + kSummed / 2 ? 1 : (n + kSummed / 2) / kSummed; }
+
+FfnPlan plan_of(const s1f_rows *d, int64_t inner, int64_t in_stride, int64_t out_stride, bool backward) {
+  FfnPlan p = {};
+  const int64_t h = d->hidden;
+  p.n = d->batch * d->rows;
+  p.planes = d->dtype == S1F_F32 ? 3 : 1;
+  p.width = up_to(h, 8);
+  p.inner_width = up_to(inner, 8);
+  p.dz_ld = up_to(2 * inner, 8);
+  p.direct_in = d->dtype == S1F_BF16 && h % 8 == 0 && in_stride % 8 == 0;
+  p.direct_out = d->dtype == S1F_BF16 && inner % 8 == 0 && out_stride % 8 == 0;
+  int64_t at = 0;
+  auto take = [&at](int64_t bytes) { const int64_t was = at; at += up_to(bytes, 256); return was; };
+  p.x = take(p.planes * 2 * p.n * p.width);
+  if (!p.direct_in) p.w_in = take(p.planes * 2 * 2 * inner * p.width);
+  if (!p.direct_out) p.w_out = take(p.planes * 2 * h * p.inner_width);
+  p.h = take(p.planes * 2 * p.n * p.inner_width);
+  const int64_t pairs = p.planes == 3 ? 6 : 1;
+  auto stages = [&](int64_t k) { return (k + kDepth - 1) / kDepth * pairs; };
+  int64_t part = 0;
+  if (!backward) {
+    // (tiles of [g | u]: as many columns of either)
+    p.up = cuts_for(p.n, 2 * up_to(inner, 16), stages(h), true, false);
+    p.down = cuts_for(p.n, h, stages(inner), true, true);
+    part = part_bytes(p.down);
+  } else {
+    p.turns = turns_of(p.n, p.planes);
+    p.per_turn = up_to((p.n + p.turns - 1) / p.turns, kDepth);
+    p.dy = take(p.planes * 2 * p.n * p.width);
+    p.dz = take(p.planes * 2 * p.n * p.dz_ld);
+    p.dh = cuts_for(p.n, inner, stages(h), true, false);
+    p.dx = cuts_for(p.n, h, stages(2 * inner), true, true);
+    p.dw_in = cuts_for(2 * inner, h, stages(p.per_turn), false, true);
+    p.dw_out = cuts_for(h, inner, stages(p.per_turn), false, true);
+    for (const Cuts &c : {p.dx, p.dw_in, p.dw_out}) part = std::max(part, part_bytes(c));
+  }
+  p.part = take(part);
+  p.bytes = at;
+  return p;
+}
+
+// Launches a product of `m` x `n` as `cuts` says.  KERNELS<tile>: the kernel, its LDS and threads, and the join of its parts.
+template <template <Tile> class KERNELS> int launch_product(const Cuts &cuts, FfnArgs a, int64_t columns, hipStream_t st) {
+  auto go = [&](auto kernels, int64_t grid) {
+    typedef decltype(kernels) K;
+    return launch_tiles<K::kernel>(K::LDS_BYTES, K::P::THREADS, grid, a, st);
+  };
+  auto tiles = [&](Tile t) {
+    a.tiles_m = (int32_t)((a.m + tile_m(t) - 1) / tile_m(t));
+    a.tiles_n = (int32_t)((columns + tile_n(t) - 1) / tile_n(t));
+    a.whole = (int32_t)cuts.whole;
+    a.rest = (int32_t)std::max<int64_t>(cuts.rest, 1);
+    a.splits = cuts.splits;
+  };
+  const int64_t grid = cuts.whole + (cuts.quarters ? 0 : cuts.rest * cuts.splits);
+  tiles(cuts.tile);
+  int e = S1F_OK;
+  if (cuts.tile == kBig) {
+    if (grid > 0) e = go(KERNELS<kBig>{}, grid);
+    if (e != S1F_OK) return e;
+    if (cuts.quarters) {
+      a.tile0 = (int32_t)cuts.whole;
+      a.quarters = 1;
+      return go(KERNELS<kMiddle>{}, 4 * cuts.rest);
+    }
+  } else {
+    e = cuts.tile == kMiddle ? go(KERNELS<kMiddle>{}, grid) : go(KERNELS<kLow>{}, grid);
+  }
+  if (e != S1F_OK || cuts.splits == 1) return e;
+  const int64_t joins = cuts.rest * (tile_m(cuts.tile) * tile_n(cuts.tile) / 1024);
+  return launch_rows_kernel(cuts.tile == kBig ? KERNELS<kBig>::join : cuts.tile == kMiddle ? KERNELS<kMiddle>::join : KERNELS<kLow>::join, joins, 256, a, st);
+}
+template <typename T, Tile TILE, bool TRA, bool TRB> struct FfnShape : TileShape<TILE> {
+  typedef TileShape<TILE> S;
+  static constexpr bool ALL = kAllPlanes<sizeof(T) == 4 ? 6 : 1, S::BM>;
+  static constexpr int WM = ALL ? 2 : S::WM;   // (one workgroup to a unit)
+  typedef Product<S::BM, S::BN, WM, S::WN, TRA, TRB, 1> P;
+  static constexpr int LDS_BYTES = ALL ? P::PLANES_LDS_BYTES : P::LDS_BYTES;
+  static constexpr void (*join)(FfnArgs) = nullptr;
+};
+template <typename T> struct Up {
+  template <Tile TILE> struct Of : FfnShape<T, TILE, false, false> {
+    typedef FfnShape<T, TILE, false, false> S;
+    static constexpr auto kernel = &ffn_up_kernel<T, S::BM, S::BN, S::WM, S::WN>;
+  };
+};
+template <typename T> struct Dh {
+  template <Tile TILE> struct Of : FfnShape<T, TILE, false, true> {
+    typedef FfnShape<T, TILE, false, true> S;
+    static constexpr auto kernel = &ffn_dh_kernel<T, S::BM, S::BN, S::WM, S::WN>;
+  };
+};
+template <typename T, bool TRA, bool TRB, Result R> struct Of3 {
+  template <Tile TILE> struct Of : FfnShape<T, TRA && TILE == kLow ? kMiddle : TILE, TRA, TRB> {
+    typedef FfnShape<T, TRA && TILE == kLow ? kMiddle : TILE, TRA, TRB> S;
+    static constexpr auto kernel = &ffn_product_kernel<sizeof(T) == 4 ? 6 : 1, S::BM, S::BN, S::WM, S::WN, TRA, TRB, R>;
+    static constexpr void (*join)(FfnArgs) = &ffn_join_kernel<S::BM, S::BN, R>;
+  };
+};
+
+// An operand of the call: as it is, or laid out anew by the launch that is collected in `a`.
+struct Operands {
+  FfnArgs &a;
+  const s1f_rows *d;
+  int64_t planes, blocks = 0;
+  Matrix add(const void *from, RowsOf rows, int64_t n, int64_t hidden, int64_t width, bool as_it_is, int64_t ld, bool wide, bool up, char *room) {
+    if (as_it_is) return Matrix{reinterpret_cast<const bf16_t *>(from), ld, 0};
+    PackJob &j = a.jobs[a.n_jobs++];
+    j = PackJob{from, rows, n, n * width, reinterpret_cast<bf16_t *>(room), (int32_t)hidden, (int32_t)width, wide, up, blocks};
+    blocks += (n * (width / 8) + 255) / 256;
+    return Matrix{j.to, width, j.plane};
+  }
+  // x or dy
+  Matrix rows(const void *from, int64_t sb, int64_t ss, bool up, int64_t width, char *room) {
+    const int64_t n = d->batch * d->rows;
+    const int64_t ld = d->rows > 1 ? ss : sb;   // (one row to a batch entry: its rows are the batch's)
+    const bool even = d->batch == 1 || d->rows == 1 || sb == d->rows * ss, wide = on16(from) && d->hidden % 8 == 0 && wide_rows(d, sb, ss);
+    const bool as_it_is = d->dtype == S1F_BF16 && wide && even && ld < kMostStride;
+    return add(from, RowsOf{sb, ss, Divisor::of(d->rows)}, n, d->hidden, width, as_it_is, n == 1 ? d->hidden : ld, wide, up, room);
+  }
+  Matrix weight(const void *from, int64_t n, int64_t hidden, int64_t stride, int64_t width, bool direct, char *room) {
+    const bool wide = hidden % 8 == 0 && stride % elements_of_16_bytes(d->dtype) == 0;
+    return add(from, RowsOf{0, stride, Divisor::of(n)}, n, hidden, width, direct, stride, wide, false, room);
+  }
+  int pack(hipStream_t st) {
+    if (a.n_jobs == 0) return S1F_OK;
+    return launch_rows_kernel(d->dtype == S1F_F32 ? &ffn_pack_kernel<float> : &ffn_pack_kernel<bf16_t>, blocks, 256, a, st);
+  }
+};
+
+void set_product(FfnArgs &a, const Matrix &ma, const Matrix &mb, int64_t m, int64_t m_limit, int64_t n, int64_t n_limit, int64_t k) {
+  a.a = ma; a.b = mb;
+  a.m = (int32_t)m; a.m_limit = (int32_t)m_limit; a.n = (int32_t)n; a.n_limit = (int32_t)n_limit; a.k = (int32_t)k;
+}
+void set_out(FfnArgs &a, void *out, RowsOf rows, bool wide, float scale) {
+  a.out = out; a.out_rows = rows; a.wide_out = wide; a.scale = scale;
+}
+bool wide_side(const s1f_rows *d, const void *p, int64_t sb, int64_t ss) { return on16(p) && wide_rows(d, sb, ss); }
+
+FfnArgs args_of(const FfnPlan &p, int64_t inner, int32_t act, const void *gate_up, char *ws) {
+  FfnArgs a = {};
+  a.inner = (int32_t)inner; a.act = act;
+  a.h = reinterpret_cast<bf16_t *>(ws + p.h);
+  a.h_ld = p.inner_width; a.h_plane = p.n * p.inner_width;
+  a.dz = reinterpret_cast<bf16_t *>(ws + p.dz);
+  a.dz_ld = p.dz_ld; a.dz_plane = p.n * p.dz_ld;
+  a.gate_up = const_cast<void *>(gate_up);
+  a.wide_gate_up = inner % 4 == 0 && on16(gate_up);
+  a.part = reinterpret_cast<float *>(ws + p.part);
+  return a;
+}
+
+template <typename T>
+int forward(const s1f_rows *d, const FfnPlan &p, const void *x, const void *w_in, int64_t in_stride, const void *w_out, int64_t out_stride, int64_t inner, int32_t act,
+            void *y, void *gate_up, char *ws, hipStream_t st) {
+  constexpr Result R = sizeof(T) == 4 ? kStoreF32 : kStoreBf16;
+  FfnArgs a = args_of(p, inner, act, gate_up, ws);
+  Operands ops{a, d, p.planes};
+  const Matrix mx = ops.rows(x, d->x_stride_b, d->x_stride_s, false, p.width, ws + p.x);
+  const Matrix mi = ops.weight(w_in, 2 * inner, d->hidden, in_stride, p.width, p.direct_in, ws + p.w_in);
+  const Matrix mo = ops.weight(w_out, d->hidden, inner, out_stride, p.inner_width, p.direct_out, ws + p.w_out);
+  int e = ops.pack(st);
+  if (e != S1F_OK) return e;
+  set_product(a, mx, mi, p.n, p.n, inner, inner, p.width);
+  e = launch_product<Up<T>::template Of>(p.up, a, 2 * up_to(inner, 16), st);
+  if (e != S1F_OK) return e;
+  set_product(a, Matrix{a.h, a.h_ld, a.h_plane}, mo, p.n, p.n, d->hidden, d->hidden, p.inner_width);
+  set_out(a, y, y_rows(d), wide_side(d, y, d->y_stride_b, d->y_stride_s), 1.f);
+  return launch_product<Of3<T, false, false, R>::template Of>(p.down, a, d->hidden, st);
+}
+
+template <typename T, Result W>
+int backward(const s1f_rows *d, const FfnPlan &p, const void *dy, const void *x, const void *w_in, int64_t in_stride, const void *w_out, int64_t out_stride, int64_t inner,
+             int32_t act, const void *gate_up, void *dx, void *dw_in, int64_t dw_in_stride, void *dw_out, int64_t dw_out_stride, char *ws, hipStream_t st) {
+  constexpr bool F32 = sizeof(T) == 4;
+  constexpr Result R = F32 ? kStoreF32 : kStoreBf16;
+  constexpr float kDown = F32 ? 1.f / kUp : 1.f;   // dy's planes, and those of what comes of it, are kUp times as large
+  FfnArgs a = args_of(p, inner, act, gate_up, ws);
+  Operands ops{a, d, p.planes};
+  const Matrix mdy = ops.rows(dy, d->y_stride_b, d->y_stride_s, F32, p.width, ws + p.dy);
+  const Matrix mx = ops.rows(x, d->x_stride_b, d->x_stride_s, false, p.width, ws + p.x);
+  const Matrix mi = ops.weight(w_in, 2 * inner, d->hidden, in_stride, p.width, p.direct_in, ws + p.w_in);
+  const Matrix mo = ops.weight(w_out, d->hidden, inner, out_stride, p.inner_width, p.direct_out, ws + p.w_out);
+  int e = ops.pack(st);
+  if (e != S1F_OK) return e;
+  const int64_t h = d->hidden, n = p.n;
+  const Matrix mdz = {a.dz, a.dz_ld, a.dz_plane}, mh = {a.h, a.h_ld, a.h_plane};
+  set_product(a, mdy, mo, n, n, inner, p.inner_width, h);
+  e = launch_product<Dh<T>::template Of>(p.dh, a, inner, st);
+  if (e != S1F_OK) return e;
+  set_product(a, mdz, mi, n, n, h, p.width, 2 * inner);
+  set_out(a, dx, x_rows(d), wide_side(d, dx, d->x_stride_b, d->x_stride_s), kDown);
+  e = launch_product<Of3<T, false, true, R>::template Of>(p.dx, a, h, st);
+  if (e != S1F_OK) return e;
+  const int64_t piece = W == kStoreBf16 ? 8 : 4;
+  auto from = [](Matrix m, int64_t row) { return Matrix{m.data + row * m.ld, m.ld, m.plane}; };
+  for (int64_t at = 0; at < n && e == S1F_OK; at += p.per_turn) {
+    const int64_t rows = std::min(p.per_turn, n - at);
+    set_product(a, from(mdz, at), from(mx, at), 2 * inner, p.dz_ld, h, p.width, rows);
+    set_out(a, dw_in, RowsOf{0, dw_in_stride, Divisor::of(2 * inner)}, on16(dw_in) && dw_in_stride % piece == 0, kDown);
+    e = launch_product<Of3<T, true, true, W>::template Of>(p.dw_in, a, h, st);
+    if (e != S1F_OK) return e;
+    set_product(a, from(mdy, at), from(mh, at), h, p.width, inner, p.inner_width, rows);
+    set_out(a, dw_out, RowsOf{0, dw_out_stride, Divisor::of(h)}, on16(dw_out) && dw_out_stride % piece == 0, kDown);
+    e = launch_product<Of3<T, true, true, W>::template Of>(p.dw_out, a, inner, st);
+  }
+  return e;
+}
+
+}  // namespace
+}  // namespace s1f
+
+using namespace s1f;
+
+extern "C" size_t s1f_gated_ffn_fwd_workspace_bytes(const s1f_rows *desc, int64_t inner, int64_t w_in_stride, int64_t w_out_stride) {
+  return check_ffn(desc, inner, w_in_stride, w_out_stride) == S1F_OK ? (size_t)plan_of(desc, inner, w_in_stride, w_out_stride, false).bytes : 0;
+}
+extern "C" size_t s1f_gated_ffn_bwd_workspace_bytes(const s1f_rows *desc, int64_t inner, int64_t w_in_stride, int64_t w_out_stride) {
+  return check_ffn(desc, inner, w_in_stride, w_out_stride) == S1F_OK ? (size_t)plan_of(desc, inner, w_in_stride, w_out_stride, true).bytes : 0;
+}
+
+extern "C" int s1f_gated_ffn_fwd(const s1f_rows *desc, const void *x, const void *w_in, int64_t w_in_stride, const void *w_out, int64_t w_out_stride,
+                                 int64_t inner, int32_t act, void *y, void *gate_up, void *workspace, size_t workspace_bytes, void *hip_stream) {
+  const int rc = check_ffn(desc, inner, w_in_stride, w_out_stride);
+  if (rc != S1F_OK) return rc;
+  if (act < S1F_SILU || act > S1F_GELU_TANH) return S1F_EINVAL;
+  if (!x || !w_in || !w_out || !y || !workspace || !on_element(x, desc->dtype) || !on_element(y, desc->dtype) || !on_element(gate_up, desc->dtype) || !on16(w_in) ||
+      !on16(w_out) || !on16(workspace))
+    return S1F_EINVAL;
+  const FfnPlan p = plan_of(desc, inner, w_in_stride, w_out_stride, false);
+  if (workspace_bytes < (size_t)p.bytes) return S1F_EINVAL;
+  char *ws = reinterpret_cast<char *>(workspace);
+  hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+  return desc->dtype == S1F_BF16 ? forward<bf16_t>(desc, p, x, w_in, w_in_stride, w_out, w_out_stride, inner, act, y, gate_up, ws, st)
+                                 : forward<float>(desc, p, x, w_in, w_in_stride, w_out, w_out_stride, inner, act, y, gate_up, ws, st);
+}
+
+extern "C" int s1f_gated_ffn_bwd(const s1f_rows *desc, const void *dy, const void *x, const void *w_in, int64_t w_in_stride, const void *w_out,
+                                 int64_t w_out_stride, int64_t inner, int32_t act, const void *gate_up, void *dx, void *dw_in, int64_t dw_in_stride, void *dw_out,
+                                 int64_t dw_out_stride, int32_t dweight_dtype, void *workspace, size_t workspace_bytes, void *hip_stream) {
+  const int rc = check_ffn(desc, inner, w_in_stride, w_out_stride);
+  if (rc != S1F_OK) return rc;
+  if (dweight_dtype != S1F_F32 && !(dweight_dtype == S1F_BF16 && desc->dtype == S1F_BF16)) return S1F_EUNSUPPORTED;
+  if (act < S1F_SILU || act > S1F_GELU_TANH || dw_in_stride < desc->hidden || (desc->hidden > 1 && dw_out_stride < inner)) return S1F_EINVAL;
+  for (const void *p : {dy, x, gate_up, (const void *)dx})
+    if (!p || !on_element(p, desc->dtype)) return S1F_EINVAL;
+  if (!w_in || !w_out || !dw_in || !dw_out || !workspace || !on16(w_in) || !on16(w_out) || !on16(workspace) || !on_element(dw_in, dweight_dtype) ||
+      !on_element(dw_out, dweight_dtype))
+    return S1F_EINVAL;
+  const FfnPlan p = plan_of(desc, inner, w_in_stride, w_out_stride, true);
+  if (workspace_bytes < (size_t)p.bytes) return S1F_EINVAL;
+  char *ws = reinterpret_cast<char *>(workspace);
+  hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+  auto go = [&](auto call) { return call(desc, p, dy, x, w_in, w_in_stride, w_out, w_out_stride, inner, act, gate_up, dx, dw_in, dw_in_stride, dw_out, dw_out_stride, ws, st); };
+  if (desc->dtype == S1F_F32) return go(&backward<float, kAddF32>);
+  return dweight_dtype == S1F_F32 ? go(&backward<bf16_t, kAddF32>) : go(&backward<bf16_t, kStoreBf16>);
+}

@@ -35,6 +35,8 @@ struct Api {
   decltype(&s1f_rope_bwd) rope_bwd;
   decltype(&s1f_qk_norm_rope_fwd) qk_norm_rope_fwd;
   decltype(&s1f_qk_norm_rope_bwd) qk_norm_rope_bwd;
+  decltype(&s1f_gated_ffn_fwd) gated_ffn_fwd;
+  decltype(&s1f_gated_ffn_bwd) gated_ffn_bwd;
 };
 Api api = {};
 PyObject *get_device = nullptr, *get_stream = nullptr;
@@ -565,6 +567,48 @@ PyObject *qk_norm_rope_bwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
   });
 }
 
+// ---- gated feed-forward block ----------------------------------------------------------------------------------------------------------
+
+bool ffn_weights_ok(const at::Tensor &x, const at::Tensor &w_in, const at::Tensor &w_out, at::ScalarType type) {
+  return matrix_ok(w_in, x.size(2), type) && w_in.size(0) % 2 == 0 && w_out.dim() == 2 && w_out.size(0) == x.size(2) && matrix_ok(w_out, w_in.size(0) / 2, type);
+}
+bool gate_up_ok(const at::Tensor &t, const at::Tensor &x, const at::Tensor &w_in) {
+  return t.scalar_type() == x.scalar_type() && t.is_contiguous() && t.dim() == 3 && t.size(0) == x.size(0) && t.size(1) == x.size(1) && t.size(2) == w_in.size(0);
+}
+// (x, w_in, w_out, act, y, gate_up or None, workspace)
+PyObject *gated_ffn_fwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  return call([&]() -> int {
+    MixedArgs a;
+    s1f_rows d;
+    if (!a.read(args, n, "tttitoo")) return kPython;
+    auto &[x, w_in, w_out, y, gate_up, ws] = reinterpret_cast<const at::Tensor *(&)[6]>(a.t);
+    if (!fits(a.whole[0]) || !rows_desc_of(x, y, &d) || !ffn_weights_ok(*x, *w_in, *w_out, x->scalar_type()) || (gate_up && !gate_up_ok(*gate_up, *x, *w_in)) ||
+        !space_ok(ws))
+      return kPython;
+    void *const p[] = {ptr(x), ptr(w_in), ptr(w_out), ptr(y), ptr_or_null(gate_up), ptr_or_null(ws)};
+    Unlocked u;
+    return api.gated_ffn_fwd(&d, p[0], p[1], matrix_stride(*w_in), p[2], matrix_stride(*w_out), w_in->size(0) / 2, (int32_t)a.whole[0], p[3], p[4], p[5], bytes(ws),
+                             a.stream);
+  });
+}
+// (dy, x, w_in, w_out, act, gate_up, dx, dw_in, dw_out, workspace)
+PyObject *gated_ffn_bwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  return call([&]() -> int {
+    MixedArgs a;
+    s1f_rows d;
+    int32_t code;
+    if (!a.read(args, n, "ttttitttto")) return kPython;
+    auto &[dy, x, w_in, w_out, gate_up, dx, dw_in, dw_out, ws] = reinterpret_cast<const at::Tensor *(&)[9]>(a.t);
+    if (!fits(a.whole[0]) || !rows_desc_of(x, dy, &d) || !same_rows(*x, *dx) || !ffn_weights_ok(*x, *w_in, *w_out, x->scalar_type()) || !dtype_of(*dw_in, &code) ||
+        !ffn_weights_ok(*x, *dw_in, *dw_out, dw_in->scalar_type()) || dw_in->sizes() != w_in->sizes() || !gate_up_ok(*gate_up, *x, *w_in) || !space_ok(ws))
+      return kPython;
+    void *const p[] = {ptr(dy), ptr(x), ptr(w_in), ptr(w_out), ptr(gate_up), ptr(dx), ptr(dw_in), ptr(dw_out), ptr_or_null(ws)};
+    Unlocked u;
+    return api.gated_ffn_bwd(&d, p[0], p[1], p[2], matrix_stride(*w_in), p[3], matrix_stride(*w_out), w_in->size(0) / 2, (int32_t)a.whole[0], p[4], p[5], p[6],
+                             matrix_stride(*dw_in), p[7], matrix_stride(*dw_out), code, p[8], bytes(ws), a.stream);
+  });
+}
+
 // (addresses of the entry points in the order of Api, torch's functions for the current device and for a device's stream)
 PyObject *bind(PyObject *, PyObject *args) {
   PyObject *addresses, *dev, *st;
@@ -605,6 +649,8 @@ PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, nullptr},
                          {"rope_bwd", S1F_METHOD(rope_bwd), METH_FASTCALL, nullptr},
                          {"qk_norm_rope_fwd", S1F_METHOD(qk_norm_rope_fwd), METH_FASTCALL, nullptr},
                          {"qk_norm_rope_bwd", S1F_METHOD(qk_norm_rope_bwd), METH_FASTCALL, nullptr},
+                         {"gated_ffn_fwd", S1F_METHOD(gated_ffn_fwd), METH_FASTCALL, nullptr},
+                         {"gated_ffn_bwd", S1F_METHOD(gated_ffn_bwd), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_torch_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
