@@ -34,7 +34,6 @@ struct FfnArgs {
   bf16_t *h, *dz;
   int64_t h_ld, h_plane, dz_ld, dz_plane;
   void *gate_up;                  // [.][2 * inner]
-  int32_t wide_gate_up;
   void *out;
   RowsOf out_rows;
   int32_t wide_out;
@@ -81,27 +80,29 @@ template <typename T> S1F_DEV float sigmoid(float x) {
   if constexpr (sizeof(T) == 4) return 1.f / (1.f + expf(-x));
   else return __builtin_amdgcn_rcpf(1.f + exp2_fast(x * -kLog2e));
 }
-// act(g), and act'(g).  The tanh form is g * sigmoid(2 sqrt(2 / pi) (g + 0.044715 g^3)), which keeps its digits where 1 + tanh would lose them, and erfc does
-// where 1 + erf would.
-template <typename T> S1F_DEV float activation(float g, int act) {
-  if (act == S1F_SILU) return g * sigmoid<T>(g);
-  if (act == S1F_GELU) return 0.5f * g * erfcf(g * -0.70710678f);
-  return g * sigmoid<T>(1.5957691216f * g * (1.f + 0.044715f * g * g));
-}
-template <typename T> S1F_DEV void activation(float g, int act, float &a, float &slope) {
-  if (act == S1F_GELU) {
-    const float p = 0.5f * erfcf(g * -0.70710678f);
-    a = g * p;
-    slope = p + g * 0.39894228f * expf(-0.5f * g * g);
-    return;
+// act(g), and act'(g).  SiLU and the tanh form are g * sigmoid(g (c0 + c1 g^2)): the latter's (1 + tanh(t)) / 2 is the sigmoid of 2t, and keeps its digits where 1 + tanh
+// would lose them, as erfc does where 1 + erf would.
+template <typename T, bool ERF> struct Activation {
+  float c0, c1;
+  S1F_DEV explicit Activation(int act) : c0(act == S1F_SILU ? 1.f : 1.5957691216f), c1(act == S1F_SILU ? 0.f : 1.5957691216f * 0.044715f) {}
+  // (past 2^60 squares are left where they are, and no sigmoid changes any more)
+  S1F_DEV static float square(float g) { return fminf(g * g, 0x1p120f); }
+  S1F_DEV float operator()(float g) const {
+    if constexpr (ERF) return g * (0.5f * erfcf(g * -0.70710678f));
+    else return g * sigmoid<T>(g * fmaf(c1, square(g), c0));
   }
-  const bool silu = act == S1F_SILU;
-  const float s = sigmoid<T>(silu ? g : 1.5957691216f * g * (1.f + 0.044715f * g * g)), rest = s * (1.f - s);
-  a = g * s;
-  // (far out, where the sigmoid does not change any more, g^2 may be infinite)
-  const float inside = silu ? 1.f : 1.5957691216f * (1.f + 0.134145f * g * g);
-  slope = rest == 0.f ? s : s + g * rest * inside;
-}
+  S1F_DEV void operator()(float g, float &a, float &slope) const {
+    if constexpr (ERF) {
+      const float p = 0.5f * erfcf(g * -0.70710678f);
+      a = g * p;
+      slope = fmaf(g * 0.39894228f, expf(-0.5f * g * g), p);
+    } else {
+      const float q = square(g), s = sigmoid<T>(g * fmaf(c1, q, c0)), rest = s * (1.f - s);
+      a = g * s;
+      slope = rest == 0.f ? s : fmaf(g * rest, fmaf(3.f * c1, q, c0), s);
+    }
+  }
+};
 
 // ---- products --------------------------------------------------------------------------------------------------------------------------
 
@@ -135,30 +136,43 @@ S1F_DEV void ffn_product(f32x4 (&acc)[P::MB][P::NB], const FfnArgs &a, int m0, i
   else P::run(acc, a.a, a.b, m0, a.m_limit, n0, a.n_limit, a.k, begin, end, lds, b_apart);
 }
 
-// Four values of a row of a bf16 matrix, or of its three planes; the first `there` of them if `some`.
-template <int PAIRS> S1F_DEV void put4(bf16_t *to, int64_t plane, f32x4 v, bool some, int there) {
+// Eight values of a row of a bf16 matrix, or of its three planes, on any element; the first `there` of them.
+template <int PAIRS> S1F_DEV void put8(bf16_t *to, int64_t plane, const float (&v)[8], int there) {
+  typedef Piece<bf16_t, false> P;
   if constexpr (PAIRS == 6) {
-    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-    const Planes q = split3(v, f32x4{0.f, 0.f, 0.f, 0.f});
+    const Planes q = split3(f32x4{v[0], v[1], v[2], v[3]}, f32x4{v[4], v[5], v[6], v[7]});
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
-      if (!some) {
-        const u32x4 w = __builtin_bit_cast(u32x4, q.p[i]);
-        *reinterpret_cast<u32x2 *>(to + i * plane) = u32x2{w[0], w[1]};
+      if (there >= 8) {
+        *reinterpret_cast<P::Loose *>(to + i * plane) = q.p[i];
       } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
+        for (int e = 0; e < 8; ++e)
           if (e < there) to[i * plane + e] = q.p[i][e];
       }
     }
   } else {
-    if (!some) {
-      store4<bf16_t>(to, v[0], v[1], v[2], v[3]);
-    } else {
+    P::store(to, there, v);
+  }
+}
+template <typename T> S1F_DEV void get8(const T *from, int there, float (&v)[8]) {
+  typedef Piece<T, false> P;
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (e < there) to[e] = (bf16_t)v[e];
-    }
+  for (int i = 0; i < 8; i += P::N) {
+    typename P::Values p;
+    P::load(from + i, there - i, p);
+#pragma unroll
+    for (int e = 0; e < P::N; ++e) v[i + e] = p[e];
+  }
+}
+template <typename T> S1F_DEV void set8(T *to, int there, const float (&v)[8]) {
+  typedef Piece<T, false> P;
+#pragma unroll
+  for (int i = 0; i < 8; i += P::N) {
+    typename P::Values p;
+#pragma unroll
+    for (int e = 0; e < P::N; ++e) p[e] = v[i + e];
+    P::store(to + i, there - i, p);
   }
 }
 template <typename T> S1F_DEV void put_values(T *to, f32x4 v, bool wide, int there) {
@@ -185,7 +199,66 @@ template <typename T> S1F_DEV f32x4 get_values(const T *from, bool wide, int the
   return v;
 }
 
-// h = act(g) * u of a tile of BM rows and BN / 2 columns.
+// What a wave's lanes have written to LDS before is what they read there behind it.
+S1F_DEV void between_lanes() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+// A wave's results on their way to memory: through LDS of its own, 16 * GM rows at a time, from where a lane takes eight neighbours of a row, so that memory sees whole lines and a
+// lane's work on them is a loop.  (From the registers of the matrix instructions, four elements to a lane: the loop over 32 blocks of a 256 x 256 tile was
+// not unrolled, its accumulators went to memory, and dh of 4897 x 7168 x 19200 took 19.7 ms.)
+template <typename P> struct Staged {
+  static constexpr int GM = P::MB < 4 ? P::MB : 4, LD = 16 * P::NB + 4, BYTES = 16 * GM * LD * 4;
+  float *base;
+  S1F_DEV explicit Staged(char *smem) : base(reinterpret_cast<float *>(smem + (threadIdx.x >> 6) * BYTES)) {}
+  S1F_DEV void put(const f32x4 (&acc)[P::MB][P::NB], int mb0) {
+    const int lane = lane_id(), n = lane & 15, j = lane >> 4;
+#pragma unroll
+    for (int mb = 0; mb < GM; ++mb)
+#pragma unroll
+      for (int nb = 0; nb < P::NB; ++nb) *reinterpret_cast<f32x4 *>(base + (16 * mb + n) * LD + 16 * nb + 4 * j) = acc[mb0 + mb][nb];
+    between_lanes();
+  }
+  S1F_DEV void get(int row, int col, float (&v)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; i += 4) {
+      const f32x4 x = *reinterpret_cast<const f32x4 *>(base + row * LD + col + i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[i + e] = x[e];
+    }
+  }
+};
+
+// h = act(g) * u of a tile of BM rows and BN / 2 columns.  m0: first row of the wave's blocks, n0: its first column.
+template <typename T, bool ERF, typename P> S1F_DEV void up_results(const f32x4 (&acc)[P::MB][P::NB], const FfnArgs &a, int m0, int n0, char *smem) {
+  constexpr int PAIRS = sizeof(T) == 4 ? 6 : 1, LANES = P::NB, ROWS = 64 / LANES;   // lanes to a row of 8 NB columns
+  const Activation<T, ERF> activation(a.act);
+  Staged<P> staged(smem);
+  // blocks of g and u take turns
+  const int lane = lane_id(), at = 8 * (lane % LANES), from = (at >> 4 << 5) + (at & 15), col = n0 + at, there = a.inner - col;
+#pragma unroll
+  for (int mb = 0; mb < P::MB; mb += Staged<P>::GM) {
+    staged.put(acc, mb);
+#pragma unroll 1
+    for (int r = lane / LANES; r < 16 * Staged<P>::GM; r += ROWS) {
+      const int row = m0 + 16 * mb + r;
+      float g[8], u[8], h[8];
+      staged.get(r, from, g);
+      staged.get(r, from + 16, u);
+      if (row >= a.m || col >= a.h_ld) continue;
+      if (a.gate_up) {
+        T *to = reinterpret_cast<T *>(a.gate_up) + (int64_t)row * 2 * a.inner + col;
+        set8<T>(to, there, g);
+        set8<T>(to + a.inner, there, u);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) h[e] = e < there ? activation(g[e]) * u[e] : 0.f;
+      put8<PAIRS>(a.h + (int64_t)row * a.h_ld + col, a.h_plane, h, 8);
+    }
+    between_lanes();
+  }
+}
 template <typename T, int BM, int BN, int WM, int WN> __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_up_kernel(const FfnArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   constexpr int PAIRS = sizeof(T) == 4 ? 6 : 1;
@@ -196,30 +269,51 @@ template <typename T, int BM, int BN, int WM, int WN> __global__ void __launch_b
   if (m0 >= a.m || n0 >= a.n) return;
   f32x4 acc[P::MB][P::NB];
   ffn_product<P, PAIRS, BM>(acc, a, m0, n0, 0, 1, to_lds_addr(smem), a.inner);
-  const int lane = lane_id(), n = lane & 15, j = lane >> 4, wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
-#pragma unroll
-  for (int mb = 0; mb < P::MB; ++mb) {
-    const int row = m0 + 16 * (wm * P::MB + mb) + n;
-    if (row >= a.m) continue;
-#pragma unroll
-    for (int p = 0; p < P::NB / 2; ++p) {
-      const int col = n0 + 16 * (wn * P::NB / 2 + p) + 4 * j, there = a.n - col;
-      if (col >= a.h_ld) continue;
-      const f32x4 g = acc[mb][2 * p], u = acc[mb][2 * p + 1];
-      if (a.gate_up) {
-        T *to = reinterpret_cast<T *>(a.gate_up) + (int64_t)row * 2 * a.inner + col;
-        put_values<T>(to, g, a.wide_gate_up, there);
-        put_values<T>(to + a.inner, u, a.wide_gate_up, there);
-      }
-      f32x4 h;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) h[e] = e < there ? activation<T>(g[e], a.act) * u[e] : 0.f;
-      put4<PAIRS>(a.h + (int64_t)row * a.h_ld + col, a.h_plane, h, false, 4);
-    }
-  }
+  const int wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
+  if (a.act == S1F_GELU) up_results<T, true, P>(acc, a, m0 + 16 * P::MB * wm, n0 + 8 * P::NB * wn, smem);
+  else up_results<T, false, P>(acc, a, m0 + 16 * P::MB * wm, n0 + 8 * P::NB * wn, smem);
 }
 
 // dh = dy W_out of a tile, and of it [dg | du] and h.
+template <typename T, bool ERF, typename P> S1F_DEV void dh_results(const f32x4 (&acc)[P::MB][P::NB], const FfnArgs &a, int m0, int n0, char *smem) {
+  constexpr int PAIRS = sizeof(T) == 4 ? 6 : 1, LANES = 2 * P::NB, ROWS = 64 / LANES;
+  const Activation<T, ERF> activation(a.act);
+  Staged<P> staged(smem);
+  const int lane = lane_id(), at = 8 * (lane % LANES), col = n0 + at, there = a.inner - col;
+#pragma unroll
+  for (int mb = 0; mb < P::MB; mb += Staged<P>::GM) {
+    staged.put(acc, mb);
+#pragma unroll 2
+    for (int r = lane / LANES; r < 16 * Staged<P>::GM; r += ROWS) {
+      const int row = m0 + 16 * mb + r;
+      if (row >= a.m || col >= a.h_ld) continue;
+      const T *from = reinterpret_cast<const T *>(a.gate_up) + (int64_t)row * 2 * a.inner + col;
+      float d[8], g[8], u[8], h[8];
+      get8<T>(from, there, g);
+      get8<T>(from + a.inner, there, u);
+      staged.get(r, at, d);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float act, slope;
+        activation(g[e], act, slope);
+        const bool is = e < there;
+        h[e] = is ? act * u[e] : 0.f;
+        g[e] = d[e] * u[e] * slope;
+        u[e] = d[e] * act;
+      }
+      put8<PAIRS>(a.h + (int64_t)row * a.h_ld + col, a.h_plane, h, 8);
+      if (there <= 0) continue;
+      bf16_t *to = a.dz + (int64_t)row * a.dz_ld + col;
+      put8<PAIRS>(to, a.dz_plane, g, there);
+      put8<PAIRS>(to + a.inner, a.dz_plane, u, there);
+      if (there <= 8)   // zeros behind the end of du, where the products read whole pieces of 8
+        for (int c = 2 * a.inner; c < a.dz_ld; ++c)
+#pragma unroll
+          for (int i = 0; i < (PAIRS == 6 ? 3 : 1); ++i) a.dz[(int64_t)row * a.dz_ld + c + i * a.dz_plane] = (bf16_t)0.f;
+    }
+    between_lanes();
+  }
+}
 template <typename T, int BM, int BN, int WM, int WN> __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_dh_kernel(const FfnArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   constexpr int PAIRS = sizeof(T) == 4 ? 6 : 1;
@@ -230,39 +324,9 @@ template <typename T, int BM, int BN, int WM, int WN> __global__ void __launch_b
   if (m0 >= a.m || n0 >= a.n) return;
   f32x4 acc[P::MB][P::NB];
   ffn_product<P, PAIRS, BM>(acc, a, m0, n0, 0, 1, to_lds_addr(smem));
-  const int lane = lane_id(), n = lane & 15, j = lane >> 4, wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
-  const bool some = a.inner % 4 != 0;   // (then du does not start where four elements do)
-#pragma unroll
-  for (int mb = 0; mb < P::MB; ++mb) {
-    const int row = m0 + 16 * (wm * P::MB + mb) + n;
-    if (row >= a.m) continue;
-#pragma unroll
-    for (int nb = 0; nb < P::NB; ++nb) {
-      const int col = n0 + 16 * (wn * P::NB + nb) + 4 * j, there = a.inner - col;
-      if (col >= a.h_ld) continue;
-      const T *from = reinterpret_cast<const T *>(a.gate_up) + (int64_t)row * 2 * a.inner + col;
-      const f32x4 g = get_values<T>(from, a.wide_gate_up, there), u = get_values<T>(from + a.inner, a.wide_gate_up, there);
-      f32x4 dg, du, h;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float act, slope;
-        activation<T>(g[e], a.act, act, slope);
-        const bool is = e < there;
-        h[e] = is ? act * u[e] : 0.f;
-        dg[e] = is ? acc[mb][nb][e] * u[e] * slope : 0.f;
-        du[e] = is ? acc[mb][nb][e] * act : 0.f;
-      }
-      put4<PAIRS>(a.h + (int64_t)row * a.h_ld + col, a.h_plane, h, false, 4);
-      if (there <= 0) continue;
-      bf16_t *to = a.dz + (int64_t)row * a.dz_ld + col;
-      put4<PAIRS>(to, a.dz_plane, dg, some, there);
-      put4<PAIRS>(to + a.inner, a.dz_plane, du, some, there);
-      if (there <= 4)   // zeros behind the end of du, where the products read whole pieces of 8
-        for (int c = 2 * a.inner; c < a.dz_ld; ++c)
-#pragma unroll
-          for (int i = 0; i < (PAIRS == 6 ? 3 : 1); ++i) a.dz[(int64_t)row * a.dz_ld + c + i * a.dz_plane] = (bf16_t)0.f;
-    }
-  }
+  const int wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
+  if (a.act == S1F_GELU) dh_results<T, true, P>(acc, a, m0 + 16 * P::MB * wm, n0 + 16 * P::NB * wn, smem);
+  else dh_results<T, false, P>(acc, a, m0 + 16 * P::MB * wm, n0 + 16 * P::NB * wn, smem);
 }
 
 enum Result { kStoreBf16, kStoreF32, kAddF32 };
@@ -461,6 +525,7 @@ template <typename T, Tile TILE, bool TRA, bool TRB> struct FfnShape : TileShape
   static constexpr int WM = ALL ? 2 : S::WM;   // (one workgroup to a unit)
   typedef Product<S::BM, S::BN, WM, S::WN, TRA, TRB, 1> P;
   static constexpr int LDS_BYTES = ALL ? P::PLANES_LDS_BYTES : P::LDS_BYTES;
+  static_assert(Staged<P>::BYTES * P::NW <= LDS_BYTES, "results pass through the operands' places");
   static constexpr void (*join)(FfnArgs) = nullptr;
 };
 template <typename T> struct Up {
@@ -530,7 +595,6 @@ FfnArgs args_of(const FfnPlan &p, int64_t inner, int32_t act, const void *gate_u
   a.dz = reinterpret_cast<bf16_t *>(ws + p.dz);
   a.dz_ld = p.dz_ld; a.dz_plane = p.n * p.dz_ld;
   a.gate_up = const_cast<void *>(gate_up);
-  a.wide_gate_up = inner % 4 == 0 && on16(gate_up);
   a.part = reinterpret_cast<float *>(ws + p.part);
   return a;
 }
