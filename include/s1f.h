@@ -267,7 +267,7 @@ int s1f_kv_grad_emit(const s1f_desc *desc, const float *dk_prefix_acc, const flo
  *   - v, v_cache (dv, dv_prefix_acc) may both be NULL.
  *   - q_rot may be q, k_cache + seg_off rows k, v_cache so v, dq dq_rot, where their strides are the same; dq may not be q.
  * Computed in fp32, rounded once.  Pointers are aligned to their element; calls are faster where rows, and half of rotary_dim unless interleaved, are made of 16 bytes.
- * Errors as for the attention calls: S1F_EINVAL, S1F_EUNSUPPORTED (dtype; head_dim odd or above 256; batch * rows > 2^26; more than 2^16 heads), S1F_ERANGE (rows < 1,
+ * Errors as for the attention calls: S1F_EINVAL, S1F_EUNSUPPORTED (dtype; head_dim odd or above 256; batch * rows > 2^26; more than 2^16 heads; batch * rows * (n_q_heads + 2 n_kv_heads) > 2^31), S1F_ERANGE (rows < 1,
  * rows outside [0, cache_capacity)), S1F_EDEVICE. */
 typedef struct {
   int32_t batch;

@@ -37,7 +37,11 @@ struct RopeArgs {
   Divisor by_rows;
   int32_t n, dim, half, rotary, items;  // batch * rows; half: pairs that are turned; items: lanes' shares of PW pairs in a row
   int32_t n_q, n_k, n_v;                // heads: the list of a row's heads is q, k, v
-  int32_t log_rows;                     // rows that a workgroup works on side by side
+  // Units of work: 2^log_rows rows of up to `unit_heads` heads of one of the tensors; units_q, units_k, units_v to a block of rows, all blocks one behind the other,
+  // `per_group` consecutive ones (the remainder one more each) to a workgroup
+  int32_t log_rows, unit_heads, units_q, units_k, units_v;
+  Divisor by_units;
+  int32_t units, per_group, remainder;
   int32_t parts;
   float magnitude, eps, inv_dim;
 };
@@ -105,208 +109,235 @@ template <int PW, bool PAIRS> struct Share {
   S1F_DEV static constexpr int second(int i) { return PAIRS ? 2 * i + 1 : PW + i; }
 };
 
-// T: type of the tensors, K: of the keys' and values' source (fp32 accumulators in the backward).  L lanes to a row, IT shares to a lane.  BACK: turn back.
-// A workgroup works on 2^log_rows rows; its groups of L lanes beyond that share the heads of a row with each other and with the workgroups of the grid's y.
-template <typename T, typename K, int PW, int L, int IT, bool PAIRS, bool NORM, bool BACK> __global__ void __launch_bounds__(256) rope_kernel(const RopeArgs a) {
-  constexpr int E = 2 * PW, U = NORM && BACK ? 2 : 4;   // U: heads asked for together
+// A lane's elements of a head as they lie in memory: fp32, or bf16 in half as many words.
+template <int PW, int IT> struct Raw {
+  uint32_t w[IT][2][PW];
+  template <typename S> S1F_DEV void load(const S *p, const int (&at)[IT][2], const bool (&has)[IT]) {
+    typedef Run<S, PW> R;
+#pragma unroll
+    for (int t = 0; t < IT; ++t)
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        if (has[t]) {
+          R r;
+          r.load(p + at[t][k]);
+          if constexpr (sizeof(S) == 2 && PW == 1) w[t][k][0] = __builtin_bit_cast(uint16_t, r.v[0][0]);
+          else __builtin_memcpy(w[t][k], r.v, sizeof(S) * PW);
+        }
+  }
+  template <typename S> S1F_DEV float get(int t, int k, int e) const {
+    if constexpr (sizeof(S) == 4) return __builtin_bit_cast(float, w[t][k][e]);
+    else return __builtin_bit_cast(float, e & 1 ? w[t][k][e / 2] & 0xffff0000u : w[t][k][e / 2] << 16);
+  }
+};
+
+enum Kind { kQ, kK, kV };
+struct Unit {
+  int block, kind, head;   // block of rows; tensor; first head
+};
+S1F_DEV Unit unit_of(const RopeArgs &a, int unit) {
+  int block, u;
+  div_mod(unit, a.by_units, block, u);
+  const int kind = u < a.units_q ? kQ : u < a.units_q + a.units_k ? kK : kV;
+  return Unit{block, kind, (u - (kind == kQ ? 0 : kind == kK ? a.units_q : a.units_q + a.units_k)) * a.unit_heads};
+}
+
+// T: type of the tensors, K: of the keys' and values' source (fp32 accumulators in the backward).  L lanes to a row, IT shares to a lane, U heads to a lane and unit.  BACK: turn back.
+// The groups of L lanes that a workgroup has beyond its 2^log_rows rows share the heads of a unit.  The elements of the next unit are asked for before those of this one are
+// worked on, and those of the first before the angles are computed.
+template <typename T, typename K, int PW, int L, int IT, int U, bool PAIRS, bool NORM, bool BACK> __global__ void __launch_bounds__(256) rope_kernel(const RopeArgs a) {
+  constexpr int E = 2 * PW;
   constexpr bool GAINS = NORM && BACK;
-  const int group = threadIdx.x / L, in_row = group & ((1 << a.log_rows) - 1);
-  const int slots_here = (256 / L) >> a.log_rows, slots = slots_here * gridDim.y, slot = blockIdx.y * slots_here + (group >> a.log_rows);
-  float dg_q[IT][E], dg_k[IT][E];
+  __shared__ float gains[NORM ? 2 : 1][NORM ? L * IT * E : 1];
+  const int lane = threadIdx.x % L, group = threadIdx.x / L, in_row = group & ((1 << a.log_rows) - 1), slot = group >> a.log_rows, slots = (256 / L) >> a.log_rows;
+  const int g = blockIdx.x, first = g * a.per_group + (g < a.remainder ? g : a.remainder), last = first + a.per_group + (g < a.remainder ? 1 : 0);
+  bool has[IT], here[IT];
+  int at[IT][2], straight[IT][2];   // the lane's elements of a row, and of values, which are not turned
+#pragma unroll
+  for (int t = 0; t < IT; ++t) {
+    const int item = lane + t * L;
+    const Share<PW, PAIRS> share(a, item);
+    has[t] = item < a.items;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      at[t][k] = share.at[k];
+      straight[t][k] = item * E + k * PW;
+    }
+  }
+  int b = 0, r = 0, block = -1;
+  bool row_is = false;
+  auto go_to = [&](int to) {
+    block = to;
+    const int row = (to << a.log_rows) + in_row;
+    row_is = row < a.n;
+    div_mod(row_is ? row : a.n - 1, a.by_rows, b, r);
+  };
+  Raw<PW, IT> in[U], x[GAINS ? U : 1];
+  auto ask = [&](const Unit &u) {
+    const int heads = u.kind == kQ ? a.n_q : a.n_k;
+    const HeadStrides &ss = u.kind == kQ ? a.src_qs : a.src_ks, &xs = u.kind == kQ ? a.dst_qs : a.dst_ks;
+    const int64_t from = b * ss.sb + r * ss.ss, from_x = b * xs.sb + r * xs.ss;
+#pragma unroll
+    for (int t = 0; t < IT; ++t) here[t] = has[t] && row_is;
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int h = u.head + slot + i * slots;
+      if (h >= heads) break;
+      if (u.kind == kQ) in[i].load(reinterpret_cast<const T *>(a.src_q) + from + h * ss.sh, at, here);
+      else if (u.kind == kK) in[i].load(reinterpret_cast<const K *>(a.src_k) + from + h * ss.sh, at, here);
+      else in[i].load(reinterpret_cast<const K *>(a.src_v) + from + h * ss.sh, straight, here);
+      if constexpr (GAINS)
+        if (u.kind != kV) x[i].load(reinterpret_cast<const T *>(u.kind == kQ ? a.x_q : a.x_k) + from_x + h * xs.sh, at, here);
+    }
+  };
+  Unit now = unit_of(a, first);
+  go_to(now.block);
+  if (first < last) ask(now);
+  if constexpr (NORM) {
+    for (int i = threadIdx.x; i < 2 * L * IT * E; i += 256) {
+      const int side = i / (L * IT * E), col = i % (L * IT * E), item = col / E, e = col % E;
+      const Share<PW, PAIRS> share(a, item);
+      gains[side][col] = item < a.items ? (float)reinterpret_cast<const T *>(side ? a.gain_k : a.gain_q)[share.at[e / PW] + e % PW] : 0.f;
+    }
+    __syncthreads();
+  }
+  float dg[2][IT][E];
   if constexpr (GAINS) {
 #pragma unroll
     for (int t = 0; t < IT; ++t)
 #pragma unroll
-      for (int e = 0; e < E; ++e) dg_q[t][e] = dg_k[t][e] = 0.f;
+      for (int e = 0; e < E; ++e) dg[0][t][e] = dg[1][t][e] = 0.f;
   }
-  for (int row = (blockIdx.x << a.log_rows) + in_row; row < a.n; row += gridDim.x << a.log_rows) {
-    int b, r;
-    div_mod(row, a.by_rows, b, r);
-    const int64_t position = a.positions ? a.positions[b * a.positions_sb + r] : a.first_position + r;
-    float c[IT][PW], s[IT][PW];
-    int at[IT][2];
-    bool has[IT];
+  float c[IT][PW], s[IT][PW];
+  int angles_of = -1;
+#pragma unroll 1
+  for (int unit = first; unit < last; ++unit) {
+    const Unit u = now;
+    const bool is = row_is;
+    const int ub = b, ur = r;
+    if (u.kind != kV && angles_of != u.block) {
+      angles_of = u.block;
+      const int64_t position = a.positions ? a.positions[b * a.positions_sb + r] : a.first_position + r;
 #pragma unroll
-    for (int t = 0; t < IT; ++t) {
-      const int item = threadIdx.x % L + t * L;
-      const Share<PW, PAIRS> share(a, item);
-      has[t] = item < a.items;
-      at[t][0] = share.at[0];
-      at[t][1] = share.at[1];
+      for (int t = 0; t < IT; ++t)
 #pragma unroll
-      for (int i = 0; i < PW; ++i) {
-        const int pair = item * PW + i;
-        c[t][i] = 1.f;
-        s[t][i] = 0.f;
-        if (pair < a.half) {
-          cos_sin((double)position * a.freqs[pair], c[t][i], s[t][i]);
-          c[t][i] *= a.magnitude;
-          s[t][i] *= BACK ? -a.magnitude : a.magnitude;
+        for (int i = 0; i < PW; ++i) {
+          const int pair = (lane + t * L) * PW + i;
+          c[t][i] = 1.f;
+          s[t][i] = 0.f;
+          if (pair < a.half) {
+            cos_sin((double)position * a.freqs[pair], c[t][i], s[t][i]);
+            c[t][i] *= a.magnitude;
+            s[t][i] *= BACK ? -a.magnitude : a.magnitude;
+          }
         }
-      }
     }
-    // heads [i, end) of the list, `from` the number of the first
-    int head = slot;
-    auto walk = [&](auto kind, int from, int end, const void *src, const HeadStrides &ss, void *dst, const HeadStrides &ds, const void *xs, const void *gains,
-                    float (&dg)[IT][E]) {
-      typedef decltype(kind) S;
-      if (head >= end) return;
-      float gain[IT][E];
-      if constexpr (NORM) {
+    // the unit's elements as numbers; then the next unit's are asked for
+    Raw<PW, IT> mine[U], own[GAINS ? U : 1];
 #pragma unroll
-        for (int t = 0; t < IT; ++t)
+    for (int i = 0; i < U; ++i) {
+      mine[i] = in[i];
+      if constexpr (GAINS) own[i] = x[i];
+    }
+    if (unit + 1 < last) {
+      now = unit_of(a, unit + 1);
+      if (now.block != block) go_to(now.block);
+      ask(now);
+    }
+    const int heads = u.kind == kQ ? a.n_q : a.n_k;
+    const HeadStrides &ds = u.kind == kQ ? a.dst_qs : a.dst_ks;
+    T *to = reinterpret_cast<T *>(u.kind == kQ ? a.dst_q : u.kind == kK ? a.dst_k : a.dst_v) + ub * ds.sb + ur * ds.ss;
+    const bool wide = sizeof(K) == 4 && u.kind != kQ;   // (where T and K differ)
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            Run<T, PW> g;
-            if (has[t]) g.load(reinterpret_cast<const T *>(gains) + at[t][h]);
+    for (int i = 0; i < U; ++i) {
+      const int h = u.head + slot + i * slots;
+      if (h >= heads) break;
+      float v[IT][E];
 #pragma unroll
-            for (int e = 0; e < PW; ++e) gain[t][h * PW + e] = has[t] ? g[e] : 0.f;
-          }
-      }
-      const S *p = reinterpret_cast<const S *>(src) + b * ss.sb + r * ss.ss;
-      T *q = reinterpret_cast<T *>(dst) + b * ds.sb + r * ds.ss;
-      const T *px = reinterpret_cast<const T *>(xs) + b * ds.sb + r * ds.ss;
-      while (head < end) {
-        Run<S, PW> in[U][IT][2];
-        Run<T, PW> x[GAINS ? U : 1][IT][2];
+      for (int t = 0; t < IT; ++t)
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int h = head + u * slots - from;
-          if (h >= end - from) break;
+        for (int e = 0; e < E; ++e) {
+          const float narrow = mine[i].template get<T>(t, e / PW, e % PW);
+          v[t][e] = sizeof(T) != sizeof(K) && wide ? mine[i].template get<K>(t, e / PW, e % PW) : narrow;
+          if (!has[t] || !is) v[t][e] = 0.f;
+        }
+      if (u.kind != kV) {
+        const float *gain = &gains[NORM && u.kind == kK ? 1 : 0][NORM ? lane * E : 0];
+        if constexpr (NORM && !BACK) {
+          float sum = 0.f;
 #pragma unroll
           for (int t = 0; t < IT; ++t)
-            if (has[t]) {
 #pragma unroll
-              for (int k = 0; k < 2; ++k) {
-                in[u][t][k].load(p + h * ss.sh + at[t][k]);
-                if constexpr (GAINS) x[u][t][k].load(px + h * ds.sh + at[t][k]);
-              }
-            }
+            for (int e = 0; e < E; ++e) sum += v[t][e] * v[t][e];
+          const float rstd = 1.f / sqrtf(sum_of<L>(sum) * a.inv_dim + a.eps);
+#pragma unroll
+          for (int t = 0; t < IT; ++t)
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[t][e] = v[t][e] * rstd * gain[t * L * E + e];
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int h = head + u * slots - from;
-          if (h >= end - from) break;
-          float v[IT][E];
+        for (int t = 0; t < IT; ++t)
 #pragma unroll
-          for (int t = 0; t < IT; ++t)
-#pragma unroll
-            for (int e = 0; e < E; ++e) v[t][e] = has[t] ? in[u][t][e / PW][e % PW] : 0.f;
-          if constexpr (NORM && !BACK) {
-            float sum = 0.f;
-#pragma unroll
-            for (int t = 0; t < IT; ++t)
-#pragma unroll
-              for (int e = 0; e < E; ++e) sum += v[t][e] * v[t][e];
-            const float rstd = 1.f / sqrtf(sum_of<L>(sum) * a.inv_dim + a.eps);
-#pragma unroll
-            for (int t = 0; t < IT; ++t)
-#pragma unroll
-              for (int e = 0; e < E; ++e) v[t][e] = v[t][e] * rstd * gain[t][e];
+          for (int p = 0; p < PW; ++p) {
+            constexpr auto F = &Share<PW, PAIRS>::first, G = &Share<PW, PAIRS>::second;
+            float &re = v[t][F(p)], &im = v[t][G(p)];
+            const bool turned = (lane + t * L) * PW + p < a.half;   // (the others stay what they are, infinities too)
+            const float was = re;
+            re = turned ? was * c[t][p] - im * s[t][p] : was;
+            im = turned ? im * c[t][p] + was * s[t][p] : im;
           }
+        if constexpr (GAINS) {
+          float w[IT][E], squares = 0.f, along = 0.f;
 #pragma unroll
           for (int t = 0; t < IT; ++t)
 #pragma unroll
-            for (int i = 0; i < PW; ++i) {
-              constexpr auto F = &Share<PW, PAIRS>::first, G = &Share<PW, PAIRS>::second;
-              float &re = v[t][F(i)], &im = v[t][G(i)];
-              const bool turned = (int)(threadIdx.x % L + t * L) * PW + i < a.half;   // (the others stay what they are, infinities too)
-              const float was = re;
-              re = turned ? was * c[t][i] - im * s[t][i] : was;
-              im = turned ? im * c[t][i] + was * s[t][i] : im;
+            for (int e = 0; e < E; ++e) {
+              w[t][e] = has[t] && is ? own[i].template get<T>(t, e / PW, e % PW) : 0.f;
+              squares += w[t][e] * w[t][e];
             }
-          if constexpr (GAINS) {
-            float w[IT][E], squares = 0.f, along = 0.f;
-#pragma unroll
-            for (int t = 0; t < IT; ++t)
-#pragma unroll
-              for (int e = 0; e < E; ++e) {
-                w[t][e] = has[t] ? x[u][t][e / PW][e % PW] : 0.f;
-                squares += w[t][e] * w[t][e];
-              }
-            const float rstd = 1.f / sqrtf(sum_of<L>(squares) * a.inv_dim + a.eps);
-#pragma unroll
-            for (int t = 0; t < IT; ++t)
-#pragma unroll
-              for (int e = 0; e < E; ++e) {
-                w[t][e] *= rstd;
-                dg[t][e] += v[t][e] * w[t][e];
-                v[t][e] *= gain[t][e];
-                along += v[t][e] * w[t][e];
-              }
-            along = sum_of<L>(along) * a.inv_dim;
-#pragma unroll
-            for (int t = 0; t < IT; ++t)
-#pragma unroll
-              for (int e = 0; e < E; ++e) v[t][e] = rstd * (v[t][e] - w[t][e] * along);
-          }
+          const float rstd = 1.f / sqrtf(sum_of<L>(squares) * a.inv_dim + a.eps);
 #pragma unroll
           for (int t = 0; t < IT; ++t)
-            if (has[t]) {
 #pragma unroll
-              for (int k = 0; k < 2; ++k) {
-                Run<T, PW> o;
-#pragma unroll
-                for (int e = 0; e < PW; ++e) o.set(e, v[t][k * PW + e]);
-                o.store(q + h * ds.sh + at[t][k]);
-              }
+            for (int e = 0; e < E; ++e) {
+              w[t][e] *= rstd;
+              const float of_gain = v[t][e] * w[t][e];
+              if (u.kind == kQ) dg[0][t][e] += of_gain;
+              else dg[1][t][e] += of_gain;
+              v[t][e] *= gain[t * L * E + e];
+              along += v[t][e] * w[t][e];
             }
+          along = sum_of<L>(along) * a.inv_dim;
+#pragma unroll
+          for (int t = 0; t < IT; ++t)
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[t][e] = rstd * (v[t][e] - w[t][e] * along);
         }
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-          if (head < end) head += slots;
       }
-    };
-    walk(T{}, 0, a.n_q, a.src_q, a.src_qs, a.dst_q, a.dst_qs, a.x_q, a.gain_q, dg_q);
-    walk(K{}, a.n_q, a.n_q + a.n_k, a.src_k, a.src_ks, a.dst_k, a.dst_ks, a.x_k, a.gain_k, dg_k);
-    // values: as they are, in runs of E elements one behind the other
-    const int first_v = a.n_q + a.n_k, end = first_v + a.n_v;
-    if (head >= end) continue;
-    const K *p = reinterpret_cast<const K *>(a.src_v) + b * a.src_ks.sb + r * a.src_ks.ss;
-    T *q = reinterpret_cast<T *>(a.dst_v) + b * a.dst_ks.sb + r * a.dst_ks.ss;
-    while (head < end) {
-      Run<K, PW> in[U][IT][2];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int h = head + u * slots - first_v;
-        if (h >= a.n_v) break;
+      for (int t = 0; t < IT; ++t)
+        if (has[t] && is) {
 #pragma unroll
-        for (int t = 0; t < IT; ++t)
-          if (has[t]) {
+          for (int k = 0; k < 2; ++k) {
+            Run<T, PW> o;
 #pragma unroll
-            for (int k = 0; k < 2; ++k) in[u][t][k].load(p + h * a.src_ks.sh + E * (threadIdx.x % L + t * L) + k * PW);
+            for (int e = 0; e < PW; ++e) o.set(e, v[t][k * PW + e]);
+            o.store(to + h * ds.sh + (u.kind == kV ? straight[t][k] : at[t][k]));
           }
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int h = head + u * slots - first_v;
-        if (h >= a.n_v) break;
-#pragma unroll
-        for (int t = 0; t < IT; ++t)
-          if (has[t]) {
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              Run<T, PW> o;
-#pragma unroll
-              for (int e = 0; e < PW; ++e) o.set(e, in[u][t][k][e]);
-              o.store(q + h * a.dst_ks.sh + E * (threadIdx.x % L + t * L) + k * PW);
-            }
-          }
-      }
-      head += U * slots;
+        }
     }
   }
   if constexpr (GAINS) {   // the groups' sums of q, then of k, in their order; columns [item][element]
     constexpr int GROUPS = 256 / L, COLS = L * IT * E;
     __shared__ float sums[GROUPS][COLS + 1];
-    float *part = a.part + (int64_t)(blockIdx.y * gridDim.x + blockIdx.x) * 2 * a.dim;
+    float *part = a.part + (int64_t)blockIdx.x * 2 * a.dim;
 #pragma unroll
     for (int side = 0; side < 2; ++side) {
       __syncthreads();
 #pragma unroll
       for (int t = 0; t < IT; ++t)
 #pragma unroll
-        for (int e = 0; e < E; ++e) sums[group][(t * E + e) * L + threadIdx.x % L] = side ? dg_k[t][e] : dg_q[t][e];
+        for (int e = 0; e < E; ++e) sums[group][(t * E + e) * L + lane] = dg[side][t][e];
       __syncthreads();
       for (int col = threadIdx.x; col < COLS; col += 256) {
         const int item = col % L + col / (L * E) * L, e = col / L % E;
@@ -344,7 +375,9 @@ __global__ void __launch_bounds__(1024) rope_join_kernel(const RopeArgs a) {
 
 constexpr int64_t kMostTokens = int64_t(1) << 26;
 constexpr int32_t kMostHeads = 1 << 16, kMostDim = 256;
-constexpr int kMostParts = 1024;   // workgroups of a backward with the norm
+constexpr int kMostParts = 1024;                  // workgroups of a backward with the norm
+constexpr int64_t kMostGroups = 4096;             // workgroups of the other calls, about
+constexpr int64_t kMostTokenHeads = int64_t(1) << 31;   // (units of work are numbered in 32 bits)
 
 bool strides_fit(const s1f_heads *d, int heads, int64_t rows, int64_t sb, int64_t sh, int64_t ss) {
   return (rows == 1 || ss >= d->head_dim) && (heads == 1 || sh >= d->head_dim) && (d->batch == 1 || sb >= d->head_dim);
@@ -357,6 +390,7 @@ int check_heads(const s1f_heads *d) {
   if (d->rotary_dim < 0 || d->rotary_dim % 2 != 0 || d->rotary_dim > d->head_dim) return S1F_EINVAL;
   if (d->rows < 1) return S1F_ERANGE;
   if (d->rows > kMostTokens || d->batch * d->rows > kMostTokens) return S1F_EUNSUPPORTED;
+  if (d->batch * d->rows * (d->n_q_heads + 2 * (int64_t)d->n_kv_heads) > kMostTokenHeads) return S1F_EUNSUPPORTED;
   if (!strides_fit(d, d->n_q_heads, d->rows, d->q_stride_b, d->q_stride_h, d->q_stride_s) || !strides_fit(d, d->n_q_heads, d->rows, d->rot_stride_b, d->rot_stride_h, d->rot_stride_s) ||
       !strides_fit(d, d->n_kv_heads, d->rows, d->kv_stride_b, d->kv_stride_h, d->kv_stride_s) ||
       !strides_fit(d, d->n_kv_heads, d->cache_capacity, d->cache_stride_b, d->cache_stride_h, d->cache_stride_s))
@@ -385,8 +419,8 @@ struct Alignment {
 };
 
 // Pairs to a lane: as many as a row's halves and all addresses allow, 8 at most (16 bytes of bf16).
-int pairs_per_lane(const s1f_heads *d, const Alignment &typed, const Alignment &wide, int64_t esz) {
-  for (int pw = 8; pw > 1; pw /= 2) {
+int pairs_per_lane(const s1f_heads *d, int most, const Alignment &typed, const Alignment &wide, int64_t esz) {
+  for (int pw = most; pw > 1; pw /= 2) {
     if (d->head_dim % (2 * pw) != 0 || (!d->interleaved && d->rotary_dim / 2 % pw != 0)) continue;
     if (typed.at_least(pw * esz) && wide.at_least(pw * 4)) return pw;
   }
@@ -395,44 +429,39 @@ int pairs_per_lane(const s1f_heads *d, const Alignment &typed, const Alignment &
 
 struct Instance {
   void (*kernel)(RopeArgs);
-  int lanes;
+  int lanes, heads;   // to a row; of a lane at once
 };
 template <typename T, typename K, bool PAIRS, bool NORM, bool BACK> Instance instance_of(int pw, int items) {
-  if (pw == 8) {
-    if (items <= 4) return {&rope_kernel<T, K, 8, 4, 1, PAIRS, NORM, BACK>, 4};
-    if (items <= 8) return {&rope_kernel<T, K, 8, 8, 1, PAIRS, NORM, BACK>, 8};
-    return {&rope_kernel<T, K, 8, 16, 1, PAIRS, NORM, BACK>, 16};
+#define S1F_ROPE_INSTANCE(PW, L, IT, U) Instance{&rope_kernel<T, K, PW, L, IT, U, PAIRS, NORM, BACK>, L, U}
+  if constexpr (sizeof(T) == 2 && !BACK) {
+    if (pw == 8) return items <= 4 ? S1F_ROPE_INSTANCE(8, 4, 1, 4) : items <= 8 ? S1F_ROPE_INSTANCE(8, 8, 1, 4) : S1F_ROPE_INSTANCE(8, 16, 1, 4);
   }
-  if (pw == 4) {
-    if (items <= 16) return {&rope_kernel<T, K, 4, 16, 1, PAIRS, NORM, BACK>, 16};
-    return {&rope_kernel<T, K, 4, 32, 1, PAIRS, NORM, BACK>, 32};
-  }
-  if (pw == 2) {
-    if (items <= 32) return {&rope_kernel<T, K, 2, 32, 1, PAIRS, NORM, BACK>, 32};
-    return {&rope_kernel<T, K, 2, 64, 1, PAIRS, NORM, BACK>, 64};
-  }
-  return {&rope_kernel<T, K, 1, 64, 2, PAIRS, NORM, BACK>, 64};
+  if (pw == 4) return items <= 8 ? S1F_ROPE_INSTANCE(4, 8, 1, 4) : items <= 16 ? S1F_ROPE_INSTANCE(4, 16, 1, 4) : S1F_ROPE_INSTANCE(4, 32, 1, 4);
+  if (pw == 2) return items <= 32 ? S1F_ROPE_INSTANCE(2, 32, 1, 4) : S1F_ROPE_INSTANCE(2, 64, 1, 4);
+  return S1F_ROPE_INSTANCE(1, 64, 2, 4);
+#undef S1F_ROPE_INSTANCE
 }
 static_assert(kMostDim / 2 <= 64 * 2, "a row has a place in the lanes");
 
-// Rows side by side in a workgroup, and workgroups: x along the rows, y along the heads.
-struct Grid {
-  int log_rows;
-  int64_t x, y;
-};
-Grid grid_for(int64_t n, int heads, int lanes, bool gains) {
-  const int groups = 256 / lanes;
-  Grid g = {0, 0, 1};
-  while ((2 << g.log_rows) <= groups && (int64_t(1) << g.log_rows) < n) ++g.log_rows;
-  g.x = (n + (int64_t(1) << g.log_rows) - 1) >> g.log_rows;
-  const int slots = groups >> g.log_rows;
-  // one head to a group of lanes where there are few, four (those asked for together) where there are many workgroups
-  const int64_t most = gains ? kMostParts : 4096;
-  const int64_t y = (heads + slots - 1) / slots;
-  while (g.y < y && g.x * g.y * 2 <= most) g.y *= 2;
-  if (g.y > y) g.y = y;
-  g.x = std::min(g.x, gains ? (int64_t)kMostParts : int64_t(1) << 20);   // (workgroups walk the rows; threads of a launch stay below 2^32)
-  return g;
+// Units of work, and workgroups.
+int64_t cut_units(RopeArgs &a, const Instance &in, bool gains) {
+  const int groups = 256 / in.lanes;
+  a.log_rows = 0;
+  while ((2 << a.log_rows) <= groups && (int64_t(1) << a.log_rows) < a.n) ++a.log_rows;
+  a.unit_heads = (groups >> a.log_rows) * in.heads;
+  auto units = [&](int heads) { return (heads + a.unit_heads - 1) / a.unit_heads; };
+  a.units_q = units(a.n_q);
+  a.units_k = units(a.n_k);
+  a.units_v = units(a.n_v);
+  const int64_t blocks = ((int64_t)a.n + (int64_t(1) << a.log_rows) - 1) >> a.log_rows, per_block = a.units_q + a.units_k + a.units_v, all = blocks * per_block;
+  a.by_units = Divisor::of(per_block);
+  a.units = (int32_t)all;
+  int64_t grid = gains ? std::min<int64_t>(all, kMostParts) : all;
+  if (!gains && all > kMostGroups) grid = (all + (all + kMostGroups - 1) / kMostGroups - 1) / ((all + kMostGroups - 1) / kMostGroups);
+  a.per_group = (int32_t)(all / grid);
+  a.remainder = (int32_t)(all % grid);
+  a.parts = (int32_t)grid;
+  return grid;
 }
 
 RopeArgs args_of(const s1f_heads *d, const double *freqs, float magnitude, const int64_t *positions, int64_t positions_sb, int64_t first_position) {
@@ -458,7 +487,7 @@ template <bool NORM, bool BACK> int launch(const s1f_heads *d, RopeArgs a, hipSt
   for (const void *p : {a.src_q, (const void *)a.dst_q, (const void *)a.dst_k, (const void *)a.dst_v, a.x_q, a.x_k, a.gain_q, a.gain_k}) typed.pointer(p);
   kv.pointer(a.src_k);
   kv.pointer(a.src_v);
-  const int pw = pairs_per_lane(d, typed, wide, esz);
+  const int pw = pairs_per_lane(d, esz == 2 && !BACK ? 8 : 4, typed, wide, esz);
   a.items = d->head_dim / (2 * pw);
   auto pick = [&](auto t, auto k) {
     typedef decltype(t) T;
@@ -466,12 +495,9 @@ template <bool NORM, bool BACK> int launch(const s1f_heads *d, RopeArgs a, hipSt
     return d->interleaved ? instance_of<T, K, true, NORM, BACK>(pw, a.items) : instance_of<T, K, false, NORM, BACK>(pw, a.items);
   };
   const Instance in = d->dtype == S1F_F32 ? pick(float{}, float{}) : BACK ? pick(bf16_t{}, float{}) : pick(bf16_t{}, bf16_t{});
-  const Grid g = grid_for(a.n, a.n_q + a.n_k + a.n_v, in.lanes, NORM && BACK);
-  a.log_rows = g.log_rows;
-  a.parts = (int32_t)(g.x * g.y);
-  void *params[] = {&a};
-  if (hipLaunchKernel(reinterpret_cast<const void *>(in.kernel), dim3((unsigned)g.x, (unsigned)g.y), dim3(256), params, 0, st) != hipSuccess) return S1F_EDEVICE;
-  if (!(NORM && BACK)) return S1F_OK;
+  const int64_t grid = cut_units(a, in, NORM && BACK);
+  const int e = launch_rows_kernel(in.kernel, grid, 256, a, st);
+  if (e != S1F_OK || !(NORM && BACK)) return e;
   return launch_rows_kernel(&rope_join_kernel, (2 * a.dim + 63) / 64, 1024, a, st);
 }
 
