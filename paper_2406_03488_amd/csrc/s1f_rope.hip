@@ -11,8 +11,10 @@
 // another lane for anything.  Angles are products in 64 bits: at position 2^20 one in 32 bits is off by 2^-4.  The norm's sums are fp32, as is everything between
 // load and store; results are rounded once.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <initializer_list>
+#include <type_traits>
 
 #include "rows.hpp"
 
@@ -39,7 +41,7 @@ struct RopeArgs {
   int32_t n_q, n_k, n_v;                // heads: the list of a row's heads is q, k, v
   // Units of work: 2^log_rows rows of up to `unit_heads` heads of one of the tensors; units_q, units_k, units_v to a block of rows, all blocks one behind the other,
   // `per_group` consecutive ones (the remainder one more each) to a workgroup
-  int32_t log_rows, unit_heads, units_q, units_k, units_v;
+  int32_t log_rows, at_once, unit_heads, units_q, units_k, units_v;   // at_once: heads of a lane in a unit
   Divisor by_units;
   int32_t units, per_group, remainder;
   int32_t parts;
@@ -55,11 +57,15 @@ template <typename T, int N> struct Run {
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) v[i] = reinterpret_cast<const Vec *>(p)[i];
   }
-  S1F_DEV float operator[](int e) const { return (float)v[e / PIECE][e % PIECE]; }
-  S1F_DEV void set(int e, float x) { v[e / PIECE][e % PIECE] = (T)x; }
-  S1F_DEV void store(T *p) const {
+  S1F_DEV static void store(T *p, const float *x) {
+    typedef float Floats __attribute__((ext_vector_type(PIECE)));
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) reinterpret_cast<Vec *>(p)[i] = v[i];
+    for (int i = 0; i < PIECES; ++i) {
+      Floats f;
+#pragma unroll
+      for (int e = 0; e < PIECE; ++e) f[e] = x[i * PIECE + e];
+      reinterpret_cast<Vec *>(p)[i] = __builtin_convertvector(f, Vec);
+    }
   }
 };
 
@@ -112,18 +118,17 @@ template <int PW, bool PAIRS> struct Share {
 // A lane's elements of a head as they lie in memory: fp32, or bf16 in half as many words.
 template <int PW, int IT> struct Raw {
   uint32_t w[IT][2][PW];
-  template <typename S> S1F_DEV void load(const S *p, const int (&at)[IT][2], const bool (&has)[IT]) {
+  template <typename S> S1F_DEV void load(const S *p, const int (&at)[IT][2]) {
     typedef Run<S, PW> R;
 #pragma unroll
     for (int t = 0; t < IT; ++t)
 #pragma unroll
-      for (int k = 0; k < 2; ++k)
-        if (has[t]) {
-          R r;
-          r.load(p + at[t][k]);
-          if constexpr (sizeof(S) == 2 && PW == 1) w[t][k][0] = __builtin_bit_cast(uint16_t, r.v[0][0]);
-          else __builtin_memcpy(w[t][k], r.v, sizeof(S) * PW);
-        }
+      for (int k = 0; k < 2; ++k) {
+        R r;
+        r.load(p + at[t][k]);
+        if constexpr (sizeof(S) == 2 && PW == 1) w[t][k][0] = __builtin_bit_cast(uint16_t, r.v[0][0]);
+        else __builtin_memcpy(w[t][k], r.v, sizeof(S) * PW);
+      }
   }
   template <typename S> S1F_DEV float get(int t, int k, int e) const {
     if constexpr (sizeof(S) == 4) return __builtin_bit_cast(float, w[t][k][e]);
@@ -143,62 +148,86 @@ S1F_DEV Unit unit_of(const RopeArgs &a, int unit) {
 }
 
 // T: type of the tensors, K: of the keys' and values' source (fp32 accumulators in the backward).  L lanes to a row, IT shares to a lane, U heads to a lane and unit.  BACK: turn back.
-// The groups of L lanes that a workgroup has beyond its 2^log_rows rows share the heads of a unit.  The elements of the next unit are asked for before those of this one are
-// worked on, and those of the first before the angles are computed.
+// The groups of L lanes that a workgroup has beyond its 2^log_rows rows share the heads of a unit.  A head of the next unit is asked for as soon as this one's has become numbers, and
+// the first unit before the angles are computed.  Lanes without a share, a row or a head of their own work on another's and leave nothing behind.
 template <typename T, typename K, int PW, int L, int IT, int U, bool PAIRS, bool NORM, bool BACK> __global__ void __launch_bounds__(256) rope_kernel(const RopeArgs a) {
-  constexpr int E = 2 * PW;
+  constexpr int E = 2 * PW, GAIN_COLS = L * IT * E;
   constexpr bool GAINS = NORM && BACK;
-  __shared__ float gains[NORM ? 2 : 1][NORM ? L * IT * E : 1];
+  __shared__ __attribute__((aligned(16))) float gains[NORM ? 2 * GAIN_COLS : 1];
   const int lane = threadIdx.x % L, group = threadIdx.x / L, in_row = group & ((1 << a.log_rows) - 1), slot = group >> a.log_rows, slots = (256 / L) >> a.log_rows;
   const int g = blockIdx.x, first = g * a.per_group + (g < a.remainder ? g : a.remainder), last = first + a.per_group + (g < a.remainder ? 1 : 0);
-  bool has[IT], here[IT];
+  bool has[IT];
   int at[IT][2], straight[IT][2];   // the lane's elements of a row, and of values, which are not turned
 #pragma unroll
   for (int t = 0; t < IT; ++t) {
-    const int item = lane + t * L;
-    const Share<PW, PAIRS> share(a, item);
+    const int item = lane + t * L, known = item < a.items ? item : 0;
+    const Share<PW, PAIRS> share(a, known);
     has[t] = item < a.items;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       at[t][k] = share.at[k];
-      straight[t][k] = item * E + k * PW;
+      straight[t][k] = known * E + k * PW;
     }
   }
-  int b = 0, r = 0, block = -1;
-  bool row_is = false;
-  auto go_to = [&](int to) {
-    block = to;
-    const int row = (to << a.log_rows) + in_row;
+  int b, r;
+  bool row_is;
+  auto go_to = [&](int block) {
+    const int row = (block << a.log_rows) + in_row;
     row_is = row < a.n;
     div_mod(row_is ? row : a.n - 1, a.by_rows, b, r);
   };
+  auto heads_of = [&](const Unit &u) { return u.kind == kQ ? a.n_q : a.n_k; };
+  auto head_of = [&](const Unit &u, int i) { return u.head + slot + i * slots; };
   Raw<PW, IT> in[U], x[GAINS ? U : 1];
-  auto ask = [&](const Unit &u) {
-    const int heads = u.kind == kQ ? a.n_q : a.n_k;
+  auto ask = [&](const Unit &u, int i) {
+    if (i >= a.at_once) return;
+    const int heads = heads_of(u), own = head_of(u, i), h = own < heads ? own : heads - 1;
     const HeadStrides &ss = u.kind == kQ ? a.src_qs : a.src_ks, &xs = u.kind == kQ ? a.dst_qs : a.dst_ks;
-    const int64_t from = b * ss.sb + r * ss.ss, from_x = b * xs.sb + r * xs.ss;
-#pragma unroll
-    for (int t = 0; t < IT; ++t) here[t] = has[t] && row_is;
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const int h = u.head + slot + i * slots;
-      if (h >= heads) break;
-      if (u.kind == kQ) in[i].load(reinterpret_cast<const T *>(a.src_q) + from + h * ss.sh, at, here);
-      else if (u.kind == kK) in[i].load(reinterpret_cast<const K *>(a.src_k) + from + h * ss.sh, at, here);
-      else in[i].load(reinterpret_cast<const K *>(a.src_v) + from + h * ss.sh, straight, here);
-      if constexpr (GAINS)
-        if (u.kind != kV) x[i].load(reinterpret_cast<const T *>(u.kind == kQ ? a.x_q : a.x_k) + from_x + h * xs.sh, at, here);
-    }
+    const int64_t from = b * ss.sb + r * ss.ss + h * ss.sh;
+    if (u.kind == kQ) in[i].load(reinterpret_cast<const T *>(a.src_q) + from, at);
+    else if (u.kind == kK) in[i].load(reinterpret_cast<const K *>(a.src_k) + from, at);
+    else in[i].load(reinterpret_cast<const K *>(a.src_v) + from, straight);
+    if constexpr (GAINS)
+      if (u.kind != kV) x[i].load(reinterpret_cast<const T *>(u.kind == kQ ? a.x_q : a.x_k) + b * xs.sb + r * xs.ss + h * xs.sh, at);
   };
-  Unit now = unit_of(a, first);
-  go_to(now.block);
-  if (first < last) ask(now);
-  if constexpr (NORM) {
-    for (int i = threadIdx.x; i < 2 * L * IT * E; i += 256) {
-      const int side = i / (L * IT * E), col = i % (L * IT * E), item = col / E, e = col % E;
+  Unit next = unit_of(a, first);
+  go_to(next.block);
+#pragma unroll
+  for (int i = 0; i < U; ++i) ask(next, i);
+  float c[IT][PW], s[IT][PW];
+  auto angles = [&]() {
+    const int64_t position = a.positions ? a.positions[b * a.positions_sb + r] : a.first_position + r;
+#pragma unroll
+    for (int t = 0; t < IT; ++t)
+#pragma unroll
+      for (int i = 0; i < PW; ++i) {
+        const int pair = (lane + t * L) * PW + i;
+        c[t][i] = 1.f;
+        s[t][i] = 0.f;
+        if (pair < a.half) {
+          cos_sin((double)position * a.freqs[pair], c[t][i], s[t][i]);
+          c[t][i] *= a.magnitude;
+          s[t][i] *= BACK ? -a.magnitude : a.magnitude;
+        }
+      }
+  };
+  int angles_of = -1;
+  if constexpr (NORM) {   // (under the angles' latencies)
+    constexpr int PER = (2 * GAIN_COLS + 255) / 256;
+    float gain[PER];
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+      const int i = threadIdx.x + 256 * p, side = i / GAIN_COLS, col = i % GAIN_COLS, item = col / E, e = col % E;
       const Share<PW, PAIRS> share(a, item);
-      gains[side][col] = item < a.items ? (float)reinterpret_cast<const T *>(side ? a.gain_k : a.gain_q)[share.at[e / PW] + e % PW] : 0.f;
+      gain[p] = side < 2 && item < a.items ? (float)reinterpret_cast<const T *>(side ? a.gain_k : a.gain_q)[share.at[e / PW] + e % PW] : 0.f;
     }
+    if (next.kind != kV) {
+      angles();
+      angles_of = next.block;
+    }
+#pragma unroll
+    for (int p = 0; p < PER; ++p)
+      if (threadIdx.x + 256 * p < 2 * GAIN_COLS) gains[threadIdx.x + 256 * p] = gain[p];
     __syncthreads();
   }
   float dg[2][IT][E];
@@ -208,68 +237,57 @@ template <typename T, typename K, int PW, int L, int IT, int U, bool PAIRS, bool
 #pragma unroll
       for (int e = 0; e < E; ++e) dg[0][t][e] = dg[1][t][e] = 0.f;
   }
-  float c[IT][PW], s[IT][PW];
-  int angles_of = -1;
 #pragma unroll 1
   for (int unit = first; unit < last; ++unit) {
-    const Unit u = now;
-    const bool is = row_is;
-    const int ub = b, ur = r;
+    const Unit u = next;
     if (u.kind != kV && angles_of != u.block) {
       angles_of = u.block;
-      const int64_t position = a.positions ? a.positions[b * a.positions_sb + r] : a.first_position + r;
-#pragma unroll
-      for (int t = 0; t < IT; ++t)
-#pragma unroll
-        for (int i = 0; i < PW; ++i) {
-          const int pair = (lane + t * L) * PW + i;
-          c[t][i] = 1.f;
-          s[t][i] = 0.f;
-          if (pair < a.half) {
-            cos_sin((double)position * a.freqs[pair], c[t][i], s[t][i]);
-            c[t][i] *= a.magnitude;
-            s[t][i] *= BACK ? -a.magnitude : a.magnitude;
-          }
-        }
+      angles();
     }
-    // the unit's elements as numbers; then the next unit's are asked for
-    Raw<PW, IT> mine[U], own[GAINS ? U : 1];
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-      mine[i] = in[i];
-      if constexpr (GAINS) own[i] = x[i];
-    }
-    if (unit + 1 < last) {
-      now = unit_of(a, unit + 1);
-      if (now.block != block) go_to(now.block);
-      ask(now);
-    }
-    const int heads = u.kind == kQ ? a.n_q : a.n_k;
+    const bool is = row_is, more = unit + 1 < last;
+    const int heads = heads_of(u);
     const HeadStrides &ds = u.kind == kQ ? a.dst_qs : a.dst_ks;
-    T *to = reinterpret_cast<T *>(u.kind == kQ ? a.dst_q : u.kind == kK ? a.dst_k : a.dst_v) + ub * ds.sb + ur * ds.ss;
-    const bool wide = sizeof(K) == 4 && u.kind != kQ;   // (where T and K differ)
+    T *to = reinterpret_cast<T *>(u.kind == kQ ? a.dst_q : u.kind == kK ? a.dst_k : a.dst_v) + b * ds.sb + r * ds.ss;
+    if (more) {
+      next = unit_of(a, unit + 1);
+      if (next.block != u.block) go_to(next.block);
+    }
+    float of_unit[IT][E];
+#pragma unroll
+    for (int t = 0; t < IT; ++t)
+#pragma unroll
+      for (int e = 0; e < E; ++e) of_unit[t][e] = 0.f;
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      const int h = u.head + slot + i * slots;
-      if (h >= heads) break;
-      float v[IT][E];
+      if (i >= a.at_once) break;
+      const int h = head_of(u, i);
+      const bool mine = is && h < heads;
+      float v[IT][E], w[IT][E];
 #pragma unroll
       for (int t = 0; t < IT; ++t)
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-          const float narrow = mine[i].template get<T>(t, e / PW, e % PW);
-          v[t][e] = sizeof(T) != sizeof(K) && wide ? mine[i].template get<K>(t, e / PW, e % PW) : narrow;
-          if (!has[t] || !is) v[t][e] = 0.f;
+          if (sizeof(T) != sizeof(K) && u.kind != kQ) v[t][e] = in[i].template get<K>(t, e / PW, e % PW);
+          else v[t][e] = in[i].template get<T>(t, e / PW, e % PW);
+          if constexpr (GAINS) w[t][e] = x[i].template get<T>(t, e / PW, e % PW);
         }
+      if (more) ask(next, i);
       if (u.kind != kV) {
-        const float *gain = &gains[NORM && u.kind == kK ? 1 : 0][NORM ? lane * E : 0];
-        if constexpr (NORM && !BACK) {
+        const float *gain = gains + (NORM ? (u.kind == kQ ? 0 : GAIN_COLS) + lane * E : 0);
+        // sum of squares of a row, and one over the root of their mean
+        auto rstd_of = [&](const float (&y)[IT][E]) {
           float sum = 0.f;
 #pragma unroll
-          for (int t = 0; t < IT; ++t)
+          for (int t = 0; t < IT; ++t) {
+            float part = 0.f;
 #pragma unroll
-            for (int e = 0; e < E; ++e) sum += v[t][e] * v[t][e];
-          const float rstd = 1.f / sqrtf(sum_of<L>(sum) * a.inv_dim + a.eps);
+            for (int e = 0; e < E; ++e) part = fmaf(y[t][e], y[t][e], part);
+            sum += has[t] ? part : 0.f;
+          }
+          return __builtin_amdgcn_rsqf(fmaf(sum_of<L>(sum), a.inv_dim, a.eps));
+        };
+        if constexpr (NORM && !BACK) {
+          const float rstd = rstd_of(v);
 #pragma unroll
           for (int t = 0; t < IT; ++t)
 #pragma unroll
@@ -287,26 +305,19 @@ template <typename T, typename K, int PW, int L, int IT, int U, bool PAIRS, bool
             im = turned ? im * c[t][p] + was * s[t][p] : im;
           }
         if constexpr (GAINS) {
-          float w[IT][E], squares = 0.f, along = 0.f;
+          const float rstd = rstd_of(w);
+          float along = 0.f;
 #pragma unroll
-          for (int t = 0; t < IT; ++t)
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-              w[t][e] = has[t] && is ? own[i].template get<T>(t, e / PW, e % PW) : 0.f;
-              squares += w[t][e] * w[t][e];
-            }
-          const float rstd = 1.f / sqrtf(sum_of<L>(squares) * a.inv_dim + a.eps);
-#pragma unroll
-          for (int t = 0; t < IT; ++t)
+          for (int t = 0; t < IT; ++t) {
+            const float by = mine && has[t] ? rstd : 0.f;
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-              w[t][e] *= rstd;
-              const float of_gain = v[t][e] * w[t][e];
-              if (u.kind == kQ) dg[0][t][e] += of_gain;
-              else dg[1][t][e] += of_gain;
+              w[t][e] *= by;
+              of_unit[t][e] = fmaf(v[t][e], w[t][e], of_unit[t][e]);
               v[t][e] *= gain[t * L * E + e];
-              along += v[t][e] * w[t][e];
+              along = fmaf(v[t][e], w[t][e], along);
             }
+          }
           along = sum_of<L>(along) * a.inv_dim;
 #pragma unroll
           for (int t = 0; t < IT; ++t)
@@ -316,14 +327,18 @@ template <typename T, typename K, int PW, int L, int IT, int U, bool PAIRS, bool
       }
 #pragma unroll
       for (int t = 0; t < IT; ++t)
-        if (has[t] && is) {
+        if (has[t] && mine) {
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            Run<T, PW> o;
+          for (int k = 0; k < 2; ++k) Run<T, PW>::store(to + h * ds.sh + (u.kind == kV ? straight[t][k] : at[t][k]), &v[t][k * PW]);
+        }
+    }
+    if constexpr (GAINS) {
 #pragma unroll
-            for (int e = 0; e < PW; ++e) o.set(e, v[t][k * PW + e]);
-            o.store(to + h * ds.sh + (u.kind == kV ? straight[t][k] : at[t][k]));
-          }
+      for (int t = 0; t < IT; ++t)
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          if (u.kind == kQ) dg[0][t][e] += of_unit[t][e];
+          else if (u.kind == kK) dg[1][t][e] += of_unit[t][e];
         }
     }
   }
@@ -375,8 +390,9 @@ __global__ void __launch_bounds__(1024) rope_join_kernel(const RopeArgs a) {
 
 constexpr int64_t kMostTokens = int64_t(1) << 26;
 constexpr int32_t kMostHeads = 1 << 16, kMostDim = 256;
-constexpr int kMostParts = 1024;                  // workgroups of a backward with the norm
+constexpr int kMostParts = 2048;                  // workgroups of a backward with the norm: as many as the device holds at once, each an equal share
 constexpr int64_t kMostGroups = 4096;             // workgroups of the other calls, about
+constexpr int64_t kFew = int64_t(1) << 20;
 constexpr int64_t kMostTokenHeads = int64_t(1) << 31;   // (units of work are numbered in 32 bits)
 
 bool strides_fit(const s1f_heads *d, int heads, int64_t rows, int64_t sb, int64_t sh, int64_t ss) {
@@ -427,36 +443,59 @@ int pairs_per_lane(const s1f_heads *d, int most, const Alignment &typed, const A
   return 1;
 }
 
+// Workgroups of a kernel that the device holds at once, asked once per device.
+template <auto KERNEL> int held_at_once() {
+  static std::atomic<int> known[64];
+  int dev = 0, per_unit = 0, units = 0;
+  if (hipGetDevice(&dev) != hipSuccess) return 512;
+  const bool cached = dev >= 0 && dev < 64;
+  if (cached && known[dev].load(std::memory_order_acquire) > 0) return known[dev].load(std::memory_order_acquire);
+  if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_unit, reinterpret_cast<const void *>(KERNEL), 256, 0) != hipSuccess ||
+      hipDeviceGetAttribute(&units, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || per_unit < 1 || units < 1) {
+    (void)hipGetLastError();
+    return 512;
+  }
+  if (cached) known[dev].store(per_unit * units, std::memory_order_release);
+  return per_unit * units;
+}
 struct Instance {
   void (*kernel)(RopeArgs);
+  int (*held)();
   int lanes, heads;   // to a row; of a lane at once
 };
 template <typename T, typename K, bool PAIRS, bool NORM, bool BACK> Instance instance_of(int pw, int items) {
-#define S1F_ROPE_INSTANCE(PW, L, IT, U) Instance{&rope_kernel<T, K, PW, L, IT, U, PAIRS, NORM, BACK>, L, U}
+#define S1F_ROPE_INSTANCE(PW, L, IT, U) Instance{&rope_kernel<T, K, PW, L, IT, U, PAIRS, NORM, BACK>, &held_at_once<&rope_kernel<T, K, PW, L, IT, U, PAIRS, NORM, BACK>>, L, U}
   if constexpr (sizeof(T) == 2 && !BACK) {
     if (pw == 8) return items <= 4 ? S1F_ROPE_INSTANCE(8, 4, 1, 4) : items <= 8 ? S1F_ROPE_INSTANCE(8, 8, 1, 4) : S1F_ROPE_INSTANCE(8, 16, 1, 4);
   }
-  if (pw == 4) return items <= 8 ? S1F_ROPE_INSTANCE(4, 8, 1, 4) : items <= 16 ? S1F_ROPE_INSTANCE(4, 16, 1, 4) : S1F_ROPE_INSTANCE(4, 32, 1, 4);
-  if (pw == 2) return items <= 32 ? S1F_ROPE_INSTANCE(2, 32, 1, 4) : S1F_ROPE_INSTANCE(2, 64, 1, 4);
-  return S1F_ROPE_INSTANCE(1, 64, 2, 4);
+  if (pw == 4) return items <= 8 ? S1F_ROPE_INSTANCE(4, 8, 1, (NORM && BACK ? 2 : 4)) : items <= 16 ? S1F_ROPE_INSTANCE(4, 16, 1, (NORM && BACK ? 2 : 4)) : S1F_ROPE_INSTANCE(4, 32, 1, (NORM && BACK ? 2 : 4));
+  if (pw == 2) return items <= 24 ? S1F_ROPE_INSTANCE(2, 8, 3, 2) : items <= 48 ? S1F_ROPE_INSTANCE(2, 16, 3, 2) : S1F_ROPE_INSTANCE(2, 32, 2, 4);
+  return items <= 64 ? S1F_ROPE_INSTANCE(1, 8, 8, 2) : S1F_ROPE_INSTANCE(1, 16, 8, 2);
 #undef S1F_ROPE_INSTANCE
 }
-static_assert(kMostDim / 2 <= 64 * 2, "a row has a place in the lanes");
+static_assert(kMostDim / 2 <= 16 * 8 && kMostDim / 4 <= 32 * 2 && kMostDim / 8 <= 32 && kMostDim / 16 <= 16, "a row has a place in the lanes");
 
 // Units of work, and workgroups.
 int64_t cut_units(RopeArgs &a, const Instance &in, bool gains) {
   const int groups = 256 / in.lanes;
   a.log_rows = 0;
   while ((2 << a.log_rows) <= groups && (int64_t(1) << a.log_rows) < a.n) ++a.log_rows;
-  a.unit_heads = (groups >> a.log_rows) * in.heads;
-  auto units = [&](int heads) { return (heads + a.unit_heads - 1) / a.unit_heads; };
-  a.units_q = units(a.n_q);
-  a.units_k = units(a.n_k);
-  a.units_v = units(a.n_v);
-  const int64_t blocks = ((int64_t)a.n + (int64_t(1) << a.log_rows) - 1) >> a.log_rows, per_block = a.units_q + a.units_k + a.units_v, all = blocks * per_block;
+  const int64_t blocks = ((int64_t)a.n + (int64_t(1) << a.log_rows) - 1) >> a.log_rows;
+  int64_t per_block = 0;
+  // (fewer heads to a unit where there would not be a unit for every compute unit)
+  for (a.at_once = in.heads; ; a.at_once /= 2) {
+    a.unit_heads = (groups >> a.log_rows) * a.at_once;
+    auto units = [&](int heads) { return (heads + a.unit_heads - 1) / a.unit_heads; };
+    a.units_q = units(a.n_q);
+    a.units_k = units(a.n_k);
+    a.units_v = units(a.n_v);
+    per_block = a.units_q + a.units_k + a.units_v;
+    if (a.at_once == 1 || blocks * per_block >= 256) break;
+  }
+  const int64_t all = blocks * per_block;
   a.by_units = Divisor::of(per_block);
   a.units = (int32_t)all;
-  int64_t grid = gains ? std::min<int64_t>(all, kMostParts) : all;
+  int64_t grid = gains ? std::min<int64_t>({all, in.held(), kMostParts}) : all;
   if (!gains && all > kMostGroups) grid = (all + (all + kMostGroups - 1) / kMostGroups - 1) / ((all + kMostGroups - 1) / kMostGroups);
   a.per_group = (int32_t)(all / grid);
   a.remainder = (int32_t)(all % grid);
@@ -487,14 +526,16 @@ template <bool NORM, bool BACK> int launch(const s1f_heads *d, RopeArgs a, hipSt
   for (const void *p : {a.src_q, (const void *)a.dst_q, (const void *)a.dst_k, (const void *)a.dst_v, a.x_q, a.x_k, a.gain_q, a.gain_k}) typed.pointer(p);
   kv.pointer(a.src_k);
   kv.pointer(a.src_v);
-  const int pw = pairs_per_lane(d, esz == 2 && !BACK ? 8 : 4, typed, wide, esz);
+  // (16 bytes of either type to a lane, but for few elements, where twice the lanes compute half as many angles each)
+  const int64_t elements = (int64_t)a.n * (a.n_q + a.n_k + a.n_v) * a.dim;
+  const int pw = pairs_per_lane(d, esz == 2 && !BACK && elements > kFew ? 8 : 4, typed, wide, esz);
   a.items = d->head_dim / (2 * pw);
-  auto pick = [&](auto t, auto k) {
+  auto pick = [&](auto t) {
     typedef decltype(t) T;
-    typedef decltype(k) K;
+    typedef std::conditional_t<BACK, float, T> K;
     return d->interleaved ? instance_of<T, K, true, NORM, BACK>(pw, a.items) : instance_of<T, K, false, NORM, BACK>(pw, a.items);
   };
-  const Instance in = d->dtype == S1F_F32 ? pick(float{}, float{}) : BACK ? pick(bf16_t{}, float{}) : pick(bf16_t{}, bf16_t{});
+  const Instance in = d->dtype == S1F_F32 ? pick(float{}) : pick(bf16_t{});
   const int64_t grid = cut_units(a, in, NORM && BACK);
   const int e = launch_rows_kernel(in.kernel, grid, 256, a, st);
   if (e != S1F_OK || !(NORM && BACK)) return e;
