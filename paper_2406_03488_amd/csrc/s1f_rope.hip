@@ -43,6 +43,7 @@ struct RopeArgs {
   // `per_group` consecutive ones (the remainder one more each) to a workgroup
   int32_t log_rows, at_once, unit_heads, units_q, units_k, units_v;   // at_once: heads of a lane in a unit
   Divisor by_units;
+  int32_t step;                         // between units of a block that follow one another (see cut_units)
   int32_t units, per_group, remainder;
   int32_t parts;
   float magnitude, eps, inv_dim;
@@ -98,12 +99,17 @@ template <int L> S1F_DEV float sum_of(float x) {
   return x;
 }
 
-// The lane's share of a row: PW pairs, the elements [col(0), +PW) and [col(1), +PW).
-template <int PW, bool PAIRS> struct Share {
+// How a row's elements and its pairs are dealt out to lanes, PW pairs or 2 PW elements to each share.
+//   kHalves  pairs (i, i + half), where half is whole shares: a share has both elements of its pairs
+//   kPairs   pairs (2i, 2i + 1): likewise, and its elements are neighbours
+//   kAny     pairs (i, i + half), half whatever it is: a share is 2 PW neighbours, and the other elements of their pairs come through LDS
+enum Layout { kHalves, kPairs, kAny };
+// The lane's elements of a row: [at[0], +PW) and [at[1], +PW).
+template <int PW, Layout LAYOUT> struct Share {
   int at[2];
   S1F_DEV Share(const RopeArgs &a, int item) {
-    if (PAIRS || item * PW >= a.half) {
-      at[0] = PAIRS ? 2 * PW * item : a.rotary + 2 * (item * PW - a.half);
+    if (LAYOUT != kHalves || item * PW >= a.half) {
+      at[0] = LAYOUT != kHalves ? 2 * PW * item : a.rotary + 2 * (item * PW - a.half);
       at[1] = at[0] + PW;
     } else {
       at[0] = item * PW;
@@ -111,9 +117,15 @@ template <int PW, bool PAIRS> struct Share {
     }
   }
   // which of the lane's elements e < 2 PW is the first, the second of its pair i
-  S1F_DEV static constexpr int first(int i) { return PAIRS ? 2 * i : i; }
-  S1F_DEV static constexpr int second(int i) { return PAIRS ? 2 * i + 1 : PW + i; }
+  S1F_DEV static constexpr int first(int i) { return LAYOUT == kPairs ? 2 * i : i; }
+  S1F_DEV static constexpr int second(int i) { return LAYOUT == kPairs ? 2 * i + 1 : PW + i; }
 };
+// What a wave's lanes have written to LDS before is what they read there behind it.
+S1F_DEV void between_lanes() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 
 // A lane's elements of a head as they lie in memory: fp32, or bf16 in half as many words.
 template <int PW, int IT> struct Raw {
@@ -141,8 +153,9 @@ struct Unit {
   int block, kind, head;   // block of rows; tensor; first head
 };
 S1F_DEV Unit unit_of(const RopeArgs &a, int unit) {
-  int block, u;
+  int block, u, unused;
   div_mod(unit, a.by_units, block, u);
+  div_mod(u * a.step, a.by_units, unused, u);
   const int kind = u < a.units_q ? kQ : u < a.units_q + a.units_k ? kK : kV;
   return Unit{block, kind, (u - (kind == kQ ? 0 : kind == kK ? a.units_q : a.units_q + a.units_k)) * a.unit_heads};
 }
@@ -150,8 +163,9 @@ S1F_DEV Unit unit_of(const RopeArgs &a, int unit) {
 // T: type of the tensors, K: of the keys' and values' source (fp32 accumulators in the backward).  L lanes to a row, IT shares to a lane, U heads to a lane and unit.  BACK: turn back.
 // The groups of L lanes that a workgroup has beyond its 2^log_rows rows share the heads of a unit.  A head of the next unit is asked for as soon as this one's has become numbers, and
 // the first unit before the angles are computed.  Lanes without a share, a row or a head of their own work on another's and leave nothing behind.
-template <typename T, typename K, int PW, int L, int IT, int U, bool PAIRS, bool NORM, bool BACK> __global__ void __launch_bounds__(256) rope_kernel(const RopeArgs a) {
-  constexpr int E = 2 * PW, GAIN_COLS = L * IT * E;
+template <typename T, typename K, int PW, int L, int IT, int U, Layout LAYOUT, bool NORM, bool BACK> __global__ void __launch_bounds__(256) rope_kernel(const RopeArgs a) {
+  constexpr int E = 2 * PW, GAIN_COLS = L * IT * E, ANGLES = LAYOUT == kAny ? E : PW;   // ANGLES: of pairs, or (kAny) of elements
+  static_assert(LAYOUT != kAny || IT == 1, "one share to a lane");
   constexpr bool GAINS = NORM && BACK;
   __shared__ __attribute__((aligned(16))) float gains[NORM ? 2 * GAIN_COLS : 1];
   const int lane = threadIdx.x % L, group = threadIdx.x / L, in_row = group & ((1 << a.log_rows) - 1), slot = group >> a.log_rows, slots = (256 / L) >> a.log_rows;
@@ -161,7 +175,7 @@ template <typename T, typename K, int PW, int L, int IT, int U, bool PAIRS, bool
 #pragma unroll
   for (int t = 0; t < IT; ++t) {
     const int item = lane + t * L, known = item < a.items ? item : 0;
-    const Share<PW, PAIRS> share(a, known);
+    const Share<PW, LAYOUT> share(a, known);
     has[t] = item < a.items;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
@@ -194,20 +208,32 @@ template <typename T, typename K, int PW, int L, int IT, int U, bool PAIRS, bool
   go_to(next.block);
 #pragma unroll
   for (int i = 0; i < U; ++i) ask(next, i);
-  float c[IT][PW], s[IT][PW];
+  // kAny: elements of the wave's rows, element e of a lane at 64 e + lane, so that neither writes nor reads meet in a bank; where the lane's elements' partners are
+  __shared__ float exchange[LAYOUT == kAny ? 4 : 1][LAYOUT == kAny ? 64 * E : 1];
+  int partner[LAYOUT == kAny ? E : 1];
+  if constexpr (LAYOUT == kAny) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int i = lane * E + e, other = i < a.half ? i + a.half : i < a.rotary ? i - a.half : i;
+      partner[e] = other % E * 64 + other / E + ((int)threadIdx.x & 63) - lane;
+    }
+  }
+  float c[IT][ANGLES], s[IT][ANGLES];
   auto angles = [&]() {
     const int64_t position = a.positions ? a.positions[b * a.positions_sb + r] : a.first_position + r;
 #pragma unroll
     for (int t = 0; t < IT; ++t)
 #pragma unroll
-      for (int i = 0; i < PW; ++i) {
-        const int pair = (lane + t * L) * PW + i;
+      for (int i = 0; i < ANGLES; ++i) {
+        const int of = (lane + t * L) * ANGLES + i;
+        const bool second = LAYOUT == kAny && of >= a.half;
+        const int pair = second ? of - a.half : of;
         c[t][i] = 1.f;
         s[t][i] = 0.f;
         if (pair < a.half) {
           cos_sin((double)position * a.freqs[pair], c[t][i], s[t][i]);
           c[t][i] *= a.magnitude;
-          s[t][i] *= BACK ? -a.magnitude : a.magnitude;
+          s[t][i] *= BACK != second ? -a.magnitude : a.magnitude;
         }
       }
   };
@@ -218,7 +244,7 @@ template <typename T, typename K, int PW, int L, int IT, int U, bool PAIRS, bool
 #pragma unroll
     for (int p = 0; p < PER; ++p) {
       const int i = threadIdx.x + 256 * p, side = i / GAIN_COLS, col = i % GAIN_COLS, item = col / E, e = col % E;
-      const Share<PW, PAIRS> share(a, item);
+      const Share<PW, LAYOUT> share(a, item);
       gain[p] = side < 2 && item < a.items ? (float)reinterpret_cast<const T *>(side ? a.gain_k : a.gain_q)[share.at[e / PW] + e % PW] : 0.f;
     }
     if (next.kind != kV) {
@@ -293,17 +319,30 @@ template <typename T, typename K, int PW, int L, int IT, int U, bool PAIRS, bool
 #pragma unroll
             for (int e = 0; e < E; ++e) v[t][e] = v[t][e] * rstd * gain[t * L * E + e];
         }
+        if constexpr (LAYOUT == kAny) {
+          float *of_wave = exchange[threadIdx.x >> 6];
 #pragma unroll
-        for (int t = 0; t < IT; ++t)
+          for (int e = 0; e < E; ++e) of_wave[64 * e + (threadIdx.x & 63)] = v[0][e];
+          between_lanes();
 #pragma unroll
-          for (int p = 0; p < PW; ++p) {
-            constexpr auto F = &Share<PW, PAIRS>::first, G = &Share<PW, PAIRS>::second;
-            float &re = v[t][F(p)], &im = v[t][G(p)];
-            const bool turned = (lane + t * L) * PW + p < a.half;   // (the others stay what they are, infinities too)
-            const float was = re;
-            re = turned ? was * c[t][p] - im * s[t][p] : was;
-            im = turned ? im * c[t][p] + was * s[t][p] : im;
+          for (int e = 0; e < E; ++e) {
+            const float other = of_wave[partner[e]];
+            v[0][e] = lane * E + e < a.rotary ? v[0][e] * c[0][e] - other * s[0][e] : v[0][e];
           }
+          between_lanes();
+        } else {
+#pragma unroll
+          for (int t = 0; t < IT; ++t)
+#pragma unroll
+            for (int p = 0; p < PW; ++p) {
+              constexpr auto F = &Share<PW, LAYOUT>::first, G = &Share<PW, LAYOUT>::second;
+              float &re = v[t][F(p)], &im = v[t][G(p)];
+              const bool turned = (lane + t * L) * PW + p < a.half;   // (the others stay what they are, infinities too)
+              const float was = re;
+              re = turned ? was * c[t][p] - im * s[t][p] : was;
+              im = turned ? im * c[t][p] + was * s[t][p] : im;
+            }
+        }
         if constexpr (GAINS) {
           const float rstd = rstd_of(w);
           float along = 0.f;
@@ -359,29 +398,30 @@ template <typename T, typename K, int PW, int L, int IT, int U, bool PAIRS, bool
         if (item >= a.items) continue;
         float sum = 0.f;
         for (int g = 0; g < GROUPS; ++g) sum += sums[g][col];
-        const Share<PW, PAIRS> share(a, item);
+        const Share<PW, LAYOUT> share(a, item);
         part[side * a.dim + share.at[e / PW] + e % PW] = sum;
       }
     }
   }
 }
 
-// Adds the workgroups' sums: 64 columns of [q, k][dim] per workgroup, its 16 waves a sixteenth of the parts each.
+// Adds the workgroups' sums: 16 columns of [q, k][dim] per workgroup, 64 shares of the parts (16 shares of 64 columns: chains of loads, 5.0 us for 768 parts of 160).
 __global__ void __launch_bounds__(1024) rope_join_kernel(const RopeArgs a) {
-  __shared__ float of_wave[16][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, width = 2 * a.dim, col = blockIdx.x * 64 + lane;
+  constexpr int SHARES = 64;
+  __shared__ float of_share[SHARES][16];
+  const int in = threadIdx.x & 15, share = threadIdx.x >> 4, width = 2 * a.dim, col = blockIdx.x * 16 + in;
   float sum = 0.f;
   if (col < width) {
-    const int begin = a.parts * wave / 16, end = a.parts * (wave + 1) / 16;
+    const int begin = a.parts * share / SHARES, end = a.parts * (share + 1) / SHARES;
 #pragma unroll 8
     for (int p = begin; p < end; ++p) sum += a.part[(int64_t)p * width + col];
   }
-  of_wave[wave][lane] = sum;
+  of_share[share][in] = sum;
   __syncthreads();
-  if (wave > 0 || col >= width) return;
+  if (share > 0 || col >= width) return;
   sum = 0.f;
-#pragma unroll
-  for (int w = 0; w < 16; ++w) sum += of_wave[w][lane];
+#pragma unroll 16
+  for (int w = 0; w < SHARES; ++w) sum += of_share[w][in];
   float *to = col < a.dim ? a.dgain_q + col : a.dgain_k + col - a.dim;
   *to += sum;
 }
@@ -434,13 +474,19 @@ struct Alignment {
   bool at_least(int64_t bytes) const { return (bits & (uint64_t)((bytes < 16 ? bytes : 16) - 1)) == 0; }
 };
 
-// Pairs to a lane: as many as a row's halves and all addresses allow, 8 at most (16 bytes of bf16).
-int pairs_per_lane(const s1f_heads *d, int most, const Alignment &typed, const Alignment &wide, int64_t esz) {
-  for (int pw = most; pw > 1; pw /= 2) {
-    if (d->head_dim % (2 * pw) != 0 || (!d->interleaved && d->rotary_dim / 2 % pw != 0)) continue;
-    if (typed.at_least(pw * esz) && wide.at_least(pw * 4)) return pw;
+// How a call's rows are dealt out, and pairs to a share: 8 or 4 (16 bytes) where addresses allow it, else 1.
+struct Dealt {
+  Layout layout;
+  int pairs;
+};
+Dealt deal(const s1f_heads *d, int most, const Alignment &typed, const Alignment &wide, int64_t esz) {
+  for (int pw = most; pw >= 4; pw /= 2) {
+    if (d->head_dim % (2 * pw) != 0 || !typed.at_least(pw * esz) || !wide.at_least(pw * 4)) continue;
+    if (d->interleaved) return {kPairs, pw};
+    if (d->rotary_dim / 2 % pw == 0) return {kHalves, pw};
+    if (pw == 4) return {kAny, pw};
   }
-  return 1;
+  return {d->interleaved ? kPairs : kHalves, 1};
 }
 
 // Workgroups of a kernel that the device holds at once, asked once per device.
@@ -463,17 +509,19 @@ struct Instance {
   int (*held)();
   int lanes, heads;   // to a row; of a lane at once
 };
-template <typename T, typename K, bool PAIRS, bool NORM, bool BACK> Instance instance_of(int pw, int items) {
-#define S1F_ROPE_INSTANCE(PW, L, IT, U) Instance{&rope_kernel<T, K, PW, L, IT, U, PAIRS, NORM, BACK>, &held_at_once<&rope_kernel<T, K, PW, L, IT, U, PAIRS, NORM, BACK>>, L, U}
-  if constexpr (sizeof(T) == 2 && !BACK) {
+template <typename T, typename K, Layout LAYOUT, bool NORM, bool BACK> Instance instance_of(int pw, int items) {
+#define S1F_ROPE_INSTANCE(PW, L, IT, U) Instance{&rope_kernel<T, K, PW, L, IT, U, LAYOUT, NORM, BACK>, &held_at_once<&rope_kernel<T, K, PW, L, IT, U, LAYOUT, NORM, BACK>>, L, U}
+  if constexpr (sizeof(T) == 2 && !BACK && LAYOUT != kAny) {
     if (pw == 8) return items <= 4 ? S1F_ROPE_INSTANCE(8, 4, 1, 4) : items <= 8 ? S1F_ROPE_INSTANCE(8, 8, 1, 4) : S1F_ROPE_INSTANCE(8, 16, 1, 4);
   }
-  if (pw == 4) return items <= 8 ? S1F_ROPE_INSTANCE(4, 8, 1, (NORM && BACK ? 2 : 4)) : items <= 16 ? S1F_ROPE_INSTANCE(4, 16, 1, (NORM && BACK ? 2 : 4)) : S1F_ROPE_INSTANCE(4, 32, 1, (NORM && BACK ? 2 : 4));
-  if (pw == 2) return items <= 24 ? S1F_ROPE_INSTANCE(2, 8, 3, 2) : items <= 48 ? S1F_ROPE_INSTANCE(2, 16, 3, 2) : S1F_ROPE_INSTANCE(2, 32, 2, 4);
-  return items <= 64 ? S1F_ROPE_INSTANCE(1, 8, 8, 2) : S1F_ROPE_INSTANCE(1, 16, 8, 2);
+  constexpr int U = NORM && BACK ? 2 : 4;
+  if constexpr (LAYOUT != kAny) {
+    if (pw == 1) return items <= 32 ? S1F_ROPE_INSTANCE(1, 8, 4, 2) : items <= 64 ? S1F_ROPE_INSTANCE(1, 16, 4, 2) : S1F_ROPE_INSTANCE(1, 32, 4, 2);
+  }
+  return items <= 8 ? S1F_ROPE_INSTANCE(4, 8, 1, U) : items <= 16 ? S1F_ROPE_INSTANCE(4, 16, 1, U) : S1F_ROPE_INSTANCE(4, 32, 1, U);
 #undef S1F_ROPE_INSTANCE
 }
-static_assert(kMostDim / 2 <= 16 * 8 && kMostDim / 4 <= 32 * 2 && kMostDim / 8 <= 32 && kMostDim / 16 <= 16, "a row has a place in the lanes");
+static_assert(kMostDim / 2 <= 32 * 4 && kMostDim / 8 <= 32 && kMostDim / 16 <= 16, "a row has a place in the lanes");
 
 // Units of work, and workgroups.
 int64_t cut_units(RopeArgs &a, const Instance &in, bool gains) {
@@ -494,6 +542,15 @@ int64_t cut_units(RopeArgs &a, const Instance &in, bool gains) {
   }
   const int64_t all = blocks * per_block;
   a.by_units = Divisor::of(per_block);
+  // Consecutive units take the tensors in turn: values are less work than the others, and a workgroup's share of some ten units would be of one kind: gradient of 2 x 1357 rows of
+  // 3 x 32 heads of 80 64.4 -> 62.8 us.
+  auto common = [](int64_t x, int64_t y) {
+    while (y) std::swap(x %= y, y);
+    return x;
+  };
+  a.step = 1;
+  if (gains && per_block > 2 && per_block < 32768)
+    for (a.step = (int32_t)(per_block * 0.618); common(per_block, a.step) != 1; ++a.step) {}
   a.units = (int32_t)all;
   int64_t grid = gains ? std::min<int64_t>({all, in.held(), kMostParts}) : all;
   if (!gains && all > kMostGroups) grid = (all + (all + kMostGroups - 1) / kMostGroups - 1) / ((all + kMostGroups - 1) / kMostGroups);
@@ -528,18 +585,20 @@ template <bool NORM, bool BACK> int launch(const s1f_heads *d, RopeArgs a, hipSt
   kv.pointer(a.src_v);
   // (16 bytes of either type to a lane, but for few elements, where twice the lanes compute half as many angles each)
   const int64_t elements = (int64_t)a.n * (a.n_q + a.n_k + a.n_v) * a.dim;
-  const int pw = pairs_per_lane(d, esz == 2 && !BACK && elements > kFew ? 8 : 4, typed, wide, esz);
-  a.items = d->head_dim / (2 * pw);
+  const Dealt dealt = deal(d, esz == 2 && !BACK && elements > kFew ? 8 : 4, typed, wide, esz);
+  a.items = d->head_dim / (2 * dealt.pairs);
   auto pick = [&](auto t) {
     typedef decltype(t) T;
     typedef std::conditional_t<BACK, float, T> K;
-    return d->interleaved ? instance_of<T, K, true, NORM, BACK>(pw, a.items) : instance_of<T, K, false, NORM, BACK>(pw, a.items);
+    if (dealt.layout == kPairs) return instance_of<T, K, kPairs, NORM, BACK>(dealt.pairs, a.items);
+    if (dealt.layout == kAny) return instance_of<T, K, kAny, NORM, BACK>(dealt.pairs, a.items);
+    return instance_of<T, K, kHalves, NORM, BACK>(dealt.pairs, a.items);
   };
   const Instance in = d->dtype == S1F_F32 ? pick(float{}) : pick(bf16_t{});
   const int64_t grid = cut_units(a, in, NORM && BACK);
   const int e = launch_rows_kernel(in.kernel, grid, 256, a, st);
   if (e != S1F_OK || !(NORM && BACK)) return e;
-  return launch_rows_kernel(&rope_join_kernel, (2 * a.dim + 63) / 64, 1024, a, st);
+  return launch_rows_kernel(&rope_join_kernel, (2 * a.dim + 15) / 16, 1024, a, st);
 }
 
 // Tensors of a call: 0 where a pointer is missing or does not lie on an element.
