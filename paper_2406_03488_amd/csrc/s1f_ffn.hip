@@ -43,6 +43,10 @@ struct FfnArgs {
   float *part;                    // [part][tile][row][column]
   PackJob jobs[kMostJobs];
   int32_t n_jobs;
+  // few rows: both operands as they lie in the call's tensors (h: rows of inner_width elements)
+  const void *rows, *weight;
+  RowsOf rows_at;
+  int64_t weight_stride;
 };
 
 // ---- operands --------------------------------------------------------------------------------------------------------------------------
@@ -80,29 +84,35 @@ template <typename T> S1F_DEV float sigmoid(float x) {
   if constexpr (sizeof(T) == 4) return 1.f / (1.f + expf(-x));
   else return __builtin_amdgcn_rcpf(1.f + exp2_fast(x * -kLog2e));
 }
-// act(g), and act'(g).  SiLU and the tanh form are g * sigmoid(g (c0 + c1 g^2)): the latter's (1 + tanh(t)) / 2 is the sigmoid of 2t, and keeps its digits where 1 + tanh
-// would lose them, as erfc does where 1 + erf would.
-template <typename T, bool ERF> struct Activation {
-  float c0, c1;
-  S1F_DEV explicit Activation(int act) : c0(act == S1F_SILU ? 1.f : 1.5957691216f), c1(act == S1F_SILU ? 0.f : 1.5957691216f * 0.044715f) {}
+// act(g), and act'(g).  The tanh form is g * sigmoid(g (c0 + c1 g^2)), (1 + tanh(t)) / 2 being the sigmoid of 2t, which keeps its digits where 1 + tanh would lose them, as erfc does
+// where 1 + erf would.
+template <typename T, int ACT> struct Activation {
+  static constexpr float c0 = 1.5957691216f, c1 = c0 * 0.044715f;
   // (past 2^60 squares are left where they are, and no sigmoid changes any more)
   S1F_DEV static float square(float g) { return fminf(g * g, 0x1p120f); }
-  S1F_DEV float operator()(float g) const {
-    if constexpr (ERF) return g * (0.5f * erfcf(g * -0.70710678f));
-    else return g * sigmoid<T>(g * fmaf(c1, square(g), c0));
+  S1F_DEV static float value(float g) {
+    if constexpr (ACT == S1F_GELU) return g * (0.5f * erfcf(g * -0.70710678f));
+    else return g * sigmoid<T>(ACT == S1F_SILU ? g : g * fmaf(c1, square(g), c0));
   }
-  S1F_DEV void operator()(float g, float &a, float &slope) const {
-    if constexpr (ERF) {
+  S1F_DEV static void both(float g, float &a, float &slope) {
+    if constexpr (ACT == S1F_GELU) {
       const float p = 0.5f * erfcf(g * -0.70710678f);
       a = g * p;
       slope = fmaf(g * 0.39894228f, expf(-0.5f * g * g), p);
     } else {
-      const float q = square(g), s = sigmoid<T>(g * fmaf(c1, q, c0)), rest = s * (1.f - s);
+      const float q = square(g), s = sigmoid<T>(ACT == S1F_SILU ? g : g * fmaf(c1, q, c0));
       a = g * s;
-      slope = rest == 0.f ? s : fmaf(g * rest, fmaf(3.f * c1, q, c0), s);
+      const float rest = a * (1.f - s);   // (0 far out, whatever the square is)
+      slope = ACT == S1F_SILU ? rest + s : fmaf(rest, fmaf(3.f * c1, q, c0), s);
     }
   }
 };
+// f(Int<act>{})
+template <typename F> S1F_DEV void with_activation(int act, F &&f) {
+  if (act == S1F_SILU) f(Int<S1F_SILU>{});
+  else if (act == S1F_GELU) f(Int<S1F_GELU>{});
+  else f(Int<S1F_GELU_TANH>{});
+}
 
 // ---- products --------------------------------------------------------------------------------------------------------------------------
 
@@ -230,10 +240,17 @@ template <typename P> struct Staged {
   }
 };
 
+// Zeros behind the end of a row.
+S1F_DEV void clear_behind(float (&v)[8], int there) {
+  if (there >= 8) return;
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (e >= there) v[e] = 0.f;
+}
+
 // h = act(g) * u of a tile of BM rows and BN / 2 columns.  m0: first row of the wave's blocks, n0: its first column.
-template <typename T, bool ERF, typename P> S1F_DEV void up_results(const f32x4 (&acc)[P::MB][P::NB], const FfnArgs &a, int m0, int n0, char *smem) {
+template <typename T, int ACT, typename P> S1F_DEV void up_results(const f32x4 (&acc)[P::MB][P::NB], const FfnArgs &a, int m0, int n0, char *smem) {
   constexpr int PAIRS = sizeof(T) == 4 ? 6 : 1, LANES = P::NB, ROWS = 64 / LANES;   // lanes to a row of 8 NB columns
-  const Activation<T, ERF> activation(a.act);
   Staged<P> staged(smem);
   // blocks of g and u take turns
   const int lane = lane_id(), at = 8 * (lane % LANES), from = (at >> 4 << 5) + (at & 15), col = n0 + at, there = a.inner - col;
@@ -253,7 +270,8 @@ template <typename T, bool ERF, typename P> S1F_DEV void up_results(const f32x4 
         set8<T>(to + a.inner, there, u);
       }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) h[e] = e < there ? activation(g[e]) * u[e] : 0.f;
+      for (int e = 0; e < 8; ++e) h[e] = Activation<T, ACT>::value(g[e]) * u[e];
+      clear_behind(h, there);
       put8<PAIRS>(a.h + (int64_t)row * a.h_ld + col, a.h_plane, h, 8);
     }
     between_lanes();
@@ -270,14 +288,12 @@ template <typename T, int BM, int BN, int WM, int WN> __global__ void __launch_b
   f32x4 acc[P::MB][P::NB];
   ffn_product<P, PAIRS, BM>(acc, a, m0, n0, 0, 1, to_lds_addr(smem), a.inner);
   const int wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
-  if (a.act == S1F_GELU) up_results<T, true, P>(acc, a, m0 + 16 * P::MB * wm, n0 + 8 * P::NB * wn, smem);
-  else up_results<T, false, P>(acc, a, m0 + 16 * P::MB * wm, n0 + 8 * P::NB * wn, smem);
+  with_activation(a.act, [&](auto act) { up_results<T, decltype(act)::value, P>(acc, a, m0 + 16 * P::MB * wm, n0 + 8 * P::NB * wn, smem); });
 }
 
-// dh = dy W_out of a tile, and of it [dg | du] and h.
-template <typename T, bool ERF, typename P> S1F_DEV void dh_results(const f32x4 (&acc)[P::MB][P::NB], const FfnArgs &a, int m0, int n0, char *smem) {
+// dh = dy W_out of a tile, and of it [dg | du] and h.  (g and u asked for four rows ahead instead of two: no faster.)
+template <typename T, int ACT, typename P> S1F_DEV void dh_results(const f32x4 (&acc)[P::MB][P::NB], const FfnArgs &a, int m0, int n0, char *smem) {
   constexpr int PAIRS = sizeof(T) == 4 ? 6 : 1, LANES = 2 * P::NB, ROWS = 64 / LANES;
-  const Activation<T, ERF> activation(a.act);
   Staged<P> staged(smem);
   const int lane = lane_id(), at = 8 * (lane % LANES), col = n0 + at, there = a.inner - col;
 #pragma unroll
@@ -295,12 +311,12 @@ template <typename T, bool ERF, typename P> S1F_DEV void dh_results(const f32x4 
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         float act, slope;
-        activation(g[e], act, slope);
-        const bool is = e < there;
-        h[e] = is ? act * u[e] : 0.f;
+        Activation<T, ACT>::both(g[e], act, slope);
+        h[e] = act * u[e];
         g[e] = d[e] * u[e] * slope;
         u[e] = d[e] * act;
       }
+      clear_behind(h, there);
       put8<PAIRS>(a.h + (int64_t)row * a.h_ld + col, a.h_plane, h, 8);
       if (there <= 0) continue;
       bf16_t *to = a.dz + (int64_t)row * a.dz_ld + col;
@@ -325,8 +341,7 @@ template <typename T, int BM, int BN, int WM, int WN> __global__ void __launch_b
   f32x4 acc[P::MB][P::NB];
   ffn_product<P, PAIRS, BM>(acc, a, m0, n0, 0, 1, to_lds_addr(smem));
   const int wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
-  if (a.act == S1F_GELU) dh_results<T, true, P>(acc, a, m0 + 16 * P::MB * wm, n0 + 16 * P::NB * wn, smem);
-  else dh_results<T, false, P>(acc, a, m0 + 16 * P::MB * wm, n0 + 16 * P::NB * wn, smem);
+  with_activation(a.act, [&](auto act) { dh_results<T, decltype(act)::value, P>(acc, a, m0 + 16 * P::MB * wm, n0 + 16 * P::NB * wn, smem); });
 }
 
 enum Result { kStoreBf16, kStoreF32, kAddF32 };
@@ -383,6 +398,127 @@ template <int BM, int BN, Result R> __global__ void __launch_bounds__(256) ffn_j
   put_result<R>(a, tm * BM + row, tn * BN + col, v);
 }
 
+// ---- few rows --------------------------------------------------------------------------------------------------------------------------
+
+// Products of few rows are bound by reading the weights, once.  A workgroup has 16 columns (of gate and up both, or of y), whose rows of the weight its waves read in parts along the
+// contraction, straight into the registers of the matrix instructions: each lane 16 bytes of its row at a time, several stages of 64 ahead, no LDS, nothing laid out anew (fp32 is split on
+// the way), any strides.  The waves' sums meet in LDS.
+template <typename T, int BLOCKS> struct Ahead {   // elements of a stage of one operand: 16 rows a block, lane (n, j) has 8j .. 8j+7 of either half of row n
+  typedef Piece<T, false> P;
+  static constexpr int PER = 8 / P::N;
+  typename P::Raw raw[BLOCKS][2][PER];
+  // k: the lane's first element
+  template <bool WHOLE> S1F_DEV void load(const T *const (&row)[BLOCKS], int64_t k, int64_t end) {
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          const int64_t at = k + 32 * h + P::N * i;
+          if constexpr (WHOLE) raw[b][h][i] = *reinterpret_cast<const typename P::Loose *>(row[b] + at);
+          else raw[b][h][i] = P::get(row[b] + at, at < end ? (int)(end - at) : 0);
+        }
+  }
+  S1F_DEV auto operand(int b, int h) const {
+    if constexpr (sizeof(T) == 4) return split3(raw[b][h][0], raw[b][h][1]);
+    else return raw[b][h][0];
+  }
+};
+template <typename T, int MB, int NB, int WAVES, int DEPTH, bool UP> __global__ void __launch_bounds__(64 * WAVES) ffn_few_kernel(const FfnArgs a) {
+  __shared__ __attribute__((aligned(16))) f32x4 sums[WAVES][MB * NB][64];
+  const int lane = lane_id(), n = lane & 15, j = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col0 = blockIdx.x * (UP ? 8 * NB : 16 * NB);   // (UP: blocks of gate and up take turns)
+  const T *rows[MB], *weight[NB];
+#pragma unroll
+  for (int b = 0; b < MB; ++b) rows[b] = reinterpret_cast<const T *>(a.rows) + a.rows_at.offset(16 * b + n < a.m ? 16 * b + n : a.m - 1);
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    const int c = col0 + 16 * (UP ? b / 2 : b) + n, known = c < a.n ? c : a.n - 1;
+    weight[b] = reinterpret_cast<const T *>(a.weight) + (int64_t)(known + (UP && b % 2 ? a.inner : 0)) * a.weight_stride;
+  }
+  f32x4 acc[MB][NB];
+#pragma unroll
+  for (int i = 0; i < MB; ++i)
+#pragma unroll
+    for (int b = 0; b < NB; ++b) acc[i][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int whole = a.k / kDepth, begin = whole * wave / WAVES, end = whole * (wave + 1) / WAVES;
+  Ahead<T, MB> x[DEPTH];
+  Ahead<T, NB> w[DEPTH];
+  auto product = [&](const Ahead<T, MB> &xs, const Ahead<T, NB> &ws) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      decltype(xs.operand(0, 0)) fx[MB], fw[NB];
+#pragma unroll
+      for (int i = 0; i < MB; ++i) fx[i] = xs.operand(i, h);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) fw[b] = ws.operand(b, h);
+#pragma unroll
+      for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) acc[i][b] = mma16(fw[b], fx[i], acc[i][b]);
+    }
+  };
+#pragma unroll
+  for (int d = 0; d < DEPTH; ++d)
+    if (begin + d < end) {
+      w[d].template load<true>(weight, (int64_t)(begin + d) * kDepth + 8 * j, 0);
+      x[d].template load<true>(rows, (int64_t)(begin + d) * kDepth + 8 * j, 0);
+    }
+#pragma unroll 1
+  for (int t = begin; t < end; t += DEPTH)
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) {
+      if (t + d >= end) break;
+      product(x[d], w[d]);
+      if (t + d + DEPTH < end) {
+        w[d].template load<true>(weight, (int64_t)(t + d + DEPTH) * kDepth + 8 * j, 0);
+        x[d].template load<true>(rows, (int64_t)(t + d + DEPTH) * kDepth + 8 * j, 0);
+      }
+    }
+  if (wave == WAVES - 1 && whole * kDepth < a.k) {
+    w[0].template load<false>(weight, (int64_t)whole * kDepth + 8 * j, a.k);
+    x[0].template load<false>(rows, (int64_t)whole * kDepth + 8 * j, a.k);
+    product(x[0], w[0]);
+  }
+#pragma unroll
+  for (int i = 0; i < MB; ++i)
+#pragma unroll
+    for (int b = 0; b < NB; ++b) sums[wave][i * NB + b][lane] = acc[i][b];
+  __syncthreads();
+  auto sum = [&](int block) {
+    f32x4 v = sums[0][block][lane];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) v += sums[w][block][lane];
+    return v;
+  };
+  // a wave takes a block of 16 x 16, or of gate and up
+#pragma unroll
+  for (int i = 0; i < (UP ? MB * NB / 2 : MB * NB); ++i) {
+    if (i % WAVES != wave) continue;
+    constexpr int COLS = UP ? NB / 2 : NB;
+    const int row = 16 * (i / COLS) + n, col = col0 + 16 * (i % COLS) + 4 * j, there = a.n - col;
+    if (row >= a.m) continue;
+    if constexpr (UP) {
+      const f32x4 g = sum(2 * i), u = sum(2 * i + 1);
+      T *h = reinterpret_cast<T *>(a.h) + (int64_t)row * a.h_ld + col, *kept = reinterpret_cast<T *>(a.gate_up) + (int64_t)row * 2 * a.inner + col;
+      with_activation(a.act, [&](auto act) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (e < there) h[e] = (T)(Activation<T, decltype(act)::value>::value(g[e]) * u[e]);
+      });
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (a.gate_up && e < there) {
+          kept[e] = (T)g[e];
+          kept[a.inner + e] = (T)u[e];
+        }
+    } else {
+      put_result<sizeof(T) == 4 ? kStoreF32 : kStoreBf16>(a, row, col, sum(i));
+    }
+  }
+}
+
 // ---- host ------------------------------------------------------------------------------------------------------------------------------
 
 constexpr int64_t kMostInner = int64_t(1) << 17, kMostStride = int64_t(1) << 22, kMostApart = int64_t(1) << 29, kMostElements = int64_t(1) << 33;
@@ -428,6 +564,7 @@ int64_t part_bytes(const Cuts &c) { return c.splits > 1 ? 4 * c.splits * c.rest 
 struct FfnPlan {
   int64_t n, planes, width, inner_width, dz_ld, turns, per_turn;   // dW's rows are taken per_turn at a time
   bool direct_in, direct_out;     // weights as they are
+  bool few;
   Cuts up, down, dh, dx, dw_in, dw_out;
   int64_t x, dy, w_in, w_out, h, dz, part, bytes;   // offsets
 };
@@ -448,6 +585,13 @@ int check_ffn(const s1f_rows *d, int64_t inner, int64_t in_stride, int64_t out_s
 constexpr int64_t kSummed = 8192;
 int64_t turns_of(int64_t n, int64_t planes) { return planes == 1 || n < kSummed + kSummed / 2 ? 1 : (n + kSummed / 2) / kSummed; }
 
+// Forwards that the kernel of few rows takes: up to 64 fp32 rows, whose weights then need not be split in memory, up to 16 bf16 ones, and more where the call is small: it reads the rows once for
+// every 16 columns, where a tile has 64 at a time.  4096 x 11008, us, few and tiles: bf16 1 row 52 and 82, 16 65 and 83, 32 84 and 84, 64 128 and 89; fp32 1 row 109 and 445, 64 254 and 457.
+// bf16 32 x 1024 x 2816 16 and 19, 64 24 and 20, 64 x 256 x 688 11.3 and 12.9, 32 x 2048 x 5632 35 and 30.
+bool few_rows(int64_t n, int32_t dtype, int64_t hidden, int64_t inner) {
+  return n <= 64 && (dtype == S1F_F32 || n <= 16 || n * hidden * inner <= int64_t(1) << 27);
+}
+
 FfnPlan plan_of(const s1f_rows *d, int64_t inner, int64_t in_stride, int64_t out_stride, bool backward) {
   FfnPlan p = {};
   const int64_t h = d->hidden;
@@ -460,6 +604,12 @@ FfnPlan plan_of(const s1f_rows *d, int64_t inner, int64_t in_stride, int64_t out
   p.direct_out = d->dtype == S1F_BF16 && inner % 8 == 0 && out_stride % 8 == 0;
   int64_t at = 0;
   auto take = [&at](int64_t bytes) { const int64_t was = at; at += up_to(bytes, 256); return was; };
+  p.few = !backward && few_rows(p.n, d->dtype, h, inner);
+  if (p.few) {
+    p.h = take(p.planes * 2 * p.n * p.inner_width);
+    p.bytes = at;
+    return p;
+  }
   p.x = take(p.planes * 2 * p.n * p.width);
   if (!p.direct_in) p.w_in = take(p.planes * 2 * 2 * inner * p.width);
   if (!p.direct_out) p.w_out = take(p.planes * 2 * h * p.inner_width);
@@ -599,11 +749,35 @@ FfnArgs args_of(const FfnPlan &p, int64_t inner, int32_t act, const void *gate_u
   return a;
 }
 
+template <typename T, int MB, int NB, int WAVES, int DEPTH, bool UP> int launch_few(const FfnArgs &a, hipStream_t st) {
+  constexpr int COLS = UP ? 8 * NB : 16 * NB;
+  const int64_t grid = (a.n + COLS - 1) / COLS;
+  return launch_rows_kernel(&ffn_few_kernel<T, MB, NB, WAVES, DEPTH, UP>, grid, 64 * WAVES, a, st);
+}
+template <typename T>
+int forward_few(const s1f_rows *d, FfnArgs a, const void *x, const void *w_in, int64_t in_stride, const void *w_out, int64_t out_stride, void *y, hipStream_t st) {
+  constexpr bool F32 = sizeof(T) == 4;
+  const int64_t n = d->batch * d->rows;
+  a.m = (int32_t)n; a.n = a.inner; a.k = d->hidden;
+  a.rows = x; a.rows_at = x_rows(d);
+  a.weight = w_in; a.weight_stride = in_stride;
+  int e = n <= 16 ? launch_few<T, 1, 2, 4, F32 ? 2 : 4, true>(a, st) : n <= 32 ? launch_few<T, 2, 2, 4, F32 ? 1 : 3, true>(a, st)
+                                                                             : launch_few<T, 4, 2, 8, F32 ? 1 : 2, true>(a, st);
+  if (e != S1F_OK) return e;
+  a.n = d->hidden; a.k = a.inner;
+  a.rows = a.h; a.rows_at = RowsOf{0, a.h_ld, Divisor::of(n)};
+  a.weight = w_out; a.weight_stride = out_stride;
+  set_out(a, y, y_rows(d), wide_side(d, y, d->y_stride_b, d->y_stride_s), 1.f);
+  return n <= 16 ? launch_few<T, 1, 1, 8, F32 ? 2 : 8, false>(a, st) : n <= 32 ? launch_few<T, 2, 1, F32 ? 8 : 16, F32 ? 2 : 4, false>(a, st)
+                                                                               : launch_few<T, 4, 1, F32 ? 8 : 16, F32 ? 1 : 2, false>(a, st);
+}
+
 template <typename T>
 int forward(const s1f_rows *d, const FfnPlan &p, const void *x, const void *w_in, int64_t in_stride, const void *w_out, int64_t out_stride, int64_t inner, int32_t act,
             void *y, void *gate_up, char *ws, hipStream_t st) {
   constexpr Result R = sizeof(T) == 4 ? kStoreF32 : kStoreBf16;
   FfnArgs a = args_of(p, inner, act, gate_up, ws);
+  if (p.few) return forward_few<T>(d, a, x, w_in, in_stride, w_out, out_stride, y, st);
   Operands ops{a, d, p.planes};
   const Matrix mx = ops.rows(x, d->x_stride_b, d->x_stride_s, false, p.width, ws + p.x);
   const Matrix mi = ops.weight(w_in, 2 * inner, d->hidden, in_stride, p.width, p.direct_in, ws + p.w_in);
