@@ -533,7 +533,17 @@ struct Cuts {
 };
 constexpr int tile_m(Tile t) { return t == kBig ? 256 : t == kMiddle ? 128 : 64; }
 constexpr int tile_n(Tile t) { return t == kBig ? 256 : 128; }
-Cuts cuts_for(int64_t m, int64_t n, int64_t stages, bool low, bool split) {
+// Predicted microseconds of `tiles` tiles of so many stages: as tiles_us has them, but that few rounds of smaller tiles count whole, too (540 tiles of 128 x 128 and 66 stages: 130 us, 512 of them
+// 65), and that low tiles of planes copy all planes of a stage at once and have a unit to themselves (1.35 us for the six products of a stage, 1.8 where an operand lies by columns).
+enum Operand { kBf16, kPlanes, kPlanesByColumns };
+double round_us(Tile tile, int64_t tiles, double stages, Operand operand) {
+  if (tile == kLow && operand != kBf16) return (double)((tiles + kUnits - 1) / kUnits) * (5.5 + (operand == kPlanes ? 0.225 : 0.3) * stages);
+  if (tile == kBig || tiles > 6 * kUnits) return tiles_us(tile, tiles, stages);
+  const int64_t rounds = tiles / (2 * kUnits), rest = tiles - rounds * 2 * kUnits;
+  return (rounds ? (double)rounds * tiles_us(tile, 2 * kUnits, stages) / 1.25 : 0.0) + (rest ? tiles_us(tile, rest, stages) : 0.0);
+}
+// low: whether there are kernels for low tiles; split: whether a sum may be cut along its contraction
+Cuts cuts_for(int64_t m, int64_t n, int64_t stages, Operand operand, bool low, bool split) {
   Cuts best = {};
   double best_us = 1e30;
   auto offer = [&](const Cuts &c, double us) {
@@ -542,20 +552,22 @@ Cuts cuts_for(int64_t m, int64_t n, int64_t stages, bool low, bool split) {
       best = c;
     }
   };
-  const Cut c = cut_for(m, n, stages, low);
-  const int64_t all = grid_of(m, n, tile_m(c.tile), tile_n(c.tile));
-  const bool quarters = c.tile == kBig && c.whole < all;
-  const int64_t at_once = c.tile == kBig ? c.whole : all;
-  offer(Cuts{c.tile, at_once, all - at_once, 1, quarters},
-        tiles_us(c.tile, at_once, (double)stages) + (quarters ? 3.0 + tiles_us(kMiddle, 4 * (all - at_once), (double)stages) : 0.0));
-  if (!split) return best;
   for (Tile tile : {kBig, kMiddle, kLow}) {
     if (tile == kLow && !low) continue;
-    const int64_t tiles = grid_of(m, n, tile_m(tile), tile_n(tile)), whole = tile == kBig ? tiles / kUnits * kUnits : 0, rest = tiles - whole;
-    if (rest == 0) continue;
-    for (int splits = 2; splits <= 32 && stages / splits >= 4 && rest * splits <= 4 * kUnits; ++splits)
-      offer(Cuts{tile, whole, rest, splits, false}, (whole ? tiles_us(tile, whole, (double)stages) : 0.0) + tiles_us(tile, rest * splits, (double)stages / splits) +
-                                                        3.0 + (double)splits * rest * tile_m(tile) * tile_n(tile) * 8 / 4e6);
+    auto time = [&](int64_t tiles, double of) { return tiles ? round_us(tile, tiles, of, operand) : 0.0; };
+    const int64_t tiles = grid_of(m, n, tile_m(tile), tile_n(tile)), round = tile == kBig || (tile == kLow && operand != kBf16) ? kUnits : 2 * kUnits, full = tiles / round * round;
+    offer(Cuts{tile, tiles, 0, 1, false}, time(tiles, (double)stages));
+    if (tile == kBig && full > 0 && full < tiles)
+      offer(Cuts{tile, full, tiles - full, 1, true}, time(full, (double)stages) + 3.0 + round_us(kMiddle, 4 * (tiles - full), (double)stages, operand));
+    if (!split) continue;
+    for (const int64_t whole : {full, int64_t(0)}) {
+      const int64_t rest = tiles - whole;
+      if (rest == 0 || (whole == 0 && tile == kBig && full > 0)) continue;
+      for (int splits = 2; splits <= 32 && stages / splits >= 4 && rest * splits <= 4 * kUnits; ++splits)
+        offer(Cuts{tile, whole, rest, splits, false}, time(whole, (double)stages) + time(rest * splits, (double)stages / splits) + 3.0 +
+                                                          (double)splits * rest * tile_m(tile) * tile_n(tile) * 8 / 4e6);
+      if (full == 0) break;
+    }
   }
   return best;
 }
@@ -616,21 +628,22 @@ FfnPlan plan_of(const s1f_rows *d, int64_t inner, int64_t in_stride, int64_t out
   p.h = take(p.planes * 2 * p.n * p.inner_width);
   const int64_t pairs = p.planes == 3 ? 6 : 1;
   auto stages = [&](int64_t k) { return (k + kDepth - 1) / kDepth * pairs; };
+  const Operand rows = p.planes == 3 ? kPlanes : kBf16, columns = p.planes == 3 ? kPlanesByColumns : kBf16;
   int64_t part = 0;
   if (!backward) {
     // (tiles of [g | u]: as many columns of either)
-    p.up = cuts_for(p.n, 2 * up_to(inner, 16), stages(h), true, false);
-    p.down = cuts_for(p.n, h, stages(inner), true, true);
+    p.up = cuts_for(p.n, 2 * up_to(inner, 16), stages(h), rows, true, false);
+    p.down = cuts_for(p.n, h, stages(inner), rows, true, true);
     part = part_bytes(p.down);
   } else {
     p.turns = turns_of(p.n, p.planes);
     p.per_turn = up_to((p.n + p.turns - 1) / p.turns, kDepth);
     p.dy = take(p.planes * 2 * p.n * p.width);
     p.dz = take(p.planes * 2 * p.n * p.dz_ld);
-    p.dh = cuts_for(p.n, inner, stages(h), true, false);
-    p.dx = cuts_for(p.n, h, stages(2 * inner), true, true);
-    p.dw_in = cuts_for(2 * inner, h, stages(p.per_turn), false, true);
-    p.dw_out = cuts_for(h, inner, stages(p.per_turn), false, true);
+    p.dh = cuts_for(p.n, inner, stages(h), columns, true, false);
+    p.dx = cuts_for(p.n, h, stages(2 * inner), columns, true, true);
+    p.dw_in = cuts_for(2 * inner, h, stages(p.per_turn), columns, false, true);
+    p.dw_out = cuts_for(h, inner, stages(p.per_turn), columns, false, true);
     for (const Cuts &c : {p.dx, p.dw_in, p.dw_out}) part = std::max(part, part_bytes(c));
   }
   p.part = take(part);
