@@ -228,3 +228,38 @@ def test_gradient_against_differences():
         slope = (ends[0] - ends[1]) / 2e-5
         # fp32 sums of fewer than 1000 terms of about 1; the difference leaves 1e-9
         assert abs(slope - (g * way).sum()) <= 1e-4 * (1 + np.abs(g * way).sum())
+
+
+# cuts that only large products take: whole big or middle tiles, and the others in parts; and 16 to 64 rows of large weights
+@pytest.mark.parametrize("n,h,f,dtype", [(4100, 4100, 1500, "f32"), (8200, 1100, 2100, "f32"), (8200, 1100, 2100, "bf16"), (600, 1100, 8200, "bf16"), (4100, 4100, 6000, "bf16"),
+                                         (4099, 4096, 11008, "bf16"), (16, 4096, 11008, "bf16"), (16, 4096, 11008, "f32"), (64, 4096, 5000, "f32")])
+def test_large_products_by_sample(n, h, f, dtype):
+    """Rows of y and dx, and rows and columns of the weights' gradients, that are drawn; the last of each among them."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(n)
+    t = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    normal = lambda *shape, scale=1.0: torch.empty(shape, device="cuda", dtype=t).normal_(0, scale, generator=gen)
+    x, dy, w_in, w_out = normal(1, n, h), normal(1, n, h), normal(2 * f, h, scale=h ** -0.5), normal(h, f, scale=f ** -0.5)
+    y, dx, gate_up = torch.full_like(x, float("nan")), torch.full_like(x, float("nan")), torch.full((1, n, 2 * f), float("nan"), device="cuda", dtype=t)
+    ws = space(s1f.gated_ffn_fwd_workspace_bytes(x, w_in, w_out))[0]
+    s1f.gated_ffn_fwd(x, w_in, w_out, s1f.SILU, y, gate_up, ws)
+    dw = [torch.zeros((2 * f, h), device="cuda"), torch.zeros((h, f), device="cuda")]
+    ws = space(s1f.gated_ffn_bwd_workspace_bytes(dy, x, w_in, w_out))[0]
+    s1f.gated_ffn_bwd(dy, x, w_in, w_out, s1f.SILU, gate_up, dx, *dw, ws)
+    assert all(torch.isfinite(v).all() for v in (y, gate_up, dx, *dw))
+    rng = np.random.default_rng(f)
+    pick = lambda limit, many: np.unique(np.concatenate([rng.integers(0, limit, many), [0, limit - 1]]))
+    rows, inner = pick(n, 60), pick(f, 60)
+    xs, ys, wi, wo = f64(x[0, rows]), f64(dy[0, rows]), f64(w_in), f64(w_out)
+    want, z, _ = L.gated_ffn(xs, wi, wo, "silu")
+    t_y, t_z = ffn_forward_tolerances(xs, wi, wo, "silu", dtype)
+    within(f64(y[0, rows]), want, t_y, "y")
+    within(f64(gate_up[0, rows]), z, t_z, "gate_up")
+    args = ys, xs, wi, wo, "silu", f64(gate_up[0, rows])
+    want, tolerance = L.gated_ffn_grad(*args)[0], ffn_backward_tolerances(*args, dtype)[0]
+    within(f64(dx[0, rows]), want, tolerance * (1 + HALF[dtype]) + HALF[dtype] * np.abs(want), "dx")
+    both = np.concatenate([inner, f + inner])
+    args = f64(dy[0]), f64(x[0]), wi[both], wo[:, inner], "silu", f64(gate_up[0][:, both])
+    want, tolerance = L.gated_ffn_grad(*args), ffn_backward_tolerances(*args, dtype)
+    within(f64(dw[0][both]), want[1], tolerance[1] + 2 * U * np.abs(want[1]), "dw_in")
+    within(f64(dw[1][:, inner]), want[2], tolerance[2] + 2 * U * np.abs(want[2]), "dw_out")

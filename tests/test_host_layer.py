@@ -9,7 +9,7 @@ import torch
 import paper_2406_03488_amd as s1f
 from oracle import layer as L
 from paper_2406_03488_amd import binding
-from paper_2406_03488_amd.binding import Heads
+from paper_2406_03488_amd.binding import Heads, Rows
 
 P, ODD, OFF = 4096, 4097, 4104     # addresses: aligned, not even, on 8 bytes (none is looked at)
 BIG = 1 << 50
@@ -132,6 +132,63 @@ def test_frequencies_refused():
     assert lib.s1f_rope_frequencies(64, 1e4, 0, 1.0, 0, 0.0, 0.0, out, None) == 1
 
 
+# ---- gated feed-forward block ----------------------------------------------------------------------------------------------------------
+
+def rows(**kw):
+    base = dict(batch=2, hidden=64, dtype=1, reserved=0, rows=5, x_stride_b=320, x_stride_s=64, y_stride_b=320, y_stride_s=64)
+    base.update(kw)
+    return Rows(**base)
+
+
+def ffn_fwd(d, x=P, w_in=P, in_stride=64, w_out=P, out_stride=96, inner=96, act=0, y=P, gate_up=P, ws=P, n=BIG):
+    return s1f.load_library().s1f_gated_ffn_fwd(ref(d), x, w_in, in_stride, w_out, out_stride, inner, act, y, gate_up, ws, n, None)
+
+
+def ffn_bwd(d, dy=P, x=P, w_in=P, in_stride=64, w_out=P, out_stride=96, inner=96, act=0, gate_up=P, dx=P, dw_in=P, dw_in_stride=64, dw_out=P, dw_out_stride=96, code=0,
+            ws=P, n=BIG):
+    return s1f.load_library().s1f_gated_ffn_bwd(ref(d), dy, x, w_in, in_stride, w_out, out_stride, inner, act, gate_up, dx, dw_in, dw_in_stride, dw_out, dw_out_stride,
+                                                code, ws, n, None)
+
+
+@pytest.mark.parametrize("call", [ffn_fwd, ffn_bwd])
+def test_ffn_refused(call):
+    assert call(None) == 1
+    for bad in (dict(batch=0), dict(batch=-1), dict(hidden=0), dict(reserved=1), dict(x_stride_s=63), dict(y_stride_s=63), dict(x_stride_b=63), dict(y_stride_b=-320)):
+        assert call(rows(**bad)) == 1, bad
+    for bad in (dict(dtype=2), dict(dtype=-1), dict(hidden=16385, x_stride_s=1 << 15, y_stride_s=1 << 15, x_stride_b=1 << 20, y_stride_b=1 << 20),
+                dict(batch=1, rows=(1 << 20) + 1), dict(batch=1 << 30, rows=1 << 34)):
+        assert call(rows(**bad), in_stride=1 << 15) == 2, bad
+    for bad in (0, -1, -(1 << 40)):
+        assert call(rows(rows=bad)) == 3
+    for bad in (dict(inner=0), dict(inner=-96), dict(in_stride=63), dict(out_stride=95), dict(act=-1), dict(act=3)):
+        assert call(rows(), **bad) == 1, bad
+    for bad in (dict(inner=(1 << 17) + 1, out_stride=1 << 18), dict(in_stride=1 << 22), dict(out_stride=1 << 22), dict(inner=1 << 17, out_stride=1 << 17, in_stride=4097)):
+        assert call(rows(), **bad, **({"dw_out_stride": 1 << 18} if call is ffn_bwd else {})) == 2, bad
+    big = dict(batch=1, rows=1 << 20)
+    assert call(rows(**big, hidden=8200, x_stride_s=8200, y_stride_s=8200), in_stride=8200) == 2
+    assert call(rows(**big), inner=4097, out_stride=4097, **({"dw_out_stride": 4097} if call is ffn_bwd else {})) == 2
+    names = ("x", "w_in", "w_out", "y", "ws") if call is ffn_fwd else ("dy", "x", "w_in", "w_out", "gate_up", "dx", "dw_in", "dw_out", "ws")
+    for name in names:
+        assert call(rows(), **{name: None}) == 1 and call(rows(), **{name: ODD}) == 1, name
+    for name in ("w_in", "w_out", "ws"):
+        assert call(rows(), **{name: OFF}) == 1, name
+    assert call(rows(), gate_up=ODD) == 1 and call(rows(), n=255) == 1 and call(rows(), n=0) == 1
+    if call is ffn_bwd:
+        assert call(rows(), code=2) == 2 and call(rows(dtype=0), code=1) == 2 and call(rows(), dw_in_stride=63) == 1 and call(rows(), dw_out_stride=95) == 1
+
+
+def test_ffn_workspaces():
+    lib = s1f.load_library()
+    for f in (lib.s1f_gated_ffn_fwd_workspace_bytes, lib.s1f_gated_ffn_bwd_workspace_bytes):
+        assert f(ref(rows()), 96, 64, 96) > 0
+        for bad in (None, rows(rows=0), rows(hidden=0), rows(dtype=5)):
+            assert f(ref(bad), 96, 64, 96) == 0
+        assert f(ref(rows()), 0, 64, 96) == 0 and f(ref(rows()), 96, 63, 96) == 0 and f(ref(rows()), 96, 64, 95) == 0
+    # a forward of bf16 rows keeps what is between its products, not the weights
+    d = rows(batch=1, rows=4096, hidden=4096, x_stride_s=4096, y_stride_s=4096)
+    assert lib.s1f_gated_ffn_fwd_workspace_bytes(ref(d), 11008, 4096, 11008) < 2 * 4096 * (4096 + 11008) + (64 << 20)
+
+
 class Library:
     def __init__(self):
         self.calls = []
@@ -166,6 +223,8 @@ def good():
     gains = [bf16(16), bf16(16)]
     return {"rope_fwd": [q, k, v, f, 1.0, False, at, 3, bf16(2, 4, 5, 16), kc, vc], "rope_bwd": [bf16(2, 4, 5, 16), ka, va, f, 1.0, False, at, 3, q, k, v],
             "qk_norm_rope_fwd": [q, k, v, *gains, 1e-6, f, 1.0, False, at, 3, bf16(2, 4, 5, 16), kc, vc],
+            "gated_ffn_fwd": [bf16(2, 5, 16), bf16(48, 16), bf16(16, 24), s1f.SILU, bf16(2, 5, 16), bf16(2, 5, 48), ws],
+            "gated_ffn_bwd": [bf16(2, 5, 16), bf16(2, 5, 16), bf16(48, 16), bf16(16, 24), s1f.GELU, bf16(2, 5, 48), bf16(2, 5, 16), f32(48, 16), f32(16, 24), ws],
             "qk_norm_rope_bwd": [bf16(2, 4, 5, 16), ka, va, bf16(2, 4, 5, 16), bf16(2, 2, 5, 16), *gains, 1e-6, f, 1.0, False, at, 3, q, k, v, f32(16),
                                  f32(16), ws]}
 
@@ -198,6 +257,13 @@ BAD += [("rope_bwd", 1, bf16(2, 2, 9, 16)), ("rope_bwd", 2, bf16(2, 2, 9, 16)), 
         ("qk_norm_rope_fwd", 3, bf16(15)), ("qk_norm_rope_fwd", 4, f32(16)), ("qk_norm_rope_fwd", 3, bf16(32)[::2]),
         ("qk_norm_rope_bwd", 3, bf16(2, 4, 5, 17)[..., 1:]), ("qk_norm_rope_bwd", 3, bf16(2, 4, 6, 16)), ("qk_norm_rope_bwd", 4, f32(2, 2, 5, 16)),
         ("qk_norm_rope_bwd", 4, bf16(2, 5, 2, 16).transpose(1, 2)), ("qk_norm_rope_bwd", 5, bf16(17)), ("qk_norm_rope_bwd", 16, bf16(16)),
+        ("gated_ffn_fwd", 0, f32(2, 5, 16)), ("gated_ffn_fwd", 0, bf16(5, 16)), ("gated_ffn_fwd", 0, bf16(2, 5, 32)[..., ::2]), ("gated_ffn_fwd", 1, bf16(47, 16)),
+        ("gated_ffn_fwd", 1, bf16(48, 15)), ("gated_ffn_fwd", 1, f32(48, 16)), ("gated_ffn_fwd", 1, bf16(16, 48).t()), ("gated_ffn_fwd", 2, bf16(16, 25)),
+        ("gated_ffn_fwd", 2, bf16(15, 24)), ("gated_ffn_fwd", 2, bf16(24, 16).t()), ("gated_ffn_fwd", 4, bf16(2, 6, 16)), ("gated_ffn_fwd", 4, f32(2, 5, 16)),
+        ("gated_ffn_fwd", 5, bf16(2, 5, 24)), ("gated_ffn_fwd", 5, f32(2, 5, 48)), ("gated_ffn_fwd", 5, bf16(2, 5, 96)[..., ::2]),
+        ("gated_ffn_fwd", 6, torch.zeros(8, 8)[:, ::2]), ("gated_ffn_bwd", 0, bf16(2, 4, 16)), ("gated_ffn_bwd", 5, bf16(2, 5, 47)), ("gated_ffn_bwd", 5, f32(2, 5, 48)),
+        ("gated_ffn_bwd", 6, bf16(2, 10, 16)[:, ::2]), ("gated_ffn_bwd", 6, f32(2, 5, 16)), ("gated_ffn_bwd", 7, f32(46, 16)), ("gated_ffn_bwd", 7, bf16(48, 16)),
+        ("gated_ffn_bwd", 8, f32(16, 23)), ("gated_ffn_bwd", 8, bf16(16, 24)), ("gated_ffn_bwd", 7, f32(48, 16).half()),
         ("qk_norm_rope_bwd", 17, f32(15)), ("qk_norm_rope_bwd", 18, torch.zeros(8, 8)[:, ::2])]
 
 
