@@ -280,23 +280,22 @@ template <int BM, int BN, int WM, int WN, bool TRA, bool TRB, int PAIRS> struct 
     __syncthreads();
   }
 
-  // The same (stages of all planes) for operands of three planes and tiles small enough that LDS holds all planes of two stages: each is copied once for the six products, and read
+  // The same for operands of three planes and tiles small enough that LDS holds all planes of two stages: each is copied once for the six products, and read
   // once into registers.  A call of few tiles is a chain of stages, of which there are then a sixth: scores of 256 rows of 256 elements over 5003 tokens 15.1 -> 11.2 us,
   // loss of 64 rows of 4096 over 30000, which reads 740 MB of planes, 865 -> 570.  Eight waves of 32 x 32, two to a SIMD, so that one's reads pass under the other's
   // products: 1.35 us per stage, four of 64 x 32 1.5.
   static constexpr int PLANES_LDS_BYTES = 2 * 3 * (SA::BYTES + SB::BYTES);
   S1F_DEV static void run_planes(f32x4 (&acc)[MB][NB], const Matrix &a, const Matrix &b, int64_t m0, int64_t m_limit, int64_t n0, int64_t n_limit,
-                                 int64_t k, int begin, int end, lds_addr lds, int64_t b_apart = 0) {
+                                 int64_t k, lds_addr lds) {
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
 #pragma unroll
     for (int i = 0; i < MB; ++i)
 #pragma unroll
       for (int j = 0; j < NB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (begin >= end) return;
     SA sa;
     SB sb;
-    sa.init(a.data, a.ld, m0, m_limit, 0, begin, wave, lane);
-    sb.init(b.data, b.ld, n0, n_limit, b_apart, begin, wave, lane);
+    sa.init(a.data, a.ld, m0, m_limit, 0, 0, wave, lane);
+    sb.init(b.data, b.ld, n0, n_limit, 0, 0, wave, lane);
     const int stages = (int)((k + kDepth - 1) / kDepth), left = (int)((k - 1) % kDepth) + 1;
     constexpr int COPIES = 3 * (SA::PER_WAVE + SB::PER_WAVE);
     auto copy_side = [&](auto &side, const Matrix &m, lds_addr at, int bytes) {
@@ -317,12 +316,12 @@ template <int BM, int BN, int WM, int WN, bool TRA, bool TRB, int PAIRS> struct 
       copy_side(sb, b, place + 3 * SA::BYTES, SB::BYTES);
     };
     const lds_addr places[2] = {lds, lds + 3 * (SA::BYTES + SB::BYTES)};
-    copy_stage(begin, places[0]);
-    if (begin + 1 < end) copy_stage(begin + 1, places[1]);
+    copy_stage(0, places[0]);
+    if (stages > 1) copy_stage(1, places[1]);
     const lds_addr lane_a = SA::at(wm * MB, lane), lane_b = SB::at(wn * NB, lane);
-    for (int t = begin; t < end; ++t) {
-      const lds_addr at_a = places[(t - begin) & 1], at_b = at_a + 3 * SA::BYTES;
-      if (t + 1 < end) wait_async_tiles_but_last<COPIES>();
+    for (int t = 0; t < stages; ++t) {
+      const lds_addr at_a = places[t & 1], at_b = at_a + 3 * SA::BYTES;
+      if (t + 1 < stages) wait_async_tiles_but_last<COPIES>();
       else wait_async_tiles();
       if (t + 1 == stages && left < kDepth) {
 #pragma unroll
@@ -352,8 +351,139 @@ template <int BM, int BN, int WM, int WN, bool TRA, bool TRB, int PAIRS> struct 
         });
       }
       __syncthreads();
-      if (t + 2 < end) copy_stage(t + 2, at_a);
+      if (t + 2 < stages) copy_stage(t + 2, at_a);
     }
+  }
+
+  // The same with B as it lies in fp32 memory, on any element: a weight that few rows are multiplied with is read once, 4 bytes an element, where laying out planes moves 16.  A
+  // lane loads the chunks that it would have copied, two stages ahead, and puts their planes where the copies would have gone.  b_ld in fp32 elements; n_limit: rows (columns) that B has; stages
+  // [begin, end) of k.  One barrier per stage: behind it nobody reads the other place any more.
+  S1F_DEV static void run_raw(f32x4 (&acc)[MB][NB], const Matrix &a, const float *b, int64_t b_ld, int64_t m0, int64_t m_limit, int64_t n0, int64_t n_limit, int64_t k, int begin,
+                              int end, lds_addr lds, int64_t b_apart = 0) {
+    typedef float Loose4 __attribute__((ext_vector_type(4), aligned(4)));
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (begin >= end) return;
+    SA sa;
+    sa.init(a.data, a.ld, m0, m_limit, 0, begin, wave, lane);
+    const int stages = (int)((k + kDepth - 1) / kDepth), left = (int)((k - 1) % kDepth) + 1;
+    constexpr int PB = SB::PER_WAVE;
+    const float *from[PB];
+    int there[PB], row[PB];   // columns that there are from the chunk on (rows: its first place in the contraction), and its row
+    const int64_t step = TRB ? kDepth * b_ld : kDepth;
+#pragma unroll
+    for (int i = 0; i < PB; ++i) {
+      int r, c;
+      SB::slot(wave * PB + i, lane, r, c);
+      row[i] = r;
+      if constexpr (TRB) {
+        there[i] = (int)(n_limit - n0) - 8 * c;
+        from[i] = b + n0 + 8 * c + (begin * (int64_t)kDepth + r) * b_ld;
+      } else {
+        there[i] = 8 * c;
+        const int second = b_apart ? (r >> 4) & 1 : 0;
+        if (b_apart) r = (r >> 5 << 4) + (r & 15);
+        if (n0 + r >= n_limit) r = (int)(n_limit - 1 - n0);
+        from[i] = b + (n0 + r + (second ? b_apart : 0)) * b_ld + 8 * c + begin * (int64_t)kDepth;
+      }
+    }
+    const bool edge = TRB && n0 + BN > n_limit;
+    const int ragged = left < kDepth ? stages - 1 : stages;   // first stage that is not whole
+    f32x4 raw[2][PB][2];
+    // (fences: the compiler counts neither the copies nor where its loads lie among them; see the wait)
+    auto load = [&](f32x4 (&v)[PB][2], int t) {
+      asm volatile("" ::: "memory");
+      if (!edge && t < ragged) {
+#pragma unroll
+        for (int i = 0; i < PB; ++i) {
+          v[i][0] = *reinterpret_cast<const Loose4 *>(from[i]);
+          v[i][1] = *reinterpret_cast<const Loose4 *>(from[i] + 4);
+        }
+      } else {
+        const int rows_left = t < ragged ? kDepth : left;
+#pragma unroll
+        for (int i = 0; i < PB; ++i) {
+          const int n = TRB ? (row[i] < rows_left ? there[i] : 0) : rows_left - there[i];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[i][e / 4][e % 4] = e < n ? from[i][e] : 0.f;
+        }
+      }
+      asm volatile("" ::: "memory");
+#pragma unroll
+      for (int i = 0; i < PB; ++i) from[i] += step;
+    };
+    auto put = [&](const f32x4 (&v)[PB][2], lds_addr at_b) {
+#pragma unroll
+      for (int i = 0; i < PB; ++i) {
+        const Planes q = split3(v[i][0], v[i][1]);
+#pragma unroll
+        for (int p = 0; p < 3; ++p)
+          *reinterpret_cast<__attribute__((address_space(3))) bf16x8 *>((uintptr_t)(at_b + (unsigned)(p * SB::BYTES + (wave * PB + i) * 1024 + 16 * lane))) = q.p[p];
+      }
+    };
+    auto copy_a = [&](int t, lds_addr at_a) {
+      if (t == ragged) sa.shorten(left, wave, lane);
+      for_each<3>([&](auto plane) {
+        constexpr int p = decltype(plane)::value;
+        const char *at = uniform_pointer(sa.next + p * a.plane * 2);
+        const unsigned to = __builtin_amdgcn_readfirstlane(at_a + (unsigned)(p * SA::BYTES + wave * SA::PER_WAVE * 1024));
+        for_each<SA::PER_WAVE>([&](auto i) { sa.template copy<decltype(i)::value>(at, to); });
+      });
+      sa.next += sa.step;
+    };
+    const lds_addr places[2] = {lds, lds + 3 * (SA::BYTES + SB::BYTES)};
+    const lds_addr lane_a = SA::at(wm * MB, lane), lane_b = SB::at(wn * NB, lane);
+    load(raw[0], begin);
+    if (begin + 1 < end) load(raw[1], begin + 1);
+    put(raw[0], places[0] + 3 * SA::BYTES);
+    copy_a(begin, places[0]);
+    if (begin + 2 < end) load(raw[0], begin + 2);
+    auto stage = [&](int t, auto parity) {
+      constexpr int Q = decltype(parity)::value;
+      const lds_addr at_a = places[Q], at_b = at_a + 3 * SA::BYTES;
+      // the copies of A's stage t, behind which only the loads of stage t + 2 have been issued: 2 PB of them, if they are whole
+      if (t + 2 < end && t + 2 < ragged && !edge) wait_async_tiles_but_last<2 * PB>();
+      else wait_async_tiles();
+      if (t >= ragged) {
+#pragma unroll
+        for (int p = 0; p < 3; ++p) sa.clear_tail(at_a + p * SA::BYTES, left, wave, lane);
+      }
+      __syncthreads();
+      if (t + 1 < end) {
+        put(raw[1 - Q], places[1 - Q] + 3 * SA::BYTES);   // (before the copies: the wait for its loads counts from their end)
+        copy_a(t + 1, places[1 - Q]);
+        if (t + 3 < end) load(raw[1 - Q], t + 3);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        bf16x8 fa[3][MB], fb[3][NB];
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+          const lds_addr pa = SA::half_of(at_a + p * SA::BYTES + lane_a, half), pb = SB::half_of(at_b + p * SB::BYTES + lane_b, half);
+#pragma unroll
+          for (int j = 0; j < NB; ++j) fb[p][j] = SB::operand(pb, j, half);
+#pragma unroll
+          for (int i = 0; i < MB; ++i) fa[p][i] = SA::operand(pa, i, half);
+        }
+        for_each<6>([&](auto pair) {   // (as above, smallest products first)
+          constexpr int P = decltype(pair)::value, PA = (0x001102 >> (4 * P)) & 3, PBB = (0x010120 >> (4 * P)) & 3;
+#pragma unroll
+          for (int i = 0; i < MB; ++i)
+#pragma unroll
+            for (int j = 0; j < NB; ++j) acc[i][j] = mma16(fb[PBB][j], fa[PA][i], acc[i][j]);
+        });
+      }
+    };
+#pragma unroll 1
+    for (int t = begin; t < end; t += 2) {
+      stage(t, Int<0>{});
+      if (t + 1 < end) stage(t + 1, Int<1>{});
+    }
+    __syncthreads();
   }
 };
 

@@ -43,10 +43,10 @@ struct FfnArgs {
   float *part;                    // [part][tile][row][column]
   PackJob jobs[kMostJobs];
   int32_t n_jobs;
-  // few rows: both operands as they lie in the call's tensors (h: rows of inner_width elements)
-  const void *rows, *weight;
-  RowsOf rows_at;
+  // the weight as it lies in memory, for kernels that read it there; few rows: the rows, too (h: rows of inner_width elements)
+  const void *weight, *rows;
   int64_t weight_stride;
+  RowsOf rows_at;
 };
 
 // ---- operands --------------------------------------------------------------------------------------------------------------------------
@@ -136,13 +136,14 @@ S1F_DEV void ffn_tile(const FfnArgs &a, int &tm, int &tn, int &tile, int &part, 
   decode_tile(a.tiles_m, a.tiles_n, tile, tm, tn);
 }
 
-// (one workgroup to a unit where LDS holds all planes of two stages)
+// fp32 products in low tiles read the weight as it lies in memory, and have all planes of two stages in LDS: one workgroup to a unit.
 template <int PAIRS, int BM> constexpr bool kAllPlanes = PAIRS == 6 && BM == 64;
 template <typename P, int PAIRS, int BM>
 S1F_DEV void ffn_product(f32x4 (&acc)[P::MB][P::NB], const FfnArgs &a, int m0, int n0, int part, int parts, lds_addr lds, int64_t b_apart = 0) {
   const int64_t stages = (a.k + kDepth - 1) / kDepth * (kAllPlanes<PAIRS, BM> ? 1 : PAIRS);
   const int begin = (int)(stages * part / parts), end = (int)(stages * (part + 1) / parts);
-  if constexpr (kAllPlanes<PAIRS, BM>) P::run_planes(acc, a.a, a.b, m0, a.m_limit, n0, a.n_limit, a.k, begin, end, lds, b_apart);
+  if constexpr (kAllPlanes<PAIRS, BM>)
+    P::run_raw(acc, a.a, reinterpret_cast<const float *>(a.weight), a.weight_stride, m0, a.m_limit, n0, a.n, a.k, begin, end, lds, b_apart);
   else P::run(acc, a.a, a.b, m0, a.m_limit, n0, a.n_limit, a.k, begin, end, lds, b_apart);
 }
 
@@ -534,19 +535,20 @@ struct Cuts {
 constexpr int tile_m(Tile t) { return t == kBig ? 256 : t == kMiddle ? 128 : 64; }
 constexpr int tile_n(Tile t) { return t == kBig ? 256 : 128; }
 // Predicted microseconds of `tiles` tiles of so many stages: as tiles_us has them, but that few rounds of smaller tiles count whole, too (540 tiles of 128 x 128 and 66 stages: 130 us, 512 of them
-// 65), and that low tiles of planes copy all planes of a stage at once and have a unit to themselves (1.35 us for the six products of a stage, 1.8 where an operand lies by columns).
+// 65), and that low tiles of fp32 work on all planes of a stage at once and have a unit to themselves (1.6 us for the six products of a stage, 1.9 where an operand lies by columns).
 enum Operand { kBf16, kPlanes, kPlanesByColumns };
 double round_us(Tile tile, int64_t tiles, double stages, Operand operand) {
-  if (tile == kLow && operand != kBf16) return (double)((tiles + kUnits - 1) / kUnits) * (5.5 + (operand == kPlanes ? 0.225 : 0.3) * stages);
+  if (tile == kLow && operand != kBf16) return (double)((tiles + kUnits - 1) / kUnits) * (5.5 + (operand == kPlanes ? 0.265 : 0.32) * stages);
   if (tile == kBig || tiles > 6 * kUnits) return tiles_us(tile, tiles, stages);
   const int64_t rounds = tiles / (2 * kUnits), rest = tiles - rounds * 2 * kUnits;
   return (rounds ? (double)rounds * tiles_us(tile, 2 * kUnits, stages) / 1.25 : 0.0) + (rest ? tiles_us(tile, rest, stages) : 0.0);
 }
-// low: whether there are kernels for low tiles; split: whether a sum may be cut along its contraction
-Cuts cuts_for(int64_t m, int64_t n, int64_t stages, Operand operand, bool low, bool split) {
+// low: whether there are kernels for low tiles; split: whether a sum may be cut along its contraction; laid_out: microseconds for a weight's planes, which low tiles do without
+Cuts cuts_for(int64_t m, int64_t n, int64_t stages, Operand operand, bool low, bool split, double laid_out = 0.0) {
   Cuts best = {};
   double best_us = 1e30;
   auto offer = [&](const Cuts &c, double us) {
+    if (c.tile != kLow) us += laid_out;
     if (us < 0.98 * best_us) {
       best_us = us;
       best = c;
@@ -622,29 +624,38 @@ FfnPlan plan_of(const s1f_rows *d, int64_t inner, int64_t in_stride, int64_t out
     p.bytes = at;
     return p;
   }
+  const bool f32 = p.planes == 3;
+  const int64_t pairs = f32 ? 6 : 1;
+  auto stages = [&](int64_t k) { return (k + kDepth - 1) / kDepth * pairs; };
+  const Operand rows = f32 ? kPlanes : kBf16, columns = f32 ? kPlanesByColumns : kBf16;
+  // planes of a weight: 4 bytes read and 6 written, and a share of a launch
+  auto laid_out = [&](int64_t elements) { return f32 ? 3.0 + (double)elements * 10 / 4.4e6 : 0.0; };
+  int64_t part = 0;
+  if (!backward) {
+    // (tiles of [g | u]: as many columns of either)
+    p.up = cuts_for(p.n, 2 * up_to(inner, 16), stages(h), rows, true, false, laid_out(2 * inner * h));
+    p.down = cuts_for(p.n, h, stages(inner), rows, true, true, laid_out(inner * h));
+    part = part_bytes(p.down);
+    p.direct_in |= f32 && p.up.tile == kLow;
+    p.direct_out |= f32 && p.down.tile == kLow;
+  } else {
+    p.turns = turns_of(p.n, p.planes);
+    p.per_turn = up_to((p.n + p.turns - 1) / p.turns, kDepth);
+    p.dh = cuts_for(p.n, inner, stages(h), columns, true, false, laid_out(inner * h));
+    p.dx = cuts_for(p.n, h, stages(2 * inner), columns, true, true, laid_out(2 * inner * h));
+    p.dw_in = cuts_for(2 * inner, h, stages(p.per_turn), columns, false, true);
+    p.dw_out = cuts_for(h, inner, stages(p.per_turn), columns, false, true);
+    for (const Cuts &c : {p.dx, p.dw_in, p.dw_out}) part = std::max(part, part_bytes(c));
+    p.direct_in |= f32 && p.dx.tile == kLow;
+    p.direct_out |= f32 && p.dh.tile == kLow;
+  }
   p.x = take(p.planes * 2 * p.n * p.width);
   if (!p.direct_in) p.w_in = take(p.planes * 2 * 2 * inner * p.width);
   if (!p.direct_out) p.w_out = take(p.planes * 2 * h * p.inner_width);
   p.h = take(p.planes * 2 * p.n * p.inner_width);
-  const int64_t pairs = p.planes == 3 ? 6 : 1;
-  auto stages = [&](int64_t k) { return (k + kDepth - 1) / kDepth * pairs; };
-  const Operand rows = p.planes == 3 ? kPlanes : kBf16, columns = p.planes == 3 ? kPlanesByColumns : kBf16;
-  int64_t part = 0;
-  if (!backward) {
-    // (tiles of [g | u]: as many columns of either)
-    p.up = cuts_for(p.n, 2 * up_to(inner, 16), stages(h), rows, true, false);
-    p.down = cuts_for(p.n, h, stages(inner), rows, true, true);
-    part = part_bytes(p.down);
-  } else {
-    p.turns = turns_of(p.n, p.planes);
-    p.per_turn = up_to((p.n + p.turns - 1) / p.turns, kDepth);
+  if (backward) {
     p.dy = take(p.planes * 2 * p.n * p.width);
     p.dz = take(p.planes * 2 * p.n * p.dz_ld);
-    p.dh = cuts_for(p.n, inner, stages(h), columns, true, false);
-    p.dx = cuts_for(p.n, h, stages(2 * inner), columns, true, true);
-    p.dw_in = cuts_for(2 * inner, h, stages(p.per_turn), columns, false, true);
-    p.dw_out = cuts_for(h, inner, stages(p.per_turn), columns, false, true);
-    for (const Cuts &c : {p.dx, p.dw_in, p.dw_out}) part = std::max(part, part_bytes(c));
   }
   p.part = take(part);
   p.bytes = at;
@@ -741,6 +752,9 @@ struct Operands {
   }
 };
 
+void set_weight(FfnArgs &a, const void *weight, int64_t stride) {
+  a.weight = weight; a.weight_stride = stride;
+}
 void set_product(FfnArgs &a, const Matrix &ma, const Matrix &mb, int64_t m, int64_t m_limit, int64_t n, int64_t n_limit, int64_t k) {
   a.a = ma; a.b = mb;
   a.m = (int32_t)m; a.m_limit = (int32_t)m_limit; a.n = (int32_t)n; a.n_limit = (int32_t)n_limit; a.k = (int32_t)k;
@@ -797,10 +811,12 @@ int forward(const s1f_rows *d, const FfnPlan &p, const void *x, const void *w_in
   const Matrix mo = ops.weight(w_out, d->hidden, inner, out_stride, p.inner_width, p.direct_out, ws + p.w_out);
   int e = ops.pack(st);
   if (e != S1F_OK) return e;
-  set_product(a, mx, mi, p.n, p.n, inner, inner, p.width);
+  set_product(a, mx, mi, p.n, p.n, inner, inner, d->hidden);
+  set_weight(a, w_in, in_stride);
   e = launch_product<Up<T>::template Of>(p.up, a, 2 * up_to(inner, 16), st);
   if (e != S1F_OK) return e;
-  set_product(a, Matrix{a.h, a.h_ld, a.h_plane}, mo, p.n, p.n, d->hidden, d->hidden, p.inner_width);
+  set_product(a, Matrix{a.h, a.h_ld, a.h_plane}, mo, p.n, p.n, d->hidden, d->hidden, inner);
+  set_weight(a, w_out, out_stride);
   set_out(a, y, y_rows(d), wide_side(d, y, d->y_stride_b, d->y_stride_s), 1.f);
   return launch_product<Of3<T, false, false, R>::template Of>(p.down, a, d->hidden, st);
 }
@@ -822,9 +838,11 @@ int backward(const s1f_rows *d, const FfnPlan &p, const void *dy, const void *x,
   const int64_t h = d->hidden, n = p.n;
   const Matrix mdz = {a.dz, a.dz_ld, a.dz_plane}, mh = {a.h, a.h_ld, a.h_plane};
   set_product(a, mdy, mo, n, n, inner, p.inner_width, h);
+  set_weight(a, w_out, out_stride);
   e = launch_product<Dh<T>::template Of>(p.dh, a, inner, st);
   if (e != S1F_OK) return e;
   set_product(a, mdz, mi, n, n, h, p.width, 2 * inner);
+  set_weight(a, w_in, in_stride);
   set_out(a, dx, x_rows(d), wide_side(d, dx, d->x_stride_b, d->x_stride_s), kDown);
   e = launch_product<Of3<T, false, true, R>::template Of>(p.dx, a, h, st);
   if (e != S1F_OK) return e;

@@ -264,7 +264,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) loss_scores_kernel(const Loss
   if (m0 >= count || n0 >= a.piece) return;
   f32x4 acc[P::MB][P::NB];
   const Matrix rows = {a.rows, a.width, a.rows_plane};
-  if constexpr (PAIRS == 6 && BM == 64) P::run_planes(acc, rows, weight_matrix(a), m0, count, n0, a.piece, a.width, 0, (a.width + kDepth - 1) / kDepth, to_lds_addr(smem));
+  if constexpr (PAIRS == 6 && BM == 64) P::run_planes(acc, rows, weight_matrix(a), m0, count, n0, a.piece, a.width, to_lds_addr(smem));
   else P::run(acc, rows, weight_matrix(a), m0, count, n0, a.piece, a.width, 0, (a.width + kDepth - 1) / kDepth * PAIRS, to_lds_addr(smem));
   const int lane = lane_id(), n = lane & 15, j = lane >> 4, wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
   if constexpr (sizeof(T) == 4) scores_plain(acc, a, count, m0 + 16 * wm * P::MB, n0 + 16 * wn * P::NB);
