@@ -127,6 +127,33 @@ def test_strided_weights():
         assert torch.equal(w[:, 3:-3], v) and (w[:, :3] == 7).all() and (w[:, -3:] == 7).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [3, 100])
+def test_weights_whose_rows_are_far_apart(n, dtype):
+    """Rows of both weights 2^22 - 8 elements apart, the farthest: the up rows lie 2^29 elements behind the gate's."""
+    c = Block((1, n, 64, 128, "dense", "dense", "silu"), dtype)
+    y, gate_up = c.forward()
+    start = c.start()
+    want = c.backward(gate_up, "f32", start)
+    far = 2 ** 22 - 8
+    big = torch.empty(255 * far + 128, dtype=c.x.dtype, device="cuda")
+    near = c.w_in, c.w_out
+    c.w_in = big.as_strided((256, 64), (far, 1))
+    c.w_in.copy_(near[0])
+    c.w_out = big.as_strided((64, 128), (far, 1), 64)      # beside it
+    c.w_out.copy_(near[1])
+    got = c.forward()
+    assert torch.equal(got[0], y) and torch.equal(got[1], gate_up)
+    assert all(torch.equal(a, b) for a, b in zip(c.backward(gate_up, "f32", start), want))
+    big = torch.empty(255 * far + 128, dtype=torch.float32, device="cuda")
+    dw = big.as_strided((256, 64), (far, 1)), big.as_strided((64, 128), (far, 1), 64)
+    for d, s in zip(dw, start):
+        d.copy_(s)
+    ws = space(s1f.gated_ffn_bwd_workspace_bytes(c.dy, c.x, c.w_in, c.w_out))[0]
+    s1f.gated_ffn_bwd(c.dy, c.x, c.w_in, c.w_out, s1f.SILU, gate_up, torch.empty_like(c.x), *dw, ws)
+    assert all(torch.equal(a, b) for a, b in zip(dw, want[1:]))
+
+
 @pytest.mark.parametrize("act", list(ACTS))
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_gates_far_out(act, dtype):

@@ -114,6 +114,15 @@ def test_forward_and_gradient(case, dtype, interleaved, norm):
 
 
 @pytest.mark.parametrize("norm", [False, True])
+@pytest.mark.parametrize("case", [(2, 2, 1, 100003, 8, 8, "rows", "dense"), (1, 3, 2, 150001, 24, 10, "dense", "dense"), (1, 40, 40, 2100, 16, 16, "dense", "dense")])
+def test_many_units_to_a_workgroup(case, norm):
+    """More rows than there are workgroups: each walks blocks of them, with heads of every tensor."""
+    c = Call(case, "bf16", False, norm, True)
+    c.check_forward(c.forward())
+    c.check_backward(c.backward())
+
+
+@pytest.mark.parametrize("norm", [False, True])
 def test_magnitude_and_no_values(norm):
     c = Call((2, 4, 2, 29, 128, 96, "rows", "dense"), "f32", False, norm, True, magnitude=1.25, values=False)
     c.check_forward(c.forward())
