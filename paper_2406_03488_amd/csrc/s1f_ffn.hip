@@ -3,7 +3,8 @@
 //   forward    [g | u] = x W_in^T,  h = act(g) * u,  y = h W_out^T
 //   backward   dh = dy W_out,  dg = dh * u * act'(g),  du = dh * act(g);  dx = [dg | du] W_in,  dW_in += [dg | du]^T x,  dW_out += dy^T h
 //
-// Bound by the matrix units: 6 n hidden inner operations and 12.  Nothing of it is a pass over memory of its own: a tile of x W_in^T holds the same columns of
+// Bound by the matrix units, at the clock that power leaves them: 6 n hidden inner operations and 12.  Forward of 4099 x 4096 x 11008 bf16 921 to 955 us, 1.16 to 1.2 PFLOP/s (a library product of
+// 16384^3 of random operands: 1.33); gradient of 4897 x 7168 x 19200 6.5 to 6.7 ms, 1.21 to 1.24.  Few rows: the weights.  Nothing of it is a pass over memory of its own: a tile of x W_in^T holds the same columns of
 // both halves, in the same lanes, so that h is what its results leave in memory (and g and u, rounded, if the caller keeps them); dh stays in registers, and the tile
 // that computes it reads g and u and leaves dg, du and h.  h, dg and du are bf16 in memory, rounded once, as the attention kernels round their probabilities and score
 // gradients; fp32 calls: three bf16 planes that hold them whole, and fp32 operands are split into such planes first.
@@ -249,7 +250,8 @@ S1F_DEV void clear_behind(float (&v)[8], int there) {
     if (e >= there) v[e] = 0.f;
 }
 
-// h = act(g) * u of a tile of BM rows and BN / 2 columns.  m0: first row of the wave's blocks, n0: its first column.
+// h = act(g) * u of a tile of BM rows and BN / 2 columns.  4099 x 4096 x 2 x 11008 bf16, g and u kept: 637 us, 1.16 PFLOP/s, matrix units 62 % busy; 17 rows of tiles for 16.01, and 6 rounds of them
+// for 5.7, are 8 % of it.  m0: first row of the wave's blocks, n0: its first column.
 template <typename T, int ACT, typename P> S1F_DEV void up_results(const f32x4 (&acc)[P::MB][P::NB], const FfnArgs &a, int m0, int n0, char *smem) {
   constexpr int PAIRS = sizeof(T) == 4 ? 6 : 1, LANES = P::NB, ROWS = 64 / LANES;   // lanes to a row of 8 NB columns
   Staged<P> staged(smem);
@@ -292,7 +294,7 @@ template <typename T, int BM, int BN, int WM, int WN> __global__ void __launch_b
   with_activation(a.act, [&](auto act) { up_results<T, decltype(act)::value, P>(acc, a, m0 + 16 * P::MB * wm, n0 + 8 * P::NB * wn, smem); });
 }
 
-// dh = dy W_out of a tile, and of it [dg | du] and h.  (g and u asked for four rows ahead instead of two: no faster.)
+// dh = dy W_out of a tile, and of it [dg | du] and h.  4897 x 7168 x 19200 bf16: 1.14 ms, 1.18 PFLOP/s.  (g and u asked for four rows ahead instead of two: no faster.)
 template <typename T, int ACT, typename P> S1F_DEV void dh_results(const f32x4 (&acc)[P::MB][P::NB], const FfnArgs &a, int m0, int n0, char *smem) {
   constexpr int PAIRS = sizeof(T) == 4 ? 6 : 1, LANES = 2 * P::NB, ROWS = 64 / LANES;
   Staged<P> staged(smem);
@@ -358,7 +360,7 @@ template <Result R> S1F_DEV void put_result(const FfnArgs &a, int row, int col, 
   }
 }
 
-// y, dx, dW_in and dW_out.  The tiles from `whole` on are cut along the contraction: their parts are added up by the join.
+// y, dx, dW_in and dW_out.  4897 x 7168 x 19200 bf16: dx 2.06 ms, 1.31 PFLOP/s, dW_out 1.05, 1.29, dW_in 2.15, 1.26; fp32, 682 x 1280 x 3413: dx 96 us, either dW 82.  The tiles from `whole` on are cut along the contraction: their parts are added up by the join.
 template <int PAIRS, int BM, int BN, int WM, int WN, bool TRA, bool TRB, Result R> __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_product_kernel(const FfnArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   typedef Product<BM, BN, WM, WN, TRA, TRB, PAIRS> P;
@@ -403,7 +405,8 @@ template <int BM, int BN, Result R> __global__ void __launch_bounds__(256) ffn_j
 
 // Products of few rows are bound by reading the weights, once.  A workgroup has 16 columns (of gate and up both, or of y), whose rows of the weight its waves read in parts along the
 // contraction, straight into the registers of the matrix instructions: each lane 16 bytes of its row at a time, several stages of 64 ahead, no LDS, nothing laid out anew (fp32 is split on
-// the way), any strides.  The waves' sums meet in LDS.
+// the way), any strides.  The waves' sums meet in LDS.  16 x 4096 x 11008 bf16: 180 MB of W_in in 36 us, 5.0 TB/s, 90 MB of W_out in 22, 4.0; the rows, which every workgroup reads, cost 12 of both
+// (one row: 52 us in all).  Two blocks of columns to a workgroup share them, but leave fewer loads in flight: 65 -> 74.
 template <typename T, int BLOCKS> struct Ahead {   // elements of a stage of one operand: 16 rows a block, lane (n, j) has 8j .. 8j+7 of either half of row n
   typedef Piece<T, false> P;
   static constexpr int PER = 8 / P::N;
@@ -599,11 +602,11 @@ int check_ffn(const s1f_rows *d, int64_t inner, int64_t in_stride, int64_t out_s
 constexpr int64_t kSummed = 8192;
 int64_t turns_of(int64_t n, int64_t planes) { return planes == 1 || n < kSummed + kSummed / 2 ? 1 : (n + kSummed / 2) / kSummed; }
 
-// Forwards that the kernel of few rows takes: up to 64 fp32 rows, whose weights then need not be split in memory, up to 16 bf16 ones, and more where the call is small: it reads the rows once for
-// every 16 columns, where a tile has 64 at a time.  4096 x 11008, us, few and tiles: bf16 1 row 52 and 82, 16 65 and 83, 32 84 and 84, 64 128 and 89; fp32 1 row 109 and 445, 64 254 and 457.
-// bf16 32 x 1024 x 2816 16 and 19, 64 24 and 20, 64 x 256 x 688 11.3 and 12.9, 32 x 2048 x 5632 35 and 30.
-bool few_rows(int64_t n, int32_t dtype, int64_t hidden, int64_t inner) {
-  return n <= 64 && (dtype == S1F_F32 || n <= 16 || n * hidden * inner <= int64_t(1) << 27);
+// Forwards that the kernel of few rows takes: up to 16 rows, and up to 64 where the call is small.  It reads the rows once for every 16 columns, where a tile has 64 at a time; a tile waits for
+// its beginning and end.  us, few and tiles: 4096 x 11008, bf16 1 row 52 and 82, 16 65 and 83, 32 84 and 84, 64 128 and 89; fp32 1 row 113 and 157, 16 128 and 161, 32 165 and 161, 64 253 and 175;
+// bf16 32 x 1024 x 2816 16 and 19, 64 24 and 20, 64 x 256 x 688 11.3 and 12.9; fp32 32 x 1024 x 2816 31 and 41, 64 x 512 x 1376 27 and 31, 64 x 2048 x 5632 106 and 82.
+bool few_rows(int64_t n, int64_t hidden, int64_t inner) {
+  return n <= 16 || (n <= 64 && n * hidden * inner <= int64_t(1) << 27);
 }
 
 FfnPlan plan_of(const s1f_rows *d, int64_t inner, int64_t in_stride, int64_t out_stride, bool backward) {
@@ -618,7 +621,7 @@ FfnPlan plan_of(const s1f_rows *d, int64_t inner, int64_t in_stride, int64_t out
   p.direct_out = d->dtype == S1F_BF16 && inner % 8 == 0 && out_stride % 8 == 0;
   int64_t at = 0;
   auto take = [&at](int64_t bytes) { const int64_t was = at; at += up_to(bytes, 256); return was; };
-  p.few = !backward && few_rows(p.n, d->dtype, h, inner);
+  p.few = !backward && few_rows(p.n, h, inner);
   if (p.few) {
     p.h = take(p.planes * 2 * p.n * p.inner_width);
     p.bytes = at;
