@@ -265,7 +265,7 @@ int s1f_kv_grad_emit(const s1f_desc *desc, const float *dk_prefix_acc, const flo
  *     by p * freqs[i] radians, an angle that is computed in 64 bits, and scaled by `magnitude`.  The others stay as they are.  rotary_dim 0: freqs may be NULL.
  *   - positions int64 [batch, rows], rows contiguous, batch entries positions_stride_b apart, of any order and sign; NULL: row r has first_position + r.
  *   - v, v_cache (dv, dv_prefix_acc) may both be NULL.
- *   - q_rot may be q, k_cache + seg_off rows k, v_cache so v, dq dq_rot, where their strides are the same; dq may not be q.
+ *   - Sides, heads and rows may not overlap, and an output may be no input, but: q_rot may be q, k_cache + seg_off rows k, v_cache so v, dq dq_rot, where their strides are the same; dq may not be q.
  * Computed in fp32, rounded once.  Pointers are aligned to their element; calls are faster where rows, and half of rotary_dim unless interleaved, are made of 16 bytes.
  * Errors as for the attention calls: S1F_EINVAL, S1F_EUNSUPPORTED (dtype; head_dim odd or above 256; batch * rows > 2^26; more than 2^16 heads; batch * rows * (n_q_heads + 2 n_kv_heads) > 2^31), S1F_ERANGE (rows < 1,
  * rows outside [0, cache_capacity)), S1F_EDEVICE. */
@@ -291,8 +291,8 @@ int s1f_rope_bwd(const s1f_heads *desc, const void *dq_rot, const float *dk_pref
                  const int64_t *positions, int64_t positions_stride_b, int64_t first_position, int64_t seg_off, void *dq, void *dk, void *dv, void *hip_stream);
 
 /* The same behind a norm of every head of q and k: x / sqrt(sum(x^2) / head_dim + eps) * gain, gains [head_dim] in the element type, eps >= 0.  The backward
- * takes q and k, and adds the gradients of the gains, sums over all rows and heads, to the fp32 accumulators dq_gain_acc, dk_gain_acc [head_dim]; the same arguments give
- * the same bits.  workspace: device memory, 16-byte aligned, of at least s1f_qk_norm_rope_bwd_workspace_bytes(desc) bytes (0: invalid arguments); contents
+ * takes q and k, and adds the gradients of the gains, sums over all rows and heads, to the fp32 accumulators dq_gain_acc, dk_gain_acc [head_dim], which may not overlap (a gain
+ * of both has the sum of two); the same arguments give the same bits.  Sums of squares are fp32: with eps 0 a head of elements below 2^-60 or so, like one above 2^60, has no norm.  workspace: device memory, 16-byte aligned, of at least s1f_qk_norm_rope_bwd_workspace_bytes(desc) bytes (0: invalid arguments); contents
  * undefined afterwards. */
 int s1f_qk_norm_rope_fwd(const s1f_heads *desc, const void *q, const void *k, const void *v, const void *q_gain, const void *k_gain, float eps,
                          const double *freqs, float magnitude, const int64_t *positions, int64_t positions_stride_b, int64_t first_position, int64_t seg_off,
@@ -396,8 +396,8 @@ size_t s1f_token_loss_bwd_workspace_bytes(const s1f_rows *desc, int64_t vocab, i
  * precision (operands as three exact bf16 parts each, but for elements below 2^-110, which keep 8 bits at least, and for dgate and dup below 2^-126), of finite numbers below 2^112; whatever an
  * infinity or a NaN takes part in may be NaN.
  * A row's y, gate_up and dx depend on that row alone.
- * Weights and d; calls are faster where hidden and inner are multiples of 8 and all rows start on 16 bytes: other bf16 operands, and all fp32 ones,
- * are laid out anew in the workspace first.  inner <= 2^17, strides of weights < 2^22, 2 * inner * w_in_stride and hidden * w_out_stride < 2^30, batch * rows * hidden and
+ * w_in and w_out are 16-byte aligned.  Calls are faster where hidden and inner are multiples of 8 and all rows start on 16 bytes: but for few rows, other bf16 operands, and fp32 ones,
+ * are laid out anew in the workspace first.  inner <= 2^17, w_in_stride and w_out_stride < 2^22, 2 * inner * w_in_stride <= 2^30, batch * rows <= 2^20, batch * rows * hidden and
  * batch * rows * 2 * inner <= 2^33.  workspace: device memory, 16-byte aligned, of at least s1f_gated_ffn_*_workspace_bytes(...) bytes (0: invalid
  * arguments); contents undefined afterwards. */
 typedef enum { S1F_SILU = 0, S1F_GELU = 1, S1F_GELU_TANH = 2 } s1f_activation;

@@ -321,7 +321,6 @@ template <typename T, int ACT, typename P> S1F_DEV void dh_results(const f32x4 (
       }
       clear_behind(h, there);
       put8<PAIRS>(a.h + (int64_t)row * a.h_ld + col, a.h_plane, h, 8);
-      if (there <= 0) continue;
       bf16_t *to = a.dz + (int64_t)row * a.dz_ld + col;
       put8<PAIRS>(to, a.dz_plane, g, there);
       put8<PAIRS>(to + a.inner, a.dz_plane, u, there);

@@ -356,7 +356,7 @@ template <typename T, typename K, int PW, int L, int IT, int U, Layout LAYOUT, b
 #pragma unroll
             for (int e = 0; e < E; ++e) {
               w[t][e] *= by;
-              of_unit[t][e] = fmaf(v[t][e], w[t][e], of_unit[t][e]);
+              of_unit[t][e] = fmaf(mine ? v[t][e] : 0.f, w[t][e], of_unit[t][e]);   // (another's may be infinite)
               v[t][e] *= gain[t * L * E + e];
               along = fmaf(v[t][e], w[t][e], along);
             }
@@ -720,6 +720,8 @@ extern "C" int s1f_qk_norm_rope_bwd(const s1f_heads *desc, const void *dq_rot, c
                                     void *dv, float *dq_gain_acc, float *dk_gain_acc, void *workspace, size_t workspace_bytes, void *hip_stream) {
   const int rc = check_backward(desc, dq_rot, dk_prefix_acc, dv_prefix_acc, seg_off, freqs, magnitude, positions, dq, dk, dv);
   if (rc != S1F_OK) return rc;
+  // (each accumulator is added to by lanes of its own)
+  if (dq_gain_acc < dk_gain_acc + desc->head_dim && dk_gain_acc < dq_gain_acc + desc->head_dim) return S1F_EINVAL;
   if (!tensors_ok(desc->dtype, {q, k, q_gain, k_gain}) || !(eps >= 0.f) || !dq_gain_acc || !dk_gain_acc || !on4(dq_gain_acc) || !on4(dk_gain_acc) ||
       !workspace || !on16(workspace) || workspace_bytes < s1f_qk_norm_rope_bwd_workspace_bytes(desc))
     return S1F_EINVAL;

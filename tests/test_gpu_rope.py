@@ -162,13 +162,20 @@ def test_in_place(dtype, norm):
     else:
         s1f.rope_fwd(q, k, v, *turn, q, k, v)
     assert torch.equal(q, want[0]) and torch.equal(k, c.rows(want[1])) and torch.equal(v, c.v)
-    if not norm:
-        dq_rot = heads(c.rng, c.q.shape, dtype, "rows")
-        dka, dva = (heads(c.rng, (2, 2, 40, 128), "f32", "dense") for _ in range(2))
-        dq, dk, dv = like(c.q), like(c.k), like(c.v)
-        s1f.rope_bwd(dq_rot, dka, dva, *c.turn, dq, dk, dv)
-        s1f.rope_bwd(dq_rot, dka, dva, *c.turn, dq_rot, dk, dv)
-        assert torch.equal(dq, dq_rot)
+    dq_rot = like(c.q).copy_(heads(c.rng, c.q.shape, dtype, "rows"))
+    dka, dva = (heads(c.rng, (2, 2, 40, 128), "f32", "dense") for _ in range(2))
+    dgains = []
+    for dq in (like(c.q), dq_rot):
+        dk, dv = like(c.k), like(c.v)
+        if norm:
+            dgains.append(torch.zeros(2, 128, device="cuda"))
+            ws, _ = space(s1f.qk_norm_rope_bwd_workspace_bytes(dq_rot, dka))
+            s1f.qk_norm_rope_bwd(dq_rot, dka, dva, c.q, c.k, *c.gains, 1e-6, *c.turn, dq, dk, dv, *dgains[-1], ws)
+        else:
+            s1f.rope_bwd(dq_rot, dka, dva, *c.turn, dq, dk, dv)
+        if dq is not dq_rot:
+            want = dq
+    assert torch.equal(want, dq_rot) and (not norm or torch.equal(*dgains))
 
 
 @pytest.mark.parametrize("interleaved", [False, True])
@@ -198,6 +205,19 @@ def test_heads_that_are_zero_or_not_finite():
     mask[1, 5] = mask[2, 6] = False
     assert torch.equal(got[0][0][0][mask], clean[0][0][0][mask]) and torch.equal(got[1][3][0][mask], clean[1][3][0][mask])
     assert torch.isfinite(got[1][3][0, 1, 5]).all() and torch.isnan(got[1][7][0]).all() and torch.isfinite(got[1][7][1]).all()
+
+
+@pytest.mark.parametrize("case", [(1, 5, 3, 7, 128, 0, "dense", "dense"), (1, 3, 1, 33, 80, 0, "dense", "dense"), (1, 3, 1, 5, 6, 0, "dense", "dense")])
+def test_infinite_gradients(case):
+    """An infinity in the last head of the last row is one share of its column of the gain's gradient."""
+    c = Call(case, "f32", False, True, False)
+    dq_rot, dka, _, _, _, _, was, _ = c.backward()
+    dq_rot[0, -1, -1, 1] = c.rows(dka)[0, -1, -1, 2] = float("inf")
+    dgains = [w.clone() for w in was]
+    ws, _ = space(s1f.qk_norm_rope_bwd_workspace_bytes(dq_rot, dka))
+    s1f.qk_norm_rope_bwd(dq_rot, dka, None, c.q, c.k, *c.gains, 1e-6, *c.turn, torch.empty_like(c.q), torch.empty_like(c.k), None, *dgains, ws)
+    for got, x, col in ((dgains[0], c.q, 1), (dgains[1], c.k, 2)):
+        assert got[col].item() == float("inf") * np.sign(x[0, -1, -1, col].item()) and torch.isfinite(got).sum() == len(got) - 1
 
 
 def test_gradients_of_gains_are_the_same_every_time():

@@ -40,7 +40,7 @@ def norm_fwd(d, q=P, k=P, v=P, q_gain=P, k_gain=P, eps=1e-6, freqs=P, magnitude=
     return s1f.load_library().s1f_qk_norm_rope_fwd(ref(d), q, k, v, q_gain, k_gain, eps, freqs, magnitude, positions, 5, 0, off, q_rot, kc, vc, None)
 
 
-def norm_bwd(d, q_rot=P, kc=P, vc=P, x=P, y=P, q_gain=P, k_gain=P, eps=1e-6, freqs=P, magnitude=1.0, positions=P, off=0, q=P, k=P, v=P, dq_gain=P, dk_gain=P,
+def norm_bwd(d, q_rot=P, kc=P, vc=P, x=P, y=P, q_gain=P, k_gain=P, eps=1e-6, freqs=P, magnitude=1.0, positions=P, off=0, q=P, k=P, v=P, dq_gain=P, dk_gain=2 * P,
              ws=P, n=BIG):
     return s1f.load_library().s1f_qk_norm_rope_bwd(ref(d), q_rot, kc, vc, x, y, q_gain, k_gain, eps, freqs, magnitude, positions, 5, 0, off, q, k, v, dq_gain,
                                                    dk_gain, ws, n, None)
@@ -88,6 +88,8 @@ def test_pointers_refused(call):
     if call in (norm_fwd, norm_bwd):
         assert call(heads(), eps=-1e-9) == 1 and call(heads(), eps=math.nan) == 1
     if call is norm_bwd:
+        for at in (P, P + 4 * 63, P - 4 * 63):                    # gains' gradients in one place
+            assert call(heads(), dk_gain=at) == 1
         assert call(heads(), ws=OFF) == 1 and call(heads(), n=s1f.load_library().s1f_qk_norm_rope_bwd_workspace_bytes(ref(heads())) - 1) == 1
 
 

@@ -28,7 +28,7 @@ for what, *shape in eval(sys.argv[2]):
         assert lib.s1f_rope_fwd(d, p, p, p, *turn, p, p, p, None) == 0
         assert lib.s1f_rope_bwd(d, p, p, p, *turn, p, p, p, None) == 0
         assert lib.s1f_qk_norm_rope_fwd(d, p, p, p, p, p, 1e-6, *turn, p, p, p, None) == 0
-        assert lib.s1f_qk_norm_rope_bwd(d, p, p, p, p, p, p, p, 1e-6, *turn, p, p, p, p, p, p, big, None) == 0
+        assert lib.s1f_qk_norm_rope_bwd(d, p, p, p, p, p, p, p, 1e-6, *turn, p, p, p, p, p + 4096, p, big, None) == 0
 """
 
 
