@@ -355,6 +355,104 @@ template <int BM, int BN, int WM, int WN, bool TRA, bool TRB, int PAIRS> struct 
     }
   }
 
+  // The same for tiles of which LDS holds five thirds of a stage: planes 0 and 1 of two stages and planes 2 of one, which arrive under the four products of the others.  stages [begin, end)
+  // of k.  128 x 128, eight waves: 2.8 us per stage, where alone on a unit six passes of run take 4.3 and beside another tile 2.7.  What bounds it are the copies, 96 KiB a stage: without the products 2.6
+  // us, without the copies 1.9.  (Stages of 32, three of them in LDS and operands read one ahead of the products: the same, half lines of memory cost what the distance gains.)
+  static constexpr int TOGETHER_LDS_BYTES = 5 * (SA::BYTES + SB::BYTES);
+  S1F_DEV static void run_together(f32x4 (&acc)[MB][NB], const Matrix &a, const Matrix &b, int64_t m0, int64_t m_limit, int64_t n0, int64_t n_limit, int64_t k, int begin, int end,
+                                   lds_addr lds, int64_t b_apart = 0) {
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (begin >= end) return;
+    SA sa;
+    SB sb;
+    sa.init(a.data, a.ld, m0, m_limit, 0, begin, wave, lane);
+    sb.init(b.data, b.ld, n0, n_limit, b_apart, begin, wave, lane);
+    const int left = (int)((k - 1) % kDepth) + 1, ragged = left < kDepth ? (int)((k - 1) / kDepth) : 0x7fffffff;   // first stage that is not whole
+    constexpr int BOTH = SA::BYTES + SB::BYTES, COPIES = 2 * (SA::PER_WAVE + SB::PER_WAVE);
+    auto copy_plane = [&](const auto &side, const Matrix &m, int plane, lds_addr at) {
+      const char *from = uniform_pointer(side.next + plane * m.plane * 2);
+      const unsigned to = __builtin_amdgcn_readfirstlane(at + (unsigned)(wave * side.PER_WAVE * 1024));
+      for_each<std::remove_reference_t<decltype(side)>::PER_WAVE>([&](auto i) { side.template copy<decltype(i)::value>(from, to); });
+    };
+    // Places of a stage's planes 0 and 1, each a's and then b's, and behind them of planes 2.
+    const lds_addr places[2] = {lds, lds + 2 * BOTH}, at_last = lds + 4 * BOTH;
+    auto copy_first = [&](int t, lds_addr at) {
+      if (t == ragged) {
+        sa.shorten(left, wave, lane);
+        sb.shorten(left, wave, lane);
+      }
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        copy_plane(sa, a, p, at + p * BOTH);
+        copy_plane(sb, b, p, at + p * BOTH + SA::BYTES);
+      }
+    };
+    auto clear_plane = [&](lds_addr at) {
+      sa.clear_tail(at, left, wave, lane);
+      sb.clear_tail(at + SA::BYTES, left, wave, lane);
+    };
+    const lds_addr lane_a = SA::at(wm * MB, lane), lane_b = SA::BYTES + SB::at(wn * NB, lane);
+    auto read = [&](bf16x8 (&xa)[MB], bf16x8 (&xb)[NB], lds_addr at, int half) {
+      const lds_addr pa = SA::half_of(at + lane_a, half), pb = SB::half_of(at + lane_b, half);
+#pragma unroll
+      for (int j = 0; j < NB; ++j) xb[j] = SB::operand(pb, j, half);
+#pragma unroll
+      for (int i = 0; i < MB; ++i) xa[i] = SA::operand(pa, i, half);
+    };
+    auto multiply = [&](const bf16x8 (&xa)[MB], const bf16x8 (&xb)[NB]) {
+#pragma unroll
+      for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) acc[i][j] = mma16(xb[j], xa[i], acc[i][j]);
+    };
+    copy_first(begin, places[0]);
+#pragma unroll 1
+    for (int t = begin; t < end; ++t) {
+      const int in = (t - begin) & 1;
+      const lds_addr at = places[in];
+      wait_async_tiles();
+      if (t >= ragged) {
+#pragma unroll
+        for (int p = 0; p < 2; ++p) clear_plane(at + p * BOTH);
+      }
+      __syncthreads();
+      copy_plane(sa, a, 2, at_last);
+      copy_plane(sb, b, 2, at_last + SA::BYTES);
+      if (t + 1 < end) {
+        sa.next += sa.step;
+        sb.next += sb.step;
+        copy_first(t + 1, places[1 - in]);
+      }
+      bf16x8 fa[2][MB], fb[2][NB];   // planes 0 of either half, for the products with planes 2, too
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        bf16x8 ga[MB], gb[NB];
+        read(fa[half], fb[half], at, half);
+        read(ga, gb, at + BOTH, half);
+        multiply(ga, gb);
+        multiply(fa[half], gb);
+        multiply(ga, fb[half]);
+        multiply(fa[half], fb[half]);
+      }
+      if (t + 1 < end) wait_async_tiles_but_last<COPIES>();
+      else wait_async_tiles();
+      if (t >= ragged) clear_plane(at_last);
+      __syncthreads();
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        bf16x8 ga[MB], gb[NB];
+        read(ga, gb, at_last, half);
+        multiply(ga, fb[half]);
+        multiply(fa[half], gb);
+      }
+    }
+    __syncthreads();
+  }
+
   // The same with B as it lies in fp32 memory, on any element: a weight that few rows are multiplied with is read once, 4 bytes an element, where laying out planes moves 16.  A
   // lane loads the chunks that it would have copied, two stages ahead, and puts their planes where the copies would have gone.  b_ld in fp32 elements; n_limit: rows (columns) that B has; stages
   // [begin, end) of k.  One barrier per stage: behind it nobody reads the other place any more.

@@ -37,7 +37,6 @@ struct FfnArgs {
   void *gate_up;                  // [.][2 * inner]
   void *out;
   RowsOf out_rows;
-  int32_t wide_out;
   float scale;                    // of the results (see kUp)
   // tiles (see Cuts)
   int32_t tiles_m, tiles_n, tile0, quarters, whole, rest, splits;
@@ -137,14 +136,17 @@ S1F_DEV void ffn_tile(const FfnArgs &a, int &tm, int &tn, int &tile, int &part, 
   decode_tile(a.tiles_m, a.tiles_n, tile, tm, tn);
 }
 
-// fp32 products in low tiles read the weight as it lies in memory, and have all planes of two stages in LDS: one workgroup to a unit.
+// fp32 products in low tiles read the weight as it lies in memory, and have all planes of two stages in LDS: one workgroup to a unit.  So do middle tiles with planes that were laid out, and have
+// five thirds of a stage there.
 template <int PAIRS, int BM> constexpr bool kAllPlanes = PAIRS == 6 && BM == 64;
+template <int PAIRS, int BM> constexpr bool kTogether = PAIRS == 6 && BM == 128;
 template <typename P, int PAIRS, int BM>
 S1F_DEV void ffn_product(f32x4 (&acc)[P::MB][P::NB], const FfnArgs &a, int m0, int n0, int part, int parts, lds_addr lds, int64_t b_apart = 0) {
-  const int64_t stages = (a.k + kDepth - 1) / kDepth * (kAllPlanes<PAIRS, BM> ? 1 : PAIRS);
+  const int64_t stages = (a.k + kDepth - 1) / kDepth * (kAllPlanes<PAIRS, BM> || kTogether<PAIRS, BM> ? 1 : PAIRS);
   const int begin = (int)(stages * part / parts), end = (int)(stages * (part + 1) / parts);
   if constexpr (kAllPlanes<PAIRS, BM>)
     P::run_raw(acc, a.a, reinterpret_cast<const float *>(a.weight), a.weight_stride, m0, a.m_limit, n0, a.n, a.k, begin, end, lds, b_apart);
+  else if constexpr (kTogether<PAIRS, BM>) P::run_together(acc, a.a, a.b, m0, a.m_limit, n0, a.n_limit, a.k, begin, end, lds, b_apart);
   else P::run(acc, a.a, a.b, m0, a.m_limit, n0, a.n_limit, a.k, begin, end, lds, b_apart);
 }
 
@@ -187,22 +189,21 @@ template <typename T> S1F_DEV void set8(T *to, int there, const float (&v)[8]) {
     P::store(to + i, there - i, p);
   }
 }
-template <typename T> S1F_DEV void put_values(T *to, f32x4 v, bool wide, int there) {
-  if (wide && there >= 4) {
-    store4<T>(to, v[0], v[1], v[2], v[3]);
+// Four values of a row, on any element; the first `there` of them.  (One access also where rows do not start on 16 bytes: gradient of 100 x 1280 x 3413 fp32 196 -> 182 us, of 1000 x 1001 x 2003 bf16 88 -> 80.)
+template <typename T> using LooseFour = T __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+template <typename T> S1F_DEV void put_values(T *to, f32x4 v, int there) {
+  if (there >= 4) {
+    *reinterpret_cast<LooseFour<T> *>(to) = __builtin_convertvector(v, LooseFour<T>);
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       if (e < there) to[e] = (T)v[e];
   }
 }
-template <typename T> S1F_DEV f32x4 get_values(const T *from, bool wide, int there) {
+template <typename T> S1F_DEV f32x4 get_values(const T *from, int there) {
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
-  if (wide && there >= 4) {
-    typedef T Four __attribute__((ext_vector_type(4)));
-    const Four x = *reinterpret_cast<const Four *>(from);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = (float)x[e];
+  if (there >= 4) {
+    v = __builtin_convertvector(*reinterpret_cast<const LooseFour<T> *>(from), f32x4);
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -351,11 +352,11 @@ template <Result R> S1F_DEV void put_result(const FfnArgs &a, int row, int col, 
   const int64_t at = a.out_rows.offset(row) + col;
   const int there = a.n - col;
   if constexpr (R == kStoreBf16) {
-    put_values<bf16_t>(reinterpret_cast<bf16_t *>(a.out) + at, v, a.wide_out, there);
+    put_values<bf16_t>(reinterpret_cast<bf16_t *>(a.out) + at, v, there);
   } else {
     float *to = reinterpret_cast<float *>(a.out) + at;
-    if constexpr (R == kAddF32) v += get_values<float>(to, a.wide_out, there);
-    put_values<float>(to, v, a.wide_out, there);
+    if constexpr (R == kAddF32) v += get_values<float>(to, there);
+    put_values<float>(to, v, there);
   }
 }
 
@@ -537,10 +538,13 @@ struct Cuts {
 constexpr int tile_m(Tile t) { return t == kBig ? 256 : t == kMiddle ? 128 : 64; }
 constexpr int tile_n(Tile t) { return t == kBig ? 256 : 128; }
 // Predicted microseconds of `tiles` tiles of so many stages: as tiles_us has them, but that few rounds of smaller tiles count whole, too (540 tiles of 128 x 128 and 66 stages: 130 us, 512 of them
-// 65), and that low tiles of fp32 work on all planes of a stage at once and have a unit to themselves (1.6 us for the six products of a stage, 1.9 where an operand lies by columns).
+// 65), and that smaller tiles of fp32 work on all planes of a stage at once and have a unit to themselves (low ones 1.6 us for the six products of a stage, 1.9 where an operand lies by columns; middle
+// ones 2.5, a single round up to 3.1: priced so, calls of 2048 x 1024 x 2816 take big tiles and 465 us instead of 455).  fp32, us, middle and low: rows of dh, 682 x 3413 of 1280: 74 and 120; 256 x 11008 of 4096 211 and 253, with planes to be laid
+// out first; 1500 x 5632 of 2048 280 and 311 (big 307).
 enum Operand { kBf16, kPlanes, kPlanesByColumns };
 double round_us(Tile tile, int64_t tiles, double stages, Operand operand) {
   if (tile == kLow && operand != kBf16) return (double)((tiles + kUnits - 1) / kUnits) * (5.5 + (operand == kPlanes ? 0.265 : 0.32) * stages);
+  if (tile == kMiddle && operand != kBf16) return (double)((tiles + kUnits - 1) / kUnits) * (6.0 + 0.42 * stages);
   if (tile == kBig || tiles > 6 * kUnits) return tiles_us(tile, tiles, stages);
   const int64_t rounds = tiles / (2 * kUnits), rest = tiles - rounds * 2 * kUnits;
   return (rounds ? (double)rounds * tiles_us(tile, 2 * kUnits, stages) / 1.25 : 0.0) + (rest ? tiles_us(tile, rest, stages) : 0.0);
@@ -559,7 +563,7 @@ Cuts cuts_for(int64_t m, int64_t n, int64_t stages, Operand operand, bool low, b
   for (Tile tile : {kBig, kMiddle, kLow}) {
     if (tile == kLow && !low) continue;
     auto time = [&](int64_t tiles, double of) { return tiles ? round_us(tile, tiles, of, operand) : 0.0; };
-    const int64_t tiles = grid_of(m, n, tile_m(tile), tile_n(tile)), round = tile == kBig || (tile == kLow && operand != kBf16) ? kUnits : 2 * kUnits, full = tiles / round * round;
+    const int64_t tiles = grid_of(m, n, tile_m(tile), tile_n(tile)), round = tile == kBig || operand != kBf16 ? kUnits : 2 * kUnits, full = tiles / round * round;
     offer(Cuts{tile, tiles, 0, 1, false}, time(tiles, (double)stages));
     if (tile == kBig && full > 0 && full < tiles)
       offer(Cuts{tile, full, tiles - full, 1, true}, time(full, (double)stages) + 3.0 + round_us(kMiddle, 4 * (tiles - full), (double)stages, operand));
@@ -697,10 +701,10 @@ template <template <Tile> class KERNELS> int launch_product(const Cuts &cuts, Ff
 }
 template <typename T, Tile TILE, bool TRA, bool TRB> struct FfnShape : TileShape<TILE> {
   typedef TileShape<TILE> S;
-  static constexpr bool ALL = kAllPlanes<sizeof(T) == 4 ? 6 : 1, S::BM>;
-  static constexpr int WM = ALL ? 2 : S::WM;   // (one workgroup to a unit)
-  typedef Product<S::BM, S::BN, WM, S::WN, TRA, TRB, 1> P;
-  static constexpr int LDS_BYTES = ALL ? P::PLANES_LDS_BYTES : P::LDS_BYTES;
+  static constexpr bool ALL = kAllPlanes<sizeof(T) == 4 ? 6 : 1, S::BM>, TOGETHER = kTogether<sizeof(T) == 4 ? 6 : 1, S::BM>;
+  static constexpr int WM = ALL ? 2 : S::WM, WN = TOGETHER ? 4 : S::WN;   // (one workgroup to a unit)
+  typedef Product<S::BM, S::BN, WM, WN, TRA, TRB, 1> P;
+  static constexpr int LDS_BYTES = ALL ? P::PLANES_LDS_BYTES : TOGETHER ? P::TOGETHER_LDS_BYTES : P::LDS_BYTES;
   static_assert(Staged<P>::BYTES * P::NW <= LDS_BYTES, "results pass through the operands' places");
   static constexpr void (*join)(FfnArgs) = nullptr;
 };
@@ -761,10 +765,9 @@ void set_product(FfnArgs &a, const Matrix &ma, const Matrix &mb, int64_t m, int6
   a.a = ma; a.b = mb;
   a.m = (int32_t)m; a.m_limit = (int32_t)m_limit; a.n = (int32_t)n; a.n_limit = (int32_t)n_limit; a.k = (int32_t)k;
 }
-void set_out(FfnArgs &a, void *out, RowsOf rows, bool wide, float scale) {
-  a.out = out; a.out_rows = rows; a.wide_out = wide; a.scale = scale;
+void set_out(FfnArgs &a, void *out, RowsOf rows, float scale) {
+  a.out = out; a.out_rows = rows; a.scale = scale;
 }
-bool wide_side(const s1f_rows *d, const void *p, int64_t sb, int64_t ss) { return on16(p) && wide_rows(d, sb, ss); }
 
 FfnArgs args_of(const FfnPlan &p, int64_t inner, int32_t act, const void *gate_up, char *ws) {
   FfnArgs a = {};
@@ -796,7 +799,7 @@ int forward_few(const s1f_rows *d, FfnArgs a, const void *x, const void *w_in, i
   a.n = d->hidden; a.k = a.inner;
   a.rows = a.h; a.rows_at = RowsOf{0, a.h_ld, Divisor::of(n)};
   a.weight = w_out; a.weight_stride = out_stride;
-  set_out(a, y, y_rows(d), wide_side(d, y, d->y_stride_b, d->y_stride_s), 1.f);
+  set_out(a, y, y_rows(d), 1.f);
   return n <= 16 ? launch_few<T, 1, 1, 8, F32 ? 2 : 8, false>(a, st) : n <= 32 ? launch_few<T, 2, 1, F32 ? 8 : 16, F32 ? 2 : 4, false>(a, st)
                                                                                : launch_few<T, 4, 1, F32 ? 8 : 16, F32 ? 1 : 2, false>(a, st);
 }
@@ -819,7 +822,7 @@ int forward(const s1f_rows *d, const FfnPlan &p, const void *x, const void *w_in
   if (e != S1F_OK) return e;
   set_product(a, Matrix{a.h, a.h_ld, a.h_plane}, mo, p.n, p.n, d->hidden, d->hidden, inner);
   set_weight(a, w_out, out_stride);
-  set_out(a, y, y_rows(d), wide_side(d, y, d->y_stride_b, d->y_stride_s), 1.f);
+  set_out(a, y, y_rows(d), 1.f);
   return launch_product<Of3<T, false, false, R>::template Of>(p.down, a, d->hidden, st);
 }
 
@@ -845,19 +848,18 @@ int backward(const s1f_rows *d, const FfnPlan &p, const void *dy, const void *x,
   if (e != S1F_OK) return e;
   set_product(a, mdz, mi, n, n, h, p.width, 2 * inner);
   set_weight(a, w_in, in_stride);
-  set_out(a, dx, x_rows(d), wide_side(d, dx, d->x_stride_b, d->x_stride_s), kDown);
+  set_out(a, dx, x_rows(d), kDown);
   e = launch_product<Of3<T, false, true, R>::template Of>(p.dx, a, h, st);
   if (e != S1F_OK) return e;
-  const int64_t piece = W == kStoreBf16 ? 8 : 4;
   auto from = [](Matrix m, int64_t row) { return Matrix{m.data + row * m.ld, m.ld, m.plane}; };
   for (int64_t at = 0; at < n && e == S1F_OK; at += p.per_turn) {
     const int64_t rows = std::min(p.per_turn, n - at);
     set_product(a, from(mdz, at), from(mx, at), 2 * inner, p.dz_ld, h, p.width, rows);
-    set_out(a, dw_in, RowsOf{0, dw_in_stride, Divisor::of(2 * inner)}, on16(dw_in) && dw_in_stride % piece == 0, kDown);
+    set_out(a, dw_in, RowsOf{0, dw_in_stride, Divisor::of(2 * inner)}, kDown);
     e = launch_product<Of3<T, true, true, W>::template Of>(p.dw_in, a, h, st);
     if (e != S1F_OK) return e;
     set_product(a, from(mdy, at), from(mh, at), h, p.width, inner, p.inner_width, rows);
-    set_out(a, dw_out, RowsOf{0, dw_out_stride, Divisor::of(h)}, on16(dw_out) && dw_out_stride % piece == 0, kDown);
+    set_out(a, dw_out, RowsOf{0, dw_out_stride, Divisor::of(h)}, kDown);
     e = launch_product<Of3<T, true, true, W>::template Of>(p.dw_out, a, inner, st);
   }
   return e;

@@ -258,7 +258,7 @@ def test_gradient_against_differences():
 
 
 # cuts that only large products take: whole big or middle tiles, and the others in parts; and 16 to 64 rows of large weights
-@pytest.mark.parametrize("n,h,f,dtype", [(4100, 4100, 1500, "f32"), (8200, 1100, 2100, "f32"), (8200, 1100, 2100, "bf16"), (600, 1100, 8200, "bf16"), (4100, 4100, 6000, "bf16"),
+@pytest.mark.parametrize("n,h,f,dtype", [(4100, 4100, 1500, "f32"), (4500, 4500, 1000, "f32"), (8200, 1100, 2100, "f32"), (8200, 1100, 2100, "bf16"), (600, 1100, 8200, "bf16"), (4100, 4100, 6000, "bf16"),
                                          (4099, 4096, 11008, "bf16"), (16, 4096, 11008, "bf16"), (16, 4096, 11008, "f32"), (64, 4096, 5000, "f32")])
 def test_large_products_by_sample(n, h, f, dtype):
     """Rows of y and dx, and rows and columns of the weights' gradients, that are drawn; the last of each among them."""

@@ -50,7 +50,7 @@ def of(done, part):
 
 
 SHAPES = [((72, 4360, 2180), (0, 1)), ((4360, 72, 2184), (0, 1)), ((4361, 4360, 68), (0, 1)), ((30000, 40, 24), (0, 1)), ((300, 640, 1000), (0, 1)), ((515, 96, 2052), (0, 1)),
-          ((130, 128, 4), (0, 1)), ((700, 72, 264), (0, 1)), ((129, 200, 332), (0, 1)), ((4100, 4100, 1500), (0,)), ((8200, 1100, 2100), (0, 1)), ((600, 1100, 8200), (1,)),
+          ((130, 128, 4), (0, 1)), ((700, 72, 264), (0, 1)), ((129, 200, 332), (0, 1)), ((4100, 4100, 1500), (0,)), ((4500, 4500, 1000), (0,)), ((8200, 1100, 2100), (0, 1)), ((600, 1100, 8200), (1,)),
           ((4100, 4100, 6000), (1,)), ((4099, 4096, 11008), (1,))]
 
 
