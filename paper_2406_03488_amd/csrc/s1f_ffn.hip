@@ -539,12 +539,15 @@ constexpr int tile_m(Tile t) { return t == kBig ? 256 : t == kMiddle ? 128 : 64;
 constexpr int tile_n(Tile t) { return t == kBig ? 256 : 128; }
 // Predicted microseconds of `tiles` tiles of so many stages: as tiles_us has them, but that few rounds of smaller tiles count whole, too (540 tiles of 128 x 128 and 66 stages: 130 us, 512 of them
 // 65), and that smaller tiles of fp32 work on all planes of a stage at once and have a unit to themselves (low ones 1.6 us for the six products of a stage, 1.9 where an operand lies by columns; middle
-// ones 2.5, a single round up to 3.1: priced so, calls of 2048 x 1024 x 2816 take big tiles and 465 us instead of 455).  fp32, us, middle and low: rows of dh, 682 x 3413 of 1280: 74 and 120; 256 x 11008 of 4096 211 and 253, with planes to be laid
+// ones 2.5, a single round up to 3.1: priced so, a gradient of 2048 x 1024 x 2816 takes big tiles and 473 us instead of 458).  fp32 dh, us, middle and low: 682 x 3413 of 1280 74 and 120; 256 x 11008 of 4096 211 and 253, with planes to be laid
 // out first; 1500 x 5632 of 2048 280 and 311 (big 307).
+// Smaller bf16 tiles alone on a unit wait longer for operands that come from memory than the loss's do: priced like those, 1000 rows of 2048 x 5632 took 123 us forward in 256 low tiles of 88 stages instead of
+// 101 in middle ones cut in two, the gradient 219 instead of 206, 512 of 4096 x 11008 183 instead of 173, the gradient of 2048 of 1024 x 2816 143 instead of 133.
 enum Operand { kBf16, kPlanes, kPlanesByColumns };
 double round_us(Tile tile, int64_t tiles, double stages, Operand operand) {
   if (tile == kLow && operand != kBf16) return (double)((tiles + kUnits - 1) / kUnits) * (5.5 + (operand == kPlanes ? 0.265 : 0.32) * stages);
   if (tile == kMiddle && operand != kBf16) return (double)((tiles + kUnits - 1) / kUnits) * (6.0 + 0.42 * stages);
+  if (tile != kBig && tiles <= kUnits) return tile == kMiddle ? 5.0 + 0.61 * stages : 4.5 + 0.50 * stages;
   if (tile == kBig || tiles > 6 * kUnits) return tiles_us(tile, tiles, stages);
   const int64_t rounds = tiles / (2 * kUnits), rest = tiles - rounds * 2 * kUnits;
   return (rounds ? (double)rounds * tiles_us(tile, 2 * kUnits, stages) / 1.25 : 0.0) + (rest ? tiles_us(tile, rest, stages) : 0.0);
