@@ -356,8 +356,8 @@ template <int BM, int BN, int WM, int WN, bool TRA, bool TRB, int PAIRS> struct 
   }
 
   // The same for tiles of which LDS holds five thirds of a stage: planes 0 and 1 of two stages and planes 2 of one, which arrive under the four products of the others.  stages [begin, end)
-  // of k.  128 x 128, eight waves: 2.8 us per stage, where alone on a unit six passes of run take 4.3 and beside another tile 2.7.  What bounds it are the copies, 96 KiB a stage: without the products 2.6
-  // us, without the copies 1.9.  (Stages of 32, three of them in LDS and operands read one ahead of the products: the same, half lines of memory cost what the distance gains.)
+  // of k.  128 x 128, eight waves: 2.5 to 3.1 us per stage, where alone on a unit six passes of run take 4.3 and beside another tile 2.7.  What bounds it are the copies, 96 KiB a stage: without the products 2.2
+  // to 3.1 us, without the copies 1.8 to 2.4.  (Stages of 32, three of them in LDS and operands read one ahead of the products: the same, half lines of memory cost what the distance gains.)
   static constexpr int TOGETHER_LDS_BYTES = 5 * (SA::BYTES + SB::BYTES);
   S1F_DEV static void run_together(f32x4 (&acc)[MB][NB], const Matrix &a, const Matrix &b, int64_t m0, int64_t m_limit, int64_t n0, int64_t n_limit, int64_t k, int begin, int end,
                                    lds_addr lds, int64_t b_apart = 0) {

@@ -360,7 +360,7 @@ template <Result R> S1F_DEV void put_result(const FfnArgs &a, int row, int col, 
   }
 }
 
-// y, dx, dW_in and dW_out.  4897 x 7168 x 19200 bf16: dx 2.06 ms, 1.31 PFLOP/s, dW_out 1.05, 1.29, dW_in 2.15, 1.26; fp32, 682 x 1280 x 3413: dx 96 us, either dW 82.  The tiles from `whole` on are cut along the contraction: their parts are added up by the join.
+// y, dx, dW_in and dW_out.  4897 x 7168 x 19200 bf16: dx 2.06 ms, 1.31 PFLOP/s, dW_out 1.05, 1.29, dW_in 2.15, 1.26; fp32, 682 x 1280 x 3413: dx 82 us, dW_in 90, dW_out 48.  The tiles from `whole` on are cut along the contraction: their parts are added up by the join.
 template <int PAIRS, int BM, int BN, int WM, int WN, bool TRA, bool TRB, Result R> __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_product_kernel(const FfnArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   typedef Product<BM, BN, WM, WN, TRA, TRB, PAIRS> P;
