@@ -8,8 +8,8 @@
 //
 // Bound by memory: each element is read and written once, between which a row's angles, computed once for all heads that a lane takes, are next to nothing.  A row of a head lies in
 // the registers of a few lanes, 16 bytes of the wider type to each, and mostly both elements of a pair in one lane.  4097 tokens of 64 and 2 x 8 heads of 128, bf16: 168 MB, 39.7 us, 4.2 TB/s
-// (a large copy: 4.65); their gradient for 4096 tokens of 3 x 32 heads, 268 MB, 58.8 us, 4.6 TB/s; norms and rotation of 4897 tokens of 3 x 56 heads, 421 MB, 92.5 us, 4.6 TB/s; the gradient of 8774
-// tokens of 64 and 2 x 8 heads, 557 MB, 128 us, 4.3 TB/s, 0.6 of which the vector units are busy.  One token of 64 + 16 heads 4.8 us, a launch.
+// (a large copy: 4.65); their gradient for 4096 tokens of 3 x 32 heads, 268 MB, 58.8 us, 4.6 TB/s; norms and rotation of 4897 tokens of 3 x 56 heads, 421 MB, 89.9 us, 4.7 TB/s; the gradient of 8774
+// tokens of 64 and 2 x 8 heads, 557 MB, 125 us, 4.4 TB/s, 0.6 of which the vector units are busy.  One token of 64 + 16 heads 4.4 us, a launch.
 // Angles are products in 64 bits: at position 2^20 one in 32 bits is off by 2^-4.  The norm's sums are fp32, as is everything between load and store; results are rounded once.
 #include <algorithm>
 #include <atomic>
@@ -118,6 +118,9 @@ template <int PW, Layout LAYOUT> struct Share {
       at[1] = at[0] + a.half;
     }
   }
+  // where element e < 2 PW lies.  (Not at[e / PW]: an array that is indexed by what is not a constant makes the compiler read the size of the workgroup out of the launch's packet, in the host's
+  // memory, one workgroup after the other: norms and rotation of 385 tokens of 32 + 2 x 8 heads of 64, fp32, 17.7 us instead of 4.9, their gradient 23.3 instead of 11.7.)
+  S1F_DEV int of(int e) const { return e < PW ? at[0] + e : at[1] + e - PW; }
   // which of the lane's elements e < 2 PW is the first, the second of its pair i
   S1F_DEV static constexpr int first(int i) { return LAYOUT == kPairs ? 2 * i : i; }
   S1F_DEV static constexpr int second(int i) { return LAYOUT == kPairs ? 2 * i + 1 : PW + i; }
@@ -249,7 +252,7 @@ template <typename T, typename K, int PW, int L, int IT, int U, Layout LAYOUT, b
     for (int p = 0; p < PER; ++p) {
       const int i = threadIdx.x + 256 * p, side = i / GAIN_COLS, col = i % GAIN_COLS, item = col / E, e = col % E;
       const Share<PW, LAYOUT> share(a, item);
-      gain[p] = side < 2 && item < a.items ? (float)reinterpret_cast<const T *>(side ? a.gain_k : a.gain_q)[share.at[e / PW] + e % PW] : 0.f;
+      gain[p] = side < 2 && item < a.items ? (float)reinterpret_cast<const T *>(side ? a.gain_k : a.gain_q)[share.of(e)] : 0.f;
     }
     if (next.kind != kV) {
       angles();
@@ -403,7 +406,7 @@ template <typename T, typename K, int PW, int L, int IT, int U, Layout LAYOUT, b
         float sum = 0.f;
         for (int g = 0; g < GROUPS; ++g) sum += sums[g][col];
         const Share<PW, LAYOUT> share(a, item);
-        part[side * a.dim + share.at[e / PW] + e % PW] = sum;
+        part[side * a.dim + share.of(e)] = sum;
       }
     }
   }
@@ -438,7 +441,7 @@ constexpr int32_t kMostHeads = 1 << 16, kMostDim = 256;
 // 128).  Of the other calls: about as many as keep memory busy, several units to each only where there are more.
 constexpr int kMostParts = 2048;
 constexpr int64_t kMostGroups = 4096;
-constexpr int64_t kFew = int64_t(1) << 20;   // elements
+constexpr int64_t kFew = int64_t(1) << 22;   // elements
 constexpr int64_t kMostTokenHeads = int64_t(1) << 31;   // (units of work are numbered in 32 bits)
 
 bool strides_fit(const s1f_heads *d, int heads, int64_t rows, int64_t sb, int64_t sh, int64_t ss) {
@@ -589,7 +592,7 @@ template <bool NORM, bool BACK> int launch(const s1f_heads *d, RopeArgs a, hipSt
   for (const void *p : {a.src_q, (const void *)a.dst_q, (const void *)a.dst_k, (const void *)a.dst_v, a.x_q, a.x_k, a.gain_q, a.gain_k}) typed.pointer(p);
   kv.pointer(a.src_k);
   kv.pointer(a.src_v);
-  // (16 bytes of either type to a lane, but for few elements, where twice the lanes compute half as many angles each: one token of 64 + 16 heads with norms 6.4 -> 4.8 us)
+  // (16 bytes of either type to a lane, but for few elements, where twice the lanes compute half as many angles each: 200 tokens of 32 + 2 x 8 heads of 128 4.8 -> 4.5 us, 600 5.8 -> 5.5)
   const int64_t elements = (int64_t)a.n * (a.n_q + a.n_k + a.n_v) * a.dim;
   const Dealt dealt = deal(d, esz == 2 && !BACK && elements > kFew ? 8 : 4, typed, wide, esz);
   a.items = d->head_dim / (2 * dealt.pairs);
