@@ -262,7 +262,7 @@ int s1f_kv_grad_emit(const s1f_desc *desc, const float *dk_prefix_acc, const flo
  *     gradients dq, dk, dv; q_rot and its gradient dq_rot (rot_stride_*); caches k_cache, v_cache and accumulators dk_prefix_acc, dv_prefix_acc
  *     [batch, n_kv_heads, cache_capacity, head_dim] (cache_stride_*), of which rows [seg_off, seg_off + rows) are written, or read.  head_dim is contiguous.
  *   - The first rotary_dim elements of a head are rotated, in pairs (i, i + rotary_dim / 2), or (2i, 2i + 1) if interleaved: pair i of the token at position p
- *     by p * freqs[i] radians, an angle that is computed in 64 bits, and scaled by `magnitude`.  The others stay as they are.  rotary_dim 0: freqs may be NULL.
+ *     by p * freqs[i] radians, an angle that is computed in 64 bits (of up to 2^79), and scaled by `magnitude`.  The others stay as they are.  rotary_dim 0: freqs may be NULL.
  *   - positions int64 [batch, rows], rows contiguous, batch entries positions_stride_b apart, of any order and sign; NULL: row r has first_position + r.
  *   - v, v_cache (dv, dv_prefix_acc) may both be NULL.
  *   - Sides, heads and rows may not overlap, and an output may be no input, but: q_rot may be q, k_cache + seg_off rows k, v_cache so v, dq dq_rot, where their strides are the same; dq may not be q.

@@ -72,10 +72,18 @@ template <typename T, int N> struct Run {
 };
 
 // cos and sin of a 64-bit angle: the quarter turn and the rest in 64 bits (pi/2 as two numbers; a fused product takes off the first exactly), the rest's
-// series in 32, to 2^-25 of the result.
+// series in 32, to 2^-25 of the result.  Past 2^48 quarter turns their number is not whole to a fraction of one any more, and what is left of the angle is reduced once again: to 2^79.
 S1F_DEV void cos_sin(double angle, float &c, float &s) {
-  const double turns = rint(angle * 0.63661977236758134308);
-  const float x = (float)fma(-turns, 6.123233995736766036e-17, fma(-turns, 1.5707963267948965580, angle));
+  constexpr double kPerQuarter = 0.63661977236758134308;
+  const auto less = [](double x, double n) { return fma(-n, 6.123233995736766036e-17, fma(-n, 1.5707963267948965580, x)); };
+  double turns = rint(angle * kPerQuarter), rest = less(angle, turns);
+  const bool far = fabs(turns) > 0x1p48;
+  if (__builtin_expect(__any(far), 0)) {
+    const double more = far ? rint(rest * kPerQuarter) : 0.0;
+    rest = less(rest, more);
+    turns = turns - 4.0 * floor(turns * 0.25) + more;
+  }
+  const float x = (float)rest;
   const int quarter = (int)(turns - 4.0 * floor(turns * 0.25));
   const float q = x * x;
   const float sn = x + x * q * (-1.f / 6 + q * (1.f / 120 + q * (-1.f / 5040 + q * (1.f / 362880))));
