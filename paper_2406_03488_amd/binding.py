@@ -1015,7 +1015,7 @@ def gated_ffn_fwd(x, w_in, w_out, act: int, y, gate_up, workspace):
 
     x, y [B, rows, hidden]; w_in [2 * inner, hidden], g's rows first; w_out [hidden, inner]; act SILU, GELU or GELU_TANH; gate_up [B, rows, 2 * inner]
     is overwritten with [g | u] for the backward, None: not kept; workspace is any device tensor of at least gated_ffn_fwd_workspace_bytes(...)
-    bytes.  Enqueued on torch's current stream.
+    bytes; y may be x.  Enqueued on torch's current stream.
     """
     if _done(_native().gated_ffn_fwd(x, w_in, w_out, act, y, gate_up, workspace), "s1f_gated_ffn_fwd"):
         return
@@ -1036,7 +1036,7 @@ def gated_ffn_bwd(dy, x, w_in, w_out, act: int, gate_up, dx, dw_in, dw_out, work
     """s1f_gated_ffn_bwd on torch device tensors, from the gate_up that the forward has kept.
 
     dx, with the shape and strides of x, is overwritten; dw_in and dw_out, of one type, are added to if they are fp32 and overwritten if they are bf16 (bf16 rows only);
-    workspace is any device tensor of at least gated_ffn_bwd_workspace_bytes(...) bytes.
+    workspace is any device tensor of at least gated_ffn_bwd_workspace_bytes(...) bytes; dx may be x or dy.
     """
     if _done(_native().gated_ffn_bwd(dy, x, w_in, w_out, act, gate_up, dx, dw_in, dw_out, workspace), "s1f_gated_ffn_bwd"):
         return

@@ -849,11 +849,6 @@ int backward(const s1f_rows *d, const FfnPlan &p, const void *dy, const void *x,
   set_weight(a, w_out, out_stride);
   e = launch_product<Dh<T>::template Of>(p.dh, a, inner, st);
   if (e != S1F_OK) return e;
-  set_product(a, mdz, mi, n, n, h, p.width, 2 * inner);
-  set_weight(a, w_in, in_stride);
-  set_out(a, dx, x_rows(d), kDown);
-  e = launch_product<Of3<T, false, true, R>::template Of>(p.dx, a, h, st);
-  if (e != S1F_OK) return e;
   auto from = [](Matrix m, int64_t row) { return Matrix{m.data + row * m.ld, m.ld, m.plane}; };
   for (int64_t at = 0; at < n && e == S1F_OK; at += p.per_turn) {
     const int64_t rows = std::min(p.per_turn, n - at);
@@ -865,7 +860,12 @@ int backward(const s1f_rows *d, const FfnPlan &p, const void *dy, const void *x,
     set_out(a, dw_out, RowsOf{0, dw_out_stride, Divisor::of(h)}, kDown);
     e = launch_product<Of3<T, true, true, W>::template Of>(p.dw_out, a, inner, st);
   }
-  return e;
+  if (e != S1F_OK) return e;
+  // (last, when nobody reads dy, x and gate_up any more: it may lie in their place)
+  set_product(a, mdz, mi, n, n, h, p.width, 2 * inner);
+  set_weight(a, w_in, in_stride);
+  set_out(a, dx, x_rows(d), kDown);
+  return launch_product<Of3<T, false, true, R>::template Of>(p.dx, a, h, st);
 }
 
 }  // namespace

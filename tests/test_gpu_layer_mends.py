@@ -1,8 +1,11 @@
-"""Calls around a layer's attention that gave wrong results, each against 64 bits."""
+"""Calls around a layer's attention that gave wrong results: against 64 bits, or against the calls that gave right ones."""
 import numpy as np
 import pytest
 import torch
 
+import paper_2406_03488_amd as s1f
+from layer_harness import like
+from test_gpu_ffn import ACTS, Block
 from test_gpu_rope import Call
 
 pytestmark = pytest.mark.gpu
@@ -22,3 +25,24 @@ def test_positions_past_2_to_50(interleaved):
     c.turn = (c.freqs, 1.0, interleaved, c.positions, c.off)
     c.check_forward(c.forward())
     c.check_backward(c.backward())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", [(1, 9, 64, 96, "dense", "dense", "silu"), (1, 300, 640, 1000, "dense", "dense", "silu"), (2, 150, 136, 1001, "view", "view", "gelu_tanh"),
+                                  (1, 2100, 512, 264, "dense", "dense", "gelu")])
+def test_block_in_the_place_of_its_rows(case, dtype):
+    """y may be x, and dx x or dy; the weights' gradients read both."""
+    c = Block(case, dtype)
+    y, gate_up = c.forward()
+    kind = "f32" if dtype == "f32" else "bf16"
+    zeros = [torch.zeros_like(w, dtype=torch.float32) for w in (c.w_in, c.w_out)]
+    want = c.backward(gate_up, kind, zeros)
+    space_of = lambda f, *rows: torch.empty(f(*rows, c.w_in, c.w_out), dtype=torch.uint8, device="cuda")
+    x = like(c.x).copy_(c.x)
+    s1f.gated_ffn_fwd(x, c.w_in, c.w_out, ACTS[c.act], x, None, space_of(s1f.gated_ffn_fwd_workspace_bytes, x))
+    assert torch.equal(x, y)
+    for place in ("x", "dy"):
+        x, dy = like(c.x).copy_(c.x), like(c.x).copy_(c.dy)
+        dx, dw = (x if place == "x" else dy), [torch.zeros_like(t) for t in want[1:]]
+        s1f.gated_ffn_bwd(dy, x, c.w_in, c.w_out, ACTS[c.act], gate_up, dx, *dw, space_of(s1f.gated_ffn_bwd_workspace_bytes, dy, x))
+        assert torch.equal(dx, want[0]) and all(torch.equal(a, b) for a, b in zip(dw, want[1:])), place
