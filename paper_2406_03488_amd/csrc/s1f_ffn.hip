@@ -586,6 +586,7 @@ int64_t part_bytes(const Cuts &c) { return c.splits > 1 ? 4 * c.splits * c.rest 
 
 struct FfnPlan {
   int64_t n, planes, width, inner_width, dz_ld, turns, per_turn;   // dW's rows are taken per_turn at a time
+  int64_t y_terms, dx_terms;      // of the sums that make y and dx, likewise
   bool direct_in, direct_out;     // weights as they are
   bool few;
   Cuts up, down, dh, dx, dw_in, dw_out;
@@ -603,8 +604,9 @@ int check_ffn(const s1f_rows *d, int64_t inner, int64_t in_stride, int64_t out_s
   return S1F_OK;
 }
 
-// Rows that one fp32 sum of a weight's gradient runs over, up to half as many again, six products for each: longer sums would be off by more than fp32 products are (the token
-// loss's, of 64 elements over 300 tokens: 8192 rows 1.0e-6 of the norm, 16384 1.4e-6, 131072 5.0e-6).  More rows take turns: each turn adds to the accumulators.
+// Terms that one fp32 sum runs over, up to half as many again, six products for each: longer sums would be off by more than fp32 products are (the token
+// loss's weight gradient, of 64 elements over 300 tokens: 8192 rows 1.0e-6 of the norm, 16384 1.4e-6, 131072 5.0e-6; dx of 2048 x 2048 x 131072 6.0e-6, a library product 4.4e-6).  More rows of a weight's gradient take turns, and
+// so does what lies between the projections for y and dx where tiles are not cut as short anyway: each turn adds to what the one before it has left.  (Sums over hidden end in an activation: one of 16384 2.1e-6, a library product 2.3e-6.)
 constexpr int64_t kSummed = 8192;
 int64_t turns_of(int64_t n, int64_t planes) { return planes == 1 || n < kSummed + kSummed / 2 ? 1 : (n + kSummed / 2) / kSummed; }
 
@@ -639,11 +641,21 @@ FfnPlan plan_of(const s1f_rows *d, int64_t inner, int64_t in_stride, int64_t out
   const Operand rows = f32 ? kPlanes : kBf16, columns = f32 ? kPlanesByColumns : kBf16;
   // planes of a weight: 4 bytes read and 6 written, and a share of a launch
   auto laid_out = [&](int64_t elements) { return f32 ? 3.0 + (double)elements * 10 / 4.4e6 : 0.0; };
+  // cuts of a product whose sums are not ended by an activation, and how many of its terms a turn takes
+  auto in_turns = [&](Cuts &c, int64_t n, int64_t terms, Operand operand, double laid) {
+    for (int64_t turns = 1;;) {
+      const int64_t per = turns == 1 ? terms : up_to((terms + turns - 1) / turns, kDepth);
+      c = cuts_for(p.n, n, stages(per), operand, true, true, laid / (double)turns);
+      const int64_t needed = turns_of(c.whole > 0 || c.splits == 1 ? per : (per + c.splits - 1) / c.splits, p.planes);
+      if (needed == 1) return per;
+      turns = std::max(turns + 1, turns * needed);
+    }
+  };
   int64_t part = 0;
   if (!backward) {
     // (tiles of [g | u]: as many columns of either)
     p.up = cuts_for(p.n, 2 * up_to(inner, 16), stages(h), rows, true, false, laid_out(2 * inner * h));
-    p.down = cuts_for(p.n, h, stages(inner), rows, true, true, laid_out(inner * h));
+    p.y_terms = in_turns(p.down, h, inner, rows, laid_out(inner * h));
     part = part_bytes(p.down);
     p.direct_in |= f32 && p.up.tile == kLow;
     p.direct_out |= f32 && p.down.tile == kLow;
@@ -651,7 +663,7 @@ FfnPlan plan_of(const s1f_rows *d, int64_t inner, int64_t in_stride, int64_t out
     p.turns = turns_of(p.n, p.planes);
     p.per_turn = up_to((p.n + p.turns - 1) / p.turns, kDepth);
     p.dh = cuts_for(p.n, inner, stages(h), columns, true, false, laid_out(inner * h));
-    p.dx = cuts_for(p.n, h, stages(2 * inner), columns, true, true, laid_out(2 * inner * h));
+    p.dx_terms = in_turns(p.dx, h, 2 * inner, columns, laid_out(2 * inner * h));
     p.dw_in = cuts_for(2 * inner, h, stages(p.per_turn), columns, false, true);
     p.dw_out = cuts_for(h, inner, stages(p.per_turn), columns, false, true);
     for (const Cuts &c : {p.dx, p.dw_in, p.dw_out}) part = std::max(part, part_bytes(c));
@@ -807,6 +819,8 @@ int forward_few(const s1f_rows *d, FfnArgs a, const void *x, const void *w_in, i
                                                                                : launch_few<T, 4, 1, F32 ? 8 : 16, F32 ? 1 : 2, false>(a, st);
 }
 
+// What a turn behind the first does with its sums (bf16 has no such turns).
+template <typename T> constexpr Result kNext = sizeof(T) == 4 ? kAddF32 : kStoreBf16;
 template <typename T>
 int forward(const s1f_rows *d, const FfnPlan &p, const void *x, const void *w_in, int64_t in_stride, const void *w_out, int64_t out_stride, int64_t inner, int32_t act,
             void *y, void *gate_up, char *ws, hipStream_t st) {
@@ -823,10 +837,13 @@ int forward(const s1f_rows *d, const FfnPlan &p, const void *x, const void *w_in
   set_weight(a, w_in, in_stride);
   e = launch_product<Up<T>::template Of>(p.up, a, 2 * up_to(inner, 16), st);
   if (e != S1F_OK) return e;
-  set_product(a, Matrix{a.h, a.h_ld, a.h_plane}, mo, p.n, p.n, d->hidden, d->hidden, inner);
-  set_weight(a, w_out, out_stride);
   set_out(a, y, y_rows(d), 1.f);
-  return launch_product<Of3<T, false, false, R>::template Of>(p.down, a, d->hidden, st);
+  for (int64_t at = 0; at < inner && e == S1F_OK; at += p.y_terms) {
+    set_product(a, Matrix{a.h + at, a.h_ld, a.h_plane}, Matrix{mo.data + at, mo.ld, mo.plane}, p.n, p.n, d->hidden, d->hidden, std::min(p.y_terms, inner - at));
+    set_weight(a, reinterpret_cast<const T *>(w_out) + at, out_stride);
+    e = at == 0 ? launch_product<Of3<T, false, false, R>::template Of>(p.down, a, d->hidden, st) : launch_product<Of3<T, false, false, kNext<T>>::template Of>(p.down, a, d->hidden, st);
+  }
+  return e;
 }
 
 template <typename T, Result W>
@@ -862,10 +879,13 @@ int backward(const s1f_rows *d, const FfnPlan &p, const void *dy, const void *x,
   }
   if (e != S1F_OK) return e;
   // (last, when nobody reads dy, x and gate_up any more: it may lie in their place)
-  set_product(a, mdz, mi, n, n, h, p.width, 2 * inner);
-  set_weight(a, w_in, in_stride);
   set_out(a, dx, x_rows(d), kDown);
-  return launch_product<Of3<T, false, true, R>::template Of>(p.dx, a, h, st);
+  for (int64_t at = 0; at < 2 * inner && e == S1F_OK; at += p.dx_terms) {
+    set_product(a, Matrix{mdz.data + at, mdz.ld, mdz.plane}, from(mi, at), n, n, h, p.width, std::min(p.dx_terms, 2 * inner - at));
+    set_weight(a, reinterpret_cast<const T *>(w_in) + at * in_stride, in_stride);
+    e = at == 0 ? launch_product<Of3<T, false, true, R>::template Of>(p.dx, a, h, st) : launch_product<Of3<T, false, true, kNext<T>>::template Of>(p.dx, a, h, st);
+  }
+  return e;
 }
 
 }  // namespace

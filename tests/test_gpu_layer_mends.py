@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import paper_2406_03488_amd as s1f
+import layer_spread as S
 from layer_harness import like
 from test_gpu_ffn import ACTS, Block
 from test_gpu_rope import Call
@@ -46,3 +47,22 @@ def test_block_in_the_place_of_its_rows(case, dtype):
         dx, dw = (x if place == "x" else dy), [torch.zeros_like(t) for t in want[1:]]
         s1f.gated_ffn_bwd(dy, x, c.w_in, c.w_out, ACTS[c.act], gate_up, dx, *dw, space_of(s1f.gated_ffn_bwd_workspace_bytes, dy, x))
         assert torch.equal(dx, want[0]) and all(torch.equal(a, b) for a, b in zip(dw, want[1:])), place
+
+
+def test_long_fp32_sums_between_the_projections():
+    """y's sums of 65536 terms and dx's of 131072, in as many tiles as there are compute units: in one sum they would be 4.0e-6 and 5.6e-6 of their norm off."""
+    n, h, f = 16384, 1024, 65536
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(3)
+    normal = lambda *shape, scale=1.0: torch.empty(shape, device="cuda").normal_(0, scale, generator=gen)
+    x, dy, w_in, w_out = normal(1, n, h), normal(1, n, h), normal(2 * f, h, scale=h ** -0.5), normal(h, f, scale=f ** -0.5)
+    y, dx, gate_up = torch.empty_like(x), torch.empty_like(x), torch.empty((1, n, 2 * f), device="cuda")
+    ws = torch.empty(s1f.gated_ffn_bwd_workspace_bytes(dy, x, w_in, w_out), dtype=torch.uint8, device="cuda")
+    assert s1f.gated_ffn_fwd_workspace_bytes(x, w_in, w_out) <= len(ws)
+    s1f.gated_ffn_fwd(x, w_in, w_out, s1f.SILU, y, gate_up, ws)
+    dw = torch.zeros_like(w_in), torch.zeros_like(w_out)
+    s1f.gated_ffn_bwd(dy, x, w_in, w_out, s1f.SILU, gate_up, dx, *dw, ws)
+    rows = torch.randint(0, n, (128,), device="cuda", generator=gen)
+    xs, ys, wi, wo = (t.double() for t in (x[0, rows], dy[0, rows], w_in, w_out))
+    S.near(y[0, rows], S.forward(xs, wi, wo, "silu", "f32")["y"], "y")
+    S.near(dx[0, rows], S.backward(ys, xs, wi, wo, "silu", gate_up[0, rows].double(), "f32", S.U)["dx"], "dx")
