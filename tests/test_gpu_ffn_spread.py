@@ -47,3 +47,19 @@ def test_block_and_gradient_as_a_whole(n, h, f, dtype):
         S.near(dx[0], expected["dx"], "dx")
         for name, got, was in zip(("dw_in", "dw_out"), dw, start):
             S.near(got, expected[name], name, was.double() if into == "f32" else None)
+
+
+def test_sums_of_weights_gradients_over_many_rows():
+    """fp32, 131072 rows of values of one sign: sums of up to 12288 terms, and their sums; one sum of all would be four times as far off, or more."""
+    n, h, f = 131072, 40, 24
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(7)
+    normal = lambda *shape: torch.empty(shape, device="cuda").normal_(0, 1, generator=gen)
+    x, dy, gate_up = normal(1, n, h).abs_(), normal(1, n, h).abs_(), 1 + 0.2 * normal(1, n, 2 * f)
+    w_in, w_out = normal(2 * f, h), normal(h, f).abs_()
+    dx, dw = torch.empty_like(x), [torch.zeros_like(w_in), torch.zeros_like(w_out)]
+    ws = space(s1f.gated_ffn_bwd_workspace_bytes(dy, x, w_in, w_out))[0]
+    s1f.gated_ffn_bwd(dy, x, w_in, w_out, s1f.SILU, gate_up, dx, *dw, ws)
+    expected = S.backward(*(t.double() for t in (dy[0], x[0], w_in, w_out)), "silu", gate_up[0].double(), "f32", S.U)
+    for name, got in (("dx", dx[0]), ("dw_in", dw[0]), ("dw_out", dw[1])):
+        S.near(got, expected[name], name)

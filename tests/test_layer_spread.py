@@ -130,3 +130,15 @@ def test_operands_rounded_to_bf16_are_rejected():
     dy, x, w_in, w_out = operands("f32")
     short = [t.bfloat16().double() for t in (dy, x, w_in, w_out)]
     assert rejected(forward(*short[1:], "silu", "f32")[1], S.forward(x, w_in, w_out, "silu", "f32")["y"])
+
+
+def test_one_sum_of_many_rows_is_rejected():
+    """131072 terms of one sign in one fp32 sum; in turns of 8192 they pass."""
+    n = 131072
+    gen = torch.Generator().manual_seed(4)
+    a, b = torch.randn((12, n), generator=gen).abs().double(), torch.randn((n, 16), generator=gen).abs().double()
+    expected = (*S.sums(a, b, "f32"), n)
+    turns = torch.zeros(12, 16)
+    for k in range(0, n, 8192):
+        turns += product(a[:, k:k + 8192], b[k:k + 8192], "f32").float()
+    assert not rejected(turns, expected) and rejected(product(a, b, "f32"), expected)
