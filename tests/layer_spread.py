@@ -109,3 +109,29 @@ def near(got, expected, what, plus=None):
         worst = int(ratio.argmax())
         at = (worst // ratio.shape[1], worst % ratio.shape[1])
         assert ratio[at] <= 1, f"{what}, {kind} {at}: {ratio[at].item():.3g} of what it may be off by, {of(error)[at].sqrt().item():.3g} of {of(want * want)[at].sqrt().item():.3g}"
+
+
+def gains_tolerance(d, x, rstd, rotary, interleaved, magnitude, chain, start):
+    """For every element of a gain: how far the sum over all rows and heads of dy * x * rstd, added to `start`, may be off.  d, x: [.., head_dim] gradients before they are turned back, and heads, rstd [.., 1], in numpy.
+
+    A term is off by 26 U of the magnitudes that make it (layer_harness: rotation 8, rstd 16, products 2), one independent of the next, but for what all have in common: as much of the sum itself, and of what a sum of
+    terms of either sign comes to.  Its additions: `chain` of them one behind the other, of running sums whose squares are at most those of all terms, and the result's.  Six times the root of the mean square."""
+    import numpy as np
+    from layer_harness import pair_sizes
+    terms = pair_sizes(d, rotary, interleaved, abs(magnitude)) * np.abs(x * rstd)
+    q = (terms ** 2).sum(tuple(range(d.ndim - 1)))
+
+    def of(result):
+        s2 = (np.abs(result) + np.abs(start)) ** 2
+        return 6 * U * np.sqrt(26 ** 2 / 3 * q + chain / 3 * (q + s2)) + 26 * U * (np.abs(result - start) + 3 * np.sqrt(q)) + U * np.abs(result)
+    return of
+
+
+def gains_chain(rows, hq, hk, dim, aligned):
+    """Additions one behind the other in a gain's gradient: three a unit of the workgroup's share, of which there are at least 256; the workgroup's groups of lanes; 2048 parts by 64 shares, and these."""
+    items = dim // 8 if dim % 8 == 0 and aligned else dim // 2
+    lanes = min(32, max(8, 1 << ((items if dim % 8 == 0 and aligned else -(-items // 4)) - 1).bit_length()))
+    groups = 256 // lanes
+    in_block = min(groups, 1 << (rows - 1).bit_length())
+    units = -(-rows // in_block) * (hq + 2 * hk)
+    return 3 * -(-units // 256) + groups + 32 + 64 + 1

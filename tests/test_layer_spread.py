@@ -142,3 +142,26 @@ def test_one_sum_of_many_rows_is_rejected():
     for k in range(0, n, 8192):
         turns += product(a[:, k:k + 8192], b[k:k + 8192], "f32").float()
     assert not rejected(turns, expected) and rejected(product(a, b, "f32"), expected)
+
+
+def test_lost_terms_of_gains_gradients_are_rejected():
+    """One row's share of one head left out of 200006 rows of two heads; the kernel's order of additions passes."""
+    import numpy as np
+    from test_gpu_rope_gains import MANY
+    b, hq, hk, n, dim, rotary = MANY[0][:6]
+    rng = np.random.default_rng(3)
+    d, x = rng.normal(size=(b, hq, n, dim)).astype(np.float32), rng.normal(size=(b, hq, n, dim)).astype(np.float32)
+    at, freqs, start = np.arange(n)[None].repeat(b, 0), L.frequencies(rotary), rng.normal(size=dim)
+    dy, rstd = L.rotate(d.astype(np.float64), at, freqs, 1.0, False, back=True), L.head_norm(x.astype(np.float64), 1.0, 1e-6)[1]
+    terms = dy * x * rstd
+    want = start + terms.sum((0, 1, 2))
+    tolerance = S.gains_tolerance(d.astype(np.float64), x.astype(np.float64), rstd, rotary, False, 1.0, S.gains_chain(b * n, hq, hk, dim, True), start)(want)
+    flat = (dy.astype(np.float32) * (x * rstd.astype(np.float32))).reshape(-1, dim)
+    lanes = 256 * 32
+    flat = np.concatenate([flat, np.zeros((-len(flat) % lanes, dim), np.float32)]).reshape(-1, lanes, dim)
+    sums = np.add.accumulate(flat, 0, dtype=np.float32)[-1]
+    got = start.astype(np.float32) + np.add.accumulate(sums.reshape(64, -1, dim), 1, dtype=np.float32)[:, -1].sum(0)
+    assert (np.abs(got - want) <= tolerance).all()
+    for lost in (terms[0, 1, 777], terms[1, 0, n - 1]):
+        assert (np.abs(got - lost - want) > tolerance).any()
+    assert S.gains_chain(200006, 2, 1, 8, True) < 600 and tolerance.max() < 0.05
