@@ -1,6 +1,10 @@
 """Launches of the calls around a layer's attention, and calls of their Python forms, that other tests pass over.  No device."""
 import pytest
+import torch
 
+import paper_2406_03488_amd as s1f
+from paper_2406_03488_amd import binding
+from test_host_layer import good
 from test_host_layer_launches import launches, of
 
 
@@ -22,3 +26,41 @@ def test_fp32_sums_between_the_projections_are_short(tmp_path, shape):
         # (the first turn writes, the others add)
         assert ["ResultE1" in name for name, _ in turns] == [True] + [False] * (len(turns) - 1) and all(g == grid for _, g in turns)
     assert not [1 for name, _ in of(launches(tmp_path, [("ffn", n, h, f, 1)]), "ffn_product") if "Lb0" in name and "ResultE2" in name]
+
+
+@pytest.mark.parametrize("name,positions,values", [("rope_fwd", 6, (2, 10)), ("rope_bwd", 6, (2, 10)), ("qk_norm_rope_fwd", 9, (2, 13)), ("qk_norm_rope_bwd", 11, (2, 15))])
+def test_a_first_position_reaches_the_library(monkeypatch, name, positions, values):
+    """An integer in the place of the positions' tensor, with values and without."""
+    calls = []
+
+    class Library:
+        def __getattr__(self, entry):
+            return lambda *args: calls.append((entry, args)) or 0
+    monkeypatch.setattr(binding, "load_library", Library)
+    monkeypatch.setattr(binding, "_stream_ptr", lambda: 0)
+    monkeypatch.setattr(binding, "_check_device", lambda *t: None)
+    monkeypatch.setattr(binding, "_native", lambda: binding._PythonForms)
+    args = good()[name]
+    assert isinstance(args[positions], torch.Tensor) and args[positions + 1] == 3
+    tensor = args[positions].data_ptr()
+    getattr(s1f, name)(*args)
+    args[positions] = -77
+    getattr(s1f, name)(*args)
+    for i in values:
+        args[i] = None
+    getattr(s1f, name)(*args)
+    assert [entry for entry, _ in calls] == ["s1f_" + name] * 3
+    # (positions, their stride, the first row's, seg_off) behind the magnitude
+    for (_, got), want in zip(calls, ((tensor, 5, 0, 3), (None, 0, -77, 3), (None, 0, -77, 3))):
+        at = next(i for i in range(len(got)) if got[i:i + 4] == want)
+        assert got[at - 1] == 1.0
+
+
+def test_a_tensor_in_the_place_of_the_segments_first_row_is_refused(monkeypatch):
+    monkeypatch.setattr(binding, "_check_device", lambda *t: None)
+    monkeypatch.setattr(binding, "_native", lambda: binding._PythonForms)
+    for name, positions in (("rope_fwd", 6), ("rope_bwd", 6), ("qk_norm_rope_fwd", 9), ("qk_norm_rope_bwd", 11)):
+        args = good()[name]
+        args[positions + 1] = args[positions]
+        with pytest.raises((TypeError, ValueError)):
+            getattr(s1f, name)(*args)
