@@ -15,6 +15,9 @@ pytestmark = pytest.mark.gpu
 CASES = [(*shape, dtype) for shape, dtypes in SHAPES for dtype in dtypes]
 # the kernel of few rows, of up to 16, 32 and 64
 CASES += [(n, h, f, dtype) for n, h, f in ((1, 1032, 2500), (16, 520, 1400), (13, 4096, 11008), (30, 520, 1400), (57, 520, 1400), (64, 193, 331)) for dtype in (0, 1)]
+# fp32 sums of y and dx in turns, in tiles of every size, in parts and not; turns that do not end a stage
+TURNS = [(65, 8192, 26000), (300, 2048, 26001), (2000, 640, 33333), (8200, 1100, 14001), (4400, 4096, 13000), (16384, 1024, 13000)]
+CASES += [(*shape, 0) for shape in TURNS]
 CASES += [(512, 4096, 11008, 0), (512, 4096, 11008, 1), (1000, 2048, 5632, 1), (4099, 4096, 11008, 0)]
 
 

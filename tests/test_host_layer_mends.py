@@ -64,3 +64,16 @@ def test_a_tensor_in_the_place_of_the_segments_first_row_is_refused(monkeypatch)
         args[positions + 1] = args[positions]
         with pytest.raises((TypeError, ValueError)):
             getattr(s1f, name)(*args)
+
+
+def test_turns_of_y_and_dx_take_tiles_of_every_size(tmp_path):
+    """tests/test_gpu_ffn_spread.py checks the values of these."""
+    from test_gpu_ffn_spread import TURNS
+    kinds = set()
+    for shape in TURNS:
+        done = launches(tmp_path, [("ffn", *shape, 0)])
+        for (name, *_), (behind, *_) in zip(done, done[1:] + [("", 0, 0, 0)]):
+            if "ffn_product" in name and "ResultE2" in name and "Lb1ELb1E" not in name:
+                side = next(s for s in ("256ELi256", "128ELi128", "64ELi128") if f"Li{s}" in name)
+                kinds.add(("y" if "Lb0ELb0E" in name else "dx", side, "join" in behind))
+    assert {(k, s, True) for k in ("y", "dx") for s in ("256ELi256", "128ELi128", "64ELi128")} <= kinds and {("y", "256ELi256", False), ("dx", "256ELi256", False)} <= kinds, kinds
