@@ -72,14 +72,14 @@ template <typename T, int N> struct Run {
 };
 
 // cos and sin of a 64-bit angle: the quarter turn and the rest in 64 bits (pi/2 as two numbers; a fused product takes off the first exactly), the rest's
-// series in 32, to 2^-25 of the result.  Past 2^48 quarter turns their number is not whole to a fraction of one any more, and what is left of the angle is reduced once again: to 2^79.
-S1F_DEV void cos_sin(double angle, float &c, float &s) {
+// series in 32, to 2^-25 of the result.  FAR: angles from kFar on, the number of whose quarter turns is not whole to a fraction of one any more: what is left of them is reduced once again, up to 2^79.
+constexpr double kFar = 0x1p48;
+template <bool FAR> S1F_DEV void cos_sin(double angle, float &c, float &s) {
   constexpr double kPerQuarter = 0.63661977236758134308;
   const auto less = [](double x, double n) { return fma(-n, 6.123233995736766036e-17, fma(-n, 1.5707963267948965580, x)); };
   double turns = rint(angle * kPerQuarter), rest = less(angle, turns);
-  const bool far = fabs(turns) > 0x1p48;
-  if (__builtin_expect(__any(far), 0)) {
-    const double more = far ? rint(rest * kPerQuarter) : 0.0;
+  if (FAR && fabs(angle) > kFar) {
+    const double more = rint(rest * kPerQuarter);
     rest = less(rest, more);
     turns = turns - 4.0 * floor(turns * 0.25) + more;
   }
@@ -236,21 +236,28 @@ template <typename T, typename K, int PW, int L, int IT, int U, Layout LAYOUT, b
   float c[IT][ANGLES], s[IT][ANGLES];
   auto angles = [&]() {
     const int64_t position = a.positions ? a.positions[b * a.positions_sb + r] : a.first_position + r;
+    bool far = false;
+    auto turn = [&](auto again) {
 #pragma unroll
-    for (int t = 0; t < IT; ++t)
+      for (int t = 0; t < IT; ++t)
 #pragma unroll
-      for (int i = 0; i < ANGLES; ++i) {
-        const int of = (lane + t * L) * ANGLES + i;
-        const bool second = LAYOUT == kAny && of >= a.half;
-        const int pair = second ? of - a.half : of;
-        c[t][i] = 1.f;
-        s[t][i] = 0.f;
-        if (pair < a.half) {
-          cos_sin((double)position * a.freqs[pair], c[t][i], s[t][i]);
-          c[t][i] *= a.magnitude;
-          s[t][i] *= BACK != second ? -a.magnitude : a.magnitude;
+        for (int i = 0; i < ANGLES; ++i) {
+          const int of = (lane + t * L) * ANGLES + i;
+          const bool second = LAYOUT == kAny && of >= a.half;
+          const int pair = second ? of - a.half : of;
+          c[t][i] = 1.f;
+          s[t][i] = 0.f;
+          if (pair < a.half) {
+            const double angle = (double)position * a.freqs[pair];
+            far = far || fabs(angle) > kFar;
+            cos_sin<decltype(again)::value>(angle, c[t][i], s[t][i]);
+            c[t][i] *= a.magnitude;
+            s[t][i] *= BACK != second ? -a.magnitude : a.magnitude;
+          }
         }
-      }
+    };
+    turn(std::false_type{});
+    if (__builtin_expect(__any(far), 0)) turn(std::true_type{});
   };
   int angles_of = -1;
   if constexpr (NORM) {   // (under the angles' latencies)
