@@ -394,7 +394,7 @@ size_t s1f_token_loss_bwd_workspace_bytes(const s1f_rows *desc, int64_t vocab, i
  *   dweight_dtype S1F_BF16  (bf16 rows only) both overwritten, rounded once: the gradients of this call alone
  * bf16: h, dgate and dup are rounded to bf16 before their products, like the probabilities and score gradients of the attention; sums are fp32.  fp32: products to fp32
  * precision (operands as three exact bf16 parts each, but for elements below 2^-110, which keep 8 bits at least, and for dgate and dup below 2^-126), of finite numbers below 2^112; whatever an
- * infinity or a NaN takes part in may be NaN.  One fp32 sum has up to 12288 terms, longer ones are made of sums of about 8192, but for those over hidden that make gate, up and dh: results are 1e-6 to 3e-6 of their norm off.
+ * infinity or a NaN takes part in may be NaN.  One fp32 sum has up to 12288 terms (up to 16 rows: 16384), longer ones are made of sums of about 8192, but for those over hidden that make gate, up and dh: results are 1e-6 to 3e-6 of their norm off.
  * A row's y, gate_up and dx depend on that row alone.  y may lie in the place of x, and dx in that of x, dy or gate_up, in whole or in part; no other output may lie in an input's.
  * w_in and w_out are 16-byte aligned.  Calls are faster where hidden and inner are multiples of 8 and all rows start on 16 bytes: but for few rows, other bf16 operands, and fp32 ones,
  * are laid out anew in the workspace first.  inner <= 2^17, w_in_stride and w_out_stride < 2^22, 2 * inner * w_in_stride <= 2^30, batch * rows <= 2^20, batch * rows * hidden and

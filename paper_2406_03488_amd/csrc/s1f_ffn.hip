@@ -4,7 +4,7 @@
 //   backward   dh = dy W_out,  dg = dh * u * act'(g),  du = dh * act(g);  dx = [dg | du] W_in,  dW_in += [dg | du]^T x,  dW_out += dy^T h
 //
 // Bound by the matrix units, at the clock that power leaves them: 6 n hidden inner operations and 12.  Forward of 4099 x 4096 x 11008 bf16 921 to 955 us, 1.16 to 1.2 PFLOP/s (a library product of
-// 16384^3 of random operands: 1.33); gradient of 4897 x 7168 x 19200 6.5 to 6.7 ms, 1.21 to 1.24.  Few rows: the weights.  Nothing of it is a pass over memory of its own: a tile of x W_in^T holds the same columns of
+// 16384^3 of random operands: 1.33); gradient of 4897 x 7168 x 19200 6.55 to 6.64 ms, 1.22 to 1.23.  Few rows: the weights.  Nothing of it is a pass over memory of its own: a tile of x W_in^T holds the same columns of
 // both halves, in the same lanes, so that h is what its results leave in memory (and g and u, rounded, if the caller keeps them); dh stays in registers, and the tile
 // that computes it reads g and u and leaves dg, du and h.  h, dg and du are bf16 in memory, rounded once, as the attention kernels round their probabilities and score
 // gradients; fp32 calls: three bf16 planes that hold them whole, and fp32 operands are split into such planes first.
@@ -85,7 +85,7 @@ template <typename T> S1F_DEV float sigmoid(float x) {
   else return __builtin_amdgcn_rcpf(1.f + exp2_fast(x * -kLog2e));
 }
 // act(g), and act'(g).  The tanh form is g * sigmoid(g (c0 + c1 g^2)), (1 + tanh(t)) / 2 being the sigmoid of 2t, which keeps its digits where 1 + tanh would lose them, as erfc does
-// where 1 + erf would.
+// where 1 + erf would (erfcf and expf per element: forward of 4099 x 4096 x 11008 bf16 964 us where the others take 928 to 933, gradient 1936 and 1874 to 1887).
 template <typename T, int ACT> struct Activation {
   static constexpr float c0 = 1.5957691216f, c1 = c0 * 0.044715f;
   // (past 2^60 squares are left where they are, and no sigmoid changes any more)
@@ -360,7 +360,7 @@ template <Result R> S1F_DEV void put_result(const FfnArgs &a, int row, int col, 
   }
 }
 
-// y, dx, dW_in and dW_out.  4897 x 7168 x 19200 bf16: dx 2.06 ms, 1.31 PFLOP/s, dW_out 1.05, 1.29, dW_in 2.15, 1.26; fp32, 682 x 1280 x 3413: dx 82 us, dW_in 90, dW_out 48.  The tiles from `whole` on are cut along the contraction: their parts are added up by the join.
+// y, dx, dW_in and dW_out.  4897 x 7168 x 19200 bf16: dx 2.06 ms, 1.31 PFLOP/s, dW_out 1.05, 1.29, dW_in 2.15, 1.26 (added into fp32 accumulators, both: 0.37 ms more); fp32, 682 x 1280 x 3413: dx 82 us, dW_in 90, dW_out 48.  The tiles from `whole` on are cut along the contraction: their parts are added up by the join.
 template <int PAIRS, int BM, int BN, int WM, int WN, bool TRA, bool TRB, Result R> __global__ void __launch_bounds__(64 * WM * WN, 2) ffn_product_kernel(const FfnArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   typedef Product<BM, BN, WM, WN, TRA, TRB, PAIRS> P;
@@ -542,7 +542,7 @@ constexpr int tile_n(Tile t) { return t == kBig ? 256 : 128; }
 // ones 2.5, a single round up to 3.1: priced so, a gradient of 2048 x 1024 x 2816 takes big tiles and 473 us instead of 458).  fp32 dh, us, middle and low: 682 x 3413 of 1280 74 and 120; 256 x 11008 of 4096 211 and 253, with planes to be laid
 // out first; 1500 x 5632 of 2048 280 and 311 (big 307).
 // Smaller bf16 tiles alone on a unit wait longer for operands that come from memory than the loss's do: priced like those, 1000 rows of 2048 x 5632 took 123 us forward in 256 low tiles of 88 stages instead of
-// 101 in middle ones cut in two, the gradient 219 instead of 206, 512 of 4096 x 11008 183 instead of 173, the gradient of 2048 of 1024 x 2816 143 instead of 133.
+// 101 in middle ones cut in two, the gradient 219 instead of 203, 512 of 4096 x 11008 183 instead of 173, the gradient of 2048 of 1024 x 2816 143 instead of 132.
 enum Operand { kBf16, kPlanes, kPlanesByColumns };
 double round_us(Tile tile, int64_t tiles, double stages, Operand operand) {
   if (tile == kLow && operand != kBf16) return (double)((tiles + kUnits - 1) / kUnits) * (5.5 + (operand == kPlanes ? 0.265 : 0.32) * stages);

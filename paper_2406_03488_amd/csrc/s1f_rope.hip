@@ -7,9 +7,9 @@
 //              g = dy * gain,  dx = rstd * (g - xhat * sum(g * xhat) / d)
 //
 // Bound by memory: each element is read and written once, between which a row's angles, computed once for all heads that a lane takes, are next to nothing.  A row of a head lies in
-// the registers of a few lanes, 16 bytes of the wider type to each, and mostly both elements of a pair in one lane.  4097 tokens of 64 and 2 x 8 heads of 128, bf16: 168 MB, 39.7 us, 4.2 TB/s
-// (a large copy: 4.65); their gradient for 4096 tokens of 3 x 32 heads, 268 MB, 58.8 us, 4.6 TB/s; norms and rotation of 4897 tokens of 3 x 56 heads, 421 MB, 89.9 us, 4.7 TB/s; the gradient of 8774
-// tokens of 64 and 2 x 8 heads, 557 MB, 125 us, 4.4 TB/s, 0.6 of which the vector units are busy.  One token of 64 + 16 heads 4.4 us, a launch.
+// the registers of a few lanes, 16 bytes of the wider type to each, and mostly both elements of a pair in one lane.  4097 tokens of 64 and 2 x 8 heads of 128, bf16: 168 MB, 39.9 us, 4.2 TB/s
+// (a large copy: 4.65); their gradient for 4096 tokens of 3 x 32 heads, 268 MB, 58.5 us, 4.6 TB/s; norms and rotation of 4897 tokens of 3 x 56 heads, 421 MB, 90.0 us, 4.7 TB/s; the gradient of 8774
+// tokens of 64 and 2 x 8 heads, 557 MB, 126 us, 4.4 TB/s, 0.6 of which the vector units are busy.  One token of 64 + 16 heads 4.4 us, a launch.
 // Angles are products in 64 bits: at position 2^20 one in 32 bits is off by 2^-4.  The norm's sums are fp32, as is everything between load and store; results are rounded once.
 #include <algorithm>
 #include <atomic>
