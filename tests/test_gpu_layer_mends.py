@@ -66,3 +66,62 @@ def test_long_fp32_sums_between_the_projections():
     xs, ys, wi, wo = (t.double() for t in (x[0, rows], dy[0, rows], w_in, w_out))
     S.near(y[0, rows], S.forward(xs, wi, wo, "silu", "f32")["y"], "y")
     S.near(dx[0, rows], S.backward(ys, xs, wi, wo, "silu", gate_up[0, rows].double(), "f32", S.U)["dx"], "dx")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [12, 517])
+def test_block_in_part_of_the_place_of_its_inputs(n, dtype):
+    """y some rows behind x, dx some rows behind x or dy, or in gate_up."""
+    c = Block((1, n, 128, 264, "dense", "dense", "silu"), dtype)
+    y, gate_up = c.forward()
+    start = c.start()
+    want = c.backward(gate_up, "f32", start)
+    ws = torch.empty(max(s1f.gated_ffn_fwd_workspace_bytes(c.x, c.w_in, c.w_out), s1f.gated_ffn_bwd_workspace_bytes(c.dy, c.x, c.w_in, c.w_out)), dtype=torch.uint8, device="cuda")
+
+    def shifted(t):
+        rows = torch.zeros((1, n + 5, 128), dtype=t.dtype, device="cuda")
+        rows[:, :n] = t
+        return rows[:, :n], rows[:, 5:]
+    x, to = shifted(c.x)
+    s1f.gated_ffn_fwd(x, c.w_in, c.w_out, s1f.SILU, to, None, ws)
+    assert torch.equal(to, y)
+    for place in ("x", "dy", "gate_up"):
+        x, dy, kept = c.x, c.dy, gate_up.clone()
+        if place == "x":
+            x, dx = shifted(x)
+        elif place == "dy":
+            dy, dx = shifted(dy)
+        else:
+            dx = kept.view(-1)[:n * 128].view(1, n, 128)
+        dw = [t.clone() for t in start]
+        s1f.gated_ffn_bwd(dy, x, c.w_in, c.w_out, s1f.SILU, kept, dx, *dw, ws)
+        assert torch.equal(dx, want[0]) and all(torch.equal(a, b) for a, b in zip(dw, want[1:])), place
+
+
+def test_turns_in_a_graph():
+    """fp32 sums in turns, captured and replayed with new inputs: the first turn writes, whatever the replay before has left."""
+    n, h, f = 65, 8192, 26000
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(11)
+    normal = lambda *shape, scale=1.0: torch.empty(shape, device="cuda").normal_(0, scale, generator=gen)
+    x, dy, w_in, w_out = normal(1, n, h), normal(1, n, h), normal(2 * f, h, scale=h ** -0.5), normal(h, f, scale=f ** -0.5)
+    y, dx, gate_up, dw = torch.empty_like(x), torch.empty_like(x), torch.empty((1, n, 2 * f), device="cuda"), [torch.zeros_like(w_in), torch.zeros_like(w_out)]
+    ws = torch.empty(s1f.gated_ffn_bwd_workspace_bytes(dy, x, w_in, w_out), dtype=torch.uint8, device="cuda")
+    ws_fwd = torch.empty(s1f.gated_ffn_fwd_workspace_bytes(x, w_in, w_out), dtype=torch.uint8, device="cuda")
+
+    def run():
+        s1f.gated_ffn_fwd(x, w_in, w_out, s1f.SILU, y, gate_up, ws_fwd)
+        s1f.gated_ffn_bwd(dy, x, w_in, w_out, s1f.SILU, gate_up, dx, *dw, ws)
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for _ in range(3):
+        x.normal_(0, 1, generator=gen)
+        run()
+        want = y.clone(), dx.clone()
+        y.fill_(float("nan")), dx.fill_(float("nan"))
+        graph.replay()
+        assert torch.equal(y, want[0]) and torch.equal(dx, want[1])
+        torch.cuda.synchronize()
